@@ -137,6 +137,47 @@ pie_status pie_mask_kvpage(pie_ctx* ctx, const int32_t* page_ids, const uint32_t
 pie_status pie_copy_kvpage(pie_ctx* ctx, const int32_t* src_pages, const int32_t* src_slots,
                            const int32_t* dst_pages, const int32_t* dst_slots, int32_t n);
 
+/* Whole pages.  A program that branches (beam search, trees of thought) forks the pages its branches will write, one that
+ * evicts tokens frees the pages they leave, one that has to make room moves pages out of the pool and back (Table 1, Allocate
+ * row; Control layer, Resource management: the caller decides which pages are whose).  All of it is enqueued on the context's
+ * stream behind the calls before it, and not waited for.  Page masks are host state and change when the call returns; batches created
+ * earlier keep what they saw. */
+
+/* Page dst_pages[i] becomes what page src_pages[i] was before the call: K and V in every layer, bit for bit, and its mask.  A
+ * source may be named any number of times, and a page may be both source and destination, so the pages of beams that were
+ * reordered may be permuted in place; src == dst does nothing.  Host int32 arrays [n].  Up to 160 pages travel as kernel
+ * arguments, so such a call may be captured into a graph (a replay repeats the copies; the masks were set when it was captured);
+ * a longer one is refused with PIE_EHIP while the stream is captured, and may allocate.
+ * Errors: PIE_EINVAL, PIE_ERANGE, PIE_ECONFLICT (a destination named twice), PIE_ENOMEM, PIE_EHIP. */
+pie_status pie_fork_kvpage(pie_ctx* ctx, const int32_t* src_pages, const int32_t* dst_pages, int32_t n);
+
+/* Saves pages into the caller's memory, and restores pages from it: image is dev bf16
+ * [n][n_layers][2: K, V][page_size][n_kv_heads][head_dim], 16-byte aligned, bits unchanged (K as it is stored: after the rotary
+ * step).  The pool pages of a save, and the image of a restore, stay as they are; page masks are neither saved nor changed.  A page
+ * may be saved twice by one call, not restored twice (PIE_ECONFLICT).  page_ids: host int32 [n].  May be captured.
+ * Errors: PIE_EINVAL, PIE_ERANGE, PIE_ECONFLICT, PIE_EHIP. */
+pie_status pie_save_kvpage(pie_ctx* ctx, const int32_t* page_ids, int32_t n, void* image);
+pie_status pie_restore_kvpage(pie_ctx* ctx, const int32_t* page_ids, int32_t n, const void* image);
+
+/* Compacts the KV cache of n_seqs sequences: the tokens that their pages' masks (pie_mask_kvpage) leave visible move to the front
+ * of the sequence's destination pages, in their order, in every layer.  Sequence s has the page table page_ids[page_indptr[s] ..
+ * page_indptr[s+1]) and kv_len[s] tokens (tokens behind them are not looked at); its destination table is dst_page_ids[
+ * dst_page_indptr[s] .. dst_page_indptr[s+1]), or, with both destination arrays NULL, its own table: in place.  out_kv_len[s]
+ * receives the number of tokens kept; the destination's first ceil(out_kv_len[s] / page_size) pages hold them and have all slots
+ * visible afterwards, slots behind the last kept token are left as they were, and the pages behind those (which the caller may now
+ * give to others) keep contents and masks, as do source pages that are no destinations.  A sequence that keeps nothing has length 0.
+ * shifts (may be NULL): host int32, one per token of the sequences one after another (sum of kv_len): the key of a kept token
+ * is rotated by that many positions more, with the model's rotary frequencies and rounded to bf16 once, as a token needs
+ * that keeps its place relative to others when a gap before it is closed; 0 leaves the bits.
+ * Pages may be shared by several sequences where no sequence of the call writes them (in place, pages in front of the first token
+ * that moves or turns are not written).  A page that is written may be no one's source in any other place: PIE_ECONFLICT.
+ * All arrays are host int32.  May allocate; refused with PIE_EHIP while the stream is captured.  On error nothing has changed.
+ * Errors: PIE_EINVAL (also: more tokens kept than the destination holds), PIE_ERANGE, PIE_EBATCH (over 2^30 tokens),
+ * PIE_ECONFLICT, PIE_ENOMEM, PIE_EHIP. */
+pie_status pie_compact_kvpage(pie_ctx* ctx, int32_t n_seqs, const int32_t* page_indptr, const int32_t* page_ids, const int32_t* kv_len,
+                              const int32_t* dst_page_indptr, const int32_t* dst_page_ids, const int32_t* shifts,
+                              int32_t* out_kv_len);
+
 /* One batch of `forward(q, ikv, iemb, okv, oemb, mask)` commands as the batch scheduler hands it
  * to the handler (Table 1 `forward`; Forward API; Batch scheduler: horizontal + vertical
  * batching).  The command queue argument is gone: batching has been done.  All arrays are host.
@@ -242,6 +283,44 @@ pie_status pie_get_next_dist(pie_ctx* ctx, const int32_t* embed_ids, int32_t n, 
  * Other errors as pie_get_next_dist. */
 pie_status pie_get_next_dist_static(pie_ctx* ctx, const int32_t* embed_ids, int32_t n, int32_t top_k,
                                     float temperature, int32_t* out_ids, float* out_probs);
+
+/* Beam search: the best candidates over beams and vocabulary together (Sample API; the paper's beam-search inferlet, for which
+ * the truncated distributions of get_next_dist would have to be merged by the program).  Rows group_indptr[g] ..
+ * group_indptr[g+1) are the beams of search g (at most 256, possibly none), row r has the cumulative score scores[r] (natural
+ * logarithm of its probability so far; NULL: all 0), and token v continues it with
+ *     score(r, v) = scores[r] + z[r][v] / temperature - log sum_u exp(z[r][u] / temperature).
+ * Of every search the n_out (at most 256) candidates of largest score are returned by descending score, equal scores by
+ * ascending beam, then ascending token; scores are compared in 64 bits and stored in 32.
+ *   - a logit of -inf or NaN is no candidate and adds nothing to the sum (a grammar's mask); +inf counts as the largest finite
+ *     value of the logits' type; the lowest finite value is a logit like any other
+ *   - a beam whose score is -inf or NaN, or whose logits are all -inf or NaN, has no candidates
+ *   - a beam with finished[r] != 0 has exactly one: (r, eos_token) with its score unchanged; its logits are not looked at
+ *   - where fewer than n_out candidates exist the rest is beam -1, token -1, score -inf */
+typedef struct {
+  int32_t n_groups;
+  const int32_t* group_indptr; /* host [n_groups + 1], from 0 */
+  const float* scores;         /* dev [rows] or NULL */
+  const uint8_t* finished;     /* dev [rows] or NULL: none is */
+  int32_t eos_token;           /* read where finished is given */
+  int32_t n_out;
+  float temperature;           /* positive and finite */
+} pie_beam_search;
+
+/* Element types of a caller's logits. */
+enum { PIE_F32 = 0, PIE_BF16 = 1, PIE_F16 = 2 };
+
+/* The selection over logits that the caller has (changed by a grammar, a penalty, a head of its own): dev [rows] of n_vocab
+ * (1 .. the model's vocab) elements, row r at logits + r * row_stride elements; any row_stride >= n_vocab, and any alignment that
+ * the element type has.  rows <= max_dist_rows.  Outputs dev [n_groups][n_out]: the beam within its group, the token, the new
+ * cumulative score.  Enqueues only and allocates nothing; may be captured into a graph.
+ * Errors: PIE_EINVAL, PIE_ERANGE (n_out, n_vocab, eos_token), PIE_EBATCH (rows, beams of a group), PIE_EHIP. */
+pie_status pie_beam_select(pie_ctx* ctx, const pie_beam_search* search, const void* logits, int32_t dtype, int64_t row_stride,
+                           int32_t n_vocab, int32_t* out_beams, int32_t* out_tokens, float* out_scores);
+
+/* The selection over Embeds: what pie_get_next_dist does up to the logits of embed_ids[0 .. rows) (host int32), then
+ * pie_beam_select over them.  Errors: as both. */
+pie_status pie_get_next_beams(pie_ctx* ctx, const pie_beam_search* search, const int32_t* embed_ids, int32_t* out_beams,
+                              int32_t* out_tokens, float* out_scores);
 
 /* Waits for the context's stream (Table 1, `synchronize`: completion of the calls issued so far). */
 pie_status pie_synchronize(pie_ctx* ctx);

@@ -38,6 +38,9 @@ Parity pins (tests/test_oracle_*.py, all CPU):
                       all-ones mask is a no-op; a fully masked page equals an omitted page
   copy_kvpage         a request over token-wise copied pages equals the request over the originals;
                       bit-exact against a hand-written slot loop, in every layer's pool
+  fork, compact       simultaneous assignment by a loop; attention over compacted pages equals attention
+                      over the masked originals; a shifted key equals the key rotated to the new position
+  beam_select         torch log_softmax + topk over the flattened group, a loop over all candidates
   full depth          torch CPU expression of a textbook L-layer Llama on one contiguous request;
                       zero Wo and Wdown in every layer -> output == input; prefill of n tokens ==
                       n-1 tokens writing pages + 1 token reading them, through all layers
@@ -454,6 +457,92 @@ def copy_kvpage(kvs, src_pages, src_slots, dst_pages, dst_slots) -> None:
         k, v = kv.k_bits[sp, ss].copy(), kv.v_bits[sp, ss].copy()
         kv.k_bits[dp, ds] = k
         kv.v_bits[dp, ds] = v
+
+
+def fork_kvpage(kvs, src_pages, dst_pages) -> None:
+    """Page dst_pages[i] becomes what page src_pages[i] was before the call: K, V and mask, in every layer."""
+    s, d = np.asarray(src_pages, dtype=np.int64), np.asarray(dst_pages, dtype=np.int64)
+    assert len(set(d.tolist())) == len(d) == len(s)
+    for kv in kvs:
+        kv.k_bits[d], kv.v_bits[d], kv.visible[d] = kv.k_bits[s].copy(), kv.v_bits[s].copy(), kv.visible[s].copy()
+
+
+def save_kvpage(kvs, page_ids) -> np.ndarray:
+    """uint16 bits [page][layer][K or V][slot][kv head][dim]."""
+    ids = np.asarray(page_ids, dtype=np.int64)
+    return np.stack([np.stack([kv.k_bits[ids], kv.v_bits[ids]], axis=1) for kv in kvs], axis=1)
+
+
+def compact_kvpage(kvs, page_indptr, page_ids, kv_len, theta, dst_page_indptr=None, dst_page_ids=None, shifts=None) -> np.ndarray:
+    """The visible tokens of every sequence move, in their order, to the front of its destination pages, in every layer; the key
+    of a token whose shift is not 0 is rotated by it and rounded to bf16.  Pages that then hold kept tokens are visible
+    throughout.  Returns the new lengths."""
+    P = kvs[0].page_size
+    if dst_page_indptr is None:
+        dst_page_indptr, dst_page_ids = page_indptr, page_ids
+    out, off, writes = [], 0, []
+    for s in range(len(kv_len)):
+        L = int(kv_len[s])
+        table = np.asarray(page_ids[page_indptr[s]:page_indptr[s + 1]], dtype=np.int64)
+        into = np.asarray(dst_page_ids[dst_page_indptr[s]:dst_page_indptr[s + 1]], dtype=np.int64)
+        keep = np.array([j for j in range(L) if kvs[0].visible[table[j // P], j % P]], dtype=np.int64)
+        by = np.zeros(L, np.int64) if shifts is None else np.asarray(shifts[off:off + L], dtype=np.int64)
+        off += L
+        out.append(len(keep))
+        for kv in kvs:
+            k, v = kv.k_bits[table[keep // P], keep % P].copy(), kv.v_bits[table[keep // P], keep % P].copy()
+            turned = by[keep] != 0
+            if turned.any():
+                with np.errstate(invalid="ignore"):
+                    x = rope(bf16_decode(k[turned]), by[keep][turned], theta)
+                ordinary = np.isfinite(x) & ((x == 0) | (np.abs(x) > 1.2e-38)) & (np.abs(x) < 2.9e38)
+                few = np.rint(np.where(ordinary, 0.0, np.nan_to_num(x, posinf=0.0, neginf=0.0)) * 2.0 ** 133) * 2.0 ** -133  # subnormals
+                k[turned] = np.where(ordinary, bf16_encode(bf16_round(np.where(ordinary, x, 0.0))),
+                                     (np.where(np.isfinite(x), few, x).astype(np.float32).view(np.uint32) >> 16).astype(np.uint16))
+            writes.append((kv, into, np.arange(len(keep)), k, v))
+    for kv, into, at, k, v in writes:
+        kv.k_bits[into[at // P], at % P] = k
+        kv.v_bits[into[at // P], at % P] = v
+        kv.visible[into[np.unique(at // P)]] = True
+    return np.array(out, dtype=np.int32)
+
+
+# --------------------------------------------------------------------------------------------
+# beam search
+# --------------------------------------------------------------------------------------------
+
+
+def beam_select(logits, group_indptr, n_out, scores=None, finished=None, eos_token=-1, temperature=1.0, largest=np.inf):
+    """Per group of rows the n_out best candidates (row, token) by scores[row] + log_softmax(logits[row] / temperature)[token],
+    then by row, then by token; (-1, -1, -inf) where there are fewer.  A logit of -inf or NaN is no candidate, +inf counts as
+    `largest`; rows of score -inf or NaN have none; a finished row has (row, eos_token) at its score."""
+    z = np.array(logits, dtype=np.float64)
+    G = len(group_indptr) - 1
+    beams, tokens = np.full((G, n_out), -1, np.int32), np.full((G, n_out), -1, np.int32)
+    best = np.full((G, n_out), -np.inf)
+    for g in range(G):
+        cand = []
+        for b, r in enumerate(range(group_indptr[g], group_indptr[g + 1])):
+            s = 0.0 if scores is None else float(scores[r])
+            s = min(s, float(np.finfo(np.float32).max))
+            if np.isnan(s) or s == -np.inf:
+                continue
+            if finished is not None and finished[r]:
+                cand.append((np.array([s]), np.array([b]), np.array([eos_token])))
+                continue
+            row = np.minimum(z[r], largest)
+            v = np.nonzero(~np.isnan(z[r]) & (z[r] > -np.inf))[0]
+            if not len(v):
+                continue
+            x = row[v] / float(temperature)
+            top = x.max()
+            cand.append((s + (x - top - math.log(np.exp(x - top).sum())), np.full(len(v), b), v))
+        if not cand:
+            continue
+        s, b, v = (np.concatenate([c[i] for c in cand]) for i in range(3))
+        order = np.lexsort((v, b, -s))[:n_out]
+        beams[g, :len(order)], tokens[g, :len(order)], best[g, :len(order)] = b[order], v[order], s[order]
+    return beams, tokens, best
 
 
 # --------------------------------------------------------------------------------------------

@@ -46,6 +46,11 @@ class ForwardBatchC(C.Structure):
                 ("mask_indptr", C.c_void_p), ("mask_words", C.c_void_p), ("adapter_ids", C.c_void_p)]
 
 
+class BeamSearchC(C.Structure):
+    _fields_ = [("n_groups", C.c_int32), ("group_indptr", C.c_void_p), ("scores", C.c_void_p), ("finished", C.c_void_p),
+                ("eos_token", C.c_int32), ("n_out", C.c_int32), ("temperature", C.c_float)]
+
+
 def lib_path() -> str:
     return os.path.join(HERE, _LIB_NAME)
 
@@ -82,6 +87,12 @@ def load_library():
         "pie_embed_txt": [vp, vp, vp, i32, vp],
         "pie_mask_kvpage": [vp, vp, vp, i32],
         "pie_copy_kvpage": [vp, vp, vp, vp, vp, i32],
+        "pie_fork_kvpage": [vp, vp, vp, i32],
+        "pie_save_kvpage": [vp, vp, i32, vp],
+        "pie_restore_kvpage": [vp, vp, i32, vp],
+        "pie_compact_kvpage": [vp, i32] + [vp] * 7,
+        "pie_beam_select": [vp, C.POINTER(BeamSearchC), vp, i32, i64, i32, vp, vp, vp],
+        "pie_get_next_beams": [vp, C.POINTER(BeamSearchC), vp, vp, vp, vp],
         "pie_forward_host": [vp, i32, C.POINTER(ForwardBatchC), i32],
         "pie_get_next_dist": [vp, vp, i32, i32, f32, vp, vp],
         "pie_get_next_dist_static": [vp, vp, i32, i32, f32, vp, vp],
@@ -190,7 +201,7 @@ class Pie:
         self.device = torch.device(device)
         torch.cuda.set_device(self.device)
         self.stream = stream if stream is not None else torch.cuda.Stream(device=self.device)
-        self.model = model
+        self.model, self.n_layers = model, n_layers
         md = ModelDescC(model.hidden, model.n_q_heads, model.n_kv_heads, model.head_dim, model.mlp_dim, model.vocab,
                         model.page_size, model.rms_eps, model.rope_theta, n_layers)
         pd = PoolDescC(n_kv_pages, n_embeds, max_batch_tokens, max_batch_requests, max_top_k, max_dist_rows,
@@ -208,7 +219,7 @@ class Pie:
         PieBatch.work / plan_info and mask_kvpage work on it; everything else raises PieError."""
         self = cls.__new__(cls)
         self.lib = load_library()
-        self.device, self.stream, self.model = None, None, model
+        self.device, self.stream, self.model, self.n_layers = None, None, model, n_layers
         md = ModelDescC(model.hidden, model.n_q_heads, model.n_kv_heads, model.head_dim, model.mlp_dim, model.vocab,
                         model.page_size, model.rms_eps, model.rope_theta, n_layers)
         pd = PoolDescC(n_kv_pages, n_embeds, max_batch_tokens, max_batch_requests, 0, 0, max_adapters, max_lora_rank)
@@ -318,6 +329,44 @@ class Pie:
             raise ValueError("copy_kvpage: four arrays of one length")
         self._check(self.lib.pie_copy_kvpage(self.ctx, *[_ptr(x) for x in a], len(a[0])))
 
+    def fork_kvpage(self, src_pages, dst_pages):
+        s, d = _i32(src_pages), _i32(dst_pages)
+        if len(s) != len(d):
+            raise ValueError("fork_kvpage: one destination per source")
+        self._check(self.lib.pie_fork_kvpage(self.ctx, _ptr(s), _ptr(d), len(s)))
+
+    def _image(self, page_ids, image: torch.Tensor) -> np.ndarray:
+        ids, m = _i32(page_ids), self.model
+        if image.dtype != torch.bfloat16 or not image.is_cuda or not image.is_contiguous() or image.dim() != 6 or \
+                image.shape[0] != len(ids) or tuple(image.shape[2:]) != (2, m.page_size, m.n_kv_heads, m.head_dim) or \
+                image.shape[1] != self.n_layers:
+            raise ValueError("an image of pages is a contiguous bfloat16 device tensor [pages, layers, 2, page_size, kv heads, head_dim]")
+        return ids
+
+    def save_kvpage(self, page_ids, image: torch.Tensor):
+        """Enqueues the copy of the pages into `image` [pages, layers, 2, page_size, kv heads, head_dim]."""
+        ids = self._image(page_ids, image)
+        self._check(self.lib.pie_save_kvpage(self.ctx, _ptr(ids), len(ids), C.c_void_p(image.data_ptr())))
+
+    def restore_kvpage(self, page_ids, image: torch.Tensor):
+        """Enqueues the copy of `image` into the pages; it has to stay as it is until the stream has got there."""
+        ids = self._image(page_ids, image)
+        self._check(self.lib.pie_restore_kvpage(self.ctx, _ptr(ids), len(ids), C.c_void_p(image.data_ptr())))
+
+    def compact_kvpage(self, page_indptr, page_ids, kv_len, shifts=None, dst_page_indptr=None, dst_page_ids=None) -> np.ndarray:
+        """Returns the sequences' new lengths; the moves are enqueued."""
+        ip, ids, kl = _i32(page_indptr), _i32(page_ids), _i32(kv_len)
+        sh = None if shifts is None else _i32(shifts)
+        if (dst_page_indptr is None) != (dst_page_ids is None):
+            raise ValueError("compact_kvpage: dst_page_indptr and dst_page_ids are given together")
+        dp, di = (None, None) if dst_page_indptr is None else (_i32(dst_page_indptr), _i32(dst_page_ids))
+        if len(ip) != len(kl) + 1 or ip[-1] != len(ids) or (sh is not None and len(sh) != kl.sum()) or \
+                (dp is not None and (len(dp) != len(kl) + 1 or dp[-1] != len(di))):
+            raise ValueError("compact_kvpage: arrays of lengths that do not belong together")
+        out = np.zeros(len(kl), dtype=np.int32)
+        self._check(self.lib.pie_compact_kvpage(self.ctx, len(kl), _ptr(ip), _ptr(ids), _ptr(kl), _ptr(dp), _ptr(di), _ptr(sh), _ptr(out)))
+        return out
+
     def kv_read(self, layer: int, page_ids, slots):
         p, s = _i32(page_ids), _i32(slots)
         m = self.model
@@ -392,6 +441,56 @@ class Pie:
         self.get_next_dist_async(embed_ids, top_k, temperature, oi, op)
         self.synchronize()
         return oi.cpu().numpy(), op.cpu().numpy()
+
+    def _beam_search(self, group_indptr, n_out, out_beams, out_tokens, out_scores, scores, finished, eos_token, temperature):
+        ip = _i32(group_indptr)
+        G, n = len(ip) - 1, int(ip[-1]) if len(ip) else 0
+        for t, dt in ((out_beams, torch.int32), (out_tokens, torch.int32), (out_scores, torch.float32)):
+            if t.dtype != dt or not t.is_cuda or not t.is_contiguous() or t.numel() != G * n_out:
+                raise ValueError("beam search: outputs are contiguous device tensors [groups, n_out] of int32, int32 and float32")
+        for t, dts in ((scores, (torch.float32,)), (finished, (torch.uint8, torch.bool))):
+            if t is not None and (t.dtype not in dts or not t.is_cuda or not t.is_contiguous() or t.numel() != n):
+                raise ValueError("beam search: scores (float32) and finished (uint8 or bool) are contiguous device tensors [rows]")
+        at = lambda t: None if t is None else t.data_ptr()
+        return BeamSearchC(G, ip.ctypes.data, at(scores), at(finished), int(eos_token), int(n_out), float(temperature)), ip
+
+    def beam_select_async(self, logits: torch.Tensor, group_indptr, n_out: int, out_beams: torch.Tensor, out_tokens: torch.Tensor,
+                          out_scores: torch.Tensor, scores: Optional[torch.Tensor] = None, finished: Optional[torch.Tensor] = None,
+                          eos_token: int = -1, temperature: float = 1.0):
+        """pie_beam_select over `logits` [rows, vocab] (float32, bfloat16 or float16; rows may be strided); the outputs are the
+        caller's tensors [groups, n_out], complete when the context's stream has got there."""
+        b, keep = self._beam_search(group_indptr, n_out, out_beams, out_tokens, out_scores, scores, finished, eos_token, temperature)
+        types = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+        if logits.dtype not in types or not logits.is_cuda or logits.dim() != 2 or logits.shape[0] != keep[-1] or \
+                (logits.shape[1] > 1 and logits.stride(1) != 1):
+            raise ValueError("beam_select: logits are a device tensor [rows, vocab] of float32, bfloat16 or float16 whose rows are contiguous")
+        stride = logits.stride(0) if logits.shape[0] > 1 else logits.shape[1]
+        self._check(self.lib.pie_beam_select(self.ctx, C.byref(b), C.c_void_p(logits.data_ptr()), types[logits.dtype], stride,
+                                             logits.shape[1], C.c_void_p(out_beams.data_ptr()), C.c_void_p(out_tokens.data_ptr()),
+                                             C.c_void_p(out_scores.data_ptr())))
+
+    def get_next_beams_async(self, embed_ids, group_indptr, n_out: int, out_beams: torch.Tensor, out_tokens: torch.Tensor,
+                             out_scores: torch.Tensor, scores: Optional[torch.Tensor] = None, finished: Optional[torch.Tensor] = None,
+                             eos_token: int = -1, temperature: float = 1.0):
+        """pie_get_next_beams; arguments as for beam_select_async."""
+        ids = _i32(embed_ids)
+        b, keep = self._beam_search(group_indptr, n_out, out_beams, out_tokens, out_scores, scores, finished, eos_token, temperature)
+        if len(ids) != keep[-1]:
+            raise ValueError("get_next_beams: one Embed per row")
+        self._check(self.lib.pie_get_next_beams(self.ctx, C.byref(b), _ptr(ids), C.c_void_p(out_beams.data_ptr()),
+                                                C.c_void_p(out_tokens.data_ptr()), C.c_void_p(out_scores.data_ptr())))
+
+    def get_next_beams(self, embed_ids, group_indptr, n_out: int, scores=None, finished=None, eos_token: int = -1, temperature: float = 1.0):
+        """The same with host arrays: (beams, tokens, scores) [groups, n_out], after the stream has been waited for."""
+        dev = lambda a, dt: None if a is None else torch.from_numpy(np.array(a, dtype=dt)).to(self.device)
+        s, f = dev(scores, np.float32), dev(finished, np.uint8)
+        G = len(_i32(group_indptr)) - 1
+        ob, ot = (torch.empty((G, n_out), dtype=torch.int32, device=self.device) for _ in range(2))
+        os_ = torch.empty((G, n_out), dtype=torch.float32, device=self.device)
+        torch.cuda.synchronize(self.device)
+        self.get_next_beams_async(embed_ids, group_indptr, n_out, ob, ot, os_, s, f, eos_token, temperature)
+        self.synchronize()
+        return ob.cpu().numpy(), ot.cpu().numpy(), os_.cpu().numpy()
 
     def synchronize(self):
         self._check(self.lib.pie_synchronize(self.ctx))

@@ -183,6 +183,12 @@ struct pie_ctx {
   uint32_t write_stamp_id = 0;
   std::vector<uint32_t> page_stamp;  // host: per pool page, the last batch plan that counted it (distinct-page statistic)
   uint32_t page_stamp_id = 0;
+  double* beam_ws = nullptr;         // workspace of the beam selection
+  unsigned char* moves_dev = nullptr;  // plan of the last page call that was too long for kernel arguments
+  size_t moves_cap = 0;
+  struct PageMark { uint32_t stamp; int32_t seq, index, flags; };
+  std::vector<PageMark> page_marks;  // host: per pool page, what the current page call says of it (others: an older stamp)
+  uint32_t page_mark_id = 0;
   int32_t* ids_dev = nullptr;  // staging for id lists of the small resource calls
   size_t ids_cap = 0;
   int last_T = 0, last_dist_n = 0;
@@ -343,3 +349,44 @@ int topk_chunks(int V, int k);  // chunks per row used by launch_topk (<= 16), 0
 // cand_ws: [n, chunks, k] 64-bit candidates; stats_ws: [n, chunks, 2] floats
 hipError_t launch_topk(const float* logits, int n, int V, int k, float inv_temp, int32_t* out_ids, float* out_probs,
                        unsigned long long* cand_ws, float* stats_ws, hipStream_t s);
+
+// Beams (beam.hip): the n_out best (row, token) of every group of rows; arguments as for pie_beam_select.
+#define BEAM_GROUPS_BY_VALUE 256  // groups of one launch, whose row ranges travel as kernel arguments
+#define BEAM_MAX_OUT 256          // most candidates a group is asked for
+#define BEAM_MAX_ROWS 256         // most beams of a group
+struct BeamArgs {
+  const void* logits;
+  int dtype;
+  int64_t stride;
+  int V;
+  const float* scores;
+  const uint8_t* finished;
+  int eos;
+  const int32_t* group_indptr;  // host [n_groups + 1]
+  int n_groups, n_out;
+  double inv_temp;
+  double* ws;  // beam_ws_doubles(rows, vocab)
+  int32_t *out_beams, *out_tokens;
+  float* out_scores;
+};
+size_t beam_ws_doubles(int rows, int vocab);
+hipError_t launch_beam_select(const BeamArgs& a, hipStream_t s);
+
+// Pages (pages.hip)
+struct PageMove { int32_t src, dst; };            // src -1: the page kept at the start of the run
+struct PageRun { int32_t first, n, keep; };       // moves [first, first + n) in order; keep >= 0: a page read before them
+#define FORK_BY_VALUE 160  // moves (and runs) of a launch that travel as kernel arguments, of which it takes 4 KiB
+hipError_t launch_fork(bf16_t* kv, size_t layer_elems, int n_layers, size_t page_elems, const PageMove* moves, int n_moves, const PageRun* runs,
+                       int n_runs, bool on_device, hipStream_t s);
+// pages host_ids[0 .. n) of F blocks each to the caller's image [n][layer][K or V][slot][kv head][dim], or back
+hipError_t launch_page_image(bf16_t* kv, size_t layer_elems, int n_layers, const int32_t* host_ids, int n, int F, int Hkv, int D, bf16_t* image,
+                             bool to_pool, hipStream_t s);
+struct CompactTile { int32_t dst_block, first, n; };  // tokens [first, first + n) of the kept tokens fill the front of a block
+struct CompactPlan {
+  const int2* chains;        // [n_chains] tiles that one workgroup walks in order
+  const CompactTile* tiles;
+  const int32_t* src;        // per kept token: block * PAGE + slot it comes from
+  const int32_t* turn;       // per kept token: row of `angles`, -1 = not rotated; null: none is
+  const float* angles;       // [turns, D] cos | sin
+};
+hipError_t launch_compact(bf16_t* kv, size_t layer_elems, int n_layers, int Hkv, int D, const CompactPlan& plan, int n_chains, hipStream_t s);

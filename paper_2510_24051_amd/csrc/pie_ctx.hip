@@ -166,6 +166,7 @@ static pie_status pie_create_impl(const pie_model_desc* m, const pie_pool_desc* 
     chk(dev_alloc(&c->en, (size_t)p->max_dist_rows * H, false, c->stream));
     chk(dev_alloc(&c->topk_cand, (size_t)p->max_dist_rows * 16 * std::max(p->max_top_k, 1), false, c->stream));
     chk(dev_alloc(&c->topk_stats, (size_t)p->max_dist_rows * 16 * 2, false, c->stream));
+    chk(dev_alloc(&c->beam_ws, beam_ws_doubles(p->max_dist_rows, m->vocab), false, c->stream));
   }
   // staging for id lists: get_next_dist stages at most max_dist_rows ids, so the serving path never outgrows it
   // (only the seeding / inspection calls may, and they re-allocate)
@@ -220,7 +221,7 @@ extern "C" pie_status pie_destroy(pie_ctx* c) {
   }
   free_packed(c->wlm);
   void* bufs[] = {c->embeds, c->kv, c->xn, c->qkv, c->attn, c->h, c->act, c->splitk, c->logits, c->en,
-                  c->ids_dev, c->inv_freq, c->g_final, c->topk_cand, c->topk_stats, c->table, c->x32, c->lora_dev, c->lora_z, c->gu32};
+                  c->ids_dev, c->inv_freq, c->g_final, c->topk_cand, c->topk_stats, c->beam_ws, c->moves_dev, c->table, c->x32, c->lora_dev, c->lora_z, c->gu32};
   for (LoraPair& lp : c->lora) {
     if (lp.A) (void)hipFree(lp.A);
     if (lp.B) (void)hipFree(lp.B);
@@ -1534,6 +1535,341 @@ extern "C" pie_status pie_batch_work(const pie_batch* b, int64_t* out) {
 }
 
 // ---------------------------------------------------------------------------------------------
+// whole pages: fork, save, restore, compact
+// ---------------------------------------------------------------------------------------------
+namespace {
+// The context's device for the length of a call, where the caller's current one is another.
+struct OnDevice {
+  int before = -1;
+  explicit OnDevice(const pie_ctx* c) {
+    int now = c->device;
+    if (hipGetDevice(&now) == hipSuccess && now != c->device && hipSetDevice(c->device) == hipSuccess) before = now;
+  }
+  ~OnDevice() { if (before >= 0) (void)hipSetDevice(before); }
+};
+
+// Moves dst[i] <- src[i] (all from the pages as they were) as runs in an order that needs no second buffer: a page is written after
+// every move that reads it.  A page that is read is a hub, its moves are emitted together (the source is loaded once), and the
+// hubs form trees (a hub's parent is the page it becomes) some of which end in a cycle.  A tree is one run, deepest hubs first;
+// one hub alone is cut into runs of FORK_FAN pages that are independent of each other.  A cycle c0 <- c1 <- .. <- c0 starts with
+// keeping c0, and its last move stores what was kept.
+#define FORK_FAN 16
+struct ForkPlan {
+  std::vector<PageMove> moves;
+  std::vector<PageRun> runs;
+  ForkPlan(const int32_t* src, const int32_t* dst, int n) {
+    for (int i = 0; i < n; ++i)
+      if (src[i] != dst[i]) given.push_back(PageMove{src[i], dst[i]});
+    std::stable_sort(given.begin(), given.end(), [](const PageMove& a, const PageMove& b) { return a.src < b.src; });
+    std::unordered_map<int32_t, int32_t> hub_of, from;  // page -> its hub; page -> the page it becomes
+    for (size_t i = 0; i < given.size(); ++i) {
+      from[given[i].dst] = given[i].src;
+      if (i == 0 || given[i].src != given[i - 1].src) {
+        hub_of[given[i].src] = (int32_t)first.size();
+        first.push_back((int32_t)i);
+      }
+    }
+    const int n_hubs = (int)first.size();
+    first.push_back((int32_t)given.size());
+    std::vector<int32_t> parent(n_hubs, -1);
+    kids.resize(n_hubs);
+    for (int h = 0; h < n_hubs; ++h) {
+      const auto it = from.find(page(h));
+      if (it == from.end()) continue;
+      parent[h] = hub_of.at(it->second);
+      kids[parent[h]].push_back(h);
+    }
+    std::vector<char> seen(n_hubs, 0);
+    moves.reserve(given.size());
+    for (int h = 0; h < n_hubs; ++h)
+      if (parent[h] < 0) {
+        const int at = (int)moves.size();
+        tree(h, seen);
+        if (kids[h].empty())
+          for (int i = at; i < (int)moves.size(); i += FORK_FAN) runs.push_back(PageRun{i, std::min(FORK_FAN, (int)moves.size() - i), -1});
+        else runs.push_back(PageRun{at, (int)moves.size() - at, -1});
+      }
+    std::vector<int32_t> cycle;
+    for (int h = 0; h < n_hubs; ++h) {
+      if (seen[h]) continue;
+      std::unordered_map<int32_t, int32_t> at_step;  // up from h until the cycle has been walked once
+      int x = h;
+      for (int step = 0; at_step.emplace(x, step).second; ++step) x = parent[x];
+      cycle.clear();
+      for (int y = x;;) {
+        cycle.push_back(y);
+        y = parent[y];
+        if (y == x) break;
+      }
+      const int at = (int)moves.size(), L = (int)cycle.size();
+      for (int y : cycle) seen[y] = 1;
+      for (int y : cycle)
+        for (int k : kids[y])
+          if (!seen[k]) tree(k, seen);
+      const int last = page(cycle[L - 1]);
+      emit(cycle[0], last);
+      for (int k = 1; k < L; ++k) emit(cycle[k], -1);
+      moves.push_back(PageMove{-1, last});
+      runs.push_back(PageRun{at, (int)moves.size() - at, page(cycle[0])});
+    }
+  }
+
+ private:
+  std::vector<PageMove> given;              // by source
+  std::vector<int32_t> first;               // [hubs + 1] into `given`
+  std::vector<std::vector<int32_t>> kids;   // hubs whose page becomes this hub's page
+  std::vector<int32_t> order;
+  int page(int h) const { return given[first[h]].src; }
+  void emit(int h, int but_not_to) {
+    for (int i = first[h]; i < first[h + 1]; ++i)
+      if (given[i].dst != but_not_to) moves.push_back(given[i]);
+  }
+  void tree(int root, std::vector<char>& seen) {
+    order.assign(1, root);
+    seen[root] = 1;
+    for (size_t i = 0; i < order.size(); ++i)
+      for (int k : kids[order[i]]) { seen[k] = 1; order.push_back(k); }
+    for (size_t i = order.size(); i-- > 0;) emit(order[i], -1);  // (children behind their parents: reversed, before them)
+  }
+};
+}  // namespace
+
+// The host image is about to be written: no capture may be under way and the copy of the last image has to be over.
+static pie_status image_begin(pie_ctx* c, const char* who) {
+  hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing(c->stream, &cap) != hipSuccess || cap != hipStreamCaptureStatusNone) {
+    (void)hipGetLastError();
+    return fail(c, PIE_EHIP, "%s: the context's stream is being captured", who);
+  }
+  if (c->blob_in_flight) {
+    const hipError_t e = hipEventSynchronize(c->blob_copied);
+    if (e != hipSuccess) return fail(c, PIE_EHIP, "%s: waiting for the previous copy: %s", who, hipGetErrorString(e));
+    c->blob_in_flight = false;
+  }
+  return PIE_OK;
+}
+
+// Copies the image to the front of the context's block for page plans, which holds `more` bytes behind it as well.
+static pie_status image_send(pie_ctx* c, const Blob& blob, size_t more, const char* who) {
+  if (!blob.ok) return fail(c, PIE_ENOMEM, "%s: no host memory for the plan", who);
+  const size_t need = blob.size + 256 + more;
+  if (need > c->moves_cap) {
+    HIP_TRY(c, hipStreamSynchronize(c->stream));  // no kernel may still read the block that is replaced
+    if (c->moves_dev) (void)hipFree(c->moves_dev);
+    c->moves_dev = nullptr;
+    c->moves_cap = 0;
+    const size_t cap = (std::max(need, (size_t)1 << 18) * 3 / 2 + 255) / 256 * 256;
+    const hipError_t e = hipMalloc(reinterpret_cast<void**>(&c->moves_dev), cap);
+    if (e != hipSuccess) {
+      (void)hipGetLastError();
+      c->moves_dev = nullptr;
+      return fail(c, PIE_ENOMEM, "%s: %s (%zu bytes)", who, hipGetErrorString(e), cap);
+    }
+    c->moves_cap = cap;
+  }
+  HIP_TRY(c, hipMemcpyAsync(c->moves_dev, blob.data(), blob.size, hipMemcpyHostToDevice, c->stream));
+  HIP_TRY(c, c->host_blob_pinned ? hipEventRecord(c->blob_copied, c->stream) : hipStreamSynchronize(c->stream));
+  c->blob_in_flight = c->host_blob_pinned;
+  return PIE_OK;
+}
+
+// A fresh stamp for the marks of the pool's pages.
+static void begin_marks(pie_ctx* c) {
+  if (c->page_marks.size() != (size_t)c->p.n_kv_pages || c->page_mark_id == UINT32_MAX) {
+    c->page_marks.assign((size_t)c->p.n_kv_pages, pie_ctx::PageMark{0, 0, 0, 0});
+    c->page_mark_id = 0;
+  }
+  ++c->page_mark_id;
+}
+
+static pie_status check_pages(pie_ctx* c, const int32_t* ids, int32_t n, const char* who) {
+  for (int i = 0; i < n; ++i)
+    if (ids[i] < 0 || ids[i] >= c->p.n_kv_pages) return fail(c, PIE_ERANGE, "%s: page id %d at %d outside [0, %d)", who, ids[i], i, c->p.n_kv_pages);
+  return PIE_OK;
+}
+
+// Each page named at most once.
+static pie_status check_once(pie_ctx* c, const int32_t* ids, int32_t n, const char* who) {
+  begin_marks(c);
+  for (int i = 0; i < n; ++i) {
+    if (c->page_marks[ids[i]].stamp == c->page_mark_id) return fail(c, PIE_ECONFLICT, "%s: page %d is written twice by one call", who, ids[i]);
+    c->page_marks[ids[i]].stamp = c->page_mark_id;
+  }
+  return PIE_OK;
+}
+
+static pie_status pie_fork_kvpage_impl(pie_ctx* c, const int32_t* src, const int32_t* dst, int32_t n) {
+  if (c->host_only) return fail(c, PIE_EINVAL, "pie_fork_kvpage: the context only plans batches (pie_create_planner)");
+  if (n < 0 || (n > 0 && (!src || !dst))) return fail(c, PIE_EINVAL, "pie_fork_kvpage: null argument");
+  if (pie_status st = check_pages(c, src, n, "pie_fork_kvpage")) return st;
+  if (pie_status st = check_pages(c, dst, n, "pie_fork_kvpage")) return st;
+  if (pie_status st = check_once(c, dst, n, "pie_fork_kvpage")) return st;
+  const ForkPlan plan(src, dst, n);
+  const int n_moves = (int)plan.moves.size(), n_runs = (int)plan.runs.size(), F = c->blocks_per_page;
+  if (n_moves == 0) return PIE_OK;
+  std::vector<uint16_t> masks((size_t)n * F);
+  for (int i = 0; i < n; ++i)
+    for (int f = 0; f < F; ++f) masks[(size_t)i * F + f] = c->page_mask[(size_t)src[i] * F + f];
+  const size_t page_elems = (size_t)F * c->m.n_kv_heads * 2 * PAGE * c->m.head_dim;
+  OnDevice on(c);
+  if (n_moves <= FORK_BY_VALUE) {  // (a run has a move at least)
+    HIP_TRY(c, launch_fork(c->kv, c->kv_layer_elems, c->m.n_layers, page_elems, plan.moves.data(), n_moves, plan.runs.data(), n_runs, false, c->stream));
+  } else {
+    if (pie_status st = image_begin(c, "pie_fork_kvpage")) return st;
+    Blob blob(c);
+    const size_t o_m = blob.add(plan.moves.data(), (size_t)n_moves * sizeof(PageMove)), o_r = blob.add(plan.runs.data(), (size_t)n_runs * sizeof(PageRun));
+    if (pie_status st = image_send(c, blob, 0, "pie_fork_kvpage")) return st;
+    HIP_TRY(c, launch_fork(c->kv, c->kv_layer_elems, c->m.n_layers, page_elems, (const PageMove*)(c->moves_dev + o_m), n_moves,
+                           (const PageRun*)(c->moves_dev + o_r), n_runs, true, c->stream));
+  }
+  for (int i = 0; i < n; ++i)
+    for (int f = 0; f < F; ++f) c->page_mask[(size_t)dst[i] * F + f] = masks[(size_t)i * F + f];
+  return PIE_OK;
+}
+
+extern "C" pie_status pie_fork_kvpage(pie_ctx* c, const int32_t* src_pages, const int32_t* dst_pages, int32_t n) {
+  if (!c) return PIE_EINVAL;
+  return guarded(c, "pie_fork_kvpage", [&]() { return pie_fork_kvpage_impl(c, src_pages, dst_pages, n); });
+}
+
+static pie_status page_image(pie_ctx* c, const int32_t* ids, int32_t n, void* image, bool to_pool, const char* who) {
+  if (c->host_only) return fail(c, PIE_EINVAL, "%s: the context only plans batches (pie_create_planner)", who);
+  if (n < 0 || (n > 0 && (!ids || !image))) return fail(c, PIE_EINVAL, "%s: null argument", who);
+  if (n > 0 && (uintptr_t)image % 16) return fail(c, PIE_EINVAL, "%s: the image must start at a multiple of 16 bytes", who);
+  if (pie_status st = check_pages(c, ids, n, who)) return st;
+  if (to_pool)
+    if (pie_status st = check_once(c, ids, n, who)) return st;
+  if (n == 0) return PIE_OK;
+  OnDevice on(c);
+  HIP_TRY(c, launch_page_image(c->kv, c->kv_layer_elems, c->m.n_layers, ids, n, c->blocks_per_page, c->m.n_kv_heads, c->m.head_dim, (bf16_t*)image,
+                               to_pool, c->stream));
+  return PIE_OK;
+}
+
+extern "C" pie_status pie_save_kvpage(pie_ctx* c, const int32_t* page_ids, int32_t n, void* image) {
+  if (!c) return PIE_EINVAL;
+  return guarded(c, "pie_save_kvpage", [&]() { return page_image(c, page_ids, n, image, false, "pie_save_kvpage"); });
+}
+
+extern "C" pie_status pie_restore_kvpage(pie_ctx* c, const int32_t* page_ids, int32_t n, const void* image) {
+  if (!c) return PIE_EINVAL;
+  return guarded(c, "pie_restore_kvpage", [&]() { return page_image(c, page_ids, n, const_cast<void*>(image), true, "pie_restore_kvpage"); });
+}
+
+#define COMPACT_CHAIN 4  // tiles of a chain where the order of the tiles does not matter
+static pie_status pie_compact_kvpage_impl(pie_ctx* c, int32_t S, const int32_t* page_indptr, const int32_t* page_ids, const int32_t* kv_len,
+                                          const int32_t* dst_indptr, const int32_t* dst_ids, const int32_t* shifts, int32_t* out_kv_len) {
+  const char* who = "pie_compact_kvpage";
+  if (c->host_only) return fail(c, PIE_EINVAL, "%s: the context only plans batches (pie_create_planner)", who);
+  if (S < 0 || (S > 0 && (!page_indptr || !kv_len || !out_kv_len)) || !dst_indptr != !dst_ids) return fail(c, PIE_EINVAL, "%s: null argument", who);
+  if (S == 0) return PIE_OK;
+  const int P = c->m.page_size, F = c->blocks_per_page, D = c->m.head_dim;
+  const bool apart = dst_indptr != nullptr;
+  if (!apart) dst_indptr = page_indptr, dst_ids = page_ids;
+  if (page_indptr[0] != 0 || dst_indptr[0] != 0) return fail(c, PIE_EINVAL, "%s: page tables must start at 0", who);
+  int64_t total = 0;
+  for (int s = 0; s < S; ++s) {
+    if (page_indptr[s + 1] < page_indptr[s] || dst_indptr[s + 1] < dst_indptr[s]) return fail(c, PIE_EINVAL, "%s: bad page table offsets", who);
+    if (kv_len[s] < 0 || (int64_t)(page_indptr[s + 1] - page_indptr[s]) * P < kv_len[s])
+      return fail(c, PIE_EINVAL, "%s: sequence %d has %d pages for %d tokens", who, s, page_indptr[s + 1] - page_indptr[s], kv_len[s]);
+    total += kv_len[s];
+  }
+  if (total > 0 && !page_ids) return fail(c, PIE_EINVAL, "%s: null argument", who);
+  if (total > (1 << 30)) return fail(c, PIE_EBATCH, "%s: %lld tokens in one call", who, (long long)total);
+  if (page_ids)
+    if (pie_status st = check_pages(c, page_ids, page_indptr[S], who)) return st;
+  if (apart)
+    if (pie_status st = check_pages(c, dst_ids, dst_indptr[S], who)) return st;
+
+  begin_marks(c);
+  auto& marks = c->page_marks;
+  const uint32_t id = c->page_mark_id;
+  enum { LISTED = 1, MANY = 2, WRITTEN = 4 };
+  for (int s = 0; s < S; ++s)
+    for (int j = 0; j * P < kv_len[s]; ++j) {
+      pie_ctx::PageMark& m = marks[page_ids[page_indptr[s] + j]];
+      if (m.stamp != id) m = pie_ctx::PageMark{id, s, j, LISTED};
+      else m.flags |= MANY;
+    }
+  std::vector<int32_t> src, turn, turns, kept(S);
+  std::vector<CompactTile> tiles;
+  std::vector<int2> chains;
+  src.reserve((size_t)total);
+  if (shifts) turn.reserve((size_t)total);
+  int64_t off = 0;
+  for (int s = 0; s < S; ++s) {
+    const int32_t* from = page_ids + page_indptr[s];
+    const int32_t* to = dst_ids + dst_indptr[s];
+    const int n_to = dst_indptr[s + 1] - dst_indptr[s], first = (int)src.size();
+    int n = 0, moved = -1;  // kept tokens so far; the first of them that does not stay as it is
+    for (int j = 0; j * PAGE < kv_len[s]; ++j) {
+      const int block = from[j / F] * F + j % F;
+      uint32_t bits = c->page_mask[block];
+      if (kv_len[s] - j * PAGE < PAGE) bits &= (1u << (kv_len[s] - j * PAGE)) - 1u;
+      for (; bits; bits &= bits - 1u, ++n) {
+        const int slot = __builtin_ctz(bits);
+        if (n / P >= n_to) return fail(c, PIE_EINVAL, "%s: sequence %d keeps more tokens than its %d destination pages hold", who, s, n_to);
+        const int32_t by = shifts ? shifts[off + j * PAGE + slot] : 0;
+        src.push_back(block * PAGE + slot);
+        if (shifts) {
+          if (by != 0 && (turns.empty() || turns.back() != by)) turns.push_back(by);
+          turn.push_back(by != 0 ? (int32_t)turns.size() - 1 : -1);
+        }
+        if (moved < 0 && (by != 0 || (to[n / P] * F + n % P / PAGE) * PAGE + n % PAGE != src.back())) moved = n;
+      }
+    }
+    kept[s] = n;
+    off += kv_len[s];
+    if (moved < 0) continue;
+    const int tile0 = (int)tiles.size();
+    bool in_order = false;  // a page that is written is read by the same sequence
+    for (int i = moved / PAGE; i * PAGE < n; ++i) {
+      if (i == moved / PAGE || i % F == 0) {
+        const int j = i / F;
+        pie_ctx::PageMark& m = marks[to[j]];
+        if (m.stamp != id) m = pie_ctx::PageMark{id, s, j, 0};
+        if ((m.flags & WRITTEN) || ((m.flags & LISTED) && ((m.flags & MANY) || m.seq != s || m.index != j)))
+          return fail(c, PIE_ECONFLICT, "%s: page %d of sequence %d is written and is in another place of the tables as well", who, to[j], s);
+        in_order |= (m.flags & LISTED) != 0;
+        m.flags |= WRITTEN;
+      }
+      tiles.push_back(CompactTile{to[i / F] * F + i % F, first + i * PAGE, std::min(PAGE, n - i * PAGE)});
+    }
+    const int step = in_order ? (int)tiles.size() - tile0 : COMPACT_CHAIN;
+    for (int t = tile0; t < (int)tiles.size(); t += step) chains.push_back(make_int2(t, std::min(t + step, (int)tiles.size())));
+  }
+  if (!chains.empty()) {
+    OnDevice on(c);
+    if (pie_status st = image_begin(c, who)) return st;
+    Blob blob(c);
+    const size_t o_c = blob.add(chains.data(), chains.size() * sizeof(int2)), o_t = blob.add(tiles.data(), tiles.size() * sizeof(CompactTile));
+    const size_t o_s = blob.add(src.data(), src.size() * 4), o_i = turns.empty() ? 0 : blob.add(turn.data(), turn.size() * 4);
+    const size_t o_v = turns.empty() ? 0 : blob.add(turns.data(), turns.size() * 4);
+    const size_t o_a = (blob.size + 255) / 256 * 256;
+    if (pie_status st = image_send(c, blob, turns.size() * D * sizeof(float), who)) return st;
+    unsigned char* d = c->moves_dev;
+    if (!turns.empty()) HIP_TRY(c, launch_rope_table((const int32_t*)(d + o_v), c->inv_freq, (int)turns.size(), D, (float*)(d + o_a), c->stream));
+    const CompactPlan plan{(const int2*)(d + o_c), (const CompactTile*)(d + o_t), (const int32_t*)(d + o_s),
+                           turns.empty() ? nullptr : (const int32_t*)(d + o_i), (const float*)(d + o_a)};
+    HIP_TRY(c, launch_compact(c->kv, c->kv_layer_elems, c->m.n_layers, c->m.n_kv_heads, D, plan, (int)chains.size(), c->stream));
+  }
+  for (int s = 0; s < S; ++s) {
+    for (int j = 0; j * P < kept[s]; ++j)
+      for (int f = 0; f < F; ++f) c->page_mask[(size_t)dst_ids[dst_indptr[s] + j] * F + f] = 0xFFFFu;
+    out_kv_len[s] = kept[s];
+  }
+  return PIE_OK;
+}
+
+extern "C" pie_status pie_compact_kvpage(pie_ctx* c, int32_t n_seqs, const int32_t* page_indptr, const int32_t* page_ids, const int32_t* kv_len,
+                                         const int32_t* dst_page_indptr, const int32_t* dst_page_ids, const int32_t* shifts, int32_t* out_kv_len) {
+  if (!c) return PIE_EINVAL;
+  return guarded(c, "pie_compact_kvpage", [&]() {
+    return pie_compact_kvpage_impl(c, n_seqs, page_indptr, page_ids, kv_len, dst_page_indptr, dst_page_ids, shifts, out_kv_len);
+  });
+}
+
+// ---------------------------------------------------------------------------------------------
 // forward
 // ---------------------------------------------------------------------------------------------
 namespace {
@@ -1806,11 +2142,10 @@ struct DistBuffers {
   unsigned long long* cand;  // [n, chunks, k]
   float* stats;              // [n, chunks, 2]
 };
-static pie_status run_dist(pie_ctx* c, const DistBuffers& w, int32_t n, int32_t top_k, float temperature,
-                           int32_t* out_ids, float* out_probs) {
+// Final norm and LM head: w.logits.
+static pie_status run_logits(pie_ctx* c, const DistBuffers& w, int32_t n, StageTimer& tm) {
   const int H = c->m.hidden, V = c->m.vocab;
   hipStream_t s = c->stream;
-  StageTimer tm(c, PIE_STAGE_HEAD_NORM, PIE_STAGE_TOPK);
   const bool few = c->g_final && w.ids_on_host && few_rows_ok(n, c->wlm, EPI_STORE_F32, FEW_EMBED_ARGS);
   if (!few) {
     tm.begin(PIE_STAGE_HEAD_NORM);
@@ -1824,11 +2159,18 @@ static pie_status run_dist(pie_ctx* c, const DistBuffers& w, int32_t n, int32_t 
   if (few) HIP_TRY(c, launch_few_f32(FewSource{FEW_EMBED_ARGS, c->embeds, H, w.ids, c->g_final, c->m.rms_eps}, n, c->wlm, w.logits, c->wave_slots / 8, s));
   else HIP_TRY(c, launch_gemm(w.en, H, n, c->wlm, e, w.splitk, w.splitk_elems, c->wave_slots / 8, s));
   tm.end(PIE_STAGE_LM_HEAD);
-  tm.begin(PIE_STAGE_TOPK);
-  HIP_TRY(c, launch_topk(w.logits, n, V, top_k, 1.0f / temperature, out_ids, out_probs, w.cand, w.stats, s));
-  tm.end(PIE_STAGE_TOPK);
   c->last_dist_n = n;
   c->last_logits = w.logits;
+  return PIE_OK;
+}
+
+static pie_status run_dist(pie_ctx* c, const DistBuffers& w, int32_t n, int32_t top_k, float temperature,
+                           int32_t* out_ids, float* out_probs) {
+  StageTimer tm(c, PIE_STAGE_HEAD_NORM, PIE_STAGE_TOPK);
+  if (pie_status st = run_logits(c, w, n, tm)) return st;
+  tm.begin(PIE_STAGE_TOPK);
+  HIP_TRY(c, launch_topk(w.logits, n, c->m.vocab, top_k, 1.0f / temperature, out_ids, out_probs, w.cand, w.stats, c->stream));
+  tm.end(PIE_STAGE_TOPK);
   return PIE_OK;
 }
 
@@ -1904,6 +2246,75 @@ static pie_status pie_forward_dist_impl(pie_ctx* c, const pie_batch* b, const in
 extern "C" pie_status pie_forward_dist(pie_ctx* c, const pie_batch* b, const int32_t* rows, int32_t n, int32_t top_k,
                                        float temperature, int32_t* out_ids, float* out_probs) {
   return guarded(c, "pie_forward_dist", [&]() { return pie_forward_dist_impl(c, b, rows, n, top_k, temperature, out_ids, out_probs); });
+}
+
+// ---------------------------------------------------------------------------------------------
+// beams
+// ---------------------------------------------------------------------------------------------
+// Checks a search over rows of n_vocab logits; on success *rows is their number.
+static pie_status check_beams(pie_ctx* c, const pie_beam_search* b, int32_t n_vocab, const void* out_beams, const void* out_tokens,
+                              const void* out_scores, int32_t* rows, const char* who) {
+  if (!b || !b->group_indptr || b->n_groups <= 0) return fail(c, PIE_EINVAL, "%s: null search or no groups", who);
+  if (!out_beams || !out_tokens || !out_scores) return fail(c, PIE_EINVAL, "%s: null output", who);
+  if (!c->beam_ws) return fail(c, PIE_EINVAL, "%s: context created without vocab / dist rows", who);
+  if (!(b->temperature > 0.f) || !std::isfinite(b->temperature)) return fail(c, PIE_EINVAL, "temperature must be positive and finite");
+  if (b->group_indptr[0] != 0) return fail(c, PIE_EINVAL, "%s: group_indptr must start at 0", who);
+  for (int g = 0; g < b->n_groups; ++g) {
+    const int64_t n = (int64_t)b->group_indptr[g + 1] - b->group_indptr[g];
+    if (n < 0) return fail(c, PIE_EINVAL, "%s: group_indptr decreases at %d", who, g);
+    if (n > BEAM_MAX_ROWS) return fail(c, PIE_EBATCH, "%s: group %d has %lld beams, at most %d are taken", who, g, (long long)n, BEAM_MAX_ROWS);
+  }
+  *rows = b->group_indptr[b->n_groups];
+  if (*rows > c->p.max_dist_rows) return fail(c, PIE_EBATCH, "%s: %d rows exceed max_dist_rows %d", who, *rows, c->p.max_dist_rows);
+  if (b->n_out <= 0 || b->n_out > BEAM_MAX_OUT) return fail(c, PIE_ERANGE, "%s: n_out %d outside [1, %d]", who, b->n_out, BEAM_MAX_OUT);
+  if (b->finished && (b->eos_token < 0 || b->eos_token >= n_vocab))
+    return fail(c, PIE_ERANGE, "%s: eos token %d outside [0, %d)", who, b->eos_token, n_vocab);
+  return PIE_OK;
+}
+
+static pie_status run_beams(pie_ctx* c, const pie_beam_search* b, const void* logits, int dtype, int64_t stride, int n_vocab, int32_t* out_beams,
+                            int32_t* out_tokens, float* out_scores) {
+  const BeamArgs a{logits, dtype, stride, n_vocab, b->scores, b->finished, b->eos_token, b->group_indptr, b->n_groups, b->n_out,
+                   1.0 / (double)b->temperature, c->beam_ws, out_beams, out_tokens, out_scores};
+  HIP_TRY(c, launch_beam_select(a, c->stream));
+  return PIE_OK;
+}
+
+extern "C" pie_status pie_beam_select(pie_ctx* c, const pie_beam_search* b, const void* logits, int32_t dtype, int64_t row_stride, int32_t n_vocab,
+                                      int32_t* out_beams, int32_t* out_tokens, float* out_scores) {
+  if (!c) return PIE_EINVAL;
+  if (c->host_only) return fail(c, PIE_EINVAL, "pie_beam_select: the context only plans batches (pie_create_planner)");
+  if (n_vocab <= 0 || n_vocab > c->m.vocab) return fail(c, PIE_ERANGE, "pie_beam_select: %d logits a row outside [1, vocab %d]", n_vocab, c->m.vocab);
+  int32_t rows = 0;
+  if (pie_status st = check_beams(c, b, n_vocab, out_beams, out_tokens, out_scores, &rows, "pie_beam_select")) return st;
+  if (dtype != PIE_F32 && dtype != PIE_BF16 && dtype != PIE_F16) return fail(c, PIE_EINVAL, "pie_beam_select: unknown type %d", dtype);
+  if (rows > 0 && (!logits || row_stride < n_vocab)) return fail(c, PIE_EINVAL, "pie_beam_select: null logits, or rows closer than they are long");
+  if ((uintptr_t)logits % (dtype == PIE_F32 ? 4 : 2)) return fail(c, PIE_EINVAL, "pie_beam_select: logits must start at a multiple of their size");
+  OnDevice on(c);
+  return run_beams(c, b, logits, dtype, row_stride, n_vocab, out_beams, out_tokens, out_scores);
+}
+
+extern "C" pie_status pie_get_next_beams(pie_ctx* c, const pie_beam_search* b, const int32_t* embed_ids, int32_t* out_beams, int32_t* out_tokens,
+                                         float* out_scores) {
+  if (!c) return PIE_EINVAL;
+  if (c->host_only) return fail(c, PIE_EINVAL, "pie_get_next_beams: the context only plans batches (pie_create_planner)");
+  int32_t n = 0;
+  if (pie_status st = check_beams(c, b, c->m.vocab, out_beams, out_tokens, out_scores, &n, "pie_get_next_beams")) return st;
+  if (!embed_ids || n == 0) return fail(c, PIE_EINVAL, "pie_get_next_beams: null ids or no rows");
+  if (!c->head_loaded) return fail(c, PIE_EINVAL, "pie_get_next_beams: no LM head loaded");
+  for (int i = 0; i < n; ++i)
+    if (embed_ids[i] < 0 || embed_ids[i] >= c->p.n_embeds) return fail(c, PIE_ERANGE, "embed id %d at %d outside [0, %d)", embed_ids[i], i, c->p.n_embeds);
+  OnDevice on(c);
+  const bool by_value = n <= IDS_BY_VALUE;
+  if (!by_value)
+    if (pie_status st = stage_ids(c, embed_ids, nullptr, n)) return st;
+  const DistBuffers w{by_value ? embed_ids : c->ids_dev, by_value, c->en, c->logits, c->splitk, c->splitk_elems, c->topk_cand, c->topk_stats};
+  StageTimer tm(c, PIE_STAGE_HEAD_NORM, PIE_STAGE_TOPK);
+  if (pie_status st = run_logits(c, w, n, tm)) return st;
+  tm.begin(PIE_STAGE_TOPK);
+  const pie_status st = run_beams(c, b, c->logits, PIE_F32, c->m.vocab, c->m.vocab, out_beams, out_tokens, out_scores);
+  tm.end(PIE_STAGE_TOPK);
+  return st;
 }
 
 extern "C" pie_status pie_synchronize(pie_ctx* c) {

@@ -1,0 +1,355 @@
+"""Host paths of the page calls and of the beam selection without a GPU: the plans of forks and compactions are read from what the
+library copies to the device (a stand-in for the HIP runtime, fake_hip.cpp) and carried out here; and every refusal."""
+import ctypes as C
+import os
+import subprocess
+import sys
+from types import SimpleNamespace
+
+import numpy as np
+import pytest
+
+from test_host_runtime_paths import MODEL, Child, fake  # noqa: F401  (the fixture builds the stand-in)
+
+INVALID, RANGE, BATCH, CONFLICT, MEMORY, HIP = -1, -2, -3, -4, -5, -6
+
+
+def up(n):
+    return (n + 255) // 256 * 256
+
+
+def i32(a):
+    return np.ascontiguousarray(a, dtype=np.int32)
+
+
+def at(a):
+    return None if a is None else a.ctypes.data_as(C.c_void_p)
+
+
+def last_image(c, ctx):
+    ctx.synchronize()
+    return c.copies()[-1]
+
+
+def carry_out(image, pages):
+    """The moves of a fork, as its kernel walks them: runs one after the other in any order, here the last one first."""
+    for split in range(1, len(image) // 8):  # moves [n] of 8 bytes, at the next multiple of 256 runs of 12
+        if up(split * 8) < len(image) and (len(image) - up(split * 8)) % 12 == 0:
+            runs = np.frombuffer(image, np.int32, offset=up(split * 8)).reshape(-1, 3)
+            if runs[:, 1].sum() == split and runs[0, 0] == 0 and (runs[1:, 0] == runs[:-1].sum(1) - runs[:-1, 2]).all() and (runs[:, 1] > 0).all():
+                break
+    moves = np.frombuffer(image, np.int32, count=2 * split).reshape(-1, 2)
+    for first, n, keep in runs[::-1]:
+        kept = pages[keep] if keep >= 0 else None
+        for src, dst in moves[first:first + n]:
+            pages[dst] = kept if src < 0 else pages[src]
+    return len(moves), len(runs)
+
+
+def fork_plans(c):
+    """Random graphs of moves, long enough that the plan is copied: carrying the runs out in order gives every page what its
+    source was, whichever run goes first."""
+    ctx = c.context(n_pages=2000)
+    rng = np.random.default_rng(5)
+    for form in ("random", "permutation", "rotation", "chain", "fan", "beams", "pairs"):
+        for _ in range(6):
+            n = int(rng.integers(200, 900))
+            dst = rng.permutation(2000)[:n]
+            if form == "random":
+                src = rng.integers(0, 2000, n)
+            elif form == "permutation":
+                src = rng.permutation(dst)
+            elif form == "rotation":
+                src = np.roll(dst, 1)
+            elif form == "chain":
+                src = np.concatenate([[int(np.setdiff1d(np.arange(2000), dst)[0])], dst[:-1]])
+            elif form == "fan":
+                src = rng.choice(np.setdiff1d(np.arange(2000), dst), 3)[rng.integers(0, 3, n)]
+            elif form == "beams":
+                src = dst[np.arange(n) // 8 * 8 + np.minimum(rng.integers(0, 8, n), n - 1 - np.arange(n) // 8 * 8)]
+            else:
+                src = np.setdiff1d(np.arange(2000), dst)[:n]
+                dst = dst[:len(src)]
+            before = np.arange(2000)
+            want, got = before.copy(), before.copy()
+            want[dst] = before[src]
+            moving = int((src != dst).sum())
+            if moving <= 160:
+                continue
+            ctx.fork_kvpage(src, dst)
+            n_moves, n_runs = carry_out(last_image(c, ctx), got)
+            assert np.array_equal(got, want), form
+            cycles = n_moves - moving
+            assert 0 <= cycles and (form != "rotation" or (cycles == 0 and n_runs == 1)), (form, cycles, n_runs)
+    ctx.close()
+
+
+def fork_masks(c):
+    """Masks go with the pages, as they were before the call; also where nothing is copied to the device."""
+    for page_size in (16, 32):
+        m = SimpleNamespace(**{**vars(MODEL), "page_size": page_size})
+        ctx = c.context(n_pages=64, m=m)
+        ctx.mask_kvpage([0, 1, 2], [0x1, 0x3, 0x7])
+        ctx.fork_kvpage([0, 1, 2, 2], [1, 2, 0, 9])  # a cycle and a copy
+        # page 1 now has one visible token, 2 two, 0 and 9 three: a decode request over each sees one page of them
+        lens = {0: 3, 1: 1, 2: 2, 9: 3, 5: page_size}
+        for p, n in lens.items():
+            out = np.zeros(1, np.int32)
+            assert ctx.compact_kvpage([0, 1], [p], [page_size], dst_page_indptr=[0, 1], dst_page_ids=[40])[0] == n
+        ctx.close()
+
+
+def compact_plans(c):
+    """Ragged sequences, both page sizes, in place and apart, with shifts: the chains, carried out in any order, leave what a
+    simultaneous move leaves, and tiles of a chain that has to go in order never read what an earlier one wrote."""
+    rng = np.random.default_rng(8)
+    for trial in range(60):
+        P = int(rng.choice([16, 32]))
+        F = P // 16
+        m = SimpleNamespace(**{**vars(MODEL), "page_size": P})
+        ctx = c.context(n_pages=400, m=m)
+        S = int(rng.integers(1, 5))
+        lens = rng.integers(0, 20 * P // F, S)
+        lens[rng.integers(0, S)] = rng.choice([0, 1, 15, 16, 17, P, 6 * P])
+        n_pages = -(-lens // P) + rng.integers(0, 2, S)
+        ids = rng.permutation(400)
+        ip = np.concatenate([[0], np.cumsum(n_pages)])
+        table = ids[:ip[-1]]
+        bits = rng.integers(0, 1 << 32, len(table), dtype=np.uint64) & (rng.integers(0, 1 << 32, len(table), dtype=np.uint64) | np.uint64(0xFF))
+        bits[rng.random(len(table)) < 0.3] = 0xFFFFFFFF
+        bits[rng.random(len(table)) < 0.2] = 0
+        if len(table):
+            ctx.mask_kvpage(table, bits)
+        visible = [np.array([(int(bits[ip[s] + j // P]) >> (j % P)) & 1 for j in range(lens[s])], bool) for s in range(S)]
+        shifts = np.concatenate([np.where(rng.random(n) < 0.5, 0, rng.integers(-3, 4, n)) for n in lens] or [[]]) if trial % 3 else None
+        apart = trial % 2 == 0
+        kept = [int(v.sum()) for v in visible]
+        dp = np.concatenate([[0], np.cumsum([-(-k // P) for k in kept])]) if apart else None
+        di = ids[ip[-1]:ip[-1] + dp[-1]] if apart else None
+        n0 = len(c.copies())
+        got = ctx.compact_kvpage(ip, table, lens, shifts=shifts, dst_page_indptr=dp, dst_page_ids=di)
+        assert got.tolist() == kept
+        pool = np.arange(400 * P).astype(object)
+        want = pool.copy()
+        off = 0
+        for s in range(S):
+            into = di[dp[s]:dp[s + 1]] if apart else table[ip[s]:ip[s + 1]]
+            for i, j in enumerate(np.nonzero(visible[s])[0]):
+                by = 0 if shifts is None else int(shifts[off + j])
+                token = int(table[ip[s] + j // P]) * P + j % P
+                want[int(into[i // P]) * P + i % P] = (token, by) if by else token
+            off += lens[s]
+        ctx.synchronize()
+        if len(c.copies()) == n0:
+            assert all(want == pool)
+            ctx.close()
+            continue
+        image = c.copies()[-1]
+        # chains, tiles, sources, then, where a key turns, rows of the table and the shifts, each at a multiple of 256
+        ints = np.frombuffer(image, np.int32)
+        n_tiles, k = 0, 0
+        while 2 * k < len(ints) and ints[2 * k] == n_tiles and ints[2 * k + 1] > n_tiles:
+            n_tiles, k = int(ints[2 * k + 1]), k + 1
+        chains = ints[:2 * k].reshape(-1, 2)
+        o = up(8 * k) // 4
+        tiles = ints[o:o + 3 * n_tiles].reshape(-1, 3)
+        o = up(4 * (o + 3 * n_tiles)) // 4
+        n_src = sum(kept)
+        src = ints[o:o + n_src]
+        turning = any(isinstance(x, tuple) for x in want)
+        turn = np.full(n_src, -1)
+        if turning:
+            o = up(4 * (o + n_src)) // 4
+            turn = ints[o:o + n_src]
+            turns = ints[up(4 * (o + n_src)) // 4:]
+            assert turn.max() == len(turns) - 1
+        have = pool.copy()
+        for a, b in chains[::-1]:
+            for block, first, n in tiles[a:b]:
+                assert 0 < n <= 16
+                moved = [(have[x], int(turns[w])) if w >= 0 else have[x] for x, w in zip(src[first:first + n], turn[first:first + n])]
+                have[block * 16:block * 16 + n] = moved  # (block * 16 + slot counts tokens as page * P + slot does)
+        assert all(x == y for x, y in zip(have, want)), trial
+        ctx.close()
+
+
+def raw(ctx, name, *args):
+    return getattr(ctx.lib, name)(ctx.ctx, *args)
+
+
+def page_refusals(c):
+    ctx = c.context(n_pages=32, layers=2)
+    a, b, one = i32([0, 1]), i32([2, 3]), i32([0, 1])
+    big = np.zeros(64, np.int8)
+    image = C.c_void_p((big.ctypes.data + 15) // 16 * 16)
+    odd = C.c_void_p(image.value + 2)
+    p = c.Pie.planner(MODEL, 32, 16, 8, 4)
+    assert c.status(lambda: p.fork_kvpage([0], [1]))[0] == INVALID
+    assert c.status(lambda: p.compact_kvpage([0, 1], [0], [3]))[0] == INVALID
+    assert raw(p, "pie_save_kvpage", at(a), 2, image) == INVALID and raw(p, "pie_restore_kvpage", at(a), 2, image) == INVALID
+    assert raw(ctx, "pie_fork_kvpage", None, at(b), 2) == INVALID and raw(ctx, "pie_fork_kvpage", at(a), at(b), -1) == INVALID
+    assert raw(ctx, "pie_fork_kvpage", None, None, 0) == 0
+    assert c.status(lambda: ctx.fork_kvpage([0, 32], [1, 2]))[0] == RANGE and c.status(lambda: ctx.fork_kvpage([0, 1], [-1, 2]))[0] == RANGE
+    assert c.status(lambda: ctx.fork_kvpage([0, 1], [2, 2]))[0] == CONFLICT
+    for name in ("pie_save_kvpage", "pie_restore_kvpage"):
+        assert raw(ctx, name, at(a), 2, None) == INVALID and raw(ctx, name, at(a), 2, odd) == INVALID and raw(ctx, name, at(a), -1, image) == INVALID
+        assert raw(ctx, name, None, 0, None) == 0
+        assert raw(ctx, name, at(i32([0, 32])), 2, image) == RANGE
+    assert raw(ctx, "pie_restore_kvpage", at(i32([4, 4])), 2, image) == CONFLICT and raw(ctx, "pie_save_kvpage", at(i32([4, 4])), 2, image) == 0
+    com = lambda *x, **k: c.status(lambda: ctx.compact_kvpage(*x, **k))  # noqa: E731
+    assert com([0, 1], [32], [3])[0] == RANGE and com([0, 1], [-1], [3])[0] == RANGE
+    assert com([0, 1], [0], [17])[0] == INVALID and com([0, 1], [0], [-1])[0] == INVALID and com([1, 1], [0], [0])[0] == INVALID
+    assert com([0, 2, 1, 2], [0, 1], [0, 0, 0])[0] == INVALID
+    assert com([0, 1], [0], [16], dst_page_indptr=[0, 0], dst_page_ids=[])[0] == INVALID  # (16 tokens kept, no page for them)
+    assert com([0, 1], [0], [16], dst_page_indptr=[0, 1], dst_page_ids=[33])[0] == RANGE
+    lens, out = i32([3]), i32([0])
+    assert raw(ctx, "pie_compact_kvpage", 1, at(i32([0, 1])), at(a), at(lens), at(i32([0, 1])), None, None, at(out)) == INVALID
+    assert raw(ctx, "pie_compact_kvpage", 1, at(i32([0, 1])), None, at(lens), None, None, None, at(out)) == INVALID
+    assert raw(ctx, "pie_compact_kvpage", 1, at(i32([0, 1])), at(a), at(lens), None, None, None, None) == INVALID
+    assert raw(ctx, "pie_compact_kvpage", -1, None, None, None, None, None, None, None) == INVALID
+    assert raw(ctx, "pie_compact_kvpage", 0, None, None, None, None, None, None, None) == 0
+    # pages that two sequences share may stay, but not be written
+    ctx.mask_kvpage([5], [0xFFFE])
+    assert com([0, 2, 4], [4, 5, 4, 6], [32, 32])[0] == 0
+    ctx.mask_kvpage([5], [0xFFFE])
+    assert com([0, 2, 4], [4, 5, 5, 6], [32, 32])[0] == CONFLICT  # page 5 is written by the first and read by the second
+    assert com([0, 2, 4], [4, 5, 7, 6], [32, 32], shifts=np.r_[np.zeros(32), np.ones(32)])[0] == 0
+    assert com([0, 2, 4], [4, 6, 4, 7], [32, 32], shifts=np.ones(64))[0] == CONFLICT
+    assert com([0, 1, 2], [4, 5], [16, 16], dst_page_indptr=[0, 1, 2], dst_page_ids=[8, 8])[0] == CONFLICT
+    assert com([0, 2], [8, 9], [32], dst_page_indptr=[0, 2], dst_page_ids=[9, 8])[0] == CONFLICT
+    assert com([0, 2], [8, 9], [32], dst_page_indptr=[0, 2], dst_page_ids=[8, 10])[0] == 0  # (the first page is its own destination)
+    # nothing of a refused call has happened: the mask of page 5 is as it was set
+    ctx.mask_kvpage([5], [0x00FF])
+    assert com([0, 2], [5, 5], [32])[0] == CONFLICT
+    assert ctx.compact_kvpage([0, 1], [5], [16], dst_page_indptr=[0, 1], dst_page_ids=[20])[0] == 8
+    ctx.close()
+
+
+def captured(c):
+    """While the stream is captured, calls whose plans fit the kernel arguments are taken and the others refused before the runtime is
+    asked for anything."""
+    ctx = c.context(n_pages=1024)
+    ctx.compact_kvpage([0, 4], [0, 1, 2, 3], [60], shifts=np.ones(60))  # a copy is in flight
+    c.fake.fake_capturing(1)
+    calls = c.fake.fake_event_syncs(), c.fake.fake_allocations()
+    ctx.fork_kvpage(np.arange(160), 500 + np.arange(160))
+    for call in (lambda: ctx.fork_kvpage(np.arange(161), 500 + np.arange(161)), lambda: ctx.compact_kvpage([0, 1], [7], [16], shifts=np.ones(16))):
+        st, msg = c.status(call)
+        assert st == HIP and "captured" in msg
+    assert calls == (c.fake.fake_event_syncs(), c.fake.fake_allocations())
+    c.fake.fake_capturing(0)
+    ctx.fork_kvpage(np.arange(161), 500 + np.arange(161))
+    ctx.close()
+
+
+def images_in_flight(c):
+    """Batches and page plans share the host image: each copy gets what its call wrote."""
+    from test_host_runtime_paths import batch_of
+    ctx = c.context(n_pages=2000)
+    src = np.arange(300)
+    ctx.fork_kvpage(src, 1000 + src)
+    want = [last_image(c, ctx)]
+    ctx.batch_create(batch_of([(1, 40), (20, 5)])).destroy()
+    want.append(last_image(c, ctx))
+    n0 = len(c.copies())
+    ctx.fork_kvpage(src, 1000 + src)
+    b = ctx.batch_create(batch_of([(1, 40), (20, 5)]))
+    c.fake.fake_fail_event_syncs(1)
+    assert c.status(lambda: ctx.fork_kvpage(src[::-1], 1000 + src))[0] == HIP
+    ctx.fork_kvpage(src[::-1], 1000 + src)
+    ctx.synchronize()
+    assert c.copies()[n0:n0 + 2] == want
+    b.destroy()
+    ctx.close()
+
+
+def no_memory(c):
+    """Every C++ allocation of a call in turn fails, and the device block: PIE_ENOMEM, and the next call does its work."""
+    for call in (lambda x: x.fork_kvpage(np.roll(np.arange(200), 1), np.arange(200)),
+                 lambda x: x.compact_kvpage([0, 20], np.arange(20), [300], shifts=np.arange(300))):
+        failed = 0
+        for k in range(1, 4000):
+            ctx = c.context(n_pages=1024)
+            ctx.mask_kvpage([0], [0xFFF0])
+            c.fake.fake_fail_new_at(k)
+            st = c.status(lambda: call(ctx))[0]
+            hit = c.fake.fake_new_failed()
+            c.fake.fake_fail_new_at(0)
+            assert st == (MEMORY if hit else 0), (k, st)
+            if hit:
+                call(ctx)
+            ctx.close()
+            if not hit:
+                break
+            failed += 1
+        assert failed > 3
+        ctx = c.context(n_pages=1024)
+        ctx.mask_kvpage([0], [0xFFF0])
+        c.fake.fake_malloc_limit(1)
+        assert c.status(lambda: call(ctx))[0] == MEMORY
+        c.fake.fake_malloc_limit(1 << 62)
+        call(ctx)
+        ctx.close()
+
+
+def beam_refusals(c):
+    m = SimpleNamespace(**{**vars(MODEL), "vocab": 512})
+    ctx = c.loaded(m=m, dist=(8, 4))
+    B = c.binding.BeamSearchC
+    room = np.zeros(4096, np.int32)
+    o = C.c_void_p(room.ctypes.data)
+
+    def search(indptr=(0, 4, 8), n_out=4, t=1.0, finished=None, eos=0):
+        ip = i32(indptr)
+        s = B(len(ip) - 1, ip.ctypes.data, None, finished, eos, n_out, t)
+        s.keep = ip
+        return s
+
+    def select(s, z=o, dtype=0, stride=512, n_vocab=512, outs=(o, o, o)):
+        return raw(ctx, "pie_beam_select", None if s is None else C.byref(s), z, dtype, stride, n_vocab, *outs)
+
+    assert select(search()) == 0 and select(search(finished=o.value, eos=511)) == 0
+    assert select(None) == INVALID and select(search((0,))) == INVALID
+    for k in range(3):
+        assert select(search(), outs=tuple(None if i == k else o for i in range(3))) == INVALID
+    assert select(search(), z=None) == INVALID and select(search((0, 0, 0)), z=None) == 0
+    for t in (0.0, -1.0, float("nan"), float("inf")):
+        assert select(search(t=t)) == INVALID
+    assert select(search(t=1e-38)) == 0
+    assert select(search((1, 4))) == INVALID and select(search((0, 4, 3))) == INVALID
+    assert select(search((0, 9))) == BATCH
+    assert select(search(n_out=0)) == RANGE and select(search(n_out=257)) == RANGE and select(search(n_out=256)) == 0
+    assert select(search(), n_vocab=0) == RANGE and select(search(), n_vocab=513, stride=513) == RANGE and select(search(), stride=511) == INVALID
+    assert select(search(), n_vocab=1, stride=1) == 0
+    assert select(search(), dtype=3) == INVALID and select(search(), dtype=-1) == INVALID
+    assert select(search(), z=C.c_void_p(o.value + 2)) == INVALID and select(search(), z=C.c_void_p(o.value + 2), dtype=1) == 0
+    assert select(search(), z=C.c_void_p(o.value + 1), dtype=2) == INVALID
+    assert select(search(finished=o.value, eos=512)) == RANGE and select(search(finished=o.value, eos=-1)) == RANGE and select(search(eos=-1)) == 0
+    wide = c.loaded(m=m, dist=(300, 4))
+    ip = i32([0, 257])
+    assert raw(wide, "pie_beam_select", C.byref(B(1, ip.ctypes.data, None, None, 0, 4, 1.0)), o, 0, 512, 512, o, o, o) == BATCH
+    beams = lambda s, ids: raw(ctx, "pie_get_next_beams", None if s is None else C.byref(s), at(ids), o, o, o)  # noqa: E731
+    assert beams(search(), i32(np.arange(8))) == 0
+    assert beams(search(), None) == INVALID and beams(search((0, 0)), i32([0])) == INVALID and beams(None, i32([0])) == INVALID
+    assert beams(search((0, 1)), i32([1024])) == RANGE and beams(search((0, 1)), i32([-1])) == RANGE and beams(search((0, 9)), i32(np.arange(9))) == BATCH
+    no_head = c.context(m=m, dist=(8, 4))
+    assert raw(no_head, "pie_get_next_beams", C.byref(search()), at(i32(np.arange(8))), o, o, o) == INVALID
+    no_vocab = c.context()
+    assert raw(no_vocab, "pie_beam_select", C.byref(search()), o, 0, 512, 512, o, o, o) == RANGE
+    p = c.Pie.planner(m, 32, 16, 8, 4)
+    assert raw(p, "pie_beam_select", C.byref(search()), o, 0, 512, 512, o, o, o) == INVALID
+    assert raw(p, "pie_get_next_beams", C.byref(search()), at(i32([0])), o, o, o) == INVALID
+
+
+CASES = {f.__name__: f for f in (fork_plans, fork_masks, compact_plans, page_refusals, captured, images_in_flight, no_memory, beam_refusals)}
+
+if __name__ == "__main__":
+    CASES[sys.argv[2]](Child(sys.argv[1]))
+    print("case passed")
+    sys.exit(0)
+
+
+@pytest.mark.parametrize("case", list(CASES))
+def test_host_path(fake, case):  # noqa: F811
+    r = subprocess.run([sys.executable, os.path.abspath(__file__), fake, case], capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0 and "case passed" in r.stdout, f"exit {r.returncode}\n{r.stdout}\n{r.stderr}"
