@@ -303,7 +303,7 @@ typedef struct {
   const uint8_t* finished;     /* dev [rows] or NULL: none is */
   int32_t eos_token;           /* read where finished is given */
   int32_t n_out;
-  float temperature;           /* positive and finite */
+  float temperature;           /* 1e-30 .. 1e30 */
 } pie_beam_search;
 
 /* Element types of a caller's logits. */

@@ -1,29 +1,32 @@
 // Selection over beams and vocabulary: per group of rows (the beams of one search) the candidates of largest score
-//   score(r, v) = s_r + z_rv / T - log sum_u exp(z_ru / T)
+//   score(r, v) = s_r + (z_rv - m_r) / T - log sum_u exp((z_ru - m_r) / T),  m_r = max_u z_ru
 // ordered by descending score, then by beam, then by token.  A logit of -inf or NaN is no candidate, +inf counts as the
 // largest finite value of its type, a row with s_r = -inf or NaN has no candidates, a finished row has exactly one.
 //
 // Scores are compared in 64 bits: candidates of different beams lie within 1e-3 of one another in every step, and one unit in
-// the last place of a 32-bit score (1e-6 at 10) reorders them now and then.
+// the last place of a 32-bit score (1e-6 at 10) reorders them now and then.  The exponentials are taken and summed in 32 bits (a few
+// dozen terms), their sums in 64: 1e-8 on the logarithm.
+//
+// Two kernels.  beam_tiles reads every logit once and leaves, per segment (what a wave loads at once), the largest, and per tile of
+// eight segments the largest and the sum of exponentials.  beam_pick, one workgroup per group, turns the segments' maxima into scores
+// and keeps the n_out best segments by (score, beam, place): no other segment can hold one of the n_out best candidates, as
+// each of those n_out has one that comes before all of its own.  Only these are read again.
 #include "internal.h"
 
 namespace {
 // One logit as the selection sees it.
-template <typename T>
-__device__ __forceinline__ float beam_logit(T x);
-template <>
-__device__ __forceinline__ float beam_logit<float>(float x) {
-  return x != x ? -INFINITY : fminf(x, 3.402823466e38f);
-}
-template <>
-__device__ __forceinline__ float beam_logit<bf16_t>(bf16_t x) {
+__device__ __forceinline__ float beam_logit(float x) { return x != x ? -INFINITY : fminf(x, 3.402823466e38f); }
+__device__ __forceinline__ float beam_logit(bf16_t x) {
   const float f = (float)x;
   return f != f ? -INFINITY : fminf(f, 3.3895313892515355e38f);
 }
-template <>
-__device__ __forceinline__ float beam_logit<_Float16>(_Float16 x) {
+__device__ __forceinline__ float beam_logit(_Float16 x) {
   const float f = (float)x;
   return f != f ? -INFINITY : fminf(f, 65504.f);
+}
+__device__ __forceinline__ float beam_score(const float* scores, int row) {  // -inf: the row has no candidates
+  const float s = scores ? scores[row] : 0.f;
+  return s != s ? -INFINITY : fminf(s, 3.402823466e38f);
 }
 
 __device__ __forceinline__ double wave_sum_f64(double v) {
@@ -32,118 +35,419 @@ __device__ __forceinline__ double wave_sum_f64(double v) {
   return v;
 }
 
-#define BR_THREADS 256
-// base[row] = (b, m) with m the largest logit and score = b + (z - m) / T: b = s_r - log sum exp((z - m) / T), -inf where the row has
-// no candidates.  (Not s_r - (m / T + log sum ..): beside a logit of 1e38 the logarithm would be lost, 64 bits or not.)
+#define BT_SEGS 8  // segments of a tile
+typedef u32x4 u32x4_at2 __attribute__((aligned(2)));
+// A row cut into segments by its tokens, wherever it lies in memory: equal rows then have equal sums, bit for bit, and so
+// equal scores.  (Cut at 16-byte addresses instead, two beams with the same logits differed in the last bits of 64.)  Loads of 16
+// bytes from rows that are aligned to their elements only are ordinary on this chip; they touch a line more now and then.
 template <typename T>
-__global__ __launch_bounds__(BR_THREADS) void beam_row_kernel(const T* __restrict__ logits, int64_t stride, int V, double inv_temp,
-                                                              const float* __restrict__ scores, const uint8_t* __restrict__ finished,
-                                                              double2* __restrict__ base) {
-  __shared__ float smax[BR_THREADS / 64];
-  __shared__ double ssum[BR_THREADS / 64];
-  const int row = blockIdx.x, tid = threadIdx.x;
-  const T* z = logits + (int64_t)row * stride;
-  float s = scores ? scores[row] : 0.f;
-  s = s != s ? -INFINITY : fminf(s, 3.402823466e38f);
-  if (finished && finished[row]) {
-    if (tid == 0) base[row] = make_double2((double)s, 0.0);
-    return;
+struct BeamRow {
+  static constexpr int VEC = 16 / sizeof(T), SEG = 64 * VEC, TILE = BT_SEGS * SEG;
+  const T* z;
+  int V;
+  __device__ BeamRow(const T* logits, int64_t stride, int row, int V_) : z(logits + (int64_t)row * stride), V(V_) {}
+  // the VEC logits from token p on, -inf in place of what is behind the row
+  __device__ __forceinline__ void load(int p, float (&x)[VEC]) const {
+    if (p + VEC <= V) {
+      unpack(*reinterpret_cast<const u32x4_at2*>(z + p), x);
+    } else {
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) x[i] = p + i < V ? beam_logit(z[p + i]) : -INFINITY;
+    }
   }
-  float m = -INFINITY;
-  for (int i = tid; i < V; i += BR_THREADS) m = fmaxf(m, beam_logit(z[i]));
-  m = wave_max(m);
-  if ((tid & 63) == 0) smax[tid >> 6] = m;
-  __syncthreads();
-  for (int w = 0; w < BR_THREADS / 64; ++w) m = fmaxf(m, smax[w]);
-  if (m == -INFINITY || s == -INFINITY) {
-    if (tid == 0) base[row] = make_double2(-INFINITY, 0.0);
-    return;
+  __device__ __forceinline__ u32x4 stream(int p) const { return __builtin_nontemporal_load(reinterpret_cast<const u32x4_at2*>(z + p)); }
+  static __device__ __forceinline__ void unpack(u32x4 u, float (&x)[VEC]) {
+    union { u32x4 u; T e[VEC]; } w;
+    w.u = u;
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) x[i] = beam_logit(w.e[i]);
   }
-  double sum = 0;
-  for (int i = tid; i < V; i += BR_THREADS) sum += exp(((double)beam_logit(z[i]) - (double)m) * inv_temp);
-  sum = wave_sum_f64(sum);
-  if ((tid & 63) == 0) ssum[tid >> 6] = sum;
+};
+template <typename T>
+constexpr int beam_tiles_of(int V) { return (V + BeamRow<T>::TILE - 1) / BeamRow<T>::TILE; }
+
+// Wave-wide maxima of eight values at once: each exchange halves how many a lane carries on, 4 + 2 + 1 + 3 instead of 8 x 6.  Lane l
+// returns the maximum of value l / 8.
+__device__ __forceinline__ float wave_max8(const float (&v)[8], int lane) {
+  float a[4], b[2], c;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {  // lanes below 32 go on with values 0 .. 3
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v[i]), __float_as_uint(v[i + 4]), false, false);
+    a[i] = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  }
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(a[i]), __float_as_uint(a[i + 2]), false, false);
+    b[i] = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  }
+  const bool up = lane & 8;
+  const float mine = up ? b[1] : b[0], other = up ? b[0] : b[1];
+  c = fmaxf(mine, __shfl_xor(other, 8));
+#pragma unroll
+  for (int o = 4; o > 0; o >>= 1) c = fmaxf(c, __shfl_xor(c, o));
+  return c;
+}
+
+#define BT_WAVES 4
+template <typename T>
+__global__ __launch_bounds__(64 * BT_WAVES) void beam_tiles_kernel(const T* __restrict__ logits, int64_t stride, int V, int n_tiles, float c_hi,
+                                                                   float c_lo, float x_min, const float* __restrict__ scores,
+                                                                   const uint8_t* __restrict__ finished, float* __restrict__ seg_max,
+                                                                   float2* __restrict__ tile_stats, int64_t total) {
+  constexpr int VEC = BeamRow<T>::VEC, SEG = BeamRow<T>::SEG;
+  const int lane = threadIdx.x & 63;
+  const int64_t at = (int64_t)blockIdx.x * BT_WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (at >= total) return;
+  const int row = (int)(at / n_tiles), tile = (int)(at % n_tiles);
+  if ((finished && finished[row]) || beam_score(scores, row) == -INFINITY) return;  // (nothing of theirs is looked at)
+  const BeamRow<T> z(logits, stride, row, V);
+  float x[BT_SEGS][VEC], top[BT_SEGS];
+  const int p0 = tile * BT_SEGS * SEG + lane * VEC;
+  if ((tile + 1) * BT_SEGS * SEG <= V) {  // (uniform: all eight loads go out at once)
+    u32x4 raw[BT_SEGS];
+#pragma unroll
+    for (int j = 0; j < BT_SEGS; ++j) raw[j] = z.stream(p0 + j * SEG);
+#pragma unroll
+    for (int j = 0; j < BT_SEGS; ++j) BeamRow<T>::unpack(raw[j], x[j]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < BT_SEGS; ++j) z.load(p0 + j * SEG, x[j]);
+  }
+#pragma unroll
+  for (int j = 0; j < BT_SEGS; ++j) {
+    top[j] = x[j][0];
+#pragma unroll
+    for (int i = 1; i < VEC; ++i) top[j] = fmaxf(top[j], x[j][i]);
+  }
+  const float seg = wave_max8(top, lane);
+  float m = seg;
+#pragma unroll
+  for (int o = 32; o >= 8; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+  if ((lane & 7) == 0) seg_max[at * BT_SEGS + (lane >> 3)] = seg;
+  // exp((x - m) / T) = exp2((x - m) (c_hi + c_lo)), c = log2(e) / T in two parts; x_min keeps infinities out (exp2 is 0 there)
+  float sum = 0.f;
+  if (m != -INFINITY) {
+#pragma unroll
+    for (int j = 0; j < BT_SEGS; ++j)
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        const float d = fmaxf(x[j][i] - m, x_min);
+        sum += __builtin_amdgcn_exp2f(__builtin_fmaf(d, c_lo, d * c_hi));
+      }
+  }
+  sum = wave_sum(sum);
+  if (lane == 0) tile_stats[at] = make_float2(m, sum);
+}
+
+// ---------------------------------------------------------------------------------------------
+// picking
+// ---------------------------------------------------------------------------------------------
+typedef unsigned long long u64;
+// Order-preserving integer of a score; 0 stands for no candidate.
+__device__ __forceinline__ u64 score_key(double s) {
+  if (s == -INFINITY) return 0;
+  const u64 u = __double_as_longlong(s + 0.0);  // (-0 and 0 are one score)
+  return u >> 63 ? ~u : u | 1ull << 63;
+}
+__device__ __forceinline__ double key_score(u64 k) { return __longlong_as_double(k >> 63 ? k & ~(1ull << 63) : ~k); }
+
+#define BP_THREADS 1024
+#define BP_SEGS 576   // segments kept for reading again: at most 2 n_out + 64
+#define BP_CANDS 512  // candidates that are ranked against each other
+#define BP_CACHED 8192  // maxima of segments kept in LDS
+struct BeamGroups { int32_t row0[BEAM_GROUPS_BY_VALUE + 1]; };
+struct PickShared {
+  double2 row[BEAM_MAX_ROWS];  // (b, m): score = b + (z - m) / T; b = -inf: no candidates
+  u64 cand_key[BP_CANDS];
+  int cand_idx[BP_CANDS], rank[BP_CANDS];
+  int segs[BP_SEGS], segs_sorted[BP_SEGS];
+  uint32_t hist[1024];
+  float maxima[BP_CACHED];
+  u64 red_lo[BP_THREADS / 64], red_hi[BP_THREADS / 64];
+  uint32_t red_n[BP_THREADS / 64];
+  uint32_t count, bin, below, upto;
+  uint8_t done[BEAM_MAX_ROWS];
+};
+
+// A bound `lo` that at least `need` of the n keys reach (all valid ones, where there are fewer) and at most `cap` do, if there is one
+// (ties at lo otherwise: then `ties` of those equal to lo, in order, belong to the first `need`).  Keys are counted in 1024 bins of
+// the range they span, and the range narrows to the bin of the need-th: one pass where the scores are spread, seven at most.
+struct Bound { u64 lo; uint32_t n; uint32_t ties; bool tied; };
+template <typename F>
+__device__ Bound pick_bound(PickShared& sh, int n, uint32_t need, uint32_t cap, F key) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  u64 lo = ~0ull, hi = 0;
+  uint32_t valid = 0;
+  for (int i = tid; i < n; i += BP_THREADS) {
+    const u64 k = key(i);
+    if (k) { lo = k < lo ? k : lo; hi = k > hi ? k : hi; ++valid; }
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    const u64 l = __shfl_xor(lo, o), h = __shfl_xor(hi, o);
+    lo = l < lo ? l : lo;
+    hi = h > hi ? h : hi;
+    valid += __shfl_xor(valid, o);
+  }
   __syncthreads();
-  if (tid == 0) {
-    sum = 0;
-    for (int w = 0; w < BR_THREADS / 64; ++w) sum += ssum[w];
-    base[row] = make_double2((double)s - log(sum), (double)m);
+  if (lane == 0) { sh.red_lo[wave] = lo; sh.red_hi[wave] = hi; sh.red_n[wave] = valid; }
+  __syncthreads();
+  valid = 0;
+#pragma unroll
+  for (int w = 0; w < BP_THREADS / 64; ++w) {
+    lo = sh.red_lo[w] < lo ? sh.red_lo[w] : lo;
+    hi = sh.red_hi[w] > hi ? sh.red_hi[w] : hi;
+    valid += sh.red_n[w];
+  }
+  if (valid <= need || valid <= cap) return Bound{valid ? lo : 1ull, valid, 0, false};
+  uint32_t above = 0;  // keys above the range
+  for (;;) {
+    const u64 span = hi - lo;
+    const int bits = span ? 64 - __clzll((long long)span) : 0, shift = bits > 10 ? bits - 10 : 0;
+    sh.hist[tid] = 0;
+    __syncthreads();
+    for (int i = tid; i < n; i += BP_THREADS) {
+      const u64 k = key(i);
+      if (k >= lo && k <= hi) atomicAdd(&sh.hist[(uint32_t)((k - lo) >> shift)], 1u);
+    }
+    __syncthreads();
+    const uint32_t c = sh.hist[BP_THREADS - 1 - tid];  // from the top down
+    uint32_t incl = c;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const uint32_t t = __shfl_up(incl, o);
+      if (lane >= o) incl += t;
+    }
+    if (lane == 63) sh.red_n[wave] = incl;
+    __syncthreads();
+    uint32_t before = above;
+    for (int w = 0; w < wave; ++w) before += sh.red_n[w];
+    incl += before;
+    if (incl >= need && incl - c < need) { sh.bin = BP_THREADS - 1 - tid; sh.below = incl - c; sh.upto = incl; }
+    __syncthreads();
+    const uint32_t bin = sh.bin, excl = sh.below, upto = sh.upto;
+    lo += (u64)bin << shift;
+    if (upto <= cap) return Bound{lo, upto, 0, false};
+    if (shift == 0) return Bound{lo, upto, need - excl, true};
+    above = excl;
+    const u64 end = lo + ((1ull << shift) - 1);
+    hi = end < hi ? end : hi;
+    __syncthreads();
   }
 }
 
-struct BeamGroups { int32_t row0[BEAM_GROUPS_BY_VALUE + 1]; };
+// put(i) for every i whose key reaches the bound, of those that tie for the last places the first ones; any order, whole
+// workgroup.  Returns how many there are.
+template <typename F, typename P>
+__device__ uint32_t pick_collect(PickShared& sh, int n, const Bound& b, F key, P put) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  __syncthreads();
+  if (tid == 0) sh.count = 0;
+  __syncthreads();
+  const u64 from = b.tied ? b.lo + 1 : b.lo;
+  for (int i = tid; i < n; i += BP_THREADS) {
+    const u64 k = key(i);
+    if (k && k >= from) put(atomicAdd(&sh.count, 1u), i, k);
+  }
+  __syncthreads();
+  uint32_t have = sh.count;
+  if (b.tied) {
+    uint32_t left = b.ties;
+    for (int i0 = 0; i0 < n && left; i0 += BP_THREADS) {  // (uniform)
+      const bool mine = i0 + tid < n && key(i0 + tid) == b.lo;
+      const u64 votes = __ballot(mine);
+      __syncthreads();
+      if (lane == 0) sh.red_n[wave] = __popcll(votes);
+      __syncthreads();
+      uint32_t at = __popcll(votes & ((1ull << lane) - 1)), all = 0;
+      for (int w = 0; w < BP_THREADS / 64; ++w) {
+        if (w < wave) at += sh.red_n[w];
+        all += sh.red_n[w];
+      }
+      if (mine && at < left) put(have + at, i0 + tid, b.lo);
+      const uint32_t took = all < left ? all : left;
+      have += took;
+      left -= took;
+    }
+  }
+  __syncthreads();
+  return have;
+}
 
-#define BG_THREADS 1024
-// n_out rounds, each taking the first candidate behind the last one taken
 template <typename T>
-__global__ __launch_bounds__(BG_THREADS) void beam_group_kernel(const T* __restrict__ logits, int64_t stride, int V, double inv_temp,
-                                                                const uint8_t* __restrict__ finished, int eos, BeamGroups groups, int n_out,
-                                                                const double2* __restrict__ base, int32_t* __restrict__ out_beams,
-                                                                int32_t* __restrict__ out_tokens, float* __restrict__ out_scores) {
-  __shared__ double skey[BG_THREADS / 64];
-  __shared__ int sidx[BG_THREADS / 64];
-  const int g = blockIdx.x, tid = threadIdx.x;
+__global__ __launch_bounds__(BP_THREADS) void beam_pick_kernel(const T* __restrict__ logits, int64_t stride, int V, int n_tiles, double inv_temp,
+                                                               const float* __restrict__ scores, const uint8_t* __restrict__ finished, int eos,
+                                                               BeamGroups groups, int n_out, const float* __restrict__ seg_max,
+                                                               const float2* __restrict__ tile_stats, int32_t* __restrict__ out_beams,
+                                                               int32_t* __restrict__ out_tokens, float* __restrict__ out_scores) {
+  constexpr int VEC = BeamRow<T>::VEC, SEG = BeamRow<T>::SEG;
+  __shared__ PickShared sh;
+  const int g = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int row0 = groups.row0[g], rows = groups.row0[g + 1] - row0;
-  double last = INFINITY;
-  int last_idx = -1;
-  for (int k = 0; k < n_out; ++k) {
-    double best = -INFINITY;
-    int best_idx = 0x7FFFFFFF;
-    for (int r = 0; r < rows; ++r) {
-      const double2 b = base[row0 + r];
-      if (b.x == -INFINITY) continue;
-      const bool done = finished && finished[row0 + r];
-      const T* z = logits + (int64_t)(row0 + r) * stride;
-      for (int v = tid; v < V; v += BG_THREADS) {
-        double key = b.x + (done ? 0.0 : ((double)beam_logit(z[v]) - b.y) * inv_temp);
-        if (done && v != eos) key = -INFINITY;
-        const int idx = r * V + v;
-        const bool after = key < last || (key == last && idx > last_idx);
-        if (after && key > best) { best = key; best_idx = idx; }  // (indices ascend)
+  const int n_segs = n_tiles * BT_SEGS, n = rows * n_segs;
+  const float* maxima = seg_max + (int64_t)row0 * n_segs;
+
+  for (int r = wave; r < rows; r += BP_THREADS / 64) {  // a wave per row: its tiles' sums
+    const float s = beam_score(scores, row0 + r);
+    const bool done = finished && finished[row0 + r];
+    double b = -INFINITY, m = 0;
+    if (done) b = s;
+    else if (s != -INFINITY) {
+      float top = -INFINITY;
+      for (int t = lane; t < n_tiles; t += 64) top = fmaxf(top, tile_stats[(int64_t)(row0 + r) * n_tiles + t].x);
+      top = wave_max(top);
+      if (top != -INFINITY) {
+        double sum = 0;
+        for (int t = lane; t < n_tiles; t += 64) {
+          const float2 st = tile_stats[(int64_t)(row0 + r) * n_tiles + t];
+          if (st.x != -INFINITY) sum += (double)st.y * exp(((double)st.x - (double)top) * inv_temp);
+        }
+        sum = wave_sum_f64(sum);
+        m = top;
+        b = (double)s - log(sum);
       }
     }
+    if (lane == 0) { sh.row[r] = make_double2(b, m); sh.done[r] = done; }
+  }
+  const bool cached = n <= BP_CACHED;
+  if (cached)
+    for (int i = tid; i < n; i += BP_THREADS) sh.maxima[i] = maxima[i];
+  __syncthreads();
+
+  const float per = 1.0f / (float)n_segs;
+  auto row_of = [&](int i) { return (int)(((float)i + 0.5f) * per); };  // (i < 256 x 512: off by 5e-5, half a segment is 1e-3)
+  auto key_of = [&](int r, float z) {
+    const double2 b = sh.row[r];
+    return b.x == -INFINITY || z == -INFINITY ? 0ull : score_key(b.x + ((double)z - b.y) * inv_temp);
+  };
+  // a finished row's one candidate stands in its first segment
+  auto seg_key = [&](int i) {
+    const int r = row_of(i);
+    if (sh.done[r]) return i == r * n_segs && sh.row[r].x != -INFINITY ? score_key(sh.row[r].x) : 0ull;
+    return key_of(r, cached ? sh.maxima[i] : maxima[i]);
+  };
+  const Bound segs = pick_bound(sh, n, (uint32_t)n_out, (uint32_t)(2 * n_out + 64), seg_key);
+  const uint32_t n_kept = pick_collect(sh, n, segs, seg_key, [&](uint32_t at, int i, u64) { sh.segs[at] = i; });
+
+  // candidates: the logits of the kept segments that reach the bound (every one, where there are fewer segments than candidates asked for)
+  const u64 floor_key = segs.n < (uint32_t)n_out ? 1ull : segs.lo;
+  const int n_elems = (int)n_kept * SEG;
+  if (tid == 0) sh.count = 0;
+  __syncthreads();
+  for (int e = tid * VEC; e < n_elems; e += BP_THREADS * VEC) {
+    const int i = sh.segs[e / SEG], r = row_of(i), p = (i - r * n_segs) * SEG + e % SEG;
+    if (sh.done[r]) {
+      if (e % SEG == 0) {
+        const uint32_t at = atomicAdd(&sh.count, 1u);
+        if (at < BP_CANDS) { sh.cand_key[at] = score_key(sh.row[r].x); sh.cand_idx[at] = r * V + eos; }
+      }
+      continue;
+    }
+    const BeamRow<T> z(logits, stride, row0 + r, V);
+    float x[VEC];
+    z.load(p, x);
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-      const double k2 = __shfl_xor(best, o);
-      const int i2 = __shfl_xor(best_idx, o);
-      if (k2 > best || (k2 == best && i2 < best_idx)) { best = k2; best_idx = i2; }
+    for (int k = 0; k < VEC; ++k) {
+      const u64 key = key_of(r, x[k]);
+      if (key >= floor_key) {
+        const uint32_t at = atomicAdd(&sh.count, 1u);
+        if (at < BP_CANDS) { sh.cand_key[at] = key; sh.cand_idx[at] = r * V + p + k; }
+      }
+    }
+  }
+  __syncthreads();
+  uint32_t n_cand = sh.count;
+  if (n_cand > BP_CANDS) {  // crowded: the same choice among the segments' logits, one by one, in order of their places
+    for (int i = tid; i < (int)n_kept; i += BP_THREADS) {
+      const int mine = sh.segs[i];
+      int at = 0;
+      for (int k = 0; k < (int)n_kept; ++k) at += sh.segs[k] < mine;
+      sh.segs_sorted[at] = mine;
     }
     __syncthreads();
-    if ((tid & 63) == 0) { skey[tid >> 6] = best; sidx[tid >> 6] = best_idx; }
-    __syncthreads();
-    for (int w = 0; w < BG_THREADS / 64; ++w)
-      if (skey[w] > best || (skey[w] == best && sidx[w] < best_idx)) { best = skey[w]; best_idx = sidx[w]; }
-    const bool none = best == -INFINITY;
-    if (tid == 0) {
-      out_beams[(int64_t)g * n_out + k] = none ? -1 : best_idx / V;
-      out_tokens[(int64_t)g * n_out + k] = none ? -1 : best_idx % V;
-      out_scores[(int64_t)g * n_out + k] = none ? -INFINITY : (float)best;
+    auto place = [&](int e, int& r, int& p) {
+      const int i = sh.segs_sorted[e / SEG];
+      r = row_of(i);
+      p = (i - r * n_segs) * SEG + e % SEG;
+    };
+    auto elem_key = [&](int e) {
+      int r, p;
+      place(e, r, p);
+      if (sh.done[r]) return e % SEG == 0 ? score_key(sh.row[r].x) : 0ull;
+      const BeamRow<T> z(logits, stride, row0 + r, V);
+      if (p >= V) return 0ull;
+      const u64 k = key_of(r, beam_logit(z.z[p]));
+      return k >= floor_key ? k : 0ull;
+    };
+    const Bound best = pick_bound(sh, n_elems, (uint32_t)n_out, (uint32_t)BP_CANDS, elem_key);
+    n_cand = pick_collect(sh, n_elems, best, elem_key, [&](uint32_t at, int e, u64 key) {
+      int r, p;
+      place(e, r, p);
+      sh.cand_key[at] = key;
+      sh.cand_idx[at] = r * V + (sh.done[r] ? eos : p);
+    });
+  }
+
+  // their ranks: each is compared with all, the work of one shared by as many threads as there are to a candidate
+  for (int i = tid; i < (int)n_cand; i += BP_THREADS) sh.rank[i] = 0;
+  __syncthreads();
+  if (n_cand) {
+    const int share = BP_THREADS / (int)n_cand > 0 ? BP_THREADS / (int)n_cand : 1;  // (n_cand <= 512)
+    const int c = tid / share, part = tid % share;
+    if (c < (int)n_cand) {
+      const u64 key = sh.cand_key[c];
+      const int idx = sh.cand_idx[c];
+      int before = 0;
+      for (int k = part; k < (int)n_cand; k += share) {
+        const u64 k2 = sh.cand_key[k];
+        before += k2 > key || (k2 == key && sh.cand_idx[k] < idx);
+      }
+      if (before) atomicAdd(&sh.rank[c], before);
     }
-    last = best;
-    last_idx = best_idx;
+  }
+  __syncthreads();
+  const int64_t o = (int64_t)g * n_out;
+  for (int i = tid; i < (int)n_cand; i += BP_THREADS) {
+    const int at = sh.rank[i];
+    if (at >= n_out) continue;
+    const int idx = sh.cand_idx[i], r = idx / V;
+    out_beams[o + at] = r;
+    out_tokens[o + at] = idx - r * V;
+    out_scores[o + at] = (float)key_score(sh.cand_key[i]);
+  }
+  for (int i = (int)n_cand + tid; i < n_out; i += BP_THREADS) {
+    out_beams[o + i] = -1;
+    out_tokens[o + i] = -1;
+    out_scores[o + i] = -INFINITY;
   }
 }
 
 template <typename T>
 hipError_t beam_select(const BeamArgs& a, hipStream_t s) {
   const T* z = reinterpret_cast<const T*>(a.logits);
-  const int n = a.group_indptr[a.n_groups];
-  if (n > 0) beam_row_kernel<T><<<dim3((unsigned)n), dim3(BR_THREADS), 0, s>>>(z, a.stride, a.V, a.inv_temp, a.scores, a.finished, reinterpret_cast<double2*>(a.ws));
+  const int rows = a.group_indptr[a.n_groups], n_tiles = beam_tiles_of<T>(a.V);
+  const int64_t total = (int64_t)rows * n_tiles;
+  float2* stats = reinterpret_cast<float2*>(a.ws);
+  float* maxima = reinterpret_cast<float*>(stats + total);
+  const double c = 1.4426950408889634074 * a.inv_temp;
+  const float c_hi = (float)c, c_lo = (float)(c - (double)c_hi), x_min = (float)(-256.0 / c);
+  if (rows > 0)
+    beam_tiles_kernel<T><<<dim3((unsigned)((total + BT_WAVES - 1) / BT_WAVES)), dim3(64 * BT_WAVES), 0, s>>>(
+        z, a.stride, a.V, n_tiles, c_hi, c_lo, x_min, a.scores, a.finished, maxima, stats, total);
   for (int g0 = 0; g0 < a.n_groups; g0 += BEAM_GROUPS_BY_VALUE) {
     const int ng = a.n_groups - g0 < BEAM_GROUPS_BY_VALUE ? a.n_groups - g0 : BEAM_GROUPS_BY_VALUE;
     BeamGroups groups{};
     for (int g = 0; g <= ng; ++g) groups.row0[g] = a.group_indptr[g0 + g];
-    beam_group_kernel<T><<<dim3((unsigned)ng), dim3(BG_THREADS), 0, s>>>(z, a.stride, a.V, a.inv_temp, a.finished, a.eos, groups, a.n_out, reinterpret_cast<double2*>(a.ws),
-                                                                         a.out_beams + (int64_t)g0 * a.n_out, a.out_tokens + (int64_t)g0 * a.n_out,
-                                                                         a.out_scores + (int64_t)g0 * a.n_out);
+    const int64_t o = (int64_t)g0 * a.n_out;
+    beam_pick_kernel<T><<<dim3((unsigned)ng), dim3(BP_THREADS), 0, s>>>(z, a.stride, a.V, n_tiles, a.inv_temp, a.scores, a.finished, a.eos, groups,
+                                                                        a.n_out, maxima, stats, a.out_beams + o, a.out_tokens + o, a.out_scores + o);
   }
   return hipGetLastError();
 }
 }  // namespace
 
-size_t beam_ws_doubles(int rows, int vocab) {
-  (void)vocab;
-  return 2 * (size_t)rows;
+size_t beam_ws_doubles(int rows, int vocab) {  // per tile: (maximum, sum) and its segments' maxima; fp32 rows have the most tiles
+  return (size_t)rows * beam_tiles_of<float>(vocab) * (1 + BT_SEGS / 2);
 }
 
 hipError_t launch_beam_select(const BeamArgs& a, hipStream_t s) {

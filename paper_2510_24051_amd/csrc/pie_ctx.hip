@@ -2257,7 +2257,7 @@ static pie_status check_beams(pie_ctx* c, const pie_beam_search* b, int32_t n_vo
   if (!b || !b->group_indptr || b->n_groups <= 0) return fail(c, PIE_EINVAL, "%s: null search or no groups", who);
   if (!out_beams || !out_tokens || !out_scores) return fail(c, PIE_EINVAL, "%s: null output", who);
   if (!c->beam_ws) return fail(c, PIE_EINVAL, "%s: context created without vocab / dist rows", who);
-  if (!(b->temperature > 0.f) || !std::isfinite(b->temperature)) return fail(c, PIE_EINVAL, "temperature must be positive and finite");
+  if (!(b->temperature >= 1e-30f) || !(b->temperature <= 1e30f)) return fail(c, PIE_EINVAL, "%s: temperature must be within [1e-30, 1e30]", who);
   if (b->group_indptr[0] != 0) return fail(c, PIE_EINVAL, "%s: group_indptr must start at 0", who);
   for (int g = 0; g < b->n_groups; ++g) {
     const int64_t n = (int64_t)b->group_indptr[g + 1] - b->group_indptr[g];

@@ -161,12 +161,16 @@ def test_scores_far_apart_and_close_together(ctx):
     check(ctx, logits(4, 20000, torch.float32, 80), [0, 4], 8, np.arange(4.0), t=1e6)
 
 
-def test_tiny_temperatures_do_not_make_nans(ctx):
+def test_the_smallest_and_largest_temperatures(ctx):
     z = logits(2, 700, torch.float32, 5)
-    for t in (1e-30, 1e-38, 1.5e-45):
+    z[0, 5], z[0, 9] = -math.inf, torch.finfo(torch.float32).min
+    for t in (1.1e-30, 1e-20):
         b, v, s = select(ctx, z, [0, 1, 2], 2, t=t)
         assert not np.isnan(s).any() and s[0, 0] == 0.0
         assert v[:, 0].tolist() == z.argmax(1).cpu().tolist()
+    for t in (1e20, 9e29):  # all the same but the masked one and, where it still counts, the lowest
+        b, v, s = select(ctx, z, [0, 1, 2], 256, t=t)
+        assert np.allclose(s, -np.log([[698], [700]]), atol=LSE) and not {5, 9} & set(v[0].tolist())
 
 
 def test_crowded_candidates(ctx):

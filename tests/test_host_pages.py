@@ -313,9 +313,9 @@ def beam_refusals(c):
     for k in range(3):
         assert select(search(), outs=tuple(None if i == k else o for i in range(3))) == INVALID
     assert select(search(), z=None) == INVALID and select(search((0, 0, 0)), z=None) == 0
-    for t in (0.0, -1.0, float("nan"), float("inf")):
+    for t in (0.0, -1.0, float("nan"), float("inf"), 9e-31, 1.1e30):
         assert select(search(t=t)) == INVALID
-    assert select(search(t=1e-38)) == 0
+    assert select(search(t=1.1e-30)) == 0 and select(search(t=9e29)) == 0
     assert select(search((1, 4))) == INVALID and select(search((0, 4, 3))) == INVALID
     assert select(search((0, 9))) == BATCH
     assert select(search(n_out=0)) == RANGE and select(search(n_out=257)) == RANGE and select(search(n_out=256)) == 0
