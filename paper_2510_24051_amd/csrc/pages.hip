@@ -48,27 +48,60 @@ struct ForkByPointer {
 // ---------------------------------------------------------------------------------------------
 struct PageIds { int32_t v[IDS_BY_VALUE]; };
 
-// One thread per 8 dims of one token of one head, K and V; the image is [page][layer][K or V][slot][kv head][dim].
-template <bool TO_POOL>
-__global__ void page_image_kernel(bf16_t* __restrict__ kv, int64_t layer_elems, int n_layers, PageIds ids, int n, int F, int Hkv, int D,
-                                  uint16_t* __restrict__ image) {
-  const int per_row = D / 8, per_block = PAGE * Hkv * per_row;
-  const int64_t idx = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-  if (idx >= (int64_t)n * F * per_block) return;
-  const int layer = blockIdx.y;
-  const int c = (int)(idx % per_row), h = (int)(idx / per_row % Hkv), t = (int)(idx / ((int64_t)per_row * Hkv) % PAGE);
-  const int f = (int)(idx / per_block % F), p = (int)(idx / ((int64_t)per_block * F));
-  const int64_t rows = (int64_t)F * PAGE, part = rows * Hkv * D;
+// The pool keeps V as 8 tokens of one dim next to each other, tokens' rows have 8 dims of one token next to each other: eight lanes
+// turn the one into the other among themselves.  Lane i of eight stands for row label(i) before and after; with
+// label(i) = i ^ (i >> 2) * 3 the three exchanges (labels that differ in bit 2, 1, 0) are a half mirror and two quad permutations.
+__device__ __forceinline__ int octet_label(int i) { return i ^ ((i >> 2 & 1) * 3); }
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp(uint32_t x) { return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, CTRL, 0xF, 0xF, true); }
+__device__ __forceinline__ u32x4 transpose8(u32x4 w, int label) {
+  const bool b2 = label & 4, b1 = label & 2, b0 = label & 1;
+  // rows i and i ^ 4: this lane goes on with columns 4 b2 .. 4 b2 + 3 of both
+  const uint32_t k0 = b2 ? w[2] : w[0], k1 = b2 ? w[3] : w[1], g0 = dpp<0x141>(b2 ? w[0] : w[2]), g1 = dpp<0x141>(b2 ? w[1] : w[3]);
+  const uint32_t a0 = b2 ? g0 : k0, a1 = b2 ? g1 : k1, c0 = b2 ? k0 : g0, c1 = b2 ? k1 : g1;  // row i & 3, row i | 4
+  // rows that differ in bit 1: two columns of each
+  const uint32_t ka = b1 ? a1 : a0, kc = b1 ? c1 : c0, ga = dpp<0x4E>(b1 ? a0 : a1), gc = dpp<0x4E>(b1 ? c0 : c1);
+  const uint32_t r0 = b1 ? ga : ka, r2 = b1 ? ka : ga, r4 = b1 ? gc : kc, r6 = b1 ? kc : gc;
+  // rows that differ in bit 0: one column of each, the two rows side by side
+  const uint32_t pick = b0 ? 0x03020706u : 0x05040100u;  // high half of the neighbour's and of this row's, or both low halves
+  u32x4 out;
+  out[0] = __builtin_amdgcn_perm(dpp<0xB1>(r0), r0, pick);
+  out[1] = __builtin_amdgcn_perm(dpp<0xB1>(r2), r2, pick);
+  out[2] = __builtin_amdgcn_perm(dpp<0xB1>(r4), r4, pick);
+  out[3] = __builtin_amdgcn_perm(dpp<0xB1>(r6), r6, pick);
+  return out;
+}
+
+// The image is [page][layer][K or V][slot][kv head][dim].  A wave takes one head of one 16-token block: D/32 times 1 KiB of K, which in
+// the pool are 16-byte pieces of 8 dims of a token already, and as much of V.  On the pool's side every access is 1 KiB
+// in one piece, on the image's 16 tokens of 64 bytes.
+#define IMAGE_WAVES 4
+template <int D, bool TO_POOL>
+__global__ __launch_bounds__(64 * IMAGE_WAVES) void page_image_kernel(bf16_t* __restrict__ kv, int64_t layer_elems, int n_layers, PageIds ids, int total,
+                                                                      int F, int Hkv, uint16_t* __restrict__ image) {
+  constexpr int N = D / 32;
+  const int lane = threadIdx.x & 63, layer = blockIdx.y;
+  const int at = blockIdx.x * IMAGE_WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (at >= total) return;
+  const int h = at % Hkv, f = at / Hkv % F, p = at / (Hkv * F);
   uint16_t* blk = reinterpret_cast<uint16_t*>(kv) + layer * layer_elems + (((int64_t)ids.v[p] * F + f) * Hkv + h) * (2 * PAGE * D);
-  uint16_t* img = image + (((int64_t)p * n_layers + layer) * 2) * part + ((int64_t)(f * PAGE + t) * Hkv + h) * D + c * 8;
-  u32x4* k = reinterpret_cast<u32x4*>(blk + k_elem_offset(t, c * 8));
-  if (TO_POOL) *k = *reinterpret_cast<const u32x4*>(img);
-  else *reinterpret_cast<u32x4*>(img) = *k;
-  img += part;
-  for (int e = 0; e < 8; ++e) {
-    uint16_t* v = blk + v_elem_offset(t, c * 8 + e, D);
-    if (TO_POOL) *v = img[e];
-    else img[e] = *v;
+  const int64_t row = (int64_t)Hkv * D, part = (int64_t)F * PAGE * row;
+  uint16_t* img = image + (((int64_t)p * n_layers + layer) * 2) * part + (int64_t)f * PAGE * row + h * D;
+  const int label = octet_label(lane & 7);
+  uint16_t* pk = blk + lane * 8;
+  uint16_t* pv = blk + PAGE * D + (lane & ~7) * 8 + label * 8;
+  uint16_t* ik = img + swap23(lane & 15) * row + (lane >> 4) * 8;
+  uint16_t* iv = img + part + ((lane >> 5) * 8 + label) * row + (lane >> 3 & 3) * 8;
+  u32x4 k[N], v[N];
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    k[j] = load_nt(reinterpret_cast<const u32x4*>(TO_POOL ? ik + j * 32 : pk + j * 512));
+    v[j] = load_nt(reinterpret_cast<const u32x4*>(TO_POOL ? iv + j * 32 : pv + j * 512));
+  }
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    *reinterpret_cast<u32x4*>(TO_POOL ? pk + j * 512 : ik + j * 32) = k[j];
+    *reinterpret_cast<u32x4*>(TO_POOL ? pv + j * 512 : iv + j * 32) = transpose8(v[j], label);
   }
 }
 
@@ -154,11 +187,13 @@ hipError_t launch_page_image(bf16_t* kv, size_t layer_elems, int n_layers, const
     const int m = n - p0 < IDS_BY_VALUE ? n - p0 : IDS_BY_VALUE;
     PageIds ids;
     for (int i = 0; i < m; ++i) ids.v[i] = host_ids[p0 + i];
-    const int64_t threads = (int64_t)m * F * PAGE * Hkv * (D / 8);
-    const dim3 grid((unsigned)((threads + 255) / 256), (unsigned)n_layers), block(256);
+    const int total = m * F * Hkv;
+    const dim3 grid((unsigned)((total + IMAGE_WAVES - 1) / IMAGE_WAVES), (unsigned)n_layers), block(64 * IMAGE_WAVES);
     uint16_t* img = reinterpret_cast<uint16_t*>(image) + p0 * page_image;
-    if (to_pool) page_image_kernel<true><<<grid, block, 0, s>>>(kv, layer_elems, n_layers, ids, m, F, Hkv, D, img);
-    else page_image_kernel<false><<<grid, block, 0, s>>>(kv, layer_elems, n_layers, ids, m, F, Hkv, D, img);
+    if (D == 128 && to_pool) page_image_kernel<128, true><<<grid, block, 0, s>>>(kv, layer_elems, n_layers, ids, total, F, Hkv, img);
+    else if (D == 128) page_image_kernel<128, false><<<grid, block, 0, s>>>(kv, layer_elems, n_layers, ids, total, F, Hkv, img);
+    else if (to_pool) page_image_kernel<64, true><<<grid, block, 0, s>>>(kv, layer_elems, n_layers, ids, total, F, Hkv, img);
+    else page_image_kernel<64, false><<<grid, block, 0, s>>>(kv, layer_elems, n_layers, ids, total, F, Hkv, img);
   }
   return hipGetLastError();
 }
