@@ -381,11 +381,17 @@ hipError_t launch_fork(bf16_t* kv, size_t layer_elems, int n_layers, size_t page
 // pages host_ids[0 .. n) of F blocks each to the caller's image [n][layer][K or V][slot][kv head][dim], or back
 hipError_t launch_page_image(bf16_t* kv, size_t layer_elems, int n_layers, const int32_t* host_ids, int n, int F, int Hkv, int D, bf16_t* image,
                              bool to_pool, hipStream_t s);
-struct CompactTile { int32_t dst_block, first, n; };  // tokens [first, first + n) of the kept tokens fill the front of a block
+// Tokens of a source block that a chain takes, the kept tokens from `first` on, and the row of `angles` that all of them turn by.
+struct CompactEntry { int32_t block; uint32_t mask; int32_t first, turn; };
+#define COMPACT_STILL (-1)  // none turns
+#define COMPACT_MIXED (-2)  // `turn` says it token by token
+// What one wave per 64 dims walks in order: the tokens of source blocks [entry0, entry1) fill the destination blocks from tiles[tile0]
+// on, 16 each.
+struct CompactChain { int32_t entry0, entry1, tile0; };
 struct CompactPlan {
-  const int2* chains;        // [n_chains] tiles that one workgroup walks in order
-  const CompactTile* tiles;
-  const int32_t* src;        // per kept token: block * PAGE + slot it comes from
+  const CompactChain* chains;
+  const CompactEntry* entries;
+  const int32_t* tiles;
   const int32_t* turn;       // per kept token: row of `angles`, -1 = not rotated; null: none is
   const float* angles;       // [turns, D] cos | sin
 };

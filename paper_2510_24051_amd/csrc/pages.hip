@@ -24,7 +24,7 @@ __global__ __launch_bounds__(FORK_THREADS) void fork_kernel(unsigned char* __res
   for (int i = r.first; i < r.first + r.n; ++i) {
     const PageMove m = plan.move(i);
     if (m.src < 0) v = kept;
-    else if (m.src != last) v = *reinterpret_cast<const u32x4*>(base + m.src * page_bytes);
+    else if (m.src != last) v = load_nt(reinterpret_cast<const u32x4*>(base + m.src * page_bytes));
     last = m.src;
     *reinterpret_cast<u32x4*>(base + m.dst * page_bytes) = v;
   }
@@ -108,57 +108,138 @@ __global__ __launch_bounds__(64 * IMAGE_WAVES) void page_image_kernel(bf16_t* __
 // ---------------------------------------------------------------------------------------------
 // compact
 // ---------------------------------------------------------------------------------------------
-// A wave owns some dims of one head of one layer and walks the tiles (16-token destination blocks) of a chain in order.  Kept tokens
-// move towards the front, so a tile's sources lie at or behind its own tokens, and every later tile's behind all of them: in place,
-// a wave's stores only ever replace tokens that it has loaded already, and no other wave touches its dims.
-//   K: waves 0 .. D/64 - 1, lane (token, 8 dims i .. i+7) with the dims D/2 above them, which the rotation pairs them with;
-//   V: waves D/64 .. 2 D/64 - 1, lane = dim, the two octets of a tile's tokens one after the other.
-template <int D>
-__global__ __launch_bounds__(2 * D) void compact_kernel(bf16_t* __restrict__ kv, int64_t layer_elems, int Hkv, CompactPlan plan) {
-  constexpr int KW = D / 64;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int chain = blockIdx.x / Hkv, h = blockIdx.x % Hkv;
-  uint16_t* pool = reinterpret_cast<uint16_t*>(kv) + (int64_t)blockIdx.y * layer_elems;
-  auto block_of = [&](int b) { return pool + ((int64_t)b * Hkv + h) * (2 * PAGE * D); };
-  const int2 tiles = plan.chains[chain];
-  for (int i = tiles.x; i < tiles.y; ++i) {
-    const CompactTile tile = plan.tiles[i];
-    uint16_t* dst = block_of(tile.dst_block);
-    if (wave < KW) {
-      const int t = lane & 15, c = wave * 4 + (lane >> 4);  // dims 8c .. 8c + 7 and D/2 above
-      if (t < tile.n) {
-        const int src = plan.src[tile.first + t], turn = plan.turn ? plan.turn[tile.first + t] : -1;
-        const uint16_t* from = block_of(src / PAGE);
-        Pack16 a, b;
-        a.u = *reinterpret_cast<const u32x4*>(from + k_elem_offset(src % PAGE, 8 * c));
-        b.u = *reinterpret_cast<const u32x4*>(from + k_elem_offset(src % PAGE, 8 * c + D / 2));
-        if (turn >= 0) {
-          const float* angles = plan.angles + (int64_t)turn * D + 8 * c;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float x = (float)a.h[e], y = (float)b.h[e], cs = angles[e], sn = angles[D / 2 + e];
-            a.h[e] = f32_to_bf16(x * cs - y * sn);
-            b.h[e] = f32_to_bf16(y * cs + x * sn);
-          }
-        }
-        *reinterpret_cast<u32x4*>(dst + k_elem_offset(t, 8 * c)) = a.u;
-        *reinterpret_cast<u32x4*>(dst + k_elem_offset(t, 8 * c + D / 2)) = b.u;
-      }
+// A wave owns 64 dims of one head of one layer, of K or of V, and walks a chain: it reads the source blocks that hold kept tokens one
+// after the other, each once and in whole KiB, puts the kept tokens' rows of 8 dims (16 bytes) behind each other into a ring of 32
+// tokens in LDS, and stores a destination block whenever 16 are there.  V is turned into rows on the way in and back on the way
+// out (transpose8).  A wave of K takes 32 dims and those D/2 above, which the rotation pairs them with.
+// In place: a kept token moves towards the front, so when a destination block is stored every token at or before its last one has
+// been read, and what the chain reads later lies behind it; no other wave touches these dims.  The reads run COMPACT_AHEAD
+// blocks in front of the stores, which only makes them earlier.
+#define COMPACT_WAVES 4
+#define COMPACT_AHEAD 4
+template <int D, bool IS_K>
+__device__ __forceinline__ void compact_walk(uint16_t* pool, int64_t block_elems, int part, CompactChain chain, u32x4* ring,
+                                             const CompactEntry* __restrict__ entries, const int32_t* __restrict__ tiles,
+                                             const int32_t* __restrict__ turn, const float* __restrict__ angles) {
+  const int lane = threadIdx.x & 63;
+  // this lane's token of a block and its place in the two KiB of it: K holds rows of 8 dims, V is taken by dims and turned
+  const int label = octet_label(lane & 7);
+  const int t = IS_K ? swap23(lane & 15) : (lane >> 5) * 8 + label;
+  const int piece = IS_K ? lane >> 4 : lane >> 3 & 3;  // dims 8 piece .. of the first KiB; pieces 4 .. 7 are the second's
+  uint16_t* at0 = pool + (IS_K ? part * 512 + lane * 8 : PAGE * D + part * 1024 + (lane & ~7) * 8 + label * 8);
+  uint16_t* at1 = at0 + (IS_K ? D * 8 : 512);
+  const uint32_t before = (1u << t) - 1u;
+  auto slot_at = [&](int slot, int q) { return (slot & 31) * 8 + (q ^ (slot & 7)); };  // (rows a bank apart, whatever the slots)
+
+  int count = 0, stored = 0;  // tokens put into the ring, blocks stored
+  auto store = [&](int n) {  // the next 16 tokens of the ring, of which n are there
+    const int64_t o = tiles[chain.tile0 + stored] * block_elems;
+    u32x4 a = ring[slot_at(stored * PAGE + t, piece)], b = ring[slot_at(stored * PAGE + t, piece + 4)];
+    ++stored;
+    if (IS_K) {
+      if (t >= n) return;
     } else {
-      const int d = (wave - KW) * 64 + lane;
-      for (int o = 0; o * 8 < tile.n; ++o) {
-        Pack16 out;
-        out.u = *reinterpret_cast<const u32x4*>(dst + v_elem_offset(8 * o, d, D));
+      a = transpose8(a, label);
+      b = transpose8(b, label);
+      const int here = n - (lane >> 5) * 8;  // tokens of this lane's octet that are there
+      if (here <= 0) return;
+      if (here < 8) {  // the others stay as they are
+        Pack16 x, y, p, q;
+        x.u = a; y.u = b;
+        p.u = *reinterpret_cast<const u32x4*>(at0 + o);
+        q.u = *reinterpret_cast<const u32x4*>(at1 + o);
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          if (8 * o + e < tile.n) {
-            const int src = plan.src[tile.first + 8 * o + e];
-            out.s[e] = block_of(src / PAGE)[v_elem_offset(src % PAGE, d, D)];
+          if (e >= here) { x.s[e] = p.s[e]; y.s[e] = q.s[e]; }
+        a = x.u;
+        b = y.u;
+      }
+    }
+    *reinterpret_cast<u32x4*>(at0 + o) = a;
+    *reinterpret_cast<u32x4*>(at1 + o) = b;
+  };
+
+  u32x4 raw[COMPACT_AHEAD][2];
+  int rows[COMPACT_AHEAD];  // of the table, where a block's tokens turn differently
+  auto request = [&](int i, u32x4 (&r)[2], int& row) {  // (the last block again behind the end: nothing depends on a branch)
+    const CompactEntry e = entries[min(i, chain.entry1 - 1)];
+    const int64_t o = e.block * block_elems;
+    r[0] = load_nt(reinterpret_cast<const u32x4*>(at0 + o));
+    r[1] = load_nt(reinterpret_cast<const u32x4*>(at1 + o));
+    if (IS_K && e.turn == COMPACT_MIXED) row = turn[e.first + min(__popc(e.mask & before), __popc(e.mask) - 1)];
+  };
+  // K: the angles of a block are asked for one block ahead, so that waiting for them does not empty the queue of reads; two sets,
+  // which blocks that turn by one row share until another row comes
+  float cs[2][8], sn[2][8];
+  int held[2] = {COMPACT_STILL, COMPACT_STILL};
+  auto take = [&](int i, int row, float (&c)[8], float (&s)[8], int& held_row) {
+    const int by = entries[min(i, chain.entry1 - 1)].turn;
+    if (by == COMPACT_STILL || (by != COMPACT_MIXED && by == held_row)) return;
+    held_row = by;
+    if (by != COMPACT_MIXED) row = by;
+    const float* a = angles + (int64_t)max(row, 0) * D + part * 32 + piece * 8;  // of 8 dims; those D/2 above turn with them
+#pragma unroll
+    for (int e = 0; e < 8; ++e) { c[e] = a[e]; s[e] = a[D / 2 + e]; }
+  };
+#pragma unroll
+  for (int q = 0; q < COMPACT_AHEAD; ++q) request(chain.entry0 + q, raw[q], rows[q]);
+  if (IS_K) take(chain.entry0, rows[0], cs[0], sn[0], held[0]);
+  for (int i0 = chain.entry0; i0 < chain.entry1; i0 += COMPACT_AHEAD) {
+#pragma unroll
+    for (int q = 0; q < COMPACT_AHEAD; ++q) {
+      if (i0 + q >= chain.entry1) break;
+      const CompactEntry e = entries[i0 + q];
+      const int slot = count + __popc(e.mask & before);
+      Pack16 a, b;
+      a.u = raw[q][0];
+      b.u = raw[q][1];
+      const int row = e.turn == COMPACT_MIXED ? rows[q] : e.turn;
+      if (IS_K) take(i0 + q + 1, rows[(q + 1) % COMPACT_AHEAD], cs[(q + 1) & 1], sn[(q + 1) & 1], held[(q + 1) & 1]);
+      request(i0 + q + COMPACT_AHEAD, raw[q], rows[q]);
+      if (IS_K) {
+        if (e.turn != COMPACT_STILL) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const float x = (float)a.h[k], y = (float)b.h[k], c = cs[q & 1][k], s = sn[q & 1][k];
+            const bf16_t u = f32_to_bf16(x * c - y * s), v = f32_to_bf16(y * c + x * s);
+            if (row >= 0) { a.h[k] = u; b.h[k] = v; }  // (else: the bits as they are)
           }
-        *reinterpret_cast<u32x4*>(dst + v_elem_offset(8 * o, d, D)) = out.u;
+        }
+      } else {
+        a.u = transpose8(a.u, label);
+        b.u = transpose8(b.u, label);
+      }
+      if (e.mask >> t & 1) {
+        ring[slot_at(slot, piece)] = a.u;
+        ring[slot_at(slot, piece + 4)] = b.u;
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // (one wave: its LDS accesses take effect in the order they have here)
+      count += __popc(e.mask);
+      if (count >= (stored + 1) * PAGE) {
+        store(PAGE);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       }
     }
   }
+  if (count > stored * PAGE) store(count - stored * PAGE);
+}
+
+template <int D>
+__global__ __launch_bounds__(64 * COMPACT_WAVES) void compact_kernel(bf16_t* __restrict__ kv, int64_t layer_elems, int Hkv, int total,
+                                                                     const CompactChain* __restrict__ chains,
+                                                                     const CompactEntry* __restrict__ entries, const int32_t* __restrict__ tiles,
+                                                                     const int32_t* __restrict__ turn, const float* __restrict__ angles) {
+  constexpr int PARTS = 2 * (D / 64);  // waves of a head: K, then V
+  __shared__ u32x4 rings[COMPACT_WAVES][32 * 8];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int at = blockIdx.x * COMPACT_WAVES + wave;
+  if (at >= total) return;
+  const int part = at % PARTS, h = at / PARTS % Hkv;
+  const CompactChain chain = chains[at / (PARTS * Hkv)];
+  uint16_t* pool = reinterpret_cast<uint16_t*>(kv) + (int64_t)blockIdx.y * layer_elems + (int64_t)h * (2 * PAGE * D);
+  const int64_t block_elems = (int64_t)Hkv * (2 * PAGE * D);
+  if (part < PARTS / 2) compact_walk<D, true>(pool, block_elems, part, chain, rings[wave], entries, tiles, turn, angles);
+  else compact_walk<D, false>(pool, block_elems, part - PARTS / 2, chain, rings[wave], entries, tiles, turn, angles);
 }
 }  // namespace
 
@@ -200,8 +281,9 @@ hipError_t launch_page_image(bf16_t* kv, size_t layer_elems, int n_layers, const
 
 hipError_t launch_compact(bf16_t* kv, size_t layer_elems, int n_layers, int Hkv, int D, const CompactPlan& plan, int n_chains, hipStream_t s) {
   if (n_chains <= 0) return hipSuccess;
-  const dim3 grid((unsigned)(n_chains * Hkv), (unsigned)n_layers);
-  if (D == 128) compact_kernel<128><<<grid, dim3(256), 0, s>>>(kv, layer_elems, Hkv, plan);
-  else compact_kernel<64><<<grid, dim3(128), 0, s>>>(kv, layer_elems, Hkv, plan);
+  const int total = n_chains * Hkv * 2 * (D / 64);
+  const dim3 grid((unsigned)((total + COMPACT_WAVES - 1) / COMPACT_WAVES), (unsigned)n_layers), block(64 * COMPACT_WAVES);
+  if (D == 128) compact_kernel<128><<<grid, block, 0, s>>>(kv, layer_elems, Hkv, total, plan.chains, plan.entries, plan.tiles, plan.turn, plan.angles);
+  else compact_kernel<64><<<grid, block, 0, s>>>(kv, layer_elems, Hkv, total, plan.chains, plan.entries, plan.tiles, plan.turn, plan.angles);
   return hipGetLastError();
 }

@@ -1756,7 +1756,7 @@ extern "C" pie_status pie_restore_kvpage(pie_ctx* c, const int32_t* page_ids, in
   return guarded(c, "pie_restore_kvpage", [&]() { return page_image(c, page_ids, n, const_cast<void*>(image), true, "pie_restore_kvpage"); });
 }
 
-#define COMPACT_CHAIN 4  // tiles of a chain where the order of the tiles does not matter
+#define COMPACT_CHAIN 8  // destination blocks of a chain where the order of the blocks does not matter
 static pie_status pie_compact_kvpage_impl(pie_ctx* c, int32_t S, const int32_t* page_indptr, const int32_t* page_ids, const int32_t* kv_len,
                                           const int32_t* dst_indptr, const int32_t* dst_ids, const int32_t* shifts, int32_t* out_kv_len) {
   const char* who = "pie_compact_kvpage";
@@ -1791,40 +1791,48 @@ static pie_status pie_compact_kvpage_impl(pie_ctx* c, int32_t S, const int32_t* 
       if (m.stamp != id) m = pie_ctx::PageMark{id, s, j, LISTED};
       else m.flags |= MANY;
     }
-  std::vector<int32_t> src, turn, turns, kept(S);
-  std::vector<CompactTile> tiles;
-  std::vector<int2> chains;
-  src.reserve((size_t)total);
+  std::vector<int32_t> tiles, turn, turns, kept(S);
+  std::vector<CompactEntry> entries, blocks;
+  std::vector<CompactChain> chains;
   if (shifts) turn.reserve((size_t)total);
-  int64_t off = 0;
+  int64_t off = 0, kept_before = 0;
   for (int s = 0; s < S; ++s) {
     const int32_t* from = page_ids + page_indptr[s];
     const int32_t* to = dst_ids + dst_indptr[s];
-    const int n_to = dst_indptr[s + 1] - dst_indptr[s], first = (int)src.size();
+    const int n_to = dst_indptr[s + 1] - dst_indptr[s];
+    const int64_t room = (int64_t)n_to * P, first = kept_before;
     int n = 0, moved = -1;  // kept tokens so far; the first of them that does not stay as it is
+    blocks.clear();
     for (int j = 0; j * PAGE < kv_len[s]; ++j) {
       const int block = from[j / F] * F + j % F;
       uint32_t bits = c->page_mask[block];
       if (kv_len[s] - j * PAGE < PAGE) bits &= (1u << (kv_len[s] - j * PAGE)) - 1u;
-      for (; bits; bits &= bits - 1u, ++n) {
-        const int slot = __builtin_ctz(bits);
-        if (n / P >= n_to) return fail(c, PIE_EINVAL, "%s: sequence %d keeps more tokens than its %d destination pages hold", who, s, n_to);
-        const int32_t by = shifts ? shifts[off + j * PAGE + slot] : 0;
-        src.push_back(block * PAGE + slot);
-        if (shifts) {
-          if (by != 0 && (turns.empty() || turns.back() != by)) turns.push_back(by);
-          turn.push_back(by != 0 ? (int32_t)turns.size() - 1 : -1);
+      if (!bits) continue;
+      if (n + __builtin_popcount(bits) > room)
+        return fail(c, PIE_EINVAL, "%s: sequence %d keeps more tokens than its %d destination pages hold", who, s, n_to);
+      blocks.push_back(CompactEntry{block, bits, (int32_t)(first + n), COMPACT_STILL});
+      if (moved < 0 || shifts) {
+        int k = n;
+        for (uint32_t left = bits; left; left &= left - 1u, ++k) {
+          const int slot = __builtin_ctz(left);
+          const int32_t by = shifts ? shifts[off + j * PAGE + slot] : 0;
+          if (shifts) {
+            if (by != 0 && (turns.empty() || turns.back() != by)) turns.push_back(by);
+            turn.push_back(by != 0 ? (int32_t)turns.size() - 1 : -1);
+          }
+          if (moved < 0 && (by != 0 || slot != k % PAGE || block != to[k / P] * F + k % P / PAGE)) moved = k;
         }
-        if (moved < 0 && (by != 0 || (to[n / P] * F + n % P / PAGE) * PAGE + n % PAGE != src.back())) moved = n;
       }
+      n += __builtin_popcount(bits);
     }
     kept[s] = n;
+    kept_before += n;
     off += kv_len[s];
     if (moved < 0) continue;
-    const int tile0 = (int)tiles.size();
+    const int first_tile = moved / PAGE, n_tiles = (n + PAGE - 1) / PAGE, tile0 = (int)tiles.size() - first_tile;
     bool in_order = false;  // a page that is written is read by the same sequence
-    for (int i = moved / PAGE; i * PAGE < n; ++i) {
-      if (i == moved / PAGE || i % F == 0) {
+    for (int i = first_tile; i < n_tiles; ++i) {
+      if (i == first_tile || i % F == 0) {
         const int j = i / F;
         pie_ctx::PageMark& m = marks[to[j]];
         if (m.stamp != id) m = pie_ctx::PageMark{id, s, j, 0};
@@ -1833,23 +1841,46 @@ static pie_status pie_compact_kvpage_impl(pie_ctx* c, int32_t S, const int32_t* 
         in_order |= (m.flags & LISTED) != 0;
         m.flags |= WRITTEN;
       }
-      tiles.push_back(CompactTile{to[i / F] * F + i % F, first + i * PAGE, std::min(PAGE, n - i * PAGE)});
+      tiles.push_back(to[i / F] * F + i % F);
     }
-    const int step = in_order ? (int)tiles.size() - tile0 : COMPACT_CHAIN;
-    for (int t = tile0; t < (int)tiles.size(); t += step) chains.push_back(make_int2(t, std::min(t + step, (int)tiles.size())));
+    // chains: runs of destination blocks with the tokens that fill them; a block of tokens for two chains is in both
+    const int step = in_order ? n_tiles : COMPACT_CHAIN;
+    size_t b = 0;
+    int at = 0;  // kept tokens in front of blocks[b]
+    for (int i = first_tile; i < n_tiles; i += step) {
+      const int t0 = i * PAGE, t1 = std::min(n, (i + step) * PAGE);
+      const int entry0 = (int)entries.size();
+      while (at + __builtin_popcount(blocks[b].mask) <= t0) at += __builtin_popcount(blocks[b++].mask);
+      while (at < t1) {
+        uint32_t mask = blocks[b].mask;
+        const int here = __builtin_popcount(mask);
+        for (int k = at; k < t0; ++k) mask &= mask - 1u;  // the first ones are the chain's before
+        for (int k = at + here; k > t1; --k) mask &= ~(0x80000000u >> __builtin_clz(mask));
+        CompactEntry e{blocks[b].block, mask, (int32_t)(first + std::max(at, t0)), COMPACT_STILL};
+        if (shifts) {
+          const int32_t* row = turn.data() + e.first;
+          e.turn = std::all_of(row, row + __builtin_popcount(mask), [&](int32_t x) { return x == row[0]; }) ? row[0] : COMPACT_MIXED;
+        }
+        entries.push_back(e);
+        if (at + here > t1) break;
+        at += here;
+        ++b;
+      }
+      chains.push_back(CompactChain{entry0, (int)entries.size(), tile0 + i});
+    }
   }
   if (!chains.empty()) {
     OnDevice on(c);
     if (pie_status st = image_begin(c, who)) return st;
     Blob blob(c);
-    const size_t o_c = blob.add(chains.data(), chains.size() * sizeof(int2)), o_t = blob.add(tiles.data(), tiles.size() * sizeof(CompactTile));
-    const size_t o_s = blob.add(src.data(), src.size() * 4), o_i = turns.empty() ? 0 : blob.add(turn.data(), turn.size() * 4);
+    const size_t o_c = blob.add(chains.data(), chains.size() * sizeof(CompactChain)), o_e = blob.add(entries.data(), entries.size() * sizeof(CompactEntry));
+    const size_t o_t = blob.add(tiles.data(), tiles.size() * 4), o_i = turns.empty() ? 0 : blob.add(turn.data(), turn.size() * 4);
     const size_t o_v = turns.empty() ? 0 : blob.add(turns.data(), turns.size() * 4);
     const size_t o_a = (blob.size + 255) / 256 * 256;
     if (pie_status st = image_send(c, blob, turns.size() * D * sizeof(float), who)) return st;
     unsigned char* d = c->moves_dev;
     if (!turns.empty()) HIP_TRY(c, launch_rope_table((const int32_t*)(d + o_v), c->inv_freq, (int)turns.size(), D, (float*)(d + o_a), c->stream));
-    const CompactPlan plan{(const int2*)(d + o_c), (const CompactTile*)(d + o_t), (const int32_t*)(d + o_s),
+    const CompactPlan plan{(const CompactChain*)(d + o_c), (const CompactEntry*)(d + o_e), (const int32_t*)(d + o_t),
                            turns.empty() ? nullptr : (const int32_t*)(d + o_i), (const float*)(d + o_a)};
     HIP_TRY(c, launch_compact(c->kv, c->kv_layer_elems, c->m.n_layers, c->m.n_kv_heads, D, plan, (int)chains.size(), c->stream));
   }

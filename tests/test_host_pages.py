@@ -145,30 +145,45 @@ def compact_plans(c):
             ctx.close()
             continue
         image = c.copies()[-1]
-        # chains, tiles, sources, then, where a key turns, rows of the table and the shifts, each at a multiple of 256
+        # chains (entries from, to; first destination block), entries (block, mask, first kept token, row of the table or -1, -2),
+        # destination blocks, then, where a key turns, rows of the table and the shifts, each at a multiple of 256
         ints = np.frombuffer(image, np.int32)
-        n_tiles, k = 0, 0
-        while 2 * k < len(ints) and ints[2 * k] == n_tiles and ints[2 * k + 1] > n_tiles:
-            n_tiles, k = int(ints[2 * k + 1]), k + 1
-        chains = ints[:2 * k].reshape(-1, 2)
-        o = up(8 * k) // 4
-        tiles = ints[o:o + 3 * n_tiles].reshape(-1, 3)
-        o = up(4 * (o + 3 * n_tiles)) // 4
-        n_src = sum(kept)
-        src = ints[o:o + n_src]
+        k = n_entries = 0
+        while 3 * k < len(ints) and ints[3 * k] == n_entries and ints[3 * k + 1] > n_entries:
+            n_entries, k = int(ints[3 * k + 1]), k + 1
+        chains = ints[:3 * k].reshape(-1, 3)
+        o = up(12 * k) // 4
+        entries = ints[o:o + 4 * n_entries].reshape(-1, 4)
+        o = up(4 * (o + 4 * n_entries)) // 4
+        tiles = ints[o:]
         turning = any(isinstance(x, tuple) for x in want)
-        turn = np.full(n_src, -1)
+        turn = np.full(sum(kept), -1)
         if turning:
-            o = up(4 * (o + n_src)) // 4
-            turn = ints[o:o + n_src]
-            turns = ints[up(4 * (o + n_src)) // 4:]
+            n_tiles = max(c0[2] + -(-sum(bin(m).count("1") for _, m, _, _ in entries[c0[0]:c0[1]]) // 16) for c0 in chains)
+            o = up(4 * (o + n_tiles)) // 4
+            turn = ints[o:o + len(turn)]
+            turns = ints[up(4 * (o + len(turn))) // 4:]
             assert turn.max() == len(turns) - 1
         have = pool.copy()
-        for a, b in chains[::-1]:
-            for block, first, n in tiles[a:b]:
-                assert 0 < n <= 16
-                moved = [(have[x], int(turns[w])) if w >= 0 else have[x] for x, w in zip(src[first:first + n], turn[first:first + n])]
-                have[block * 16:block * 16 + n] = moved  # (block * 16 + slot counts tokens as page * P + slot does)
+        for e0, e1, tile in chains[::-1]:
+            ring, n_stored = [], 0
+            for block, mask, k, row in entries[e0:e1]:
+                assert 0 < mask < 1 << 16
+                some = set(turn[k:k + bin(mask).count("1")].tolist())
+                assert row == (some.pop() if len(some) == 1 else -2)
+                for slot in range(16):
+                    if mask >> slot & 1:
+                        x = have[block * 16 + slot]  # (block * 16 + slot counts tokens as page * P + slot does)
+                        ring.append((x, int(turns[turn[k]])) if turn[k] >= 0 else x)
+                        k += 1
+                while len(ring) >= 16 * (n_stored + 1):
+                    b0 = int(tiles[tile + n_stored]) * 16
+                    have[b0:b0 + 16] = ring[16 * n_stored:16 * n_stored + 16]
+                    n_stored += 1
+            rest = ring[16 * n_stored:]
+            if rest:
+                b0 = int(tiles[tile + n_stored]) * 16
+                have[b0:b0 + len(rest)] = rest
         assert all(x == y for x, y in zip(have, want)), trial
         ctx.close()
 
