@@ -156,16 +156,17 @@ __device__ __forceinline__ double key_score(u64 k) { return __longlong_as_double
 #define BP_CANDS 512  // candidates that are ranked against each other
 #define BP_CACHED 8192  // maxima of segments kept in LDS
 struct BeamGroups { int32_t row0[BEAM_GROUPS_BY_VALUE + 1]; };
+#define BP_HELD (BP_CACHED / BP_THREADS)
 struct PickShared {
   double2 row[BEAM_MAX_ROWS];  // (b, m): score = b + (z - m) / T; b = -inf: no candidates
   u64 cand_key[BP_CANDS];
-  int cand_idx[BP_CANDS], rank[BP_CANDS];
+  int cand_idx[BP_CANDS];
   int segs[BP_SEGS], segs_sorted[BP_SEGS];
   uint32_t hist[1024];
   float maxima[BP_CACHED];
   u64 red_lo[BP_THREADS / 64], red_hi[BP_THREADS / 64];
   uint32_t red_n[BP_THREADS / 64];
-  uint32_t count, bin, below, upto;
+  uint32_t count, n_cand, bin, below, upto;
   uint8_t done[BEAM_MAX_ROWS];
 };
 
@@ -274,97 +275,128 @@ __device__ uint32_t pick_collect(PickShared& sh, int n, const Bound& b, F key, P
   return have;
 }
 
+// How far a score is behind the best of the group, as a bin: 64 to an octave from half a nat on (a bin is 0.008 wide at the front,
+// then 1/64 to 1/128 of the distance), up to 32767 nats.  Distances are sums of two terms of one sign in fp32, off by 1e-6 of
+// themselves: whoever takes one bin more than needed misses nobody.
+#define BP_BINS 1024
+__device__ __forceinline__ uint32_t far_bin(float d) { return min((__float_as_uint(d + 0.5f) >> 17) - (__float_as_uint(0.5f) >> 17), (uint32_t)BP_BINS - 1u); }
+
 template <typename T>
-__global__ __launch_bounds__(BP_THREADS) void beam_pick_kernel(const T* __restrict__ logits, int64_t stride, int V, int n_tiles, double inv_temp,
-                                                               const float* __restrict__ scores, const uint8_t* __restrict__ finished, int eos,
-                                                               BeamGroups groups, int n_out, const float* __restrict__ seg_max,
-                                                               const float2* __restrict__ tile_stats, int32_t* __restrict__ out_beams,
-                                                               int32_t* __restrict__ out_tokens, float* __restrict__ out_scores) {
-  constexpr int VEC = BeamRow<T>::VEC, SEG = BeamRow<T>::SEG;
-  __shared__ PickShared sh;
-  const int g = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int row0 = groups.row0[g], rows = groups.row0[g + 1] - row0;
-  const int n_segs = n_tiles * BT_SEGS, n = rows * n_segs;
-  const float* maxima = seg_max + (int64_t)row0 * n_segs;
+struct Picker {
+  static constexpr int VEC = BeamRow<T>::VEC, SEG = BeamRow<T>::SEG;
+  PickShared& sh;
+  const T* logits;
+  int64_t stride;
+  int V, n_segs, n, n_out, row0, rows, eos;
+  double inv_temp;
+  float per;             // 1 / n_segs
+  const float* maxima;   // of the group's segments, in LDS or not
+  int tid, lane, wave;
 
-  for (int r = wave; r < rows; r += BP_THREADS / 64) {  // a wave per row: its tiles' sums
-    const float s = beam_score(scores, row0 + r);
-    const bool done = finished && finished[row0 + r];
-    double b = -INFINITY, m = 0;
-    if (done) b = s;
-    else if (s != -INFINITY) {
-      float top = -INFINITY;
-      for (int t = lane; t < n_tiles; t += 64) top = fmaxf(top, tile_stats[(int64_t)(row0 + r) * n_tiles + t].x);
-      top = wave_max(top);
-      if (top != -INFINITY) {
-        double sum = 0;
-        for (int t = lane; t < n_tiles; t += 64) {
-          const float2 st = tile_stats[(int64_t)(row0 + r) * n_tiles + t];
-          if (st.x != -INFINITY) sum += (double)st.y * exp(((double)st.x - (double)top) * inv_temp);
-        }
-        sum = wave_sum_f64(sum);
-        m = top;
-        b = (double)s - log(sum);
-      }
-    }
-    if (lane == 0) { sh.row[r] = make_double2(b, m); sh.done[r] = done; }
-  }
-  const bool cached = n <= BP_CACHED;
-  if (cached)
-    for (int i = tid; i < n; i += BP_THREADS) sh.maxima[i] = maxima[i];
-  __syncthreads();
-
-  const float per = 1.0f / (float)n_segs;
-  auto row_of = [&](int i) { return (int)(((float)i + 0.5f) * per); };  // (i < 256 x 512: off by 5e-5, half a segment is 1e-3)
-  auto key_of = [&](int r, float z) {
+  __device__ int row_of(int i) const { return (int)(((float)i + 0.5f) * per); }  // (i < 256 x 512: off by 5e-5, half a segment is 1e-3)
+  __device__ u64 key_of(int r, float z) const {
     const double2 b = sh.row[r];
     return b.x == -INFINITY || z == -INFINITY ? 0ull : score_key(b.x + ((double)z - b.y) * inv_temp);
-  };
-  // a finished row's one candidate stands in its first segment
-  auto seg_key = [&](int i) {
-    const int r = row_of(i);
-    if (sh.done[r]) return i == r * n_segs && sh.row[r].x != -INFINITY ? score_key(sh.row[r].x) : 0ull;
-    return key_of(r, cached ? sh.maxima[i] : maxima[i]);
-  };
-  const Bound segs = pick_bound(sh, n, (uint32_t)n_out, (uint32_t)(2 * n_out + 64), seg_key);
-  const uint32_t n_kept = pick_collect(sh, n, segs, seg_key, [&](uint32_t at, int i, u64) { sh.segs[at] = i; });
-
-  // candidates: the logits of the kept segments that reach the bound (every one, where there are fewer segments than candidates asked for)
-  const u64 floor_key = segs.n < (uint32_t)n_out ? 1ull : segs.lo;
-  const int n_elems = (int)n_kept * SEG;
-  if (tid == 0) sh.count = 0;
-  __syncthreads();
-  for (int e = tid * VEC; e < n_elems; e += BP_THREADS * VEC) {
-    const int i = sh.segs[e / SEG], r = row_of(i), p = (i - r * n_segs) * SEG + e % SEG;
-    if (sh.done[r]) {
-      if (e % SEG == 0) {
-        const uint32_t at = atomicAdd(&sh.count, 1u);
-        if (at < BP_CANDS) { sh.cand_key[at] = score_key(sh.row[r].x); sh.cand_idx[at] = r * V + eos; }
-      }
-      continue;
-    }
-    const BeamRow<T> z(logits, stride, row0 + r, V);
-    float x[VEC];
-    z.load(p, x);
-#pragma unroll
-    for (int k = 0; k < VEC; ++k) {
-      const u64 key = key_of(r, x[k]);
-      if (key >= floor_key) {
-        const uint32_t at = atomicAdd(&sh.count, 1u);
-        if (at < BP_CANDS) { sh.cand_key[at] = key; sh.cand_idx[at] = r * V + p + k; }
-      }
-    }
   }
-  __syncthreads();
-  uint32_t n_cand = sh.count;
-  if (n_cand > BP_CANDS) {  // crowded: the same choice among the segments' logits, one by one, in order of their places
-    for (int i = tid; i < (int)n_kept; i += BP_THREADS) {
+
+  // The usual call: the group's candidates by their distances in fp32, one pass over the segments' maxima (in registers) and one over
+  // the logits of those kept.  Returns how many candidates it left in sh, or -1 where that does not serve: candidates further
+  // apart than the bins reach or more of them in a bin than there is room for.
+  template <typename H>
+  __device__ int quick(const H& held) {
+    double best = -INFINITY;
+    for (int r = lane; r < rows; r += 64) best = fmax(best, sh.row[r].x);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) best = fmax(best, __shfl_xor(best, o));
+    if (best == -INFINITY) return 0;  // (uniform over the workgroup)
+    const float c = (float)inv_temp;
+    auto bin_of = [&](int r, float z) {  // BP_BINS - 1: not counted
+      const double2 b = sh.row[r];
+      return far_bin((float)(best - b.x) + ((float)b.y - z) * c);  // (-inf: infinitely far)
+    };
+    uint32_t bins[BP_HELD];
+#pragma unroll
+    for (int j = 0; j < BP_HELD; ++j) {
+      const int i = tid + j * BP_THREADS;
+      bins[j] = BP_BINS - 1;
+      if (i < n) {
+        const int r = row_of(i);
+        bins[j] = sh.done[r] ? (i == r * n_segs ? far_bin((float)(best - sh.row[r].x)) : BP_BINS - 1u) : bin_of(r, held[j]);
+        if (bins[j] < BP_BINS - 1) atomicAdd(&sh.hist[bins[j]], 1u);
+      }
+    }
+    __syncthreads();
+    // every wave finds the bin of the n_out-th segment for itself, 16 bins to a lane
+    uint32_t h[16], mine = 0;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) { h[k] = sh.hist[lane * 16 + k]; mine += h[k]; }
+    uint32_t incl = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const uint32_t up = __shfl_up(incl, o);
+      if (lane >= o) incl += up;
+    }
+    const u64 reached = __ballot(incl >= (uint32_t)n_out);
+    if (!reached) return -1;
+    const int at = __ffsll((long long)reached) - 1;
+    uint32_t run = incl - mine, bin = 0;
+    bool found = false;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+      run += h[k];
+      if (!found && run >= (uint32_t)n_out) { found = true; bin = lane * 16 + k; }
+    }
+    bin = __shfl(bin, at) + 1;  // (one more: see far_bin)
+    if (bin >= BP_BINS - 1) return -1;
+#pragma unroll
+    for (int j = 0; j < BP_HELD; ++j)
+      if (bins[j] <= bin) {
+        const uint32_t k = atomicAdd(&sh.count, 1u);
+        if (k < BP_SEGS) sh.segs[k] = tid + j * BP_THREADS;
+      }
+    __syncthreads();
+    const int kept = (int)sh.count;
+    if (kept > BP_SEGS) return -1;
+    for (int e = tid * VEC; e < kept * SEG; e += BP_THREADS * VEC) {
+      const int i = sh.segs[e / SEG], r = row_of(i), p = (i - r * n_segs) * SEG + e % SEG;
+      if (sh.done[r]) {
+        if (e % SEG == 0) put(score_key(sh.row[r].x), r * V + eos);
+        continue;
+      }
+      const BeamRow<T> z(logits, stride, row0 + r, V);
+      float x[VEC];
+      z.load(p, x);
+#pragma unroll
+      for (int k = 0; k < VEC; ++k)
+        if (bin_of(r, x[k]) <= bin) put(key_of(r, x[k]), r * V + p + k);
+    }
+    __syncthreads();
+    return sh.n_cand <= BP_CANDS ? (int)sh.n_cand : -1;
+  }
+  __device__ void put(u64 key, int idx) {
+    const uint32_t at = atomicAdd(&sh.n_cand, 1u);
+    if (at < BP_CANDS) { sh.cand_key[at] = key; sh.cand_idx[at] = idx; }
+  }
+
+  // Any group: the same choice by exact bounds, twice.
+  __device__ int exactly() {
+    // a finished row's one candidate stands in its first segment
+    auto seg_key = [&](int i) {
+      const int r = row_of(i);
+      if (sh.done[r]) return i == r * n_segs && sh.row[r].x != -INFINITY ? score_key(sh.row[r].x) : 0ull;
+      return key_of(r, maxima[i]);
+    };
+    const Bound segs = pick_bound(sh, n, (uint32_t)n_out, (uint32_t)(2 * n_out + 64), seg_key);
+    const int kept = (int)pick_collect(sh, n, segs, seg_key, [&](uint32_t at, int i, u64) { sh.segs[at] = i; });
+    for (int i = tid; i < kept; i += BP_THREADS) {  // in order of their places
       const int mine = sh.segs[i];
       int at = 0;
-      for (int k = 0; k < (int)n_kept; ++k) at += sh.segs[k] < mine;
+      for (int k = 0; k < kept; ++k) at += sh.segs[k] < mine;
       sh.segs_sorted[at] = mine;
     }
     __syncthreads();
+    // candidates: the kept segments' logits that reach the bound (all, where there are fewer segments than candidates asked for)
+    const u64 floor_key = segs.n < (uint32_t)n_out ? 1ull : segs.lo;
     auto place = [&](int e, int& r, int& p) {
       const int i = sh.segs_sorted[e / SEG];
       r = row_of(i);
@@ -374,48 +406,90 @@ __global__ __launch_bounds__(BP_THREADS) void beam_pick_kernel(const T* __restri
       int r, p;
       place(e, r, p);
       if (sh.done[r]) return e % SEG == 0 ? score_key(sh.row[r].x) : 0ull;
-      const BeamRow<T> z(logits, stride, row0 + r, V);
       if (p >= V) return 0ull;
-      const u64 k = key_of(r, beam_logit(z.z[p]));
+      const u64 k = key_of(r, beam_logit(logits[(int64_t)(row0 + r) * stride + p]));
       return k >= floor_key ? k : 0ull;
     };
-    const Bound best = pick_bound(sh, n_elems, (uint32_t)n_out, (uint32_t)BP_CANDS, elem_key);
-    n_cand = pick_collect(sh, n_elems, best, elem_key, [&](uint32_t at, int e, u64 key) {
+    const Bound best = pick_bound(sh, kept * SEG, (uint32_t)n_out, (uint32_t)BP_CANDS, elem_key);
+    return (int)pick_collect(sh, kept * SEG, best, elem_key, [&](uint32_t at, int e, u64 key) {
       int r, p;
       place(e, r, p);
       sh.cand_key[at] = key;
       sh.cand_idx[at] = r * V + (sh.done[r] ? eos : p);
     });
   }
+};
 
-  // their ranks: each is compared with all, the work of one shared by as many threads as there are to a candidate
-  for (int i = tid; i < (int)n_cand; i += BP_THREADS) sh.rank[i] = 0;
+template <typename T>
+__global__ __launch_bounds__(BP_THREADS) void beam_pick_kernel(const T* __restrict__ logits, int64_t stride, int V, int n_tiles, double inv_temp,
+                                                               const float* __restrict__ scores, const uint8_t* __restrict__ finished, int eos,
+                                                               BeamGroups groups, int n_out, const float* __restrict__ seg_max,
+                                                               const float2* __restrict__ tile_stats, int32_t* __restrict__ out_beams,
+                                                               int32_t* __restrict__ out_tokens, float* __restrict__ out_scores) {
+  __shared__ PickShared sh;
+  const int g = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int row0 = groups.row0[g], rows = groups.row0[g + 1] - row0;
+  const int n_segs = n_tiles * BT_SEGS, n = rows * n_segs;
+  const float* maxima = seg_max + (int64_t)row0 * n_segs;
+  const bool cached = n <= BP_CACHED;
+  float held[BP_HELD];
+#pragma unroll
+  for (int j = 0; j < BP_HELD; ++j) held[j] = cached && tid + j * BP_THREADS < n ? maxima[tid + j * BP_THREADS] : 0.f;
+
+  for (int r = wave; r < rows; r += BP_THREADS / 64) {  // a wave per row: its tiles' sums
+    const float s = beam_score(scores, row0 + r);
+    const bool done = finished && finished[row0 + r];
+    double b = -INFINITY, m = 0;
+    if (done) b = s;
+    else if (s != -INFINITY) {
+      const float2* stats = tile_stats + (int64_t)(row0 + r) * n_tiles;  // (64 at most)
+      const float2 st = lane < n_tiles ? stats[lane] : make_float2(-INFINITY, 0.f);
+      const float top = wave_max(st.x);
+      if (top != -INFINITY) {
+        const double sum = wave_sum_f64(st.x == -INFINITY ? 0.0 : (double)st.y * exp(((double)st.x - (double)top) * inv_temp));
+        m = top;
+        b = (double)s - log(sum);
+      }
+    }
+    if (lane == 0) { sh.row[r] = make_double2(b, m); sh.done[r] = done; }
+  }
+  if (cached) {
+#pragma unroll
+    for (int j = 0; j < BP_HELD; ++j)
+      if (tid + j * BP_THREADS < n) sh.maxima[tid + j * BP_THREADS] = held[j];
+  }
+  sh.hist[tid] = 0;
+  if (tid == 0) sh.count = sh.n_cand = 0;
   __syncthreads();
+
+  Picker<T> pick{sh, logits, stride, V, n_segs, n, n_out, row0, rows, eos, inv_temp, 1.0f / (float)n_segs, cached ? sh.maxima : maxima, tid, lane, wave};
+  int n_cand = cached ? pick.quick(held) : -1;
+  if (n_cand < 0) n_cand = pick.exactly();  // (uniform)
+
+  // their ranks: each is compared with all by a group of lanes
+  const int64_t o = (int64_t)g * n_out;
   if (n_cand) {
-    const int share = BP_THREADS / (int)n_cand > 0 ? BP_THREADS / (int)n_cand : 1;  // (n_cand <= 512)
-    const int c = tid / share, part = tid % share;
-    if (c < (int)n_cand) {
+    int share = 64;  // lanes to a candidate (n_cand <= 512)
+    while (share * n_cand > BP_THREADS) share >>= 1;
+    const int c = tid / share;
+    if (c < n_cand) {
       const u64 key = sh.cand_key[c];
       const int idx = sh.cand_idx[c];
-      int before = 0;
-      for (int k = part; k < (int)n_cand; k += share) {
+      int at = 0;
+      for (int k = tid % share; k < n_cand; k += share) {
         const u64 k2 = sh.cand_key[k];
-        before += k2 > key || (k2 == key && sh.cand_idx[k] < idx);
+        at += k2 > key || (k2 == key && sh.cand_idx[k] < idx);
       }
-      if (before) atomicAdd(&sh.rank[c], before);
+      for (int d = share >> 1; d > 0; d >>= 1) at += __shfl_xor(at, d);
+      if (tid % share == 0 && at < n_out) {
+        const int r = idx / V;
+        out_beams[o + at] = r;
+        out_tokens[o + at] = idx - r * V;
+        out_scores[o + at] = (float)key_score(key);
+      }
     }
   }
-  __syncthreads();
-  const int64_t o = (int64_t)g * n_out;
-  for (int i = tid; i < (int)n_cand; i += BP_THREADS) {
-    const int at = sh.rank[i];
-    if (at >= n_out) continue;
-    const int idx = sh.cand_idx[i], r = idx / V;
-    out_beams[o + at] = r;
-    out_tokens[o + at] = idx - r * V;
-    out_scores[o + at] = (float)key_score(sh.cand_key[i]);
-  }
-  for (int i = (int)n_cand + tid; i < n_out; i += BP_THREADS) {
+  for (int i = n_cand + tid; i < n_out; i += BP_THREADS) {
     out_beams[o + i] = -1;
     out_tokens[o + i] = -1;
     out_scores[o + i] = -INFINITY;
