@@ -145,10 +145,10 @@ pie_status pie_copy_kvpage(pie_ctx* ctx, const int32_t* src_pages, const int32_t
 
 /* Page dst_pages[i] becomes what page src_pages[i] was before the call: K and V in every layer, bit for bit, and its mask.  A
  * source may be named any number of times, and a page may be both source and destination, so the pages of beams that were
- * reordered may be permuted in place; src == dst does nothing.  Host int32 arrays [n].  Up to 160 pages travel as kernel
- * arguments, so such a call may be captured into a graph (a replay repeats the copies; the masks were set when it was captured);
- * a longer one is refused with PIE_EHIP while the stream is captured, and may allocate.
- * Errors: PIE_EINVAL, PIE_ERANGE, PIE_ECONFLICT (a destination named twice), PIE_ENOMEM, PIE_EHIP. */
+ * reordered may be permuted in place; src == dst does nothing.  Host int32 arrays [n].  The pages' numbers travel as kernel
+ * arguments, 160 to a launch: nothing is allocated on the device, and the call may be captured into a graph (a replay repeats the
+ * copies; the masks were set when it was captured).
+ * Errors: PIE_EINVAL, PIE_ERANGE, PIE_ECONFLICT (a destination named twice), PIE_ENOMEM (host), PIE_EHIP. */
 pie_status pie_fork_kvpage(pie_ctx* ctx, const int32_t* src_pages, const int32_t* dst_pages, int32_t n);
 
 /* Saves pages into the caller's memory, and restores pages from it: image is dev bf16

@@ -145,6 +145,11 @@ def _ptr(a: Optional[np.ndarray]):
     return None if a is None else a.ctypes.data_as(C.c_void_p)
 
 
+def _at(a):
+    """Address of an array that the caller keeps until the call has returned (_ptr keeps it itself and takes longer)."""
+    return None if a is None else a.__array_interface__["data"][0]
+
+
 class PieBatch:
     def __init__(self, owner: "Pie", handle, keepalive):
         self.owner, self.handle, self._keep = owner, handle, keepalive
@@ -333,7 +338,7 @@ class Pie:
         s, d = _i32(src_pages), _i32(dst_pages)
         if len(s) != len(d):
             raise ValueError("fork_kvpage: one destination per source")
-        self._check(self.lib.pie_fork_kvpage(self.ctx, _ptr(s), _ptr(d), len(s)))
+        self._check(self.lib.pie_fork_kvpage(self.ctx, _at(s), _at(d), len(s)))
 
     def _image(self, page_ids, image: torch.Tensor) -> np.ndarray:
         ids, m = _i32(page_ids), self.model
@@ -346,12 +351,12 @@ class Pie:
     def save_kvpage(self, page_ids, image: torch.Tensor):
         """Enqueues the copy of the pages into `image` [pages, layers, 2, page_size, kv heads, head_dim]."""
         ids = self._image(page_ids, image)
-        self._check(self.lib.pie_save_kvpage(self.ctx, _ptr(ids), len(ids), C.c_void_p(image.data_ptr())))
+        self._check(self.lib.pie_save_kvpage(self.ctx, _at(ids), len(ids), image.data_ptr()))
 
     def restore_kvpage(self, page_ids, image: torch.Tensor):
         """Enqueues the copy of `image` into the pages; it has to stay as it is until the stream has got there."""
         ids = self._image(page_ids, image)
-        self._check(self.lib.pie_restore_kvpage(self.ctx, _ptr(ids), len(ids), C.c_void_p(image.data_ptr())))
+        self._check(self.lib.pie_restore_kvpage(self.ctx, _at(ids), len(ids), image.data_ptr()))
 
     def compact_kvpage(self, page_indptr, page_ids, kv_len, shifts=None, dst_page_indptr=None, dst_page_ids=None) -> np.ndarray:
         """Returns the sequences' new lengths; the moves are enqueued."""
@@ -364,7 +369,7 @@ class Pie:
                 (dp is not None and (len(dp) != len(kl) + 1 or dp[-1] != len(di))):
             raise ValueError("compact_kvpage: arrays of lengths that do not belong together")
         out = np.zeros(len(kl), dtype=np.int32)
-        self._check(self.lib.pie_compact_kvpage(self.ctx, len(kl), _ptr(ip), _ptr(ids), _ptr(kl), _ptr(dp), _ptr(di), _ptr(sh), _ptr(out)))
+        self._check(self.lib.pie_compact_kvpage(self.ctx, len(kl), _at(ip), _at(ids), _at(kl), _at(dp), _at(di), _at(sh), _at(out)))
         return out
 
     def kv_read(self, layer: int, page_ids, slots):
@@ -452,7 +457,7 @@ class Pie:
             if t is not None and (t.dtype not in dts or not t.is_cuda or not t.is_contiguous() or t.numel() != n):
                 raise ValueError("beam search: scores (float32) and finished (uint8 or bool) are contiguous device tensors [rows]")
         at = lambda t: None if t is None else t.data_ptr()
-        return BeamSearchC(G, ip.ctypes.data, at(scores), at(finished), int(eos_token), int(n_out), float(temperature)), ip
+        return BeamSearchC(G, _at(ip), at(scores), at(finished), int(eos_token), int(n_out), float(temperature)), ip
 
     def beam_select_async(self, logits: torch.Tensor, group_indptr, n_out: int, out_beams: torch.Tensor, out_tokens: torch.Tensor,
                           out_scores: torch.Tensor, scores: Optional[torch.Tensor] = None, finished: Optional[torch.Tensor] = None,
@@ -465,9 +470,8 @@ class Pie:
                 (logits.shape[1] > 1 and logits.stride(1) != 1):
             raise ValueError("beam_select: logits are a device tensor [rows, vocab] of float32, bfloat16 or float16 whose rows are contiguous")
         stride = logits.stride(0) if logits.shape[0] > 1 else logits.shape[1]
-        self._check(self.lib.pie_beam_select(self.ctx, C.byref(b), C.c_void_p(logits.data_ptr()), types[logits.dtype], stride,
-                                             logits.shape[1], C.c_void_p(out_beams.data_ptr()), C.c_void_p(out_tokens.data_ptr()),
-                                             C.c_void_p(out_scores.data_ptr())))
+        self._check(self.lib.pie_beam_select(self.ctx, C.byref(b), logits.data_ptr(), types[logits.dtype], stride, logits.shape[1],
+                                             out_beams.data_ptr(), out_tokens.data_ptr(), out_scores.data_ptr()))
 
     def get_next_beams_async(self, embed_ids, group_indptr, n_out: int, out_beams: torch.Tensor, out_tokens: torch.Tensor,
                              out_scores: torch.Tensor, scores: Optional[torch.Tensor] = None, finished: Optional[torch.Tensor] = None,
@@ -477,8 +481,7 @@ class Pie:
         b, keep = self._beam_search(group_indptr, n_out, out_beams, out_tokens, out_scores, scores, finished, eos_token, temperature)
         if len(ids) != keep[-1]:
             raise ValueError("get_next_beams: one Embed per row")
-        self._check(self.lib.pie_get_next_beams(self.ctx, C.byref(b), _ptr(ids), C.c_void_p(out_beams.data_ptr()),
-                                                C.c_void_p(out_tokens.data_ptr()), C.c_void_p(out_scores.data_ptr())))
+        self._check(self.lib.pie_get_next_beams(self.ctx, C.byref(b), _at(ids), out_beams.data_ptr(), out_tokens.data_ptr(), out_scores.data_ptr()))
 
     def get_next_beams(self, embed_ids, group_indptr, n_out: int, scores=None, finished=None, eos_token: int = -1, temperature: float = 1.0):
         """The same with host arrays: (beams, tokens, scores) [groups, n_out], after the stream has been waited for."""

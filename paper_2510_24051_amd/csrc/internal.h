@@ -9,6 +9,7 @@
 
 #include "../../include/pie_mi355.h"
 #include "common.h"
+#include "page_plans.h"
 
 #define PAGE 16  // tokens per block of the KvPage pool the kernels are built for (a KvPage is one or two blocks)
 
@@ -373,11 +374,8 @@ size_t beam_ws_doubles(int rows, int vocab);
 hipError_t launch_beam_select(const BeamArgs& a, hipStream_t s);
 
 // Pages (pages.hip)
-struct PageMove { int32_t src, dst; };            // src -1: the page kept at the start of the run
-struct PageRun { int32_t first, n, keep; };       // moves [first, first + n) in order; keep >= 0: a page read before them
-#define FORK_BY_VALUE 160  // moves (and runs) of a launch that travel as kernel arguments, of which it takes 4 KiB
 hipError_t launch_fork(bf16_t* kv, size_t layer_elems, int n_layers, size_t page_elems, const PageMove* moves, int n_moves, const PageRun* runs,
-                       int n_runs, bool on_device, hipStream_t s);
+                       int n_runs, hipStream_t s);
 // pages host_ids[0 .. n) of F blocks each to the caller's image [n][layer][K or V][slot][kv head][dim], or back
 hipError_t launch_page_image(bf16_t* kv, size_t layer_elems, int n_layers, const int32_t* host_ids, int n, int F, int Hkv, int D, bf16_t* image,
                              bool to_pool, hipStream_t s);
@@ -392,7 +390,11 @@ struct CompactPlan {
   const CompactChain* chains;
   const CompactEntry* entries;
   const int32_t* tiles;
-  const int32_t* turn;       // per kept token: row of `angles`, -1 = not rotated; null: none is
+  const int32_t* turn;       // per kept token: row of `angles`, -1 = not rotated (read for COMPACT_MIXED entries)
   const float* angles;       // [turns, D] cos | sin
 };
+#define PLAN_BY_VALUE 3584  // bytes of a plan that travel as kernel arguments, of which a launch takes 4 KiB
+// plan -> dev, and the table [n_turns, D] of cos | sin of the n_turns shifts at byte `turns` of it
+hipError_t launch_put_plan(const unsigned char* plan, size_t size, unsigned char* dev, size_t turns, int n_turns, const double* inv_freq, int D,
+                           float* angles, hipStream_t s);
 hipError_t launch_compact(bf16_t* kv, size_t layer_elems, int n_layers, int Hkv, int D, const CompactPlan& plan, int n_chains, hipStream_t s);

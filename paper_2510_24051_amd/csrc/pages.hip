@@ -10,38 +10,29 @@ namespace {
 // A thread owns the same 16 bytes of every page of its layer and walks the moves of one run in order.  The host orders them so that
 // a page is written only after every move that reads it, so within a thread each load comes before the store that replaces what it
 // reads, and no other thread touches those bytes: any graph of moves, permutations included, needs no second buffer and no
-// synchronisation.  A run with a cycle starts by keeping the page that the cycle's last move reads (PageRun::keep).
+// synchronisation.  A run with a cycle starts by keeping the page that the cycle's last move reads (PageRun::keep; the
+// order: page_plans.h).
 #define FORK_THREADS 256
-template <typename Plan>
+struct ForkMoves {
+  PageMove moves[FORK_MOVES];
+  PageRun runs[FORK_MOVES];
+};
 __global__ __launch_bounds__(FORK_THREADS) void fork_kernel(unsigned char* __restrict__ kv, int64_t layer_bytes, int64_t page_bytes, int slices,
-                                                            Plan plan) {
+                                                            ForkMoves plan) {
   const int run = blockIdx.x / slices, slice = blockIdx.x % slices;
   unsigned char* base = kv + (int64_t)blockIdx.y * layer_bytes + ((int64_t)slice * FORK_THREADS + threadIdx.x) * 16;
-  const PageRun r = plan.run(run);
+  const PageRun r = plan.runs[run];
   u32x4 kept = {0, 0, 0, 0}, v = {0, 0, 0, 0};
   if (r.keep >= 0) kept = *reinterpret_cast<const u32x4*>(base + r.keep * page_bytes);
   int last = -1;
   for (int i = r.first; i < r.first + r.n; ++i) {
-    const PageMove m = plan.move(i);
+    const PageMove m = plan.moves[i];
     if (m.src < 0) v = kept;
     else if (m.src != last) v = load_nt(reinterpret_cast<const u32x4*>(base + m.src * page_bytes));
     last = m.src;
     *reinterpret_cast<u32x4*>(base + m.dst * page_bytes) = v;
   }
 }
-
-struct ForkByValue {
-  PageMove moves[FORK_BY_VALUE];
-  PageRun runs[FORK_BY_VALUE];
-  __device__ PageRun run(int i) const { return runs[i]; }
-  __device__ PageMove move(int i) const { return moves[i]; }
-};
-struct ForkByPointer {
-  const PageMove* moves;
-  const PageRun* runs;
-  __device__ PageRun run(int i) const { return runs[i]; }
-  __device__ PageMove move(int i) const { return moves[i]; }
-};
 
 // ---------------------------------------------------------------------------------------------
 // save and restore
@@ -241,23 +232,32 @@ __global__ __launch_bounds__(64 * COMPACT_WAVES) void compact_kernel(bf16_t* __r
   if (part < PARTS / 2) compact_walk<D, true>(pool, block_elems, part, chain, rings[wave], entries, tiles, turn, angles);
   else compact_walk<D, false>(pool, block_elems, part - PARTS / 2, chain, rings[wave], entries, tiles, turn, angles);
 }
+
+// A small plan, as kernel arguments, into device memory, and the angles of its shifts (64 bits, rounded once: a shift may be long).
+struct PlanBytes { uint32_t w[PLAN_BY_VALUE / 4]; };
+__global__ void put_plan_kernel(PlanBytes plan, int words, uint32_t* __restrict__ dev, int turn0, int n_turns, const double* __restrict__ inv_freq,
+                                int D, float* __restrict__ angles) {
+  const int idx = blockIdx.x * blockDim.x + threadIdx.x, half = D / 2;
+  if (idx < words) dev[idx] = plan.w[idx];
+  if (idx >= n_turns * half) return;
+  const int r = idx / half, i = idx % half;
+  double sn, cs;
+  sincos((double)(int32_t)plan.w[turn0 + r] * inv_freq[i], &sn, &cs);
+  angles[(int64_t)r * D + i] = (float)cs;
+  angles[(int64_t)r * D + half + i] = (float)sn;
+}
 }  // namespace
 
 hipError_t launch_fork(bf16_t* kv, size_t layer_elems, int n_layers, size_t page_elems, const PageMove* moves, int n_moves, const PageRun* runs,
-                       int n_runs, bool on_device, hipStream_t s) {
+                       int n_runs, hipStream_t s) {
+  if (n_moves > FORK_MOVES || n_runs > FORK_MOVES) return hipErrorInvalidValue;
   if (n_runs <= 0) return hipSuccess;
   const int slices = (int)(page_elems * sizeof(bf16_t) / (FORK_THREADS * 16));  // (a page has a multiple of 4 KiB in a layer)
-  const dim3 grid((unsigned)(n_runs * slices), (unsigned)n_layers), block(FORK_THREADS);
-  unsigned char* p = reinterpret_cast<unsigned char*>(kv);
-  if (on_device) {
-    fork_kernel<ForkByPointer><<<grid, block, 0, s>>>(p, layer_elems * 2, page_elems * 2, slices, ForkByPointer{moves, runs});
-    return hipGetLastError();
-  }
-  if (n_moves > FORK_BY_VALUE || n_runs > FORK_BY_VALUE) return hipErrorInvalidValue;
-  ForkByValue plan;
+  ForkMoves plan;
   for (int i = 0; i < n_moves; ++i) plan.moves[i] = moves[i];
   for (int i = 0; i < n_runs; ++i) plan.runs[i] = runs[i];
-  fork_kernel<ForkByValue><<<grid, block, 0, s>>>(p, layer_elems * 2, page_elems * 2, slices, plan);
+  fork_kernel<<<dim3((unsigned)(n_runs * slices), (unsigned)n_layers), dim3(FORK_THREADS), 0, s>>>(
+      reinterpret_cast<unsigned char*>(kv), layer_elems * 2, page_elems * 2, slices, plan);
   return hipGetLastError();
 }
 
@@ -276,6 +276,17 @@ hipError_t launch_page_image(bf16_t* kv, size_t layer_elems, int n_layers, const
     else if (to_pool) page_image_kernel<64, true><<<grid, block, 0, s>>>(kv, layer_elems, n_layers, ids, total, F, Hkv, img);
     else page_image_kernel<64, false><<<grid, block, 0, s>>>(kv, layer_elems, n_layers, ids, total, F, Hkv, img);
   }
+  return hipGetLastError();
+}
+
+hipError_t launch_put_plan(const unsigned char* plan, size_t size, unsigned char* dev, size_t turns, int n_turns, const double* inv_freq, int D,
+                           float* angles, hipStream_t s) {
+  if (size > PLAN_BY_VALUE || size % 4 || turns % 4 || turns + (size_t)n_turns * 4 > size) return hipErrorInvalidValue;
+  PlanBytes bytes;
+  __builtin_memcpy(bytes.w, plan, size);
+  const int words = (int)(size / 4), threads = words > n_turns * (D / 2) ? words : n_turns * (D / 2);
+  put_plan_kernel<<<dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s>>>(bytes, words, reinterpret_cast<uint32_t*>(dev), (int)(turns / 4), n_turns,
+                                                                                inv_freq, D, angles);
   return hipGetLastError();
 }
 

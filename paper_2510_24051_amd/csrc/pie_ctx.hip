@@ -1547,112 +1547,33 @@ struct OnDevice {
   }
   ~OnDevice() { if (before >= 0) (void)hipSetDevice(before); }
 };
-
-// Moves dst[i] <- src[i] (all from the pages as they were) as runs in an order that needs no second buffer: a page is written after
-// every move that reads it.  A page that is read is a hub, its moves are emitted together (the source is loaded once), and the
-// hubs form trees (a hub's parent is the page it becomes) some of which end in a cycle.  A tree is one run, deepest hubs first;
-// one hub alone is cut into runs of FORK_FAN pages that are independent of each other.  A cycle c0 <- c1 <- .. <- c0 starts with
-// keeping c0, and its last move stores what was kept.
-#define FORK_FAN 16
-struct ForkPlan {
-  std::vector<PageMove> moves;
-  std::vector<PageRun> runs;
-  ForkPlan(const int32_t* src, const int32_t* dst, int n) {
-    for (int i = 0; i < n; ++i)
-      if (src[i] != dst[i]) given.push_back(PageMove{src[i], dst[i]});
-    std::stable_sort(given.begin(), given.end(), [](const PageMove& a, const PageMove& b) { return a.src < b.src; });
-    std::unordered_map<int32_t, int32_t> hub_of, from;  // page -> its hub; page -> the page it becomes
-    for (size_t i = 0; i < given.size(); ++i) {
-      from[given[i].dst] = given[i].src;
-      if (i == 0 || given[i].src != given[i - 1].src) {
-        hub_of[given[i].src] = (int32_t)first.size();
-        first.push_back((int32_t)i);
-      }
-    }
-    const int n_hubs = (int)first.size();
-    first.push_back((int32_t)given.size());
-    std::vector<int32_t> parent(n_hubs, -1);
-    kids.resize(n_hubs);
-    for (int h = 0; h < n_hubs; ++h) {
-      const auto it = from.find(page(h));
-      if (it == from.end()) continue;
-      parent[h] = hub_of.at(it->second);
-      kids[parent[h]].push_back(h);
-    }
-    std::vector<char> seen(n_hubs, 0);
-    moves.reserve(given.size());
-    for (int h = 0; h < n_hubs; ++h)
-      if (parent[h] < 0) {
-        const int at = (int)moves.size();
-        tree(h, seen);
-        if (kids[h].empty())
-          for (int i = at; i < (int)moves.size(); i += FORK_FAN) runs.push_back(PageRun{i, std::min(FORK_FAN, (int)moves.size() - i), -1});
-        else runs.push_back(PageRun{at, (int)moves.size() - at, -1});
-      }
-    std::vector<int32_t> cycle;
-    for (int h = 0; h < n_hubs; ++h) {
-      if (seen[h]) continue;
-      std::unordered_map<int32_t, int32_t> at_step;  // up from h until the cycle has been walked once
-      int x = h;
-      for (int step = 0; at_step.emplace(x, step).second; ++step) x = parent[x];
-      cycle.clear();
-      for (int y = x;;) {
-        cycle.push_back(y);
-        y = parent[y];
-        if (y == x) break;
-      }
-      const int at = (int)moves.size(), L = (int)cycle.size();
-      for (int y : cycle) seen[y] = 1;
-      for (int y : cycle)
-        for (int k : kids[y])
-          if (!seen[k]) tree(k, seen);
-      const int last = page(cycle[L - 1]);
-      emit(cycle[0], last);
-      for (int k = 1; k < L; ++k) emit(cycle[k], -1);
-      moves.push_back(PageMove{-1, last});
-      runs.push_back(PageRun{at, (int)moves.size() - at, page(cycle[0])});
-    }
-  }
-
- private:
-  std::vector<PageMove> given;              // by source
-  std::vector<int32_t> first;               // [hubs + 1] into `given`
-  std::vector<std::vector<int32_t>> kids;   // hubs whose page becomes this hub's page
-  std::vector<int32_t> order;
-  int page(int h) const { return given[first[h]].src; }
-  void emit(int h, int but_not_to) {
-    for (int i = first[h]; i < first[h + 1]; ++i)
-      if (given[i].dst != but_not_to) moves.push_back(given[i]);
-  }
-  void tree(int root, std::vector<char>& seen) {
-    order.assign(1, root);
-    seen[root] = 1;
-    for (size_t i = 0; i < order.size(); ++i)
-      for (int k : kids[order[i]]) { seen[k] = 1; order.push_back(k); }
-    for (size_t i = order.size(); i-- > 0;) emit(order[i], -1);  // (children behind their parents: reversed, before them)
-  }
-};
 }  // namespace
 
-// The host image is about to be written: no capture may be under way and the copy of the last image has to be over.
-static pie_status image_begin(pie_ctx* c, const char* who) {
+// Arrays of a page plan, put into one block one after the other.
+struct PlanImage {
+  std::vector<unsigned char> bytes;
+  template <typename T>
+  size_t add(const std::vector<T>& v) {
+    const size_t at = (bytes.size() + 15) / 16 * 16;
+    bytes.resize(at + v.size() * sizeof(T));
+    if (!v.empty()) std::memcpy(bytes.data() + at, v.data(), v.size() * sizeof(T));
+    return at;
+  }
+};
+
+static pie_status refuse_capture(pie_ctx* c, const char* who) {  // (before the runtime is asked for anything else)
   hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
-  if (hipStreamIsCapturing(c->stream, &cap) != hipSuccess || cap != hipStreamCaptureStatusNone) {
-    (void)hipGetLastError();
-    return fail(c, PIE_EHIP, "%s: the context's stream is being captured", who);
-  }
-  if (c->blob_in_flight) {
-    const hipError_t e = hipEventSynchronize(c->blob_copied);
-    if (e != hipSuccess) return fail(c, PIE_EHIP, "%s: waiting for the previous copy: %s", who, hipGetErrorString(e));
-    c->blob_in_flight = false;
-  }
-  return PIE_OK;
+  if (hipStreamIsCapturing(c->stream, &cap) == hipSuccess && cap == hipStreamCaptureStatusNone) return PIE_OK;
+  (void)hipGetLastError();
+  return fail(c, PIE_EHIP, "%s: the context's stream is being captured", who);
 }
 
-// Copies the image to the front of the context's block for page plans, which holds `more` bytes behind it as well.
-static pie_status image_send(pie_ctx* c, const Blob& blob, size_t more, const char* who) {
-  if (!blob.ok) return fail(c, PIE_ENOMEM, "%s: no host memory for the plan", who);
-  const size_t need = blob.size + 256 + more;
+// Brings a plan to the front of the context's block for page plans, and behind it (at a multiple of 256) the table [n_turns, D] of the
+// angles that its n_turns shifts (at `turns` of the image) turn by.  Small plans travel as arguments of the kernel that makes the
+// table; long ones are copied from the context's host image, which has to wait for the copy before it.
+static pie_status send_plan(pie_ctx* c, const PlanImage& plan, size_t turns, int n_turns, float** angles, const char* who) {
+  const int D = c->m.head_dim;
+  const size_t size = plan.bytes.size(), o_angles = (size + 255) / 256 * 256, need = o_angles + (size_t)n_turns * D * sizeof(float);
   if (need > c->moves_cap) {
     HIP_TRY(c, hipStreamSynchronize(c->stream));  // no kernel may still read the block that is replaced
     if (c->moves_dev) (void)hipFree(c->moves_dev);
@@ -1667,9 +1588,23 @@ static pie_status image_send(pie_ctx* c, const Blob& blob, size_t more, const ch
     }
     c->moves_cap = cap;
   }
-  HIP_TRY(c, hipMemcpyAsync(c->moves_dev, blob.data(), blob.size, hipMemcpyHostToDevice, c->stream));
+  *angles = reinterpret_cast<float*>(c->moves_dev + o_angles);
+  if (size <= PLAN_BY_VALUE) {
+    HIP_TRY(c, launch_put_plan(plan.bytes.data(), size, c->moves_dev, turns, n_turns, c->inv_freq, D, *angles, c->stream));
+    return PIE_OK;
+  }
+  if (c->blob_in_flight) {
+    const hipError_t e = hipEventSynchronize(c->blob_copied);
+    if (e != hipSuccess) return fail(c, PIE_EHIP, "%s: waiting for the previous copy: %s", who, hipGetErrorString(e));
+    c->blob_in_flight = false;
+  }
+  Blob blob(c);
+  blob.append(plan.bytes.data(), size);
+  if (!blob.ok) return fail(c, PIE_ENOMEM, "%s: no host memory for the plan", who);
+  HIP_TRY(c, hipMemcpyAsync(c->moves_dev, blob.data(), size, hipMemcpyHostToDevice, c->stream));
   HIP_TRY(c, c->host_blob_pinned ? hipEventRecord(c->blob_copied, c->stream) : hipStreamSynchronize(c->stream));
   c->blob_in_flight = c->host_blob_pinned;
+  if (n_turns > 0) HIP_TRY(c, launch_rope_table((const int32_t*)(c->moves_dev + turns), c->inv_freq, n_turns, D, *angles, c->stream));
   return PIE_OK;
 }
 
@@ -1705,23 +1640,15 @@ static pie_status pie_fork_kvpage_impl(pie_ctx* c, const int32_t* src, const int
   if (pie_status st = check_pages(c, dst, n, "pie_fork_kvpage")) return st;
   if (pie_status st = check_once(c, dst, n, "pie_fork_kvpage")) return st;
   const ForkPlan plan(src, dst, n);
-  const int n_moves = (int)plan.moves.size(), n_runs = (int)plan.runs.size(), F = c->blocks_per_page;
-  if (n_moves == 0) return PIE_OK;
+  const int F = c->blocks_per_page;
   std::vector<uint16_t> masks((size_t)n * F);
   for (int i = 0; i < n; ++i)
     for (int f = 0; f < F; ++f) masks[(size_t)i * F + f] = c->page_mask[(size_t)src[i] * F + f];
   const size_t page_elems = (size_t)F * c->m.n_kv_heads * 2 * PAGE * c->m.head_dim;
   OnDevice on(c);
-  if (n_moves <= FORK_BY_VALUE) {  // (a run has a move at least)
-    HIP_TRY(c, launch_fork(c->kv, c->kv_layer_elems, c->m.n_layers, page_elems, plan.moves.data(), n_moves, plan.runs.data(), n_runs, false, c->stream));
-  } else {
-    if (pie_status st = image_begin(c, "pie_fork_kvpage")) return st;
-    Blob blob(c);
-    const size_t o_m = blob.add(plan.moves.data(), (size_t)n_moves * sizeof(PageMove)), o_r = blob.add(plan.runs.data(), (size_t)n_runs * sizeof(PageRun));
-    if (pie_status st = image_send(c, blob, 0, "pie_fork_kvpage")) return st;
-    HIP_TRY(c, launch_fork(c->kv, c->kv_layer_elems, c->m.n_layers, page_elems, (const PageMove*)(c->moves_dev + o_m), n_moves,
-                           (const PageRun*)(c->moves_dev + o_r), n_runs, true, c->stream));
-  }
+  for (const ForkPlan::Launch& l : plan.launches)
+    HIP_TRY(c, launch_fork(c->kv, c->kv_layer_elems, c->m.n_layers, page_elems, plan.moves.data() + l.move0, l.n_moves, plan.runs.data() + l.run0,
+                           l.n_runs, c->stream));
   for (int i = 0; i < n; ++i)
     for (int f = 0; f < F; ++f) c->page_mask[(size_t)dst[i] * F + f] = masks[(size_t)i * F + f];
   return PIE_OK;
@@ -1796,6 +1723,7 @@ static pie_status pie_compact_kvpage_impl(pie_ctx* c, int32_t S, const int32_t* 
   std::vector<CompactChain> chains;
   if (shifts) turn.reserve((size_t)total);
   int64_t off = 0, kept_before = 0;
+  bool mixed = false;  // some block's tokens turn differently
   for (int s = 0; s < S; ++s) {
     const int32_t* from = page_ids + page_indptr[s];
     const int32_t* to = dst_ids + dst_indptr[s];
@@ -1860,6 +1788,7 @@ static pie_status pie_compact_kvpage_impl(pie_ctx* c, int32_t S, const int32_t* 
         if (shifts) {
           const int32_t* row = turn.data() + e.first;
           e.turn = std::all_of(row, row + __builtin_popcount(mask), [&](int32_t x) { return x == row[0]; }) ? row[0] : COMPACT_MIXED;
+          mixed |= e.turn == COMPACT_MIXED;
         }
         entries.push_back(e);
         if (at + here > t1) break;
@@ -1871,17 +1800,14 @@ static pie_status pie_compact_kvpage_impl(pie_ctx* c, int32_t S, const int32_t* 
   }
   if (!chains.empty()) {
     OnDevice on(c);
-    if (pie_status st = image_begin(c, who)) return st;
-    Blob blob(c);
-    const size_t o_c = blob.add(chains.data(), chains.size() * sizeof(CompactChain)), o_e = blob.add(entries.data(), entries.size() * sizeof(CompactEntry));
-    const size_t o_t = blob.add(tiles.data(), tiles.size() * 4), o_i = turns.empty() ? 0 : blob.add(turn.data(), turn.size() * 4);
-    const size_t o_v = turns.empty() ? 0 : blob.add(turns.data(), turns.size() * 4);
-    const size_t o_a = (blob.size + 255) / 256 * 256;
-    if (pie_status st = image_send(c, blob, turns.size() * D * sizeof(float), who)) return st;
-    unsigned char* d = c->moves_dev;
-    if (!turns.empty()) HIP_TRY(c, launch_rope_table((const int32_t*)(d + o_v), c->inv_freq, (int)turns.size(), D, (float*)(d + o_a), c->stream));
-    const CompactPlan plan{(const CompactChain*)(d + o_c), (const CompactEntry*)(d + o_e), (const int32_t*)(d + o_t),
-                           turns.empty() ? nullptr : (const int32_t*)(d + o_i), (const float*)(d + o_a)};
+    if (pie_status st = refuse_capture(c, who)) return st;
+    if (!mixed) turn.clear();  // (every block's tokens turn alike: the entries say by which row)
+    PlanImage image;
+    const size_t o_c = image.add(chains), o_e = image.add(entries), o_t = image.add(tiles), o_i = image.add(turn), o_v = image.add(turns);
+    float* angles = nullptr;
+    if (pie_status st = send_plan(c, image, o_v, (int)turns.size(), &angles, who)) return st;
+    const unsigned char* d = c->moves_dev;
+    const CompactPlan plan{(const CompactChain*)(d + o_c), (const CompactEntry*)(d + o_e), (const int32_t*)(d + o_t), (const int32_t*)(d + o_i), angles};
     HIP_TRY(c, launch_compact(c->kv, c->kv_layer_elems, c->m.n_layers, c->m.n_kv_heads, D, plan, (int)chains.size(), c->stream));
   }
   for (int s = 0; s < S; ++s) {

@@ -1,5 +1,6 @@
-"""Host paths of the page calls and of the beam selection without a GPU: the plans of forks and compactions are read from what the
-library copies to the device (a stand-in for the HIP runtime, fake_hip.cpp) and carried out here; and every refusal."""
+"""Host paths of the page calls and of the beam selection without a GPU: the plans of forks are compiled on their own, those of
+compactions read from what the library copies to the device (a stand-in for the HIP runtime, fake_hip.cpp), and both are carried out
+here; and every refusal."""
 import ctypes as C
 import os
 import subprocess
@@ -9,13 +10,13 @@ from types import SimpleNamespace
 import numpy as np
 import pytest
 
-from test_host_runtime_paths import MODEL, Child, fake  # noqa: F401  (the fixture builds the stand-in)
+from test_host_runtime_paths import MODEL, ROOT, Child, fake  # noqa: F401  (the fixture builds the stand-in)
 
 INVALID, RANGE, BATCH, CONFLICT, MEMORY, HIP = -1, -2, -3, -4, -5, -6
 
 
 def up(n):
-    return (n + 255) // 256 * 256
+    return (n + 15) // 16 * 16
 
 
 def i32(a):
@@ -31,57 +32,93 @@ def last_image(c, ctx):
     return c.copies()[-1]
 
 
-def carry_out(image, pages):
-    """The moves of a fork, as its kernel walks them: runs one after the other in any order, here the last one first."""
-    for split in range(1, len(image) // 8):  # moves [n] of 8 bytes, at the next multiple of 256 runs of 12
-        if up(split * 8) < len(image) and (len(image) - up(split * 8)) % 12 == 0:
-            runs = np.frombuffer(image, np.int32, offset=up(split * 8)).reshape(-1, 3)
-            if runs[:, 1].sum() == split and runs[0, 0] == 0 and (runs[1:, 0] == runs[:-1].sum(1) - runs[:-1, 2]).all() and (runs[:, 1] > 0).all():
-                break
-    moves = np.frombuffer(image, np.int32, count=2 * split).reshape(-1, 2)
-    for first, n, keep in runs[::-1]:
-        kept = pages[keep] if keep >= 0 else None
-        for src, dst in moves[first:first + n]:
-            pages[dst] = kept if src < 0 else pages[src]
-    return len(moves), len(runs)
+PLAN = r"""
+#include "page_plans.h"
+// src, dst [n]; pages [p]: carries the plan out, the runs of a launch one after the other from the last to the first; what a launch
+// holds at most; returns launches, or -1 where one holds more moves than it may
+extern "C" int carry_out(const int32_t* src, const int32_t* dst, int n, int32_t* pages, int32_t* counts) {
+  const ForkPlan plan(src, dst, n);
+  counts[0] = (int)plan.moves.size();
+  counts[1] = (int)plan.runs.size();
+  for (const ForkPlan::Launch& l : plan.launches) {
+    if (l.n_moves > FORK_MOVES || l.n_moves < 1) return -1;
+    int next = 0;
+    for (int r = 0; r < l.n_runs; ++r) {
+      const PageRun& run = plan.runs[l.run0 + r];
+      if (run.first != next || run.n < 1) return -1;
+      next += run.n;
+    }
+    if (next != l.n_moves) return -1;
+    for (int r = l.n_runs; r-- > 0;) {
+      const PageRun& run = plan.runs[l.run0 + r];
+      const int32_t kept = run.keep >= 0 ? pages[run.keep] : -1;
+      for (int i = run.first; i < run.first + run.n; ++i) {
+        const PageMove m = plan.moves[l.move0 + i];
+        pages[m.dst] = m.src < 0 ? kept : pages[m.src];
+      }
+    }
+  }
+  return (int)plan.launches.size();
+}
+"""
 
 
-def fork_plans(c):
-    """Random graphs of moves, long enough that the plan is copied: carrying the runs out in order gives every page what its
-    source was, whichever run goes first."""
-    ctx = c.context(n_pages=2000)
+@pytest.fixture(scope="module")
+def plans(tmp_path_factory):
+    where = tmp_path_factory.mktemp("plan")
+    src, so = where / "plan.cpp", str(where / "plan.so")
+    src.write_text(PLAN)
+    subprocess.run(["g++", "-O1", "-std=c++17", "-shared", "-fPIC", "-Wall", "-Werror", "-D_GLIBCXX_ASSERTIONS", "-I", os.path.join(ROOT, "paper_2510_24051_amd", "csrc"),
+                    "-o", so, str(src)], check=True)
+    return C.CDLL(so)
+
+
+@pytest.mark.parametrize("form", ["random", "permutation", "rotation", "two cycles", "chain", "fan", "wide fans on a cycle", "beams", "pairs", "one", "swap", "none"])
+def test_fork_plans(form, plans):
+    """Carried out in order, whichever run of a launch goes first, a plan gives every page what its source was; no move more than pages
+    change but one for a cycle and one for each launch that it runs into."""
     rng = np.random.default_rng(5)
-    for form in ("random", "permutation", "rotation", "chain", "fan", "beams", "pairs"):
-        for _ in range(6):
-            n = int(rng.integers(200, 900))
-            dst = rng.permutation(2000)[:n]
-            if form == "random":
-                src = rng.integers(0, 2000, n)
-            elif form == "permutation":
-                src = rng.permutation(dst)
-            elif form == "rotation":
-                src = np.roll(dst, 1)
-            elif form == "chain":
-                src = np.concatenate([[int(np.setdiff1d(np.arange(2000), dst)[0])], dst[:-1]])
-            elif form == "fan":
-                src = rng.choice(np.setdiff1d(np.arange(2000), dst), 3)[rng.integers(0, 3, n)]
-            elif form == "beams":
-                src = dst[np.arange(n) // 8 * 8 + np.minimum(rng.integers(0, 8, n), n - 1 - np.arange(n) // 8 * 8)]
-            else:
-                src = np.setdiff1d(np.arange(2000), dst)[:n]
-                dst = dst[:len(src)]
-            before = np.arange(2000)
-            want, got = before.copy(), before.copy()
-            want[dst] = before[src]
-            moving = int((src != dst).sum())
-            if moving <= 160:
-                continue
-            ctx.fork_kvpage(src, dst)
-            n_moves, n_runs = carry_out(last_image(c, ctx), got)
-            assert np.array_equal(got, want), form
-            cycles = n_moves - moving
-            assert 0 <= cycles and (form != "rotation" or (cycles == 0 and n_runs == 1)), (form, cycles, n_runs)
-    ctx.close()
+    every = np.arange(2000)
+    for trial in range(40):
+        n = int(rng.integers(1, 900))
+        dst = rng.permutation(2000)[:n]
+        others = np.setdiff1d(every, dst)
+        if form == "random":
+            src = rng.integers(0, 2000, n)
+        elif form == "permutation":
+            src = rng.permutation(dst)
+        elif form == "rotation":
+            src = np.roll(dst, 1)
+        elif form == "two cycles":
+            src = np.concatenate([np.roll(dst[:n // 2], 1), np.roll(dst[n // 2:], -1)])
+        elif form == "chain":
+            src = np.concatenate([others[:1], dst[:-1]])
+        elif form == "fan":
+            src = rng.choice(others, 3)[rng.integers(0, 3, n)]
+        elif form == "wide fans on a cycle":
+            k = max(2, n // 8)  # a cycle of k pages, every other destination a copy of one of them or of a copy
+            k = min(k, n)
+            src = np.concatenate([np.roll(dst[:k], 1), dst[rng.integers(0, np.arange(k, n))]]) if n > k else np.roll(dst[:k], 1)
+        elif form == "beams":
+            src = dst[np.arange(n) // 8 * 8 + np.minimum(rng.integers(0, 8, n), n - 1 - np.arange(n) // 8 * 8)]
+        elif form == "pairs":
+            src = others[:n]
+            dst = dst[:len(src)]
+        elif form == "one":
+            src, dst = others[:1], dst[:1]
+        elif form == "swap":
+            dst = np.array([3, 9])
+            src = dst[::-1]
+        else:
+            src = dst
+        src, dst = i32(src), i32(dst)
+        want, got, counts = every.copy(), i32(every).copy(), np.zeros(2, np.int32)
+        want[dst] = every[src]
+        launches = plans.carry_out(at(src), at(dst), len(src), at(got), at(counts))
+        assert launches >= 0 and np.array_equal(got, want), (form, n)
+        moving = int((src != dst).sum())
+        # each cycle saves one load and needs no move more; what it puts down at the end of a launch is one
+        assert moving <= counts[0] <= moving + launches and launches <= moving // 159 + 1, (form, n, counts, launches)
 
 
 def fork_masks(c):
@@ -103,16 +140,17 @@ def compact_plans(c):
     """Ragged sequences, both page sizes, in place and apart, with shifts: the chains, carried out in any order, leave what a
     simultaneous move leaves, and tiles of a chain that has to go in order never read what an earlier one wrote."""
     rng = np.random.default_rng(8)
-    for trial in range(60):
+    checked = 0
+    for trial in range(40):
         P = int(rng.choice([16, 32]))
         F = P // 16
         m = SimpleNamespace(**{**vars(MODEL), "page_size": P})
-        ctx = c.context(n_pages=400, m=m)
+        ctx = c.context(n_pages=1600, m=m)
         S = int(rng.integers(1, 5))
-        lens = rng.integers(0, 20 * P // F, S)
+        lens = rng.integers(0, 250 * P // F, S)
         lens[rng.integers(0, S)] = rng.choice([0, 1, 15, 16, 17, P, 6 * P])
         n_pages = -(-lens // P) + rng.integers(0, 2, S)
-        ids = rng.permutation(400)
+        ids = rng.permutation(1600)
         ip = np.concatenate([[0], np.cumsum(n_pages)])
         table = ids[:ip[-1]]
         bits = rng.integers(0, 1 << 32, len(table), dtype=np.uint64) & (rng.integers(0, 1 << 32, len(table), dtype=np.uint64) | np.uint64(0xFF))
@@ -129,7 +167,7 @@ def compact_plans(c):
         n0 = len(c.copies())
         got = ctx.compact_kvpage(ip, table, lens, shifts=shifts, dst_page_indptr=dp, dst_page_ids=di)
         assert got.tolist() == kept
-        pool = np.arange(400 * P).astype(object)
+        pool = np.arange(1600 * P).astype(object)
         want = pool.copy()
         off = 0
         for s in range(S):
@@ -140,13 +178,13 @@ def compact_plans(c):
                 want[int(into[i // P]) * P + i % P] = (token, by) if by else token
             off += lens[s]
         ctx.synchronize()
-        if len(c.copies()) == n0:
-            assert all(want == pool)
+        if len(c.copies()) == n0:  # nothing moves, or the plan is small and travels as kernel arguments
             ctx.close()
             continue
+        checked += 1
         image = c.copies()[-1]
         # chains (entries from, to; first destination block), entries (block, mask, first kept token, row of the table or -1, -2),
-        # destination blocks, then, where a key turns, rows of the table and the shifts, each at a multiple of 256
+        # destination blocks, then, where a block's keys turn differently, rows of the table, and the shifts, each at a multiple of 16
         ints = np.frombuffer(image, np.int32)
         k = n_entries = 0
         while 3 * k < len(ints) and ints[3 * k] == n_entries and ints[3 * k + 1] > n_entries:
@@ -154,15 +192,21 @@ def compact_plans(c):
         chains = ints[:3 * k].reshape(-1, 3)
         o = up(12 * k) // 4
         entries = ints[o:o + 4 * n_entries].reshape(-1, 4)
-        o = up(4 * (o + 4 * n_entries)) // 4
+        o += 4 * n_entries
         tiles = ints[o:]
         turning = any(isinstance(x, tuple) for x in want)
         turn = np.full(sum(kept), -1)
         if turning:
             n_tiles = max(c0[2] + -(-sum(bin(m).count("1") for _, m, _, _ in entries[c0[0]:c0[1]]) // 16) for c0 in chains)
             o = up(4 * (o + n_tiles)) // 4
-            turn = ints[o:o + len(turn)]
-            turns = ints[up(4 * (o + len(turn))) // 4:]
+            mixed = (entries[:, 3] == -2).any()
+            if mixed:
+                turn = ints[o:o + len(turn)]
+                o = up(4 * (o + len(turn))) // 4
+            else:
+                for _, mask, k, row in entries:
+                    turn[k:k + bin(mask).count("1")] = row
+            turns = ints[o:]
             assert turn.max() == len(turns) - 1
         have = pool.copy()
         for e0, e1, tile in chains[::-1]:
@@ -186,6 +230,7 @@ def compact_plans(c):
                 have[b0:b0 + len(rest)] = rest
         assert all(x == y for x, y in zip(have, want)), trial
         ctx.close()
+    assert checked > 20, checked
 
 
 def raw(ctx, name, *args):
@@ -247,13 +292,13 @@ def captured(c):
     ctx.compact_kvpage([0, 4], [0, 1, 2, 3], [60], shifts=np.ones(60))  # a copy is in flight
     c.fake.fake_capturing(1)
     calls = c.fake.fake_event_syncs(), c.fake.fake_allocations()
-    ctx.fork_kvpage(np.arange(160), 500 + np.arange(160))
-    for call in (lambda: ctx.fork_kvpage(np.arange(161), 500 + np.arange(161)), lambda: ctx.compact_kvpage([0, 1], [7], [16], shifts=np.ones(16))):
-        st, msg = c.status(call)
+    ctx.fork_kvpage(np.arange(400), 500 + np.arange(400))
+    for n in (16, 1000):
+        st, msg = c.status(lambda: ctx.compact_kvpage([0, 70], np.arange(70), [n], shifts=np.ones(n)))
         assert st == HIP and "captured" in msg
     assert calls == (c.fake.fake_event_syncs(), c.fake.fake_allocations())
     c.fake.fake_capturing(0)
-    ctx.fork_kvpage(np.arange(161), 500 + np.arange(161))
+    ctx.compact_kvpage([0, 70], np.arange(70), [1000], shifts=np.ones(1000))
     ctx.close()
 
 
@@ -261,19 +306,22 @@ def images_in_flight(c):
     """Batches and page plans share the host image: each copy gets what its call wrote."""
     from test_host_runtime_paths import batch_of
     ctx = c.context(n_pages=2000)
-    src = np.arange(300)
-    ctx.fork_kvpage(src, 1000 + src)
+    shifts = [np.arange(6000), np.arange(6000)[::-1]]
+    compact = lambda k: ctx.compact_kvpage([0, 375], np.arange(375), [6000], shifts=shifts[k])  # noqa: E731
+    compact(0)
     want = [last_image(c, ctx)]
     ctx.batch_create(batch_of([(1, 40), (20, 5)])).destroy()
     want.append(last_image(c, ctx))
+    compact(1)
+    want.append(last_image(c, ctx))
     n0 = len(c.copies())
-    ctx.fork_kvpage(src, 1000 + src)
+    compact(0)
     b = ctx.batch_create(batch_of([(1, 40), (20, 5)]))
     c.fake.fake_fail_event_syncs(1)
-    assert c.status(lambda: ctx.fork_kvpage(src[::-1], 1000 + src))[0] == HIP
-    ctx.fork_kvpage(src[::-1], 1000 + src)
+    assert c.status(lambda: compact(1))[0] == HIP
+    compact(1)
     ctx.synchronize()
-    assert c.copies()[n0:n0 + 2] == want
+    assert c.copies()[n0:] == want
     b.destroy()
     ctx.close()
 
@@ -300,6 +348,8 @@ def no_memory(c):
         assert failed > 3
         ctx = c.context(n_pages=1024)
         ctx.mask_kvpage([0], [0xFFF0])
+        if "compact" not in call.__code__.co_names[0]:
+            continue  # (a fork allocates nothing on the device)
         c.fake.fake_malloc_limit(1)
         assert c.status(lambda: call(ctx))[0] == MEMORY
         c.fake.fake_malloc_limit(1 << 62)
@@ -356,7 +406,7 @@ def beam_refusals(c):
     assert raw(p, "pie_get_next_beams", C.byref(search()), at(i32([0])), o, o, o) == INVALID
 
 
-CASES = {f.__name__: f for f in (fork_plans, fork_masks, compact_plans, page_refusals, captured, images_in_flight, no_memory, beam_refusals)}
+CASES = {f.__name__: f for f in (fork_masks, compact_plans, page_refusals, captured, images_in_flight, no_memory, beam_refusals)}
 
 if __name__ == "__main__":
     CASES[sys.argv[2]](Child(sys.argv[1]))
