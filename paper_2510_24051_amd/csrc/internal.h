@@ -392,9 +392,12 @@ struct CompactPlan {
   const int32_t* tiles;
   const int32_t* turn;       // per kept token: row of `angles`, -1 = not rotated (read for COMPACT_MIXED entries)
   const float* angles;       // [turns, D] cos | sin
+  const bf16_t* src;         // blocks of the entries and of the tiles, and how far the layers are apart
+  bf16_t* dst;
+  size_t src_layer, dst_layer;
 };
 #define PLAN_BY_VALUE 3584  // bytes of a plan that travel as kernel arguments, of which a launch takes 4 KiB
 // plan -> dev, and the table [n_turns, D] of cos | sin of the n_turns shifts at byte `turns` of it
 hipError_t launch_put_plan(const unsigned char* plan, size_t size, unsigned char* dev, size_t turns, int n_turns, const double* inv_freq, int D,
                            float* angles, hipStream_t s);
-hipError_t launch_compact(bf16_t* kv, size_t layer_elems, int n_layers, int Hkv, int D, const CompactPlan& plan, int n_chains, hipStream_t s);
+hipError_t launch_compact(const CompactPlan& plan, int n_chains, int n_layers, int Hkv, int D, hipStream_t s);

@@ -109,7 +109,7 @@ __global__ __launch_bounds__(64 * IMAGE_WAVES) void page_image_kernel(bf16_t* __
 #define COMPACT_WAVES 4
 #define COMPACT_AHEAD 4
 template <int D, bool IS_K>
-__device__ __forceinline__ void compact_walk(uint16_t* pool, int64_t block_elems, int part, CompactChain chain, u32x4* ring,
+__device__ __forceinline__ void compact_walk(const uint16_t* src, uint16_t* dst, int64_t block_elems, int part, CompactChain chain, u32x4* ring,
                                              const CompactEntry* __restrict__ entries, const int32_t* __restrict__ tiles,
                                              const int32_t* __restrict__ turn, const float* __restrict__ angles) {
   const int lane = threadIdx.x & 63;
@@ -117,14 +117,13 @@ __device__ __forceinline__ void compact_walk(uint16_t* pool, int64_t block_elems
   const int label = octet_label(lane & 7);
   const int t = IS_K ? swap23(lane & 15) : (lane >> 5) * 8 + label;
   const int piece = IS_K ? lane >> 4 : lane >> 3 & 3;  // dims 8 piece .. of the first KiB; pieces 4 .. 7 are the second's
-  uint16_t* at0 = pool + (IS_K ? part * 512 + lane * 8 : PAGE * D + part * 1024 + (lane & ~7) * 8 + label * 8);
-  uint16_t* at1 = at0 + (IS_K ? D * 8 : 512);
+  const int o0 = IS_K ? part * 512 + lane * 8 : PAGE * D + part * 1024 + (lane & ~7) * 8 + label * 8, o1 = o0 + (IS_K ? D * 8 : 512);
   const uint32_t before = (1u << t) - 1u;
   auto slot_at = [&](int slot, int q) { return (slot & 31) * 8 + (q ^ (slot & 7)); };  // (rows a bank apart, whatever the slots)
 
   int count = 0, stored = 0;  // tokens put into the ring, blocks stored
   auto store = [&](int n) {  // the next 16 tokens of the ring, of which n are there
-    const int64_t o = tiles[chain.tile0 + stored] * block_elems;
+    uint16_t* to = dst + tiles[chain.tile0 + stored] * block_elems;
     u32x4 a = ring[slot_at(stored * PAGE + t, piece)], b = ring[slot_at(stored * PAGE + t, piece + 4)];
     ++stored;
     if (IS_K) {
@@ -137,8 +136,8 @@ __device__ __forceinline__ void compact_walk(uint16_t* pool, int64_t block_elems
       if (here < 8) {  // the others stay as they are
         Pack16 x, y, p, q;
         x.u = a; y.u = b;
-        p.u = *reinterpret_cast<const u32x4*>(at0 + o);
-        q.u = *reinterpret_cast<const u32x4*>(at1 + o);
+        p.u = *reinterpret_cast<const u32x4*>(to + o0);
+        q.u = *reinterpret_cast<const u32x4*>(to + o1);
 #pragma unroll
         for (int e = 0; e < 8; ++e)
           if (e >= here) { x.s[e] = p.s[e]; y.s[e] = q.s[e]; }
@@ -146,17 +145,17 @@ __device__ __forceinline__ void compact_walk(uint16_t* pool, int64_t block_elems
         b = y.u;
       }
     }
-    *reinterpret_cast<u32x4*>(at0 + o) = a;
-    *reinterpret_cast<u32x4*>(at1 + o) = b;
+    *reinterpret_cast<u32x4*>(to + o0) = a;
+    *reinterpret_cast<u32x4*>(to + o1) = b;
   };
 
   u32x4 raw[COMPACT_AHEAD][2];
   int rows[COMPACT_AHEAD];  // of the table, where a block's tokens turn differently
   auto request = [&](int i, u32x4 (&r)[2], int& row) {  // (the last block again behind the end: nothing depends on a branch)
     const CompactEntry e = entries[min(i, chain.entry1 - 1)];
-    const int64_t o = e.block * block_elems;
-    r[0] = load_nt(reinterpret_cast<const u32x4*>(at0 + o));
-    r[1] = load_nt(reinterpret_cast<const u32x4*>(at1 + o));
+    const uint16_t* from = src + e.block * block_elems;
+    r[0] = load_nt(reinterpret_cast<const u32x4*>(from + o0));
+    r[1] = load_nt(reinterpret_cast<const u32x4*>(from + o1));
     if (IS_K && e.turn == COMPACT_MIXED) row = turn[e.first + min(__popc(e.mask & before), __popc(e.mask) - 1)];
   };
   // K: the angles of a block are asked for one block ahead, so that waiting for them does not empty the queue of reads; two sets,
@@ -216,7 +215,7 @@ __device__ __forceinline__ void compact_walk(uint16_t* pool, int64_t block_elems
 }
 
 template <int D>
-__global__ __launch_bounds__(64 * COMPACT_WAVES) void compact_kernel(bf16_t* __restrict__ kv, int64_t layer_elems, int Hkv, int total,
+__global__ __launch_bounds__(64 * COMPACT_WAVES) void compact_kernel(const bf16_t* src, int64_t src_layer, bf16_t* dst, int64_t dst_layer, int Hkv, int total,
                                                                      const CompactChain* __restrict__ chains,
                                                                      const CompactEntry* __restrict__ entries, const int32_t* __restrict__ tiles,
                                                                      const int32_t* __restrict__ turn, const float* __restrict__ angles) {
@@ -227,10 +226,11 @@ __global__ __launch_bounds__(64 * COMPACT_WAVES) void compact_kernel(bf16_t* __r
   if (at >= total) return;
   const int part = at % PARTS, h = at / PARTS % Hkv;
   const CompactChain chain = chains[at / (PARTS * Hkv)];
-  uint16_t* pool = reinterpret_cast<uint16_t*>(kv) + (int64_t)blockIdx.y * layer_elems + (int64_t)h * (2 * PAGE * D);
+  const uint16_t* from = reinterpret_cast<const uint16_t*>(src) + (int64_t)blockIdx.y * src_layer + (int64_t)h * (2 * PAGE * D);  // (in place: the same)
+  uint16_t* to = reinterpret_cast<uint16_t*>(dst) + (int64_t)blockIdx.y * dst_layer + (int64_t)h * (2 * PAGE * D);
   const int64_t block_elems = (int64_t)Hkv * (2 * PAGE * D);
-  if (part < PARTS / 2) compact_walk<D, true>(pool, block_elems, part, chain, rings[wave], entries, tiles, turn, angles);
-  else compact_walk<D, false>(pool, block_elems, part - PARTS / 2, chain, rings[wave], entries, tiles, turn, angles);
+  if (part < PARTS / 2) compact_walk<D, true>(from, to, block_elems, part, chain, rings[wave], entries, tiles, turn, angles);
+  else compact_walk<D, false>(from, to, block_elems, part - PARTS / 2, chain, rings[wave], entries, tiles, turn, angles);
 }
 
 // A small plan, as kernel arguments, into device memory, and the angles of its shifts (64 bits, rounded once: a shift may be long).
@@ -290,11 +290,11 @@ hipError_t launch_put_plan(const unsigned char* plan, size_t size, unsigned char
   return hipGetLastError();
 }
 
-hipError_t launch_compact(bf16_t* kv, size_t layer_elems, int n_layers, int Hkv, int D, const CompactPlan& plan, int n_chains, hipStream_t s) {
+hipError_t launch_compact(const CompactPlan& p, int n_chains, int n_layers, int Hkv, int D, hipStream_t s) {
   if (n_chains <= 0) return hipSuccess;
   const int total = n_chains * Hkv * 2 * (D / 64);
   const dim3 grid((unsigned)((total + COMPACT_WAVES - 1) / COMPACT_WAVES), (unsigned)n_layers), block(64 * COMPACT_WAVES);
-  if (D == 128) compact_kernel<128><<<grid, block, 0, s>>>(kv, layer_elems, Hkv, total, plan.chains, plan.entries, plan.tiles, plan.turn, plan.angles);
-  else compact_kernel<64><<<grid, block, 0, s>>>(kv, layer_elems, Hkv, total, plan.chains, plan.entries, plan.tiles, plan.turn, plan.angles);
+  auto* kernel = D == 128 ? compact_kernel<128> : compact_kernel<64>;
+  kernel<<<grid, block, 0, s>>>(p.src, (int64_t)p.src_layer, p.dst, (int64_t)p.dst_layer, Hkv, total, p.chains, p.entries, p.tiles, p.turn, p.angles);
   return hipGetLastError();
 }

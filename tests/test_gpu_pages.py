@@ -251,3 +251,14 @@ def test_fork_save_and_restore_in_a_graph():
         image.zero_()
         torch.cuda.synchronize()
         b.same(f"replay {replay}")
+
+
+@pytest.mark.parametrize("D,Hkv,P,layers", [(64, 1, 16, 1), (128, 2, 32, 1)])
+@pytest.mark.parametrize("form,shift", [("half", False), ("half", True), ("most", False), ("window", True), ("pages", True)])
+def test_compact_few_waves_in_place(D, Hkv, P, layers, form, shift):
+    """Long contexts with few heads and layers: through scratch blocks, or side by side where a gap is long enough; short ones beside
+    them go in order, and the last block is as full as it is."""
+    b, _ = compact_case(D, Hkv, P, layers, [5003, 40, 1601, 3200], FORMS[form], True, shift, 31 + D)
+    check_compacted(b)
+    b2, _ = compact_case(D, Hkv, P, layers, [5003, 40, 1601, 3200], FORMS[form], False, shift, 32 + D)
+    check_compacted(b2)

@@ -140,7 +140,8 @@ def compact_plans(c):
     """Ragged sequences, both page sizes, in place and apart, with shifts: the chains, carried out in any order, leave what a
     simultaneous move leaves, and tiles of a chain that has to go in order never read what an earlier one wrote."""
     rng = np.random.default_rng(8)
-    checked = 0
+    checked = scratched = 0
+    c.fake.fake_watch(b"compact_kernel", 5)  # waves of a layer: chains x kv heads x 2 (head_dim 64)
     for trial in range(40):
         P = int(rng.choice([16, 32]))
         F = P // 16
@@ -165,7 +166,11 @@ def compact_plans(c):
         dp = np.concatenate([[0], np.cumsum([-(-k // P) for k in kept])]) if apart else None
         di = ids[ip[-1]:ip[-1] + dp[-1]] if apart else None
         n0 = len(c.copies())
+        if trial % 4 == 1:  # no room for scratch blocks: the same in order
+            c.fake.fake_malloc_limit(1 << 19)
+        c.launches()
         got = ctx.compact_kvpage(ip, table, lens, shifts=shifts, dst_page_indptr=dp, dst_page_ids=di)
+        c.fake.fake_malloc_limit(1 << 62)
         assert got.tolist() == kept
         pool = np.arange(1600 * P).astype(object)
         want = pool.copy()
@@ -182,6 +187,11 @@ def compact_plans(c):
             ctx.close()
             continue
         checked += 1
+        phases = [int(x.split()[1]) // (2 * m.n_kv_heads) for x in c.launches() if "compact_kernel" in x]
+        # into destinations at once; or into scratch blocks, and from there; or both
+        n_direct, n_in, n_back = {1: phases + [0, 0], 2: [0] + phases, 3: phases}[len(phases)]
+        assert trial % 4 != 1 or n_in == 0
+        scratched += n_in > 0
         image = c.copies()[-1]
         # chains (entries from, to; first destination block), entries (block, mask, first kept token, row of the table or -1, -2),
         # destination blocks, then, where a block's keys turn differently, rows of the table, and the shifts, each at a multiple of 16
@@ -204,33 +214,39 @@ def compact_plans(c):
                 turn = ints[o:o + len(turn)]
                 o = up(4 * (o + len(turn))) // 4
             else:
-                for _, mask, k, row in entries:
+                for _, mask, k, row in entries[:chains[k - n_back - 1][1]]:
                     turn[k:k + bin(mask).count("1")] = row
             turns = ints[o:]
             assert turn.max() == len(turns) - 1
-        have = pool.copy()
-        for e0, e1, tile in chains[::-1]:
+        have, scratch = pool.copy(), np.full(20000, -1, object)
+        order = [x for a, b in ((0, n_direct), (n_direct, n_direct + n_in), (n_direct + n_in, len(chains))) for x in range(b - 1, a - 1, -1)]
+        assert len(chains) == n_direct + n_in + n_back
+        for x in order:
+            e0, e1, tile = chains[x]
+            back = x >= n_direct + n_in
+            source, dest = (scratch if back else have), (scratch if n_direct <= x < n_direct + n_in else have)
             ring, n_stored = [], 0
             for block, mask, k, row in entries[e0:e1]:
                 assert 0 < mask < 1 << 16
-                some = set(turn[k:k + bin(mask).count("1")].tolist())
+                some = {-1} if back else set(turn[k:k + bin(mask).count("1")].tolist())
                 assert row == (some.pop() if len(some) == 1 else -2)
                 for slot in range(16):
                     if mask >> slot & 1:
-                        x = have[block * 16 + slot]  # (block * 16 + slot counts tokens as page * P + slot does)
-                        ring.append((x, int(turns[turn[k]])) if turn[k] >= 0 else x)
+                        x = source[block * 16 + slot]  # (block * 16 + slot counts tokens as page * P + slot does)
+                        ring.append((x, int(turns[turn[k]])) if not back and turn[k] >= 0 else x)
                         k += 1
                 while len(ring) >= 16 * (n_stored + 1):
                     b0 = int(tiles[tile + n_stored]) * 16
-                    have[b0:b0 + 16] = ring[16 * n_stored:16 * n_stored + 16]
+                    dest[b0:b0 + 16] = ring[16 * n_stored:16 * n_stored + 16]
                     n_stored += 1
             rest = ring[16 * n_stored:]
             if rest:
                 b0 = int(tiles[tile + n_stored]) * 16
-                have[b0:b0 + len(rest)] = rest
+                dest[b0:b0 + len(rest)] = rest
         assert all(x == y for x, y in zip(have, want)), trial
         ctx.close()
-    assert checked > 20, checked
+    c.fake.fake_watch(None, 0)
+    assert checked > 20 and scratched > 5, (checked, scratched)
 
 
 def raw(ctx, name, *args):
