@@ -1685,10 +1685,9 @@ extern "C" pie_status pie_restore_kvpage(pie_ctx* c, const int32_t* page_ids, in
   return guarded(c, "pie_restore_kvpage", [&]() { return page_image(c, page_ids, n, const_cast<void*>(image), true, "pie_restore_kvpage"); });
 }
 
-#define COMPACT_CHAIN 8  // destination blocks of a chain where the order of the blocks does not matter
 #define COMPACT_SCRATCH ((int64_t)256 << 20)  // bytes of scratch blocks that a compaction may use
 struct CompactSeq {  // a sequence of which something moves: its source blocks, kept tokens, destination blocks [first_tile, n_tiles)
-  int block0, block1, first, n, first_tile, n_tiles, tile0;
+  int block0, block1, first, n, first_tile, n_tiles, tile0, step;  // step: destination blocks of a chain
   bool in_order;
 };
 static pie_status pie_compact_kvpage_impl(pie_ctx* c, int32_t S, const int32_t* page_indptr, const int32_t* page_ids, const int32_t* kv_len,
@@ -1785,24 +1784,34 @@ static pie_status pie_compact_kvpage_impl(pie_ctx* c, int32_t S, const int32_t* 
       }
       tiles.push_back(to[i / F] * F + i % F);
     }
-    CompactSeq q{block0, (int)blocks.size(), (int)first, n, first_tile, n_tiles, tile0, in_order};
-    // in place, chains may still run side by side where none reads a block that another one writes (a gap as long as what moves up)
-    if (in_order) {
-      bool apart_all = true;
-      for (int b = block0, at = 0; b < q.block1 && apart_all; at += __builtin_popcount(blocks[b++].mask)) {
-        const int j = where[b], last = (at + __builtin_popcount(blocks[b].mask) - 1) / PAGE;
-        if (last < first_tile || j < first_tile || j >= n_tiles) continue;
-        const int mine = (j - first_tile) / COMPACT_CHAIN;
-        apart_all = (std::max(at / PAGE, first_tile) - first_tile) / COMPACT_CHAIN == mine && (last - first_tile) / COMPACT_CHAIN == mine;
-      }
-      q.in_order = !apart_all;
+    seqs.push_back(CompactSeq{block0, (int)blocks.size(), (int)first, n, first_tile, n_tiles, tile0, n_tiles - first_tile, in_order});
+  }
+  // Destination blocks of a chain: as many as leave 2048 waves (8 a compute unit; half kept of 8000 tokens, 32 layers, into other
+  // pages: 366 us in chains of 8, 351 of 32, 348 of 125), or 8192 where keys turn one by one and wait for their angles (415 us in chains of 4, 397, 387 and
+  // 396 of 8, 16 and 32, 421 of 125); but 8 at least, and a sequence's chains of one length.
+  int64_t all_tiles = 0;
+  for (const CompactSeq& q : seqs) all_tiles += q.n_tiles - q.first_tile;
+  const int64_t waves = (int64_t)c->m.n_kv_heads * 2 * (D / 64) * c->m.n_layers;  // of a chain
+  const int64_t wanted = turns.size() > 8 * seqs.size() ? 8192 : 2048;
+  const int most = (int)std::max<int64_t>(8, (all_tiles * waves + wanted - 1) / wanted);
+  // in place, chains may run side by side where none reads a block that another one writes (a gap as long as what moves up)
+  for (CompactSeq& q : seqs) {
+    const int n_chains = (q.n_tiles - q.first_tile + most - 1) / most, step = (q.n_tiles - q.first_tile + n_chains - 1) / n_chains;
+    q.step = step;
+    if (!q.in_order) continue;
+    q.in_order = false;
+    if (n_chains == 1) continue;
+    for (int b = q.block0, at = 0; b < q.block1; at += __builtin_popcount(blocks[b++].mask)) {
+      const int j = where[b], last = (at + __builtin_popcount(blocks[b].mask) - 1) / PAGE;
+      if (last < q.first_tile || j < q.first_tile || j >= q.n_tiles) continue;
+      const int mine = (j - q.first_tile) / step;
+      if ((std::max(at / PAGE, q.first_tile) - q.first_tile) / step != mine || (last - q.first_tile) / step != mine) q.in_order = true;
     }
-    seqs.push_back(q);
   }
   // Sequences whose chains have to go in order: one wave per 64 dims walks each, 0.45 us a source block (0.85 where every key turns by an
   // angle of its own) as long as there are few of them, whatever their number.  Through a block of scratch memory instead, all
-  // chains side by side, twice: 10 us and the bytes at 4.5 TB/s.  (8000 tokens of an 8B-shaped layer, half kept: 231 us in order; 1, 4,
-  // 8 and 32 layers 231, 249, 252, 336 us.)
+  // chains side by side, twice: 10 us and the bytes at 4.5 TB/s.  (8000 tokens of an 8B-shaped layer, half kept, 1, 4, 8 and
+  // 32 layers: 231, 249, 252 and 336 us in order, 50, 90, 141 and more through scratch blocks.)
   const int64_t block_bytes = (int64_t)c->m.n_layers * c->m.n_kv_heads * 2 * PAGE * D * (int64_t)sizeof(bf16_t);
   int64_t n_scratch = 0, longest = 0, moved_blocks = 0;
   for (const CompactSeq& q : seqs)
@@ -1812,14 +1821,14 @@ static pie_status pie_compact_kvpage_impl(pie_ctx* c, int32_t S, const int32_t* 
       longest = std::max<int64_t>(longest, q.block1 - q.block0);
     }
   const bool through_scratch = may_scratch && n_scratch > 0 && n_scratch * block_bytes <= COMPACT_SCRATCH &&
-                               0.45 * longest > 10.0 + (double)moved_blocks * (double)block_bytes / 4.5e6;
+                               (wanted == 8192 ? 0.85 : 0.45) * (double)longest > 10.0 + (double)moved_blocks * (double)block_bytes / 4.5e6;
   if (!through_scratch) n_scratch = 0;
   bool mixed = false;  // some block's tokens turn differently
-  // the sequence's chains of `step` destination blocks each, tiles[tile0 ..] on; a block with tokens for two chains is in both
-  auto cut = [&](const CompactSeq& q, int step, int tile0) {
+  // the sequence's chains of `of` destination blocks each, tiles[tile0 ..] on; a block with tokens for two chains is in both
+  auto cut = [&](const CompactSeq& q, int of, int tile0) {
     int b = q.block0, at = 0;  // kept tokens in front of blocks[b]
-    for (int i = q.first_tile; i < q.n_tiles; i += step) {
-      const int t0 = i * PAGE, t1 = std::min(q.n, (i + step) * PAGE);
+    for (int i = q.first_tile; i < q.n_tiles; i += of) {
+      const int t0 = i * PAGE, t1 = std::min(q.n, (i + of) * PAGE);
       const int entry0 = (int)entries.size();
       while (at + __builtin_popcount(blocks[b].mask) <= t0) at += __builtin_popcount(blocks[b++].mask);
       while (at < t1) {
@@ -1842,7 +1851,7 @@ static pie_status pie_compact_kvpage_impl(pie_ctx* c, int32_t S, const int32_t* 
     }
   };
   for (const CompactSeq& q : seqs)
-    if (!q.in_order || !through_scratch) cut(q, q.in_order ? q.n_tiles : COMPACT_CHAIN, q.tile0);
+    if (!q.in_order || !through_scratch) cut(q, q.in_order ? q.n_tiles : q.step, q.tile0);
   const int n_direct = (int)chains.size();
   if (through_scratch) {  // into scratch blocks 0, 1, .. and from there, the last one of a sequence as full as it is
     const int scratch0 = (int)tiles.size();
@@ -1850,7 +1859,7 @@ static pie_status pie_compact_kvpage_impl(pie_ctx* c, int32_t S, const int32_t* 
     int at = scratch0;
     for (const CompactSeq& q : seqs)
       if (q.in_order) {
-        cut(q, COMPACT_CHAIN, at);
+        cut(q, q.step, at);
         at += q.n_tiles - q.first_tile;
       }
   }
@@ -1859,8 +1868,8 @@ static pie_status pie_compact_kvpage_impl(pie_ctx* c, int32_t S, const int32_t* 
     int at = 0;
     for (const CompactSeq& q : seqs)
       if (q.in_order)
-        for (int i = q.first_tile; i < q.n_tiles; i += COMPACT_CHAIN) {
-          const int entry0 = (int)entries.size(), end = std::min(q.n_tiles, i + COMPACT_CHAIN);
+        for (int i = q.first_tile; i < q.n_tiles; i += q.step) {
+          const int entry0 = (int)entries.size(), end = std::min(q.n_tiles, i + q.step);
           for (int k = i; k < end; ++k, ++at) {
             const int here = std::min(PAGE, q.n - k * PAGE);
             entries.push_back(CompactEntry{at, (1u << here) - 1u, 0, COMPACT_STILL});
