@@ -326,7 +326,60 @@ struct Picker {
       }
     }
     __syncthreads();
-    // every wave finds the bin of the n_out-th segment for itself, 16 bins to a lane
+    // one bin more than the n_out-th segment's (see far_bin); all, where there are fewer segments
+    int bin = cut_bin();
+    bool by_logit = bin < 0;
+    if (by_logit) {
+      if (n > BP_SEGS) return -1;
+      bin = BP_BINS - 2;
+    }
+#pragma unroll
+    for (int j = 0; j < BP_HELD; ++j)
+      if ((int)bins[j] <= bin) {
+        const uint32_t k = atomicAdd(&sh.count, 1u);
+        if (k < BP_SEGS) sh.segs[k] = tid + j * BP_THREADS;
+      }
+    __syncthreads();
+    const int kept = (int)sh.count;
+    if (kept > BP_SEGS) return -1;
+    // the kept segments' logits: take(bin, row, token, logit)
+    auto each = [&](auto take) {
+      for (int e = tid * VEC; e < kept * SEG; e += BP_THREADS * VEC) {
+        const int i = sh.segs[e / SEG], r = row_of(i), p = (i - r * n_segs) * SEG + e % SEG;
+        if (sh.done[r]) {
+          if (e % SEG == 0) take((int)far_bin((float)(best - sh.row[r].x)), r, eos, 0.f);
+          continue;
+        }
+        const BeamRow<T> z(logits, stride, row0 + r, V);
+        float x[VEC];
+        z.load(p, x);
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) take((int)bin_of(r, x[k]), r, p + k, x[k]);
+      }
+    };
+    auto collect = [&](int b, int r, int v, float z) {
+      if (b <= bin) put(sh.done[r] ? score_key(sh.row[r].x) : key_of(r, z), r * V + v);
+    };
+    if (!by_logit) {
+      each(collect);
+      __syncthreads();
+      if (sh.n_cand <= BP_CANDS) return (int)sh.n_cand;
+      __syncthreads();
+    }
+    // fewer segments than candidates asked for, or many candidates in them: the bins of the logits themselves
+    sh.hist[tid] = 0;
+    if (tid == 0) sh.n_cand = 0;
+    __syncthreads();
+    each([&](int b, int, int, float) { if (b <= bin) atomicAdd(&sh.hist[b], 1u); });
+    __syncthreads();
+    bin = cut_bin();
+    if (bin < 0) return -1;
+    each(collect);
+    __syncthreads();
+    return sh.n_cand <= BP_CANDS ? (int)sh.n_cand : -1;
+  }
+  // One bin more than that of the n_out-th counted in sh.hist, -1 where fewer are; every wave finds it for itself, 16 bins to a lane.
+  __device__ int cut_bin() const {
     uint32_t h[16], mine = 0;
 #pragma unroll
     for (int k = 0; k < 16; ++k) { h[k] = sh.hist[lane * 16 + k]; mine += h[k]; }
@@ -338,40 +391,15 @@ struct Picker {
     }
     const u64 reached = __ballot(incl >= (uint32_t)n_out);
     if (!reached) return -1;
-    const int at = __ffsll((long long)reached) - 1;
-    uint32_t run = incl - mine, bin = 0;
-    bool found = false;
+    uint32_t run = incl - mine;
+    int bin = BP_BINS;
 #pragma unroll
     for (int k = 0; k < 16; ++k) {
       run += h[k];
-      if (!found && run >= (uint32_t)n_out) { found = true; bin = lane * 16 + k; }
+      if (bin == BP_BINS && run >= (uint32_t)n_out) bin = lane * 16 + k;
     }
-    bin = __shfl(bin, at) + 1;  // (one more: see far_bin)
-    if (bin >= BP_BINS - 1) return -1;
-#pragma unroll
-    for (int j = 0; j < BP_HELD; ++j)
-      if (bins[j] <= bin) {
-        const uint32_t k = atomicAdd(&sh.count, 1u);
-        if (k < BP_SEGS) sh.segs[k] = tid + j * BP_THREADS;
-      }
-    __syncthreads();
-    const int kept = (int)sh.count;
-    if (kept > BP_SEGS) return -1;
-    for (int e = tid * VEC; e < kept * SEG; e += BP_THREADS * VEC) {
-      const int i = sh.segs[e / SEG], r = row_of(i), p = (i - r * n_segs) * SEG + e % SEG;
-      if (sh.done[r]) {
-        if (e % SEG == 0) put(score_key(sh.row[r].x), r * V + eos);
-        continue;
-      }
-      const BeamRow<T> z(logits, stride, row0 + r, V);
-      float x[VEC];
-      z.load(p, x);
-#pragma unroll
-      for (int k = 0; k < VEC; ++k)
-        if (bin_of(r, x[k]) <= bin) put(key_of(r, x[k]), r * V + p + k);
-    }
-    __syncthreads();
-    return sh.n_cand <= BP_CANDS ? (int)sh.n_cand : -1;
+    bin = __shfl(bin, __ffsll((long long)reached) - 1) + 1;
+    return bin < BP_BINS - 1 ? bin : -1;
   }
   __device__ void put(u64 key, int idx) {
     const uint32_t at = atomicAdd(&sh.n_cand, 1u);

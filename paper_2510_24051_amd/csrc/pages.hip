@@ -13,6 +13,7 @@ namespace {
 // synchronisation.  A run with a cycle starts by keeping the page that the cycle's last move reads (PageRun::keep; the
 // order: page_plans.h).
 #define FORK_THREADS 256
+#define FORK_AHEAD 8  // moves whose sources are read before the first of them is stored: a read only ever comes too late, never too early
 struct ForkMoves {
   PageMove moves[FORK_MOVES];
   PageRun runs[FORK_MOVES];
@@ -22,15 +23,29 @@ __global__ __launch_bounds__(FORK_THREADS) void fork_kernel(unsigned char* __res
   const int run = blockIdx.x / slices, slice = blockIdx.x % slices;
   unsigned char* base = kv + (int64_t)blockIdx.y * layer_bytes + ((int64_t)slice * FORK_THREADS + threadIdx.x) * 16;
   const PageRun r = plan.runs[run];
-  u32x4 kept = {0, 0, 0, 0}, v = {0, 0, 0, 0};
+  u32x4 kept = {0, 0, 0, 0}, now = {0, 0, 0, 0};
   if (r.keep >= 0) kept = *reinterpret_cast<const u32x4*>(base + r.keep * page_bytes);
-  int last = -1;
-  for (int i = r.first; i < r.first + r.n; ++i) {
-    const PageMove m = plan.moves[i];
-    if (m.src < 0) v = kept;
-    else if (m.src != last) v = load_nt(reinterpret_cast<const u32x4*>(base + m.src * page_bytes));
-    last = m.src;
-    *reinterpret_cast<u32x4*>(base + m.dst * page_bytes) = v;
+  const int end = r.first + r.n;
+  int before = -1;  // source of the move in front
+  for (int i = r.first; i < end; i += FORK_AHEAD) {
+    u32x4 v[FORK_AHEAD];
+    int last = before;
+#pragma unroll
+    for (int q = 0; q < FORK_AHEAD; ++q) {
+      if (i + q >= end) break;
+      const int src = plan.moves[i + q].src;
+      if (src >= 0 && src != last) v[q] = load_nt(reinterpret_cast<const u32x4*>(base + src * page_bytes));
+      last = src;
+    }
+#pragma unroll
+    for (int q = 0; q < FORK_AHEAD; ++q) {
+      if (i + q >= end) break;
+      const PageMove m = plan.moves[i + q];
+      if (m.src < 0) now = kept;
+      else if (m.src != before) now = v[q];
+      before = m.src;
+      *reinterpret_cast<u32x4*>(base + m.dst * page_bytes) = now;
+    }
   }
 }
 
