@@ -153,7 +153,8 @@ __device__ __forceinline__ double key_score(u64 k) { return __longlong_as_double
 
 #define BP_THREADS 1024
 #define BP_SEGS 576   // segments kept for reading again: at most 2 n_out + 64
-#define BP_CANDS 512  // candidates that are ranked against each other
+#define BP_CANDS 512  // candidates that are put in order
+#define BP_COUNTED 192  // of which so many by counting
 #define BP_CACHED 8192  // maxima of segments kept in LDS
 struct BeamGroups { int32_t row0[BEAM_GROUPS_BY_VALUE + 1]; };
 #define BP_HELD (BP_CACHED / BP_THREADS)
@@ -303,26 +304,33 @@ struct Picker {
   // the logits of those kept.  Returns how many candidates it left in sh, or -1 where that does not serve: candidates further
   // apart than the bins reach or more of them in a bin than there is room for.
   template <typename H>
-  __device__ int quick(const H& held) {
+  __device__ int quick(const H& held, bool cached) {
     double best = -INFINITY;
     for (int r = lane; r < rows; r += 64) best = fmax(best, sh.row[r].x);
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) best = fmax(best, __shfl_xor(best, o));
     if (best == -INFINITY) return 0;  // (uniform over the workgroup)
     const float c = (float)inv_temp;
-    auto bin_of = [&](int r, float z) {  // BP_BINS - 1: not counted
-      const double2 b = sh.row[r];
-      return far_bin((float)(best - b.x) + ((float)b.y - z) * c);  // (-inf: infinitely far)
+    // (behind, m): a row's best score behind the group's and its largest logit; z is far_bin(behind + (m - z) c) away, -inf infinitely
+    auto row_at = [&](int r) { return make_float2((float)(best - sh.row[r].x), (float)sh.row[r].y); };
+    auto seg_bin = [&](int i, float z) {  // BP_BINS - 1: not counted
+      const int r = row_of(i);
+      const float2 at = row_at(r);
+      if (sh.done[r]) return i == r * n_segs ? far_bin(at.x) : BP_BINS - 1u;
+      return far_bin(at.x + (at.y - z) * c);
     };
     uint32_t bins[BP_HELD];
+    if (cached) {
 #pragma unroll
-    for (int j = 0; j < BP_HELD; ++j) {
-      const int i = tid + j * BP_THREADS;
-      bins[j] = BP_BINS - 1;
-      if (i < n) {
-        const int r = row_of(i);
-        bins[j] = sh.done[r] ? (i == r * n_segs ? far_bin((float)(best - sh.row[r].x)) : BP_BINS - 1u) : bin_of(r, held[j]);
+      for (int j = 0; j < BP_HELD; ++j) {
+        const int i = tid + j * BP_THREADS;
+        bins[j] = i < n ? seg_bin(i, held[j]) : BP_BINS - 1;
         if (bins[j] < BP_BINS - 1) atomicAdd(&sh.hist[bins[j]], 1u);
+      }
+    } else {
+      for (int i = tid; i < n; i += BP_THREADS) {
+        const uint32_t b = seg_bin(i, maxima[i]);
+        if (b < BP_BINS - 1) atomicAdd(&sh.hist[b], 1u);
       }
     }
     __syncthreads();
@@ -333,28 +341,49 @@ struct Picker {
       if (n > BP_SEGS) return -1;
       bin = BP_BINS - 2;
     }
+    auto keep = [&](int i) {
+      const uint32_t k = atomicAdd(&sh.count, 1u);
+      if (k < BP_SEGS) sh.segs[k] = i;
+    };
+    if (cached) {
 #pragma unroll
-    for (int j = 0; j < BP_HELD; ++j)
-      if ((int)bins[j] <= bin) {
-        const uint32_t k = atomicAdd(&sh.count, 1u);
-        if (k < BP_SEGS) sh.segs[k] = tid + j * BP_THREADS;
-      }
+      for (int j = 0; j < BP_HELD; ++j)
+        if ((int)bins[j] <= bin) keep(tid + j * BP_THREADS);
+    } else {
+      for (int i = tid; i < n; i += BP_THREADS)
+        if ((int)seg_bin(i, maxima[i]) <= bin) keep(i);
+    }
     __syncthreads();
     const int kept = (int)sh.count;
     if (kept > BP_SEGS) return -1;
-    // the kept segments' logits: take(bin, row, token, logit)
+    // the kept segments' logits, 8 of a thread at a time (16 bits: four of these spill): take(bin, row, token, logit)
     auto each = [&](auto take) {
-      for (int e = tid * VEC; e < kept * SEG; e += BP_THREADS * VEC) {
-        const int i = sh.segs[e / SEG], r = row_of(i), p = (i - r * n_segs) * SEG + e % SEG;
-        if (sh.done[r]) {
-          if (e % SEG == 0) take((int)far_bin((float)(best - sh.row[r].x)), r, eos, 0.f);
-          continue;
-        }
-        const BeamRow<T> z(logits, stride, row0 + r, V);
-        float x[VEC];
-        z.load(p, x);
+      constexpr int U = 8 / VEC;
+      for (int e0 = tid * VEC; e0 < kept * SEG; e0 += U * BP_THREADS * VEC) {
+        float x[U][VEC];
+        int row[U], p[U];
 #pragma unroll
-        for (int k = 0; k < VEC; ++k) take((int)bin_of(r, x[k]), r, p + k, x[k]);
+        for (int u = 0; u < U; ++u) {
+          const int e = e0 + u * BP_THREADS * VEC;
+          row[u] = -1;
+          if (e >= kept * SEG) continue;
+          const int i = sh.segs[e / SEG], r = row_of(i);
+          p[u] = (i - r * n_segs) * SEG + e % SEG;
+          row[u] = r;
+          if (!sh.done[r]) BeamRow<T>(logits, stride, row0 + r, V).load(p[u], x[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int r = row[u];
+          if (r < 0) continue;
+          const float2 at = row_at(r);
+          if (sh.done[r]) {
+            if (p[u] == 0) take((int)far_bin(at.x), r, eos, 0.f);  // (its one candidate stands in its first segment)
+            continue;
+          }
+#pragma unroll
+          for (int k = 0; k < VEC; ++k) take((int)far_bin(at.x + (at.y - x[u][k]) * c), r, p[u] + k, x[u][k]);
+        }
       }
     };
     auto collect = [&](int b, int r, int v, float z) {
@@ -491,13 +520,19 @@ __global__ __launch_bounds__(BP_THREADS) void beam_pick_kernel(const T* __restri
   __syncthreads();
 
   Picker<T> pick{sh, logits, stride, V, n_segs, n, n_out, row0, rows, eos, inv_temp, 1.0f / (float)n_segs, cached ? sh.maxima : maxima, tid, lane, wave};
-  int n_cand = cached ? pick.quick(held) : -1;
+  int n_cand = pick.quick(held, cached);
   if (n_cand < 0) n_cand = pick.exactly();  // (uniform)
 
-  // their ranks: each is compared with all by a group of lanes
   const int64_t o = (int64_t)g * n_out;
-  if (n_cand) {
-    int share = 64;  // lanes to a candidate (n_cand <= 512)
+  auto tell = [&](int at, u64 key, int idx) {
+    if (at >= n_out) return;
+    const int r = idx / V;
+    out_beams[o + at] = r;
+    out_tokens[o + at] = idx - r * V;
+    out_scores[o + at] = (float)key_score(key);
+  };
+  if (n_cand <= BP_COUNTED) {  // ranks: each candidate is compared with all by a group of lanes
+    int share = 64;  // lanes to a candidate
     while (share * n_cand > BP_THREADS) share >>= 1;
     const int c = tid / share;
     if (c < n_cand) {
@@ -509,13 +544,26 @@ __global__ __launch_bounds__(BP_THREADS) void beam_pick_kernel(const T* __restri
         at += k2 > key || (k2 == key && sh.cand_idx[k] < idx);
       }
       for (int d = share >> 1; d > 0; d >>= 1) at += __shfl_xor(at, d);
-      if (tid % share == 0 && at < n_out) {
-        const int r = idx / V;
-        out_beams[o + at] = r;
-        out_tokens[o + at] = idx - r * V;
-        out_scores[o + at] = (float)key_score(key);
-      }
+      if (tid % share == 0) tell(at, key, idx);
     }
+  } else {  // sorted (400 candidates: 3 us for 15)
+    for (int i = n_cand + tid; i < BP_CANDS; i += BP_THREADS) { sh.cand_key[i] = 0; sh.cand_idx[i] = 0x7FFFFFFF; }
+    for (int size = 2; size <= BP_CANDS; size <<= 1)
+      for (int d = size >> 1; d > 0; d >>= 1) {
+        __syncthreads();
+        if (tid < BP_CANDS / 2) {
+          const int a = (tid & ~(d - 1)) * 2 + (tid & (d - 1)), b = a + d;
+          const u64 ka = sh.cand_key[a], kb = sh.cand_key[b];
+          const int ia = sh.cand_idx[a], ib = sh.cand_idx[b];
+          const bool b_first = kb > ka || (kb == ka && ib < ia);
+          if (b_first == ((a & size) == 0)) {
+            sh.cand_key[a] = kb; sh.cand_key[b] = ka;
+            sh.cand_idx[a] = ib; sh.cand_idx[b] = ia;
+          }
+        }
+      }
+    __syncthreads();
+    for (int i = tid; i < n_cand; i += BP_THREADS) tell(i, sh.cand_key[i], sh.cand_idx[i]);
   }
   for (int i = n_cand + tid; i < n_out; i += BP_THREADS) {
     out_beams[o + i] = -1;
