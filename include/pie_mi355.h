@@ -171,7 +171,8 @@ pie_status pie_restore_kvpage(pie_ctx* ctx, const int32_t* page_ids, int32_t n, 
  * that keeps its place relative to others when a gap before it is closed; 0 leaves the bits.
  * Pages may be shared by several sequences where no sequence of the call writes them (in place, pages in front of the first token
  * that moves or turns are not written).  A page that is written may be no one's source in any other place: PIE_ECONFLICT.
- * All arrays are host int32.  May allocate; refused with PIE_EHIP while the stream is captured.  On error nothing has changed.
+ * All arrays are host int32.  May allocate; refused with PIE_EHIP while the stream is captured.  On an error other than a
+ * PIE_EHIP of a failed launch nothing has changed.
  * Errors: PIE_EINVAL (also: more tokens kept than the destination holds), PIE_ERANGE, PIE_EBATCH (over 2^30 tokens),
  * PIE_ECONFLICT, PIE_ENOMEM, PIE_EHIP. */
 pie_status pie_compact_kvpage(pie_ctx* ctx, int32_t n_seqs, const int32_t* page_indptr, const int32_t* page_ids, const int32_t* kv_len,
@@ -312,7 +313,7 @@ enum { PIE_F32 = 0, PIE_BF16 = 1, PIE_F16 = 2 };
 /* The selection over logits that the caller has (changed by a grammar, a penalty, a head of its own): dev [rows] of n_vocab
  * (1 .. the model's vocab) elements, row r at logits + r * row_stride elements; any row_stride >= n_vocab, and any alignment that
  * the element type has.  rows <= max_dist_rows.  Outputs dev [n_groups][n_out]: the beam within its group, the token, the new
- * cumulative score.  Enqueues only and allocates nothing; may be captured into a graph.
+ * cumulative score (-inf where it is below what 32 bits hold); they must not overlap the inputs.  Enqueues only and allocates nothing; may be captured into a graph.
  * Errors: PIE_EINVAL, PIE_ERANGE (n_out, n_vocab, eos_token), PIE_EBATCH (rows, beams of a group), PIE_EHIP. */
 pie_status pie_beam_select(pie_ctx* ctx, const pie_beam_search* search, const void* logits, int32_t dtype, int64_t row_stride,
                            int32_t n_vocab, int32_t* out_beams, int32_t* out_tokens, float* out_scores);

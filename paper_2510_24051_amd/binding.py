@@ -240,6 +240,12 @@ class Pie:
         if st != 0:
             raise PieError(st, self.lib.pie_last_error(self.ctx).decode())
 
+    def _device(self) -> torch.device:
+        """The context's device with its number, as its tensors name it."""
+        if self.device.index is None:
+            self.device = torch.device(self.device.type, torch.cuda.current_device())
+        return self.device
+
     def _dev_bf16(self, bits) -> torch.Tensor:
         if isinstance(bits, torch.Tensor):
             assert bits.dtype == torch.bfloat16 and bits.is_cuda and bits.is_contiguous()
@@ -342,7 +348,7 @@ class Pie:
 
     def _image(self, page_ids, image: torch.Tensor) -> np.ndarray:
         ids, m = _i32(page_ids), self.model
-        if image.dtype != torch.bfloat16 or not image.is_cuda or not image.is_contiguous() or image.dim() != 6 or \
+        if image.dtype != torch.bfloat16 or image.device != self._device() or not image.is_contiguous() or image.dim() != 6 or \
                 image.shape[0] != len(ids) or tuple(image.shape[2:]) != (2, m.page_size, m.n_kv_heads, m.head_dim) or \
                 image.shape[1] != self.n_layers:
             raise ValueError("an image of pages is a contiguous bfloat16 device tensor [pages, layers, 2, page_size, kv heads, head_dim]")
@@ -449,12 +455,12 @@ class Pie:
 
     def _beam_search(self, group_indptr, n_out, out_beams, out_tokens, out_scores, scores, finished, eos_token, temperature):
         ip = _i32(group_indptr)
-        G, n = len(ip) - 1, int(ip[-1]) if len(ip) else 0
+        G, n, dev = len(ip) - 1, int(ip[-1]) if len(ip) else 0, self._device()
         for t, dt in ((out_beams, torch.int32), (out_tokens, torch.int32), (out_scores, torch.float32)):
-            if t.dtype != dt or not t.is_cuda or not t.is_contiguous() or t.numel() != G * n_out:
+            if t.dtype != dt or t.device != dev or not t.is_contiguous() or t.numel() != G * n_out:
                 raise ValueError("beam search: outputs are contiguous device tensors [groups, n_out] of int32, int32 and float32")
         for t, dts in ((scores, (torch.float32,)), (finished, (torch.uint8, torch.bool))):
-            if t is not None and (t.dtype not in dts or not t.is_cuda or not t.is_contiguous() or t.numel() != n):
+            if t is not None and (t.dtype not in dts or t.device != dev or not t.is_contiguous() or t.numel() != n):
                 raise ValueError("beam search: scores (float32) and finished (uint8 or bool) are contiguous device tensors [rows]")
         at = lambda t: None if t is None else t.data_ptr()
         return BeamSearchC(G, _at(ip), at(scores), at(finished), int(eos_token), int(n_out), float(temperature)), ip
@@ -466,7 +472,7 @@ class Pie:
         caller's tensors [groups, n_out], complete when the context's stream has got there."""
         b, keep = self._beam_search(group_indptr, n_out, out_beams, out_tokens, out_scores, scores, finished, eos_token, temperature)
         types = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
-        if logits.dtype not in types or not logits.is_cuda or logits.dim() != 2 or logits.shape[0] != keep[-1] or \
+        if logits.dtype not in types or logits.device != self._device() or logits.dim() != 2 or logits.shape[0] != keep[-1] or \
                 (logits.shape[1] > 1 and logits.stride(1) != 1):
             raise ValueError("beam_select: logits are a device tensor [rows, vocab] of float32, bfloat16 or float16 whose rows are contiguous")
         stride = logits.stride(0) if logits.shape[0] > 1 else logits.shape[1]

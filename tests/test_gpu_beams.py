@@ -240,6 +240,21 @@ def test_from_embeds(ctx):
         np.testing.assert_allclose(s, so, atol=4e-3)  # logits within 1e-3, twice, over 0.75
 
 
+def test_groups_without_any_beam(ctx):
+    b, v, s = select(ctx, torch.empty((0, 1000), device="cuda"), [0, 0, 0], 3)
+    assert (b == -1).all() and (v == -1).all() and np.isneginf(s).all()
+
+
+def test_what_lies_behind_the_outputs_stays(ctx):
+    z = logits(8, 3000, torch.float32, 2)
+    room = [torch.full((64,), 77, dtype=dt, device="cuda") for dt in (torch.int32, torch.int32, torch.float32)]
+    torch.cuda.synchronize()
+    ctx.beam_select_async(z, [0, 3, 8], 5, *[r[20:30].view(2, 5) for r in room])
+    ctx.synchronize()
+    for r in room:
+        assert (r[:20] == 77).all() and (r[30:] == 77).all() and (r[20:30] != 77).all()
+
+
 def test_wrong_tensors_are_refused(ctx):
     o = [torch.zeros((1, 4), dtype=torch.int32, device="cuda"), torch.zeros((1, 4), dtype=torch.int32, device="cuda"), torch.zeros((1, 4), device="cuda")]
     z = torch.zeros((2, 64), device="cuda")

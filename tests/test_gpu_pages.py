@@ -224,6 +224,98 @@ def test_a_far_shift_is_exact():
     assert ok.mean() > 0.99 and np.all(np.abs(g - w)[moderate] <= 2 * bf16_step(w)[moderate] + 40 * 2.0 ** -24 * 100)
 
 
+def test_pages_behind_four_gigabytes():
+    """Offsets of pages within a layer, of layers and of images pass 32 bits."""
+    from paper_2510_24051_amd import Pie
+    m = model(128, 8, 16)
+    ctx = Pie(m, 70000, 1, max_batch_tokens=1, max_batch_requests=1, n_layers=2)  # 4.6 GB a layer
+    rng = np.random.default_rng(9)
+    bits = (rng.integers(0, 1 << 16, (6, 2, 2, 16, 8, 128)) & 0xBFFF).astype(np.uint16)  # (no infinities or NaN)
+
+    def tensor(b):
+        return torch.from_numpy(np.ascontiguousarray(b).view(np.int16)).to(ctx.device).view(torch.bfloat16)
+
+    def read(ids):
+        t = torch.empty((len(ids), 2, 2, 16, 8, 128), dtype=torch.bfloat16, device=ctx.device)
+        torch.cuda.synchronize()
+        ctx.save_kvpage(ids, t)
+        ctx.synchronize()
+        return t.view(torch.int16).cpu().numpy().view(np.uint16)
+
+    far = [69999, 69990, 65537, 65536, 3, 66000]
+    given = tensor(bits)
+    torch.cuda.synchronize()
+    ctx.restore_kvpage(far, given)
+    assert np.array_equal(read(far), bits)
+    k, v = ctx.kv_read(1, [69999, 3], [5, 6])
+    assert np.array_equal(k, bits[[0, 4], 1, 0, [5, 6]]) and np.array_equal(v, bits[[0, 4], 1, 1, [5, 6]])
+    ctx.fork_kvpage([69999, 3, 65536], [65536, 69999, 68000])  # (65536 first goes to 68000)
+    assert np.array_equal(read([65536, 69999, 68000, 3]), bits[[0, 4, 3, 4]])
+    ctx.mask_kvpage([69990, 66000], [0xF00F, 0x00FF])
+    assert ctx.compact_kvpage([0, 2], [69990, 66000], [32])[0] == 16
+    keep = np.concatenate([bits[1][:, :, [0, 1, 2, 3, 12, 13, 14, 15]], bits[5][:, :, :8]], axis=2)
+    assert np.array_equal(read([69990])[0], keep)
+    ctx.close()
+
+
+def test_shared_pages():
+    """Sequences on one prefix: compacted into pages of their own, and in place where the prefix stays as it is."""
+    for P in (16, 32):
+        b = Both(model(64, 2, P), 40, 2, P)
+        prefix, own = [3, 4, 5], [[10, 11], [12, 13], [14, 15]]
+        lens = [4 * P, 5 * P - 3, 5 * P]
+        b.ctx.mask_kvpage([4, 11, 12, 13, 14], [0x0F0F0F0F, 0xFF00FF00, 0x1, 0xAAAAAAAA, 0x0])
+        O.mask_kvpage(b.kvs, [4, 11, 12, 13, 14], [0x0F0F0F0F, 0xFF00FF00, 0x1, 0xAAAAAAAA, 0x0])
+        ip, ids = [0, 5, 10, 15], np.concatenate([prefix + o for o in own])
+        dp, di = [0, 5, 10, 15], np.arange(20, 35)
+        for args in (dict(dst_page_indptr=dp, dst_page_ids=di), dict(dst_page_indptr=dp, dst_page_ids=di, shifts=np.arange(sum(lens)) % 5 - 2)):
+            n = b.ctx.compact_kvpage(ip, ids, lens, **args)
+            assert np.array_equal(n, O.compact_kvpage(b.kvs, ip, ids, lens, THETA, **args))
+            check_compacted(b)
+            b.restore(di, O.save_kvpage(b.kvs, di))
+        b.ctx.mask_kvpage([4], [0xFFFFFFFF])
+        O.mask_kvpage(b.kvs, [4], [0xFFFFFFFF])
+        n = b.ctx.compact_kvpage(ip, ids, lens)
+        assert np.array_equal(n, O.compact_kvpage(b.kvs, ip, ids, lens, THETA))
+        b.same("in place behind a shared prefix")
+
+
+def test_a_compaction_is_refused_in_a_capture_and_does_not_end_it():
+    from paper_2510_24051_amd import PieError
+    s = torch.cuda.Stream()
+    b = Both(model(64, 2, 16), 16, 1, 2, stream=s)
+    b.ctx.mask_kvpage([0], [0xFFF0])
+    O.mask_kvpage(b.kvs, [0], [0xFFF0])
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=s):
+        b.ctx.fork_kvpage([1], [2])
+        with pytest.raises(PieError) as e:
+            b.ctx.compact_kvpage([0, 2], [0, 1], [32])
+        assert e.value.status == -6
+    with torch.cuda.stream(s):
+        g.replay()
+    s.synchronize()
+    O.fork_kvpage(b.kvs, [1], [2])
+    b.same("the capture's fork")
+    assert b.ctx.compact_kvpage([0, 2], [0, 1], [32])[0] == 28
+    O.compact_kvpage(b.kvs, [0, 2], [0, 1], [32], THETA)
+    b.same("and the compaction behind it")
+
+
+def test_wrong_images_are_refused():
+    b = Both(model(64, 2, 16), 8, 2, 3)
+    good = torch.zeros((2, 2, 2, 16, 2, 64), dtype=torch.bfloat16, device=b.ctx.device)
+    for image in (good[:1], good[:, :1], good.float(), good.cpu(), good.transpose(4, 5), good[..., :32], good[..., 0]):
+        for call in (b.ctx.save_kvpage, b.ctx.restore_kvpage):
+            with pytest.raises(ValueError):
+                call([0, 1], image)
+    with pytest.raises(ValueError):
+        b.ctx.fork_kvpage([0, 1], [2])
+    for bad in (dict(page_indptr=[0, 1, 2]), dict(kv_len=[3, 4]), dict(shifts=[1]), dict(dst_page_indptr=[0, 1]), dict(page_ids=[0, 1])):
+        with pytest.raises(ValueError):
+            b.ctx.compact_kvpage(**{**dict(page_indptr=[0, 1], page_ids=[0], kv_len=[5]), **bad})
+
+
 def test_fork_save_and_restore_in_a_graph():
     """Captured once and replayed with eager calls in between; every replay does what the eager calls do."""
     s = torch.cuda.Stream()

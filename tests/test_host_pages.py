@@ -33,6 +33,8 @@ def last_image(c, ctx):
 
 
 PLAN = r"""
+#include <map>
+
 #include "page_plans.h"
 // src, dst [n]; pages [p]: carries the plan out, the runs of a launch one after the other from the last to the first; what a launch
 // holds at most; returns launches, or -1 where one holds more moves than it may
@@ -49,6 +51,17 @@ extern "C" int carry_out(const int32_t* src, const int32_t* dst, int n, int32_t*
       next += run.n;
     }
     if (next != l.n_moves) return -1;
+    std::map<int32_t, int> writer;  // runs of a launch may go at the same time: what one writes no other touches
+    for (int r = 0; r < l.n_runs; ++r)
+      for (int i = 0; i < plan.runs[l.run0 + r].n; ++i) writer[plan.moves[l.move0 + plan.runs[l.run0 + r].first + i].dst] = r;
+    for (int r = 0; r < l.n_runs; ++r) {
+      const PageRun& run = plan.runs[l.run0 + r];
+      if (run.keep >= 0 && writer.count(run.keep) && writer[run.keep] != r) return -2;
+      for (int i = 0; i < run.n; ++i) {
+        const PageMove m = plan.moves[l.move0 + run.first + i];
+        if (writer[m.dst] != r || (m.src >= 0 && writer.count(m.src) && writer[m.src] != r)) return -2;
+      }
+    }
     for (int r = l.n_runs; r-- > 0;) {
       const PageRun& run = plan.runs[l.run0 + r];
       const int32_t kept = run.keep >= 0 ? pages[run.keep] : -1;
@@ -221,6 +234,16 @@ def compact_plans(c):
         have, scratch = pool.copy(), np.full(20000, -1, object)
         order = [x for a, b in ((0, n_direct), (n_direct, n_direct + n_in), (n_direct + n_in, len(chains))) for x in range(b - 1, a - 1, -1)]
         assert len(chains) == n_direct + n_in + n_back
+        # chains of a phase may go at the same time: a block that one writes no other reads or writes
+        for a, b in ((0, n_direct), (n_direct, n_direct + n_in), (n_direct + n_in, len(chains))):
+            writer = {}
+            for x in range(a, b):
+                e0, e1, tile = chains[x]
+                for i in range(-(-sum(bin(mask).count("1") for _, mask, _, _ in entries[e0:e1]) // 16)):
+                    assert writer.setdefault(int(tiles[tile + i]), x) == x
+            for x in range(a, min(b, n_direct)):  # (what goes through scratch blocks reads one memory and writes the other)
+                for block, _, _, _ in entries[chains[x][0]:chains[x][1]]:
+                    assert writer.get(int(block), x) == x
         for x in order:
             e0, e1, tile = chains[x]
             back = x >= n_direct + n_in
