@@ -163,9 +163,10 @@ pie_status pie_restore_kvpage(pie_ctx* ctx, const int32_t* page_ids, int32_t n, 
  * of the sequence's destination pages, in their order, in every layer.  Sequence s has the page table page_ids[page_indptr[s] ..
  * page_indptr[s+1]) and kv_len[s] tokens (tokens behind them are not looked at); its destination table is dst_page_ids[
  * dst_page_indptr[s] .. dst_page_indptr[s+1]), or, with both destination arrays NULL, its own table: in place.  out_kv_len[s]
- * receives the number of tokens kept; the destination's first ceil(out_kv_len[s] / page_size) pages hold them and have all slots
- * visible afterwards, slots behind the last kept token are left as they were, and the pages behind those (which the caller may now
- * give to others) keep contents and masks, as do source pages that are no destinations.  A sequence that keeps nothing has length 0.
+ * receives the number of tokens kept; the destination's first ceil(out_kv_len[s] / page_size) pages hold them.  Of these, pages that
+ * the call writes have all slots visible afterwards; slots behind the last kept token are left as they were.  The pages behind them
+ * (which the caller may now give to others) keep contents and masks, as do source pages that are no destinations.  A sequence that
+ * keeps nothing has length 0.
  * shifts (may be NULL): host int32, one per token of the sequences one after another (sum of kv_len): the key of a kept token
  * is rotated by that many positions more, with the model's rotary frequencies and rounded to bf16 once, as a token needs
  * that keeps its place relative to others when a gap before it is closed; 0 leaves the bits.
@@ -294,7 +295,8 @@ pie_status pie_get_next_dist_static(pie_ctx* ctx, const int32_t* embed_ids, int3
  * ascending beam, then ascending token; scores are compared in 64 bits and stored in 32.
  *   - a logit of -inf or NaN is no candidate and adds nothing to the sum (a grammar's mask); +inf counts as the largest finite
  *     value of the logits' type; the lowest finite value is a logit like any other
- *   - a beam whose score is -inf or NaN, or whose logits are all -inf or NaN, has no candidates
+ *   - a beam whose score is -inf or NaN, or whose logits are all -inf or NaN, has no candidates; a score of +inf counts as the
+ *     largest finite one
  *   - a beam with finished[r] != 0 has exactly one: (r, eos_token) with its score unchanged; its logits are not looked at
  *   - where fewer than n_out candidates exist the rest is beam -1, token -1, score -inf */
 typedef struct {

@@ -475,8 +475,8 @@ def save_kvpage(kvs, page_ids) -> np.ndarray:
 
 def compact_kvpage(kvs, page_indptr, page_ids, kv_len, theta, dst_page_indptr=None, dst_page_ids=None, shifts=None) -> np.ndarray:
     """The visible tokens of every sequence move, in their order, to the front of its destination pages, in every layer; the key
-    of a token whose shift is not 0 is rotated by it and rounded to bf16.  Pages that then hold kept tokens are visible
-    throughout.  Returns the new lengths."""
+    of a token whose shift is not 0 is rotated by it and rounded to bf16.  Pages from the first token on that is not what and
+    where it was are written, and visible throughout afterwards.  Returns the new lengths."""
     P = kvs[0].page_size
     if dst_page_indptr is None:
         dst_page_indptr, dst_page_ids = page_indptr, page_ids
@@ -499,7 +499,10 @@ def compact_kvpage(kvs, page_indptr, page_ids, kv_len, theta, dst_page_indptr=No
                 few = np.rint(np.where(ordinary, 0.0, np.nan_to_num(x, posinf=0.0, neginf=0.0)) * 2.0 ** 133) * 2.0 ** -133  # subnormals
                 k[turned] = np.where(ordinary, bf16_encode(bf16_round(np.where(ordinary, x, 0.0))),
                                      (np.where(np.isfinite(x), few, x).astype(np.float32).view(np.uint32) >> 16).astype(np.uint16))
-            writes.append((kv, into, np.arange(len(keep)), k, v))
+            at = np.arange(len(keep))
+            still = (table[keep // P] == into[at // P]) & (keep % P == at % P) & ~turned
+            first = int(np.argmin(still)) // P * P if not still.all() else len(keep)
+            writes.append((kv, into, at[first:], k[first:], v[first:]))
     for kv, into, at, k, v in writes:
         kv.k_bits[into[at // P], at % P] = k
         kv.v_bits[into[at // P], at % P] = v

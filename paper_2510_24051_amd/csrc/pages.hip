@@ -165,7 +165,7 @@ __device__ __forceinline__ void compact_walk(const uint16_t* src, uint16_t* dst,
   };
 
   u32x4 raw[COMPACT_AHEAD][2];
-  int rows[COMPACT_AHEAD];  // of the table, where a block's tokens turn differently
+  int rows[COMPACT_AHEAD] = {};  // of the table, where a block's tokens turn differently
   auto request = [&](int i, u32x4 (&r)[2], int& row) {  // (the last block again behind the end: nothing depends on a branch)
     const CompactEntry e = entries[min(i, chain.entry1 - 1)];
     const uint16_t* from = src + e.block * block_elems;

@@ -1823,6 +1823,7 @@ static pie_status pie_compact_kvpage_impl(pie_ctx* c, int32_t S, const int32_t* 
   const bool through_scratch = may_scratch && n_scratch > 0 && n_scratch * block_bytes <= COMPACT_SCRATCH &&
                                (wanted == 8192 ? 0.85 : 0.45) * (double)longest > 10.0 + (double)moved_blocks * (double)block_bytes / 4.5e6;
   if (!through_scratch) n_scratch = 0;
+  const std::vector<int32_t> written(tiles);
   bool mixed = false;  // some block's tokens turn differently
   // the sequence's chains of `of` destination blocks each, tiles[tile0 ..] on; a block with tokens for two chains is in both
   auto cut = [&](const CompactSeq& q, int of, int tile0) {
@@ -1906,11 +1907,9 @@ static pie_status pie_compact_kvpage_impl(pie_ctx* c, int32_t S, const int32_t* 
     plan.dst_layer = c->kv_layer_elems;
     HIP_TRY(c, launch_compact(plan, n_back, c->m.n_layers, c->m.n_kv_heads, D, c->stream));
   }
-  for (int s = 0; s < S; ++s) {
-    for (int j = 0; j * P < kept[s]; ++j)
-      for (int f = 0; f < F; ++f) c->page_mask[(size_t)dst_ids[dst_indptr[s] + j] * F + f] = 0xFFFFu;
-    out_kv_len[s] = kept[s];
-  }
+  for (int32_t block : written)  // (a page in front of them is as it was, and may be someone else's as well)
+    for (int f = 0; f < F; ++f) c->page_mask[(size_t)block / F * F + f] = 0xFFFFu;
+  for (int s = 0; s < S; ++s) out_kv_len[s] = kept[s];
   return PIE_OK;
 }
 

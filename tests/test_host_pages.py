@@ -272,6 +272,20 @@ def compact_plans(c):
     assert checked > 20 and scratched > 5, (checked, scratched)
 
 
+def compact_masks(c):
+    """Pages that are written become visible throughout; what stays keeps its mask, also where another sequence sees more of it."""
+    for P in (16, 32):
+        ctx = c.context(n_pages=64, m=SimpleNamespace(**{**vars(MODEL), "page_size": P}))
+        every = (1 << P) - 1
+        visible = lambda p: int(ctx.compact_kvpage([0, 1], [p], [P], dst_page_indptr=[0, 1], dst_page_ids=[40])[0])  # noqa: E731
+        ctx.mask_kvpage([1, 2, 3], [every & ~(1 << (P - 2)), every & ~2, every & ~4])
+        # 4 tokens of page 1 (its hidden one is behind them) stay; page 2 loses one, pages 3's first token moves into it
+        assert ctx.compact_kvpage([0, 1, 3], [1, 2, 3], [4, P + 1]).tolist() == [4, P]
+        assert visible(1) == P - 1 and visible(2) == P and visible(3) == P - 1
+        assert ctx.compact_kvpage([0, 1], [3], [P]).tolist() == [P - 1] and visible(3) == P
+        ctx.close()
+
+
 def raw(ctx, name, *args):
     return getattr(ctx.lib, name)(ctx.ctx, *args)
 
@@ -445,7 +459,7 @@ def beam_refusals(c):
     assert raw(p, "pie_get_next_beams", C.byref(search()), at(i32([0])), o, o, o) == INVALID
 
 
-CASES = {f.__name__: f for f in (fork_masks, compact_plans, page_refusals, captured, images_in_flight, no_memory, beam_refusals)}
+CASES = {f.__name__: f for f in (fork_masks, compact_masks, compact_plans, page_refusals, captured, images_in_flight, no_memory, beam_refusals)}
 
 if __name__ == "__main__":
     CASES[sys.argv[2]](Child(sys.argv[1]))
