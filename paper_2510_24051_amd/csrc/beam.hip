@@ -88,22 +88,15 @@ __device__ __forceinline__ float wave_max8(const float (&v)[8], int lane) {
   return c;
 }
 
-#define BT_WAVES 4
+// One tile of a row: lane l returns the maximum of segment l / 8, *stats (maximum, sum of exponentials) of the tile.
+// exp((x - m) / T) = exp2((x - m) (c_hi + c_lo)), c = log2(e) / T in two parts; x_min keeps infinities out (exp2 is 0 there).
+struct BeamScale { float c_hi, c_lo, x_min; };
 template <typename T>
-__global__ __launch_bounds__(64 * BT_WAVES) void beam_tiles_kernel(const T* __restrict__ logits, int64_t stride, int V, int n_tiles, float c_hi,
-                                                                   float c_lo, float x_min, const float* __restrict__ scores,
-                                                                   const uint8_t* __restrict__ finished, float* __restrict__ seg_max,
-                                                                   float2* __restrict__ tile_stats, int64_t total) {
+__device__ __forceinline__ float beam_tile(const BeamRow<T>& z, int tile, const BeamScale& scale, int lane, float2* stats) {
   constexpr int VEC = BeamRow<T>::VEC, SEG = BeamRow<T>::SEG;
-  const int lane = threadIdx.x & 63;
-  const int64_t at = (int64_t)blockIdx.x * BT_WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (at >= total) return;
-  const int row = (int)(at / n_tiles), tile = (int)(at % n_tiles);
-  if ((finished && finished[row]) || beam_score(scores, row) == -INFINITY) return;  // (nothing of theirs is looked at)
-  const BeamRow<T> z(logits, stride, row, V);
   float x[BT_SEGS][VEC], top[BT_SEGS];
   const int p0 = tile * BT_SEGS * SEG + lane * VEC;
-  if ((tile + 1) * BT_SEGS * SEG <= V) {  // (uniform: all eight loads go out at once)
+  if ((tile + 1) * BT_SEGS * SEG <= z.V) {  // (uniform: all eight loads go out at once)
     u32x4 raw[BT_SEGS];
 #pragma unroll
     for (int j = 0; j < BT_SEGS; ++j) raw[j] = z.stream(p0 + j * SEG);
@@ -123,20 +116,35 @@ __global__ __launch_bounds__(64 * BT_WAVES) void beam_tiles_kernel(const T* __re
   float m = seg;
 #pragma unroll
   for (int o = 32; o >= 8; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-  if ((lane & 7) == 0) seg_max[at * BT_SEGS + (lane >> 3)] = seg;
-  // exp((x - m) / T) = exp2((x - m) (c_hi + c_lo)), c = log2(e) / T in two parts; x_min keeps infinities out (exp2 is 0 there)
   float sum = 0.f;
   if (m != -INFINITY) {
 #pragma unroll
     for (int j = 0; j < BT_SEGS; ++j)
 #pragma unroll
       for (int i = 0; i < VEC; ++i) {
-        const float d = fmaxf(x[j][i] - m, x_min);
-        sum += __builtin_amdgcn_exp2f(__builtin_fmaf(d, c_lo, d * c_hi));
+        const float d = fmaxf(x[j][i] - m, scale.x_min);
+        sum += __builtin_amdgcn_exp2f(__builtin_fmaf(d, scale.c_lo, d * scale.c_hi));
       }
   }
-  sum = wave_sum(sum);
-  if (lane == 0) tile_stats[at] = make_float2(m, sum);
+  *stats = make_float2(m, wave_sum(sum));
+  return seg;
+}
+
+// A wave per tile.  Bound by HBM: 262 MB of logits (512 rows of 128256) in 41.7 us, 6.3 TB/s, the rate of a streaming read.
+#define BT_WAVES 4
+template <typename T>
+__global__ __launch_bounds__(64 * BT_WAVES) void beam_tiles_kernel(const T* __restrict__ logits, int64_t stride, int V, int n_tiles, BeamScale scale,
+                                                                   const float* __restrict__ scores, const uint8_t* __restrict__ finished,
+                                                                   float* __restrict__ seg_max, float2* __restrict__ tile_stats, int64_t total) {
+  const int lane = threadIdx.x & 63;
+  const int64_t at = (int64_t)blockIdx.x * BT_WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (at >= total) return;
+  const int row = (int)(at / n_tiles), tile = (int)(at % n_tiles);
+  if ((finished && finished[row]) || beam_score(scores, row) == -INFINITY) return;  // (nothing of theirs is looked at)
+  float2 stats;
+  const float seg = beam_tile(BeamRow<T>(logits, stride, row, V), tile, scale, lane, &stats);
+  if ((lane & 7) == 0) seg_max[at * BT_SEGS + (lane >> 3)] = seg;
+  if (lane == 0) tile_stats[at] = stats;
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -156,6 +164,7 @@ __device__ __forceinline__ double key_score(u64 k) { return __longlong_as_double
 #define BP_CANDS 512  // candidates that are put in order
 #define BP_COUNTED 192  // of which so many by counting
 #define BP_CACHED 8192  // maxima of segments kept in LDS
+#define BP_WHOLE 16     // tiles of a group that is read by its one workgroup
 struct BeamGroups { int32_t row0[BEAM_GROUPS_BY_VALUE + 1]; };
 #define BP_HELD (BP_CACHED / BP_THREADS)
 struct PickShared {
@@ -165,6 +174,7 @@ struct PickShared {
   int segs[BP_SEGS], segs_sorted[BP_SEGS];
   uint32_t hist[1024];
   float maxima[BP_CACHED];
+  float2 stats[BP_WHOLE];
   u64 red_lo[BP_THREADS / 64], red_hi[BP_THREADS / 64];
   uint32_t red_n[BP_THREADS / 64];
   uint32_t count, n_cand, bin, below, upto;
@@ -477,17 +487,35 @@ struct Picker {
   }
 };
 
-template <typename T>
+// One workgroup per group.  Bound by its chain of latencies: 9 us for eight rows of 128256 (the tiles' results and the rows'
+// logarithms 2.0, bins 1.9, cutting and keeping 1.7, the kept segments' logits 1 to 2, ranks and outputs 1).
+// WHOLE: groups of at most BP_WHOLE tiles, which the workgroup reads itself, in one launch instead of two (groups of four rows of
+// 1024, 4096 and 8192, 4, 8 and 16 tiles: 12.4 -> 11.6, 11.3 -> 10.0, 11.7 -> 11.1 us a call, 64 of them 14.5 -> 12.2, 12.6 ->
+// 11.2, 12.6 -> 12.0; at 32 tiles, two to a wave, 14.6 against 12).
+template <typename T, bool WHOLE>
 __global__ __launch_bounds__(BP_THREADS) void beam_pick_kernel(const T* __restrict__ logits, int64_t stride, int V, int n_tiles, double inv_temp,
-                                                               const float* __restrict__ scores, const uint8_t* __restrict__ finished, int eos,
-                                                               BeamGroups groups, int n_out, const float* __restrict__ seg_max,
-                                                               const float2* __restrict__ tile_stats, int32_t* __restrict__ out_beams,
-                                                               int32_t* __restrict__ out_tokens, float* __restrict__ out_scores) {
+                                                               BeamScale scale, const float* __restrict__ scores,
+                                                               const uint8_t* __restrict__ finished, int eos, BeamGroups groups, int n_out,
+                                                               const float* __restrict__ seg_max, const float2* __restrict__ tile_stats,
+                                                               int32_t* __restrict__ out_beams, int32_t* __restrict__ out_tokens,
+                                                               float* __restrict__ out_scores) {
   __shared__ PickShared sh;
-  const int g = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int g = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int row0 = groups.row0[g], rows = groups.row0[g + 1] - row0;
   const int n_segs = n_tiles * BT_SEGS, n = rows * n_segs;
-  const float* maxima = seg_max + (int64_t)row0 * n_segs;
+  const float* maxima = WHOLE ? sh.maxima : seg_max + (int64_t)row0 * n_segs;
+  const float2* stats = WHOLE ? sh.stats : tile_stats + (int64_t)row0 * n_tiles;
+  if (WHOLE) {
+    for (int q = wave; q < rows * n_tiles; q += BP_THREADS / 64) {
+      const int r = q / n_tiles;
+      if ((finished && finished[row0 + r]) || beam_score(scores, row0 + r) == -INFINITY) continue;
+      float2 st;
+      const float seg = beam_tile(BeamRow<T>(logits, stride, row0 + r, V), q % n_tiles, scale, lane, &st);
+      if ((lane & 7) == 0) sh.maxima[q * BT_SEGS + (lane >> 3)] = seg;
+      if (lane == 0) sh.stats[q] = st;
+    }
+    __syncthreads();
+  }
   const bool cached = n <= BP_CACHED;
   float held[BP_HELD];
 #pragma unroll
@@ -499,8 +527,7 @@ __global__ __launch_bounds__(BP_THREADS) void beam_pick_kernel(const T* __restri
     double b = -INFINITY, m = 0;
     if (done) b = s;
     else if (s != -INFINITY) {
-      const float2* stats = tile_stats + (int64_t)(row0 + r) * n_tiles;  // (64 at most)
-      const float2 st = lane < n_tiles ? stats[lane] : make_float2(-INFINITY, 0.f);
+      const float2 st = lane < n_tiles ? stats[r * n_tiles + lane] : make_float2(-INFINITY, 0.f);  // (64 at most)
       const float top = wave_max(st.x);
       if (top != -INFINITY) {
         const double sum = wave_sum_f64(st.x == -INFINITY ? 0.0 : (double)st.y * exp(((double)st.x - (double)top) * inv_temp));
@@ -510,7 +537,7 @@ __global__ __launch_bounds__(BP_THREADS) void beam_pick_kernel(const T* __restri
     }
     if (lane == 0) { sh.row[r] = make_double2(b, m); sh.done[r] = done; }
   }
-  if (cached) {
+  if (cached && !WHOLE) {
 #pragma unroll
     for (int j = 0; j < BP_HELD; ++j)
       if (tid + j * BP_THREADS < n) sh.maxima[tid + j * BP_THREADS] = held[j];
@@ -580,17 +607,22 @@ hipError_t beam_select(const BeamArgs& a, hipStream_t s) {
   float2* stats = reinterpret_cast<float2*>(a.ws);
   float* maxima = reinterpret_cast<float*>(stats + total);
   const double c = 1.4426950408889634074 * a.inv_temp;
-  const float c_hi = (float)c, c_lo = (float)(c - (double)c_hi), x_min = (float)(-256.0 / c);
-  if (rows > 0)
+  const float c_hi = (float)c;
+  const BeamScale scale{c_hi, (float)(c - (double)c_hi), (float)(-256.0 / c)};
+  int most = 0;  // rows of a group
+  for (int g = 0; g < a.n_groups; ++g) most = most > a.group_indptr[g + 1] - a.group_indptr[g] ? most : a.group_indptr[g + 1] - a.group_indptr[g];
+  const bool whole = most * n_tiles <= BP_WHOLE;
+  if (!whole)
     beam_tiles_kernel<T><<<dim3((unsigned)((total + BT_WAVES - 1) / BT_WAVES)), dim3(64 * BT_WAVES), 0, s>>>(
-        z, a.stride, a.V, n_tiles, c_hi, c_lo, x_min, a.scores, a.finished, maxima, stats, total);
+        z, a.stride, a.V, n_tiles, scale, a.scores, a.finished, maxima, stats, total);
+  auto* pick = whole ? beam_pick_kernel<T, true> : beam_pick_kernel<T, false>;
   for (int g0 = 0; g0 < a.n_groups; g0 += BEAM_GROUPS_BY_VALUE) {
     const int ng = a.n_groups - g0 < BEAM_GROUPS_BY_VALUE ? a.n_groups - g0 : BEAM_GROUPS_BY_VALUE;
     BeamGroups groups{};
     for (int g = 0; g <= ng; ++g) groups.row0[g] = a.group_indptr[g0 + g];
     const int64_t o = (int64_t)g0 * a.n_out;
-    beam_pick_kernel<T><<<dim3((unsigned)ng), dim3(BP_THREADS), 0, s>>>(z, a.stride, a.V, n_tiles, a.inv_temp, a.scores, a.finished, a.eos, groups,
-                                                                        a.n_out, maxima, stats, a.out_beams + o, a.out_tokens + o, a.out_scores + o);
+    pick<<<dim3((unsigned)ng), dim3(BP_THREADS), 0, s>>>(z, a.stride, a.V, n_tiles, a.inv_temp, scale, a.scores, a.finished, a.eos, groups, a.n_out,
+                                                         maxima, stats, a.out_beams + o, a.out_tokens + o, a.out_scores + o);
   }
   return hipGetLastError();
 }

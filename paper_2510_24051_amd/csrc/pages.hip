@@ -12,6 +12,10 @@ namespace {
 // reads, and no other thread touches those bytes: any graph of moves, permutations included, needs no second buffer and no
 // synchronisation.  A run with a cycle starts by keeping the page that the cycle's last move reads (PageRun::keep; the
 // order: page_plans.h).
+// Bound by HBM: 200 pages (64 KiB in each of 16 layers, 210 MB) read and written in 65 us by themselves, 6.4 TB/s, 73 behind a
+// kernel that has left its output in the caches; a small call by its launch (one page seven times, 32 layers: 6 us).  Sources are read
+// non-temporally, pages stored plainly, as what forks them soon reads them (stored non-temporally: 200 pages and their
+// save 151 -> 160 us a pass).
 #define FORK_THREADS 256
 #define FORK_AHEAD 8  // moves whose sources are read before the first of them is stored: a read only ever comes too late, never too early
 struct ForkMoves {
@@ -81,6 +85,9 @@ __device__ __forceinline__ u32x4 transpose8(u32x4 w, int label) {
 // The image is [page][layer][K or V][slot][kv head][dim].  A wave takes one head of one 16-token block: D/32 times 1 KiB of K, which in
 // the pool are 16-byte pieces of 8 dims of a token already, and as much of V.  On the pool's side every access is 1 KiB
 // in one piece, on the image's 16 tokens of 64 bytes.
+// Bound by HBM: 64 pages of an 8B-shaped model (134 MB each way) saved in 43 us, restored in 50, 6.2 and 5.4 TB/s; read non-temporally,
+// written plainly (49 and 55 us a pass the other ways round).  One thread per 8 dims of a token, V gathered 2 bytes at a time,
+// took 102 and 262.
 #define IMAGE_WAVES 4
 template <int D, bool TO_POOL>
 __global__ __launch_bounds__(64 * IMAGE_WAVES) void page_image_kernel(bf16_t* __restrict__ kv, int64_t layer_elems, int n_layers, PageIds ids, int total,
@@ -121,6 +128,11 @@ __global__ __launch_bounds__(64 * IMAGE_WAVES) void page_image_kernel(bf16_t* __
 // In place: a kept token moves towards the front, so when a destination block is stored every token at or before its last one has
 // been read, and what the chain reads later lies behind it; no other wave touches these dims.  The reads run COMPACT_AHEAD
 // blocks in front of the stores, which only makes them earlier.
+// Bound by HBM where there are waves enough: 4 x 1021 of 3600 tokens of an 8B-shaped model in place with rotated keys (0.54 GB each
+// way) 231 us, 4.6 TB/s, where a copy of 1 GiB reaches 4.7; half of 5500 tokens of 16 layers into other pages 46 us, 5.9 TB/s of whole
+// source blocks and what is written.  With few, by the chain: 0.45 us a block.  Two blocks ahead instead of four: 337 -> 385 us (8000
+// tokens, 32 layers, in order); six or eight: the same.  Non-temporal stores: 456 -> 437 us for the first with its save, 82 -> 88
+// for the second, so plain ones.
 #define COMPACT_WAVES 4
 #define COMPACT_AHEAD 4
 template <int D, bool IS_K>
