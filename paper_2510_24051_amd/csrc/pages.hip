@@ -129,7 +129,7 @@ __global__ __launch_bounds__(64 * IMAGE_WAVES) void page_image_kernel(bf16_t* __
 // been read, and what the chain reads later lies behind it; no other wave touches these dims.  The reads run COMPACT_AHEAD
 // blocks in front of the stores, which only makes them earlier.
 // Bound by HBM where there are waves enough: 4 x 1021 of 3600 tokens of an 8B-shaped model in place with rotated keys (0.54 GB each
-// way) 231 us, 4.6 TB/s, where a copy of 1 GiB reaches 4.7; half of 5500 tokens of 16 layers into other pages 46 us, 5.9 TB/s of whole
+// way) 231 us, 4.6 TB/s, where a copy of 1 GiB reaches 4.7; half of 4830 tokens of 16 layers into other pages 46 us, 5.5 TB/s of whole
 // source blocks and what is written.  With few, by the chain: 0.45 us a block.  Two blocks ahead instead of four: 337 -> 385 us (8000
 // tokens, 32 layers, in order); six or eight: the same.  Non-temporal stores: 456 -> 437 us for the first with its save, 82 -> 88
 // for the second, so plain ones.
