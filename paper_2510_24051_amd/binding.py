@@ -145,9 +145,19 @@ def _ptr(a: Optional[np.ndarray]):
     return None if a is None else a.ctypes.data_as(C.c_void_p)
 
 
+_NOTHING = C.c_int32(0)  # where an empty array is said to be: some pointers must not be null
+
+
 def _at(a):
-    """Address of an array that the caller keeps until the call has returned (_ptr keeps it itself and takes longer)."""
-    return None if a is None else a.__array_interface__["data"][0]
+    """Address of an array that the caller keeps until the call has returned (_ptr keeps it itself and takes four times as long)."""
+    if a is None:
+        return None
+    if a.size == 0:
+        return C.addressof(_NOTHING)
+    try:
+        return C.addressof(C.c_char.from_buffer(a))
+    except TypeError:  # a read-only array
+        return a.__array_interface__["data"][0]
 
 
 class PieBatch:
@@ -348,9 +358,8 @@ class Pie:
 
     def _image(self, page_ids, image: torch.Tensor) -> np.ndarray:
         ids, m = _i32(page_ids), self.model
-        if image.dtype != torch.bfloat16 or image.device != self._device() or not image.is_contiguous() or image.dim() != 6 or \
-                image.shape[0] != len(ids) or tuple(image.shape[2:]) != (2, m.page_size, m.n_kv_heads, m.head_dim) or \
-                image.shape[1] != self.n_layers:
+        if tuple(image.shape) != (len(ids), self.n_layers, 2, m.page_size, m.n_kv_heads, m.head_dim) or image.dtype != torch.bfloat16 or \
+                image.device != self._device() or not image.is_contiguous():
             raise ValueError("an image of pages is a contiguous bfloat16 device tensor [pages, layers, 2, page_size, kv heads, head_dim]")
         return ids
 

@@ -165,7 +165,8 @@ __device__ __forceinline__ double key_score(u64 k) { return __longlong_as_double
 #define BP_COUNTED 192  // of which so many by counting
 #define BP_CACHED 8192  // maxima of segments kept in LDS
 #define BP_WHOLE 16     // tiles of a group that is read by its one workgroup
-struct BeamGroups { int32_t row0[BEAM_GROUPS_BY_VALUE + 1]; };
+template <int N>
+struct BeamGroups { int32_t row0[N + 1]; };  // (a short list has a small block: calls back to back 3.4 us of the host's time each, 6.4 with the large one)
 #define BP_HELD (BP_CACHED / BP_THREADS)
 struct PickShared {
   double2 row[BEAM_MAX_ROWS];  // (b, m): score = b + (z - m) / T; b = -inf: no candidates
@@ -492,10 +493,10 @@ struct Picker {
 // WHOLE: groups of at most BP_WHOLE tiles, which the workgroup reads itself, in one launch instead of two (groups of four rows of
 // 1024, 4096 and 8192, 4, 8 and 16 tiles: 12.4 -> 11.6, 11.3 -> 10.0, 11.7 -> 11.1 us a call, 64 of them 14.5 -> 12.2, 12.6 ->
 // 11.2, 12.6 -> 12.0; at 32 tiles, two to a wave, 14.6 against 12).
-template <typename T, bool WHOLE>
+template <typename T, bool WHOLE, int N>
 __global__ __launch_bounds__(BP_THREADS) void beam_pick_kernel(const T* __restrict__ logits, int64_t stride, int V, int n_tiles, double inv_temp,
                                                                BeamScale scale, const float* __restrict__ scores,
-                                                               const uint8_t* __restrict__ finished, int eos, BeamGroups groups, int n_out,
+                                                               const uint8_t* __restrict__ finished, int eos, BeamGroups<N> groups, int n_out,
                                                                const float* __restrict__ seg_max, const float2* __restrict__ tile_stats,
                                                                int32_t* __restrict__ out_beams, int32_t* __restrict__ out_tokens,
                                                                float* __restrict__ out_scores) {
@@ -615,14 +616,18 @@ hipError_t beam_select(const BeamArgs& a, hipStream_t s) {
   if (!whole)
     beam_tiles_kernel<T><<<dim3((unsigned)((total + BT_WAVES - 1) / BT_WAVES)), dim3(64 * BT_WAVES), 0, s>>>(
         z, a.stride, a.V, n_tiles, scale, a.scores, a.finished, maxima, stats, total);
-  auto* pick = whole ? beam_pick_kernel<T, true> : beam_pick_kernel<T, false>;
   for (int g0 = 0; g0 < a.n_groups; g0 += BEAM_GROUPS_BY_VALUE) {
     const int ng = a.n_groups - g0 < BEAM_GROUPS_BY_VALUE ? a.n_groups - g0 : BEAM_GROUPS_BY_VALUE;
-    BeamGroups groups{};
-    for (int g = 0; g <= ng; ++g) groups.row0[g] = a.group_indptr[g0 + g];
     const int64_t o = (int64_t)g0 * a.n_out;
-    pick<<<dim3((unsigned)ng), dim3(BP_THREADS), 0, s>>>(z, a.stride, a.V, n_tiles, a.inv_temp, scale, a.scores, a.finished, a.eos, groups, a.n_out,
-                                                         maxima, stats, a.out_beams + o, a.out_tokens + o, a.out_scores + o);
+    auto go = [&](auto groups) {
+      constexpr int N = sizeof(groups) / sizeof(int32_t) - 1;
+      for (int g = 0; g <= ng; ++g) groups.row0[g] = a.group_indptr[g0 + g];
+      auto* pick = whole ? beam_pick_kernel<T, true, N> : beam_pick_kernel<T, false, N>;
+      pick<<<dim3((unsigned)ng), dim3(BP_THREADS), 0, s>>>(z, a.stride, a.V, n_tiles, a.inv_temp, scale, a.scores, a.finished, a.eos, groups, a.n_out,
+                                                           maxima, stats, a.out_beams + o, a.out_tokens + o, a.out_scores + o);
+    };
+    if (ng <= 16) go(BeamGroups<16>{});
+    else go(BeamGroups<BEAM_GROUPS_BY_VALUE>{});
   }
   return hipGetLastError();
 }

@@ -18,12 +18,14 @@ namespace {
 // save 151 -> 160 us a pass).
 #define FORK_THREADS 256
 #define FORK_AHEAD 8  // moves whose sources are read before the first of them is stored: a read only ever comes too late, never too early
+template <int N>
 struct ForkMoves {
-  PageMove moves[FORK_MOVES];
-  PageRun runs[FORK_MOVES];
+  PageMove moves[N];
+  PageRun runs[N];
 };
+template <int N>
 __global__ __launch_bounds__(FORK_THREADS) void fork_kernel(unsigned char* __restrict__ kv, int64_t layer_bytes, int64_t page_bytes, int slices,
-                                                            ForkMoves plan) {
+                                                            ForkMoves<N> plan) {
   const int run = blockIdx.x / slices, slice = blockIdx.x % slices;
   unsigned char* base = kv + (int64_t)blockIdx.y * layer_bytes + ((int64_t)slice * FORK_THREADS + threadIdx.x) * 16;
   const PageRun r = plan.runs[run];
@@ -56,7 +58,11 @@ __global__ __launch_bounds__(FORK_THREADS) void fork_kernel(unsigned char* __res
 // ---------------------------------------------------------------------------------------------
 // save and restore
 // ---------------------------------------------------------------------------------------------
-struct PageIds { int32_t v[IDS_BY_VALUE]; };
+// (Kernel arguments cost the host time, here and below, so short lists have a small block of their own.  Calls back to back, the host's
+// time for each with the large block and with the small one: two pages saved 3.35 and 3.20 us, a fork with the call's checks 4.7 and 4.4,
+// a fork after an append 15.1 and 11.1, a short compaction's plan 13.1 and 12.9.)
+template <int N>
+struct PageIds { int32_t v[N]; };
 
 // The pool keeps V as 8 tokens of one dim next to each other, tokens' rows have 8 dims of one token next to each other: eight lanes
 // turn the one into the other among themselves.  Lane i of eight stands for row label(i) before and after; with
@@ -89,8 +95,8 @@ __device__ __forceinline__ u32x4 transpose8(u32x4 w, int label) {
 // written plainly (49 and 55 us a pass the other ways round).  One thread per 8 dims of a token, V gathered 2 bytes at a time,
 // took 102 and 262.
 #define IMAGE_WAVES 4
-template <int D, bool TO_POOL>
-__global__ __launch_bounds__(64 * IMAGE_WAVES) void page_image_kernel(bf16_t* __restrict__ kv, int64_t layer_elems, int n_layers, PageIds ids, int total,
+template <int D, bool TO_POOL, int IDS>
+__global__ __launch_bounds__(64 * IMAGE_WAVES) void page_image_kernel(bf16_t* __restrict__ kv, int64_t layer_elems, int n_layers, PageIds<IDS> ids, int total,
                                                                       int F, int Hkv, uint16_t* __restrict__ image) {
   constexpr int N = D / 32;
   const int lane = threadIdx.x & 63, layer = blockIdx.y;
@@ -261,8 +267,10 @@ __global__ __launch_bounds__(64 * COMPACT_WAVES) void compact_kernel(const bf16_
 }
 
 // A small plan, as kernel arguments, into device memory, and the angles of its shifts (64 bits, rounded once: a shift may be long).
-struct PlanBytes { uint32_t w[PLAN_BY_VALUE / 4]; };
-__global__ void put_plan_kernel(PlanBytes plan, int words, uint32_t* __restrict__ dev, int turn0, int n_turns, const double* __restrict__ inv_freq,
+template <int N>
+struct PlanBytes { uint32_t w[N]; };
+template <int N>
+__global__ void put_plan_kernel(PlanBytes<N> plan, int words, uint32_t* __restrict__ dev, int turn0, int n_turns, const double* __restrict__ inv_freq,
                                 int D, float* __restrict__ angles) {
   const int idx = blockIdx.x * blockDim.x + threadIdx.x, half = D / 2;
   if (idx < words) dev[idx] = plan.w[idx];
@@ -280,11 +288,14 @@ hipError_t launch_fork(bf16_t* kv, size_t layer_elems, int n_layers, size_t page
   if (n_moves > FORK_MOVES || n_runs > FORK_MOVES) return hipErrorInvalidValue;
   if (n_runs <= 0) return hipSuccess;
   const int slices = (int)(page_elems * sizeof(bf16_t) / (FORK_THREADS * 16));  // (a page has a multiple of 4 KiB in a layer)
-  ForkMoves plan;
-  for (int i = 0; i < n_moves; ++i) plan.moves[i] = moves[i];
-  for (int i = 0; i < n_runs; ++i) plan.runs[i] = runs[i];
-  fork_kernel<<<dim3((unsigned)(n_runs * slices), (unsigned)n_layers), dim3(FORK_THREADS), 0, s>>>(
-      reinterpret_cast<unsigned char*>(kv), layer_elems * 2, page_elems * 2, slices, plan);
+  auto go = [&](auto plan) {
+    for (int i = 0; i < n_moves; ++i) plan.moves[i] = moves[i];
+    for (int i = 0; i < n_runs; ++i) plan.runs[i] = runs[i];
+    fork_kernel<<<dim3((unsigned)(n_runs * slices), (unsigned)n_layers), dim3(FORK_THREADS), 0, s>>>(
+        reinterpret_cast<unsigned char*>(kv), layer_elems * 2, page_elems * 2, slices, plan);
+  };
+  if (n_moves <= 16) go(ForkMoves<16>());  // (a run has a move at least)
+  else go(ForkMoves<FORK_MOVES>());
   return hipGetLastError();
 }
 
@@ -293,15 +304,18 @@ hipError_t launch_page_image(bf16_t* kv, size_t layer_elems, int n_layers, const
   const int64_t page_image = (int64_t)n_layers * 2 * F * PAGE * Hkv * D;
   for (int p0 = 0; p0 < n; p0 += IDS_BY_VALUE) {
     const int m = n - p0 < IDS_BY_VALUE ? n - p0 : IDS_BY_VALUE;
-    PageIds ids;
-    for (int i = 0; i < m; ++i) ids.v[i] = host_ids[p0 + i];
     const int total = m * F * Hkv;
     const dim3 grid((unsigned)((total + IMAGE_WAVES - 1) / IMAGE_WAVES), (unsigned)n_layers), block(64 * IMAGE_WAVES);
     uint16_t* img = reinterpret_cast<uint16_t*>(image) + p0 * page_image;
-    if (D == 128 && to_pool) page_image_kernel<128, true><<<grid, block, 0, s>>>(kv, layer_elems, n_layers, ids, total, F, Hkv, img);
-    else if (D == 128) page_image_kernel<128, false><<<grid, block, 0, s>>>(kv, layer_elems, n_layers, ids, total, F, Hkv, img);
-    else if (to_pool) page_image_kernel<64, true><<<grid, block, 0, s>>>(kv, layer_elems, n_layers, ids, total, F, Hkv, img);
-    else page_image_kernel<64, false><<<grid, block, 0, s>>>(kv, layer_elems, n_layers, ids, total, F, Hkv, img);
+    auto go = [&](auto ids) {
+      constexpr int N = sizeof(ids) / sizeof(int32_t);
+      for (int i = 0; i < m; ++i) ids.v[i] = host_ids[p0 + i];
+      auto* kernel = D == 128 ? (to_pool ? page_image_kernel<128, true, N> : page_image_kernel<128, false, N>)
+                              : (to_pool ? page_image_kernel<64, true, N> : page_image_kernel<64, false, N>);
+      kernel<<<grid, block, 0, s>>>(kv, layer_elems, n_layers, ids, total, F, Hkv, img);
+    };
+    if (m <= 64) go(PageIds<64>());
+    else go(PageIds<IDS_BY_VALUE>());
   }
   return hipGetLastError();
 }
@@ -309,11 +323,14 @@ hipError_t launch_page_image(bf16_t* kv, size_t layer_elems, int n_layers, const
 hipError_t launch_put_plan(const unsigned char* plan, size_t size, unsigned char* dev, size_t turns, int n_turns, const double* inv_freq, int D,
                            float* angles, hipStream_t s) {
   if (size > PLAN_BY_VALUE || size % 4 || turns % 4 || turns + (size_t)n_turns * 4 > size) return hipErrorInvalidValue;
-  PlanBytes bytes;
-  __builtin_memcpy(bytes.w, plan, size);
   const int words = (int)(size / 4), threads = words > n_turns * (D / 2) ? words : n_turns * (D / 2);
-  put_plan_kernel<<<dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s>>>(bytes, words, reinterpret_cast<uint32_t*>(dev), (int)(turns / 4), n_turns,
-                                                                                inv_freq, D, angles);
+  auto go = [&](auto bytes) {
+    __builtin_memcpy(bytes.w, plan, size);
+    put_plan_kernel<<<dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s>>>(bytes, words, reinterpret_cast<uint32_t*>(dev), (int)(turns / 4), n_turns,
+                                                                                  inv_freq, D, angles);
+  };
+  if (words <= 192) go(PlanBytes<192>());
+  else go(PlanBytes<PLAN_BY_VALUE / 4>());
   return hipGetLastError();
 }
 
