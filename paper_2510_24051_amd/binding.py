@@ -251,9 +251,9 @@ class Pie:
             raise PieError(st, self.lib.pie_last_error(self.ctx).decode())
 
     def _device(self) -> torch.device:
-        """The context's device with its number, as its tensors name it."""
-        if self.device.index is None:
-            self.device = torch.device(self.device.type, torch.cuda.current_device())
+        """The context's device (a number belongs to it), as its tensors name it."""
+        if self.device is None:
+            raise PieError(-1, "the context only plans batches (pie_create_planner)")
         return self.device
 
     def _dev_bf16(self, bits) -> torch.Tensor:
