@@ -265,3 +265,10 @@ def test_wrong_tensors_are_refused(ctx):
         args.update(change)
         with pytest.raises(ValueError):
             ctx.beam_select_async(**args)
+
+
+@pytest.mark.parametrize("V", [300, 40000])
+@pytest.mark.parametrize("n", [15, 16, 17, 255, 256, 257])
+def test_as_many_groups_as_a_launch_names(ctx, V, n):
+    indptr = np.concatenate([[0], np.cumsum(np.arange(n) % 2 if n > 20 else np.full(n, 2))])
+    check(ctx, logits(int(indptr[-1]), V, torch.bfloat16, n), indptr, 3, np.random.default_rng(n).standard_normal(int(indptr[-1])))

@@ -354,3 +354,25 @@ def test_compact_few_waves_in_place(D, Hkv, P, layers, form, shift):
     check_compacted(b)
     b2, _ = compact_case(D, Hkv, P, layers, [5003, 40, 1601, 3200], FORMS[form], False, shift, 32 + D)
     check_compacted(b2)
+
+
+@pytest.mark.parametrize("n", [1, 15, 16, 17, 63, 64, 65, 160])
+def test_lists_about_as_long_as_an_argument_block(n):
+    b = Both(model(64, 1, 16), 2 * n + 1, 2, n)
+    src, dst = np.arange(n), np.arange(2 * n, n, -1)
+    b.ctx.fork_kvpage(src, dst)
+    O.fork_kvpage(b.kvs, src, dst)
+    b.same("one to one")
+    b.ctx.fork_kvpage(np.roll(dst, 1), dst)
+    O.fork_kvpage(b.kvs, np.roll(dst, 1), dst)
+    b.same("turned")
+    image = b.save(dst)
+    assert np.array_equal(image, O.save_kvpage(b.kvs, dst))
+    b.restore(src, image)
+    for layer, kv in enumerate(b.kvs):
+        kv.k_bits[src], kv.v_bits[src] = image[:, layer, 0], image[:, layer, 1]
+    b.same("restored")
+    lens = np.full(n, 13)
+    assert (b.ctx.compact_kvpage(np.arange(n + 1), src, lens, dst_page_indptr=np.arange(n + 1), dst_page_ids=dst) == 13).all()
+    O.compact_kvpage(b.kvs, np.arange(n + 1), src, lens, THETA, dst_page_indptr=np.arange(n + 1), dst_page_ids=dst)
+    b.same("compacted")
