@@ -321,6 +321,9 @@ struct Picker {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) best = fmax(best, __shfl_xor(best, o));
     if (best == -INFINITY) return 0;  // (uniform over the workgroup)
+    // One step of a 64-bit score at 2^40 is 2^-12, a thirtieth of the narrowest bin.  Far beyond, scores swallow what tells their
+    // logits apart, and candidates that are bins apart here are equal there and go by beam and token.
+    if (fabs(best) > 1099511627776.0) return -1;
     const float c = (float)inv_temp;
     // (behind, m): a row's best score behind the group's and its largest logit; z is far_bin(behind + (m - z) c) away, -inf infinitely
     auto row_at = [&](int r) { return make_float2((float)(best - sh.row[r].x), (float)sh.row[r].y); };
