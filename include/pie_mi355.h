@@ -292,7 +292,9 @@ pie_status pie_get_next_dist_static(pie_ctx* ctx, const int32_t* embed_ids, int3
  * logarithm of its probability so far; NULL: all 0), and token v continues it with
  *     score(r, v) = scores[r] + z[r][v] / temperature - log sum_u exp(z[r][u] / temperature).
  * Of every search the n_out (at most 256) candidates of largest score are returned by descending score, equal scores by
- * ascending beam, then ascending token; scores are compared in 64 bits and stored in 32.
+ * ascending beam, then ascending token; scores are compared in 64 bits and stored in 32.  A row's logarithm sums exponentials
+ * of 32 bits, in 64: it is off by 2.4e-6 at most, a few 1e-8 on a language model's logits, and beams closer than that may stand in either
+ * order (a beam's own candidates and those of beams with equal logits never do).
  *   - a logit of -inf or NaN is no candidate and adds nothing to the sum (a grammar's mask); +inf counts as the largest finite
  *     value of the logits' type; the lowest finite value is a logit like any other
  *   - a beam whose score is -inf or NaN, or whose logits are all -inf or NaN, has no candidates; a score of +inf counts as the

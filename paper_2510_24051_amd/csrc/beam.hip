@@ -4,8 +4,10 @@
 // largest finite value of its type, a row with s_r = -inf or NaN has no candidates, a finished row has exactly one.
 //
 // Scores are compared in 64 bits: candidates of different beams lie within 1e-3 of one another in every step, and one unit in
-// the last place of a 32-bit score (1e-6 at 10) reorders them now and then.  The exponentials are taken and summed in 32 bits (a few
-// dozen terms), their sums in 64: 1e-8 on the logarithm.
+// the last place of a 32-bit score (1e-6 at 10) reorders them now and then.  The exponentials are taken in 32 bits, each off
+// by its argument's three roundings and a step, and summed in 64 (in 32, small terms beside a large one are lost: 1e-7 to 1e-6 on the
+// logarithm of a peaked row).  2.4e-6 on the logarithm at most, a few 1e-8 on a language model's rows, 1e-9 where one token has nearly all
+// of the probability.  512 rows of 128256 with sums in 64 bits and in 32: fp32 53.8 and 53.1 us a call, 16 bits 41.7 and 39.5.
 //
 // Two kernels.  beam_tiles reads every logit once and leaves, per segment (what a wave loads at once), the largest, and per tile of
 // eight segments the largest and the sum of exponentials.  beam_pick, one workgroup per group, turns the segments' maxima into scores
@@ -91,8 +93,9 @@ __device__ __forceinline__ float wave_max8(const float (&v)[8], int lane) {
 // One tile of a row: lane l returns the maximum of segment l / 8, *stats (maximum, sum of exponentials) of the tile.
 // exp((x - m) / T) = exp2((x - m) (c_hi + c_lo)), c = log2(e) / T in two parts; x_min keeps infinities out (exp2 is 0 there).
 struct BeamScale { float c_hi, c_lo, x_min; };
+struct __attribute__((aligned(16))) TileStats { double sum; float m; };
 template <typename T>
-__device__ __forceinline__ float beam_tile(const BeamRow<T>& z, int tile, const BeamScale& scale, int lane, float2* stats) {
+__device__ __forceinline__ float beam_tile(const BeamRow<T>& z, int tile, const BeamScale& scale, int lane, TileStats* stats) {
   constexpr int VEC = BeamRow<T>::VEC, SEG = BeamRow<T>::SEG;
   float x[BT_SEGS][VEC], top[BT_SEGS];
   const int p0 = tile * BT_SEGS * SEG + lane * VEC;
@@ -116,17 +119,17 @@ __device__ __forceinline__ float beam_tile(const BeamRow<T>& z, int tile, const 
   float m = seg;
 #pragma unroll
   for (int o = 32; o >= 8; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-  float sum = 0.f;
+  double sum = 0;
   if (m != -INFINITY) {
 #pragma unroll
     for (int j = 0; j < BT_SEGS; ++j)
 #pragma unroll
       for (int i = 0; i < VEC; ++i) {
         const float d = fmaxf(x[j][i] - m, scale.x_min);
-        sum += __builtin_amdgcn_exp2f(__builtin_fmaf(d, scale.c_lo, d * scale.c_hi));
+        sum += (double)__builtin_amdgcn_exp2f(__builtin_fmaf(d, scale.c_lo, d * scale.c_hi));
       }
   }
-  *stats = make_float2(m, wave_sum(sum));
+  *stats = TileStats{wave_sum_f64(sum), m};
   return seg;
 }
 
@@ -135,13 +138,13 @@ __device__ __forceinline__ float beam_tile(const BeamRow<T>& z, int tile, const 
 template <typename T>
 __global__ __launch_bounds__(64 * BT_WAVES) void beam_tiles_kernel(const T* __restrict__ logits, int64_t stride, int V, int n_tiles, BeamScale scale,
                                                                    const float* __restrict__ scores, const uint8_t* __restrict__ finished,
-                                                                   float* __restrict__ seg_max, float2* __restrict__ tile_stats, int64_t total) {
+                                                                   float* __restrict__ seg_max, TileStats* __restrict__ tile_stats, int64_t total) {
   const int lane = threadIdx.x & 63;
   const int64_t at = (int64_t)blockIdx.x * BT_WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (at >= total) return;
   const int row = (int)(at / n_tiles), tile = (int)(at % n_tiles);
   if ((finished && finished[row]) || beam_score(scores, row) == -INFINITY) return;  // (nothing of theirs is looked at)
-  float2 stats;
+  TileStats stats;
   const float seg = beam_tile(BeamRow<T>(logits, stride, row, V), tile, scale, lane, &stats);
   if ((lane & 7) == 0) seg_max[at * BT_SEGS + (lane >> 3)] = seg;
   if (lane == 0) tile_stats[at] = stats;
@@ -175,7 +178,7 @@ struct PickShared {
   int segs[BP_SEGS], segs_sorted[BP_SEGS];
   uint32_t hist[1024];
   float maxima[BP_CACHED];
-  float2 stats[BP_WHOLE];
+  TileStats stats[BP_WHOLE];
   u64 red_lo[BP_THREADS / 64], red_hi[BP_THREADS / 64];
   uint32_t red_n[BP_THREADS / 64];
   uint32_t count, n_cand, bin, below, upto;
@@ -500,7 +503,7 @@ template <typename T, bool WHOLE, int N>
 __global__ __launch_bounds__(BP_THREADS) void beam_pick_kernel(const T* __restrict__ logits, int64_t stride, int V, int n_tiles, double inv_temp,
                                                                BeamScale scale, const float* __restrict__ scores,
                                                                const uint8_t* __restrict__ finished, int eos, BeamGroups<N> groups, int n_out,
-                                                               const float* __restrict__ seg_max, const float2* __restrict__ tile_stats,
+                                                               const float* __restrict__ seg_max, const TileStats* __restrict__ tile_stats,
                                                                int32_t* __restrict__ out_beams, int32_t* __restrict__ out_tokens,
                                                                float* __restrict__ out_scores) {
   __shared__ PickShared sh;
@@ -508,12 +511,12 @@ __global__ __launch_bounds__(BP_THREADS) void beam_pick_kernel(const T* __restri
   const int row0 = groups.row0[g], rows = groups.row0[g + 1] - row0;
   const int n_segs = n_tiles * BT_SEGS, n = rows * n_segs;
   const float* maxima = WHOLE ? sh.maxima : seg_max + (int64_t)row0 * n_segs;
-  const float2* stats = WHOLE ? sh.stats : tile_stats + (int64_t)row0 * n_tiles;
+  const TileStats* stats = WHOLE ? sh.stats : tile_stats + (int64_t)row0 * n_tiles;
   if (WHOLE) {
     for (int q = wave; q < rows * n_tiles; q += BP_THREADS / 64) {
       const int r = q / n_tiles;
       if ((finished && finished[row0 + r]) || beam_score(scores, row0 + r) == -INFINITY) continue;
-      float2 st;
+      TileStats st;
       const float seg = beam_tile(BeamRow<T>(logits, stride, row0 + r, V), q % n_tiles, scale, lane, &st);
       if ((lane & 7) == 0) sh.maxima[q * BT_SEGS + (lane >> 3)] = seg;
       if (lane == 0) sh.stats[q] = st;
@@ -531,10 +534,10 @@ __global__ __launch_bounds__(BP_THREADS) void beam_pick_kernel(const T* __restri
     double b = -INFINITY, m = 0;
     if (done) b = s;
     else if (s != -INFINITY) {
-      const float2 st = lane < n_tiles ? stats[r * n_tiles + lane] : make_float2(-INFINITY, 0.f);  // (64 at most)
-      const float top = wave_max(st.x);
+      const TileStats st = lane < n_tiles ? stats[r * n_tiles + lane] : TileStats{0, -INFINITY};  // (64 at most)
+      const float top = wave_max(st.m);
       if (top != -INFINITY) {
-        const double sum = wave_sum_f64(st.x == -INFINITY ? 0.0 : (double)st.y * exp(((double)st.x - (double)top) * inv_temp));
+        const double sum = wave_sum_f64(st.m == -INFINITY ? 0.0 : st.sum * exp(((double)st.m - (double)top) * inv_temp));
         m = top;
         b = (double)s - log(sum);
       }
@@ -608,7 +611,7 @@ hipError_t beam_select(const BeamArgs& a, hipStream_t s) {
   const T* z = reinterpret_cast<const T*>(a.logits);
   const int rows = a.group_indptr[a.n_groups], n_tiles = beam_tiles_of<T>(a.V);
   const int64_t total = (int64_t)rows * n_tiles;
-  float2* stats = reinterpret_cast<float2*>(a.ws);
+  TileStats* stats = reinterpret_cast<TileStats*>(a.ws);
   float* maxima = reinterpret_cast<float*>(stats + total);
   const double c = 1.4426950408889634074 * a.inv_temp;
   const float c_hi = (float)c;
@@ -636,8 +639,8 @@ hipError_t beam_select(const BeamArgs& a, hipStream_t s) {
 }
 }  // namespace
 
-size_t beam_ws_doubles(int rows, int vocab) {  // per tile: (maximum, sum) and its segments' maxima; fp32 rows have the most tiles
-  return (size_t)rows * beam_tiles_of<float>(vocab) * (1 + BT_SEGS / 2);
+size_t beam_ws_doubles(int rows, int vocab) {  // per tile: its maximum and sum, and its segments' maxima; fp32 rows have the most tiles
+  return (size_t)rows * beam_tiles_of<float>(vocab) * (sizeof(TileStats) / sizeof(double) + BT_SEGS / 2);
 }
 
 hipError_t launch_beam_select(const BeamArgs& a, hipStream_t s) {

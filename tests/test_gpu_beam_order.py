@@ -1,4 +1,6 @@
 """Which candidates a selection names and in which order."""
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -49,3 +51,25 @@ def test_finished_beams_among_scores_that_absorb_the_logits(ctx):
     b, v, s = select(ctx, z, [0, 5], 6, [1e30, 1e30, 1e30, 0.0, np.inf], [0, 1, 0, 0, 1], eos=2999)
     assert list(zip(b[0], v[0])) == [(4, 2999), (0, 0), (0, 1), (0, 2), (0, 3), (0, 4)]
     assert s[0, 0] == np.finfo(np.float32).max and (s[0, 1:] == np.float32(1e30)).all()
+
+
+# ---- rows of which one token has nearly all of the probability ---------------------------------------------------------------
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("V", [1024, 4096, 4099, 32000, 131072])
+def test_many_small_terms_beside_a_large_one(ctx, dtype, V):
+    """exp(-16.75) is less than half of fp32's step at 1: added to the likeliest token's 1 one by one in 32 bits, the others vanish.
+    Each term is off by its argument's roundings (three of 2^-24 at 24.2, in units of log 2) and 2^-23: 5e-6 of itself, the likeliest
+    token's not at all; so is the logarithm, beside its rounding to fp32."""
+    for at in (0, V - 1, V // 2):
+        z = torch.full((2, V), -16.75, dtype=dtype, device="cuda")
+        z[0, at] = 0.0
+        z[1] = -math.inf
+        z[1, 5] = 3.0  # (its score is the beam's)
+        want = -math.log1p((V - 1) * math.exp(-16.75))
+        _, _, s = select(ctx, z, [0, 1, 2], 1, np.zeros(2))
+        assert abs(float(s[0, 0]) - want) <= abs(want) * (5e-6 + 2.0 ** -24) and s[1, 0] == 0.0
+        for behind in (False, True):  # a beam next to it, on either side: 2e-5 of that sum away
+            other = np.float32(want * (1.00002 if behind else 0.99998))
+            b, v, _ = select(ctx, z, [0, 2], 2, np.array([0.0, other]))
+            order = [(0, at), (1, 5)] if behind else [(1, 5), (0, at)]
+            assert list(zip(b[0], v[0])) == order, (at, behind)
