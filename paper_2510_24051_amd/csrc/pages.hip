@@ -91,11 +91,15 @@ __device__ __forceinline__ u32x4 transpose8(u32x4 w, int label) {
 // The image is [page][layer][K or V][slot][kv head][dim].  A wave takes one head of one 16-token block: D/32 times 1 KiB of K, which in
 // the pool are 16-byte pieces of 8 dims of a token already, and as much of V.  On the pool's side every access is 1 KiB
 // in one piece, on the image's 16 tokens of 64 bytes.
-// Bound by HBM: 64 pages of an 8B-shaped model (134 MB each way) saved in 43 us, restored in 50, 6.2 and 5.4 TB/s; read non-temporally,
-// written plainly (49 and 55 us a pass the other ways round).  One thread per 8 dims of a token, V gathered 2 bytes at a time,
-// took 102 and 262.
+// Bound by HBM: 64 pages of an 8B-shaped model (134 MB each way) saved in 43 us, restored in 50, 6.2 and 5.4 TB/s.  One thread per 8 dims
+// of a token, V gathered 2 bytes at a time, took 102 and 262.
+// Written plainly.  Read so where the image is a fifth of the 256 MB cache in front of the memory at most, which then often holds the
+// pages, and non-temporally (ONCE) from there on.  Three sets of pages and images in turn, plain and non-temporal: 16.8 MB 6.6 and 8.2 us,
+// 33.6 MB 10.8 and 13.9, 46 MB 18 both, 67 MB 29.2 and 24.2, 134 MB 52 and 50; half of 4830 tokens compacted and their pages
+// (79 MB) saved 96 and 81.  (The same pages again and again: 67 MB 17.9 and 24.2, 134 MB 44.7 and 41.9, 268 MB 102 and 77.)
 #define IMAGE_WAVES 4
-template <int D, bool TO_POOL, int IDS>
+#define IMAGE_ONCE ((int64_t)48 << 20)
+template <int D, bool TO_POOL, int IDS, bool ONCE>
 __global__ __launch_bounds__(64 * IMAGE_WAVES) void page_image_kernel(bf16_t* __restrict__ kv, int64_t layer_elems, int n_layers, PageIds<IDS> ids, int total,
                                                                       int F, int Hkv, uint16_t* __restrict__ image) {
   constexpr int N = D / 32;
@@ -114,8 +118,10 @@ __global__ __launch_bounds__(64 * IMAGE_WAVES) void page_image_kernel(bf16_t* __
   u32x4 k[N], v[N];
 #pragma unroll
   for (int j = 0; j < N; ++j) {
-    k[j] = load_nt(reinterpret_cast<const u32x4*>(TO_POOL ? ik + j * 32 : pk + j * 512));
-    v[j] = load_nt(reinterpret_cast<const u32x4*>(TO_POOL ? iv + j * 32 : pv + j * 512));
+    const u32x4* from_k = reinterpret_cast<const u32x4*>(TO_POOL ? ik + j * 32 : pk + j * 512);
+    const u32x4* from_v = reinterpret_cast<const u32x4*>(TO_POOL ? iv + j * 32 : pv + j * 512);
+    k[j] = ONCE ? load_nt(from_k) : *from_k;
+    v[j] = ONCE ? load_nt(from_v) : *from_v;
   }
 #pragma unroll
   for (int j = 0; j < N; ++j) {
@@ -307,15 +313,17 @@ hipError_t launch_page_image(bf16_t* kv, size_t layer_elems, int n_layers, const
     const int total = m * F * Hkv;
     const dim3 grid((unsigned)((total + IMAGE_WAVES - 1) / IMAGE_WAVES), (unsigned)n_layers), block(64 * IMAGE_WAVES);
     uint16_t* img = reinterpret_cast<uint16_t*>(image) + p0 * page_image;
-    auto go = [&](auto ids) {
+    auto go = [&](auto ids, auto once) {
       constexpr int N = sizeof(ids) / sizeof(int32_t);
+      constexpr bool ONCE = decltype(once)::value;
       for (int i = 0; i < m; ++i) ids.v[i] = host_ids[p0 + i];
-      auto* kernel = D == 128 ? (to_pool ? page_image_kernel<128, true, N> : page_image_kernel<128, false, N>)
-                              : (to_pool ? page_image_kernel<64, true, N> : page_image_kernel<64, false, N>);
+      auto* kernel = D == 128 ? (to_pool ? page_image_kernel<128, true, N, ONCE> : page_image_kernel<128, false, N, ONCE>)
+                              : (to_pool ? page_image_kernel<64, true, N, ONCE> : page_image_kernel<64, false, N, ONCE>);
       kernel<<<grid, block, 0, s>>>(kv, layer_elems, n_layers, ids, total, F, Hkv, img);
     };
-    if (m <= 64) go(PageIds<64>());
-    else go(PageIds<IDS_BY_VALUE>());
+    if (n * page_image * (int64_t)sizeof(bf16_t) >= IMAGE_ONCE) go(PageIds<IDS_BY_VALUE>(), std::true_type());
+    else if (m <= 64) go(PageIds<64>(), std::false_type());
+    else go(PageIds<IDS_BY_VALUE>(), std::false_type());
   }
   return hipGetLastError();
 }
