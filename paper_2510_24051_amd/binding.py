@@ -226,6 +226,7 @@ class Pie:
         if st != 0:
             raise PieError(st, self.lib.pie_last_error(None).decode())
         self.ctx = h
+        self._raw_stream, self._before, self._after = self.stream.cuda_stream, torch.cuda.Event(), torch.cuda.Event()
 
     @classmethod
     def planner(cls, model, n_kv_pages: int, n_embeds: int, max_batch_tokens: int, max_batch_requests: int,
@@ -249,6 +250,19 @@ class Pie:
     def _check(self, st: int):
         if st != 0:
             raise PieError(st, self.lib.pie_last_error(self.ctx).decode())
+
+    def _ordered(self, call, *args):
+        """A call that works on the caller's tensors: on the context's stream, behind what torch's current stream holds (what made them,
+        what their memory was used for before), and in front of what that stream gets afterwards."""
+        if torch._C._cuda_getCurrentRawStream(self.device.index) == self._raw_stream:
+            return self._check(call(*args))
+        current = torch.cuda.current_stream(self.device)
+        self._before.record(current)
+        self.stream.wait_event(self._before)
+        st = call(*args)
+        self._after.record(self.stream)
+        current.wait_event(self._after)
+        self._check(st)
 
     def _device(self) -> torch.device:
         """The context's device (a number belongs to it), as its tensors name it."""
@@ -364,14 +378,16 @@ class Pie:
         return ids
 
     def save_kvpage(self, page_ids, image: torch.Tensor):
-        """Enqueues the copy of the pages into `image` [pages, layers, 2, page_size, kv heads, head_dim]."""
+        """Enqueues the copy of the pages into `image` [pages, layers, 2, page_size, kv heads, head_dim]; torch's current stream sees it
+        whole.  The pages' masks are not in it."""
         ids = self._image(page_ids, image)
-        self._check(self.lib.pie_save_kvpage(self.ctx, _at(ids), len(ids), image.data_ptr()))
+        self._ordered(self.lib.pie_save_kvpage, self.ctx, _at(ids), len(ids), image.data_ptr())
 
     def restore_kvpage(self, page_ids, image: torch.Tensor):
-        """Enqueues the copy of `image` into the pages; it has to stay as it is until the stream has got there."""
+        """Enqueues the copy of `image`, as torch's current stream leaves it, into the pages; that stream may write it again at once.
+        The pages keep the masks that they have."""
         ids = self._image(page_ids, image)
-        self._check(self.lib.pie_restore_kvpage(self.ctx, _at(ids), len(ids), image.data_ptr()))
+        self._ordered(self.lib.pie_restore_kvpage, self.ctx, _at(ids), len(ids), image.data_ptr())
 
     def compact_kvpage(self, page_indptr, page_ids, kv_len, shifts=None, dst_page_indptr=None, dst_page_ids=None) -> np.ndarray:
         """Returns the sequences' new lengths; the moves are enqueued."""
@@ -478,25 +494,26 @@ class Pie:
                           out_scores: torch.Tensor, scores: Optional[torch.Tensor] = None, finished: Optional[torch.Tensor] = None,
                           eos_token: int = -1, temperature: float = 1.0):
         """pie_beam_select over `logits` [rows, vocab] (float32, bfloat16 or float16; rows may be strided); the outputs are the
-        caller's tensors [groups, n_out], complete when the context's stream has got there."""
+        caller's tensors [groups, n_out], complete when the context's stream has got there.  Inputs are as torch's current stream
+        leaves them, and what that stream gets afterwards sees the outputs."""
         b, keep = self._beam_search(group_indptr, n_out, out_beams, out_tokens, out_scores, scores, finished, eos_token, temperature)
         types = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
         if logits.dtype not in types or logits.device != self._device() or logits.dim() != 2 or logits.shape[0] != keep[-1] or \
                 (logits.shape[1] > 1 and logits.stride(1) != 1):
             raise ValueError("beam_select: logits are a device tensor [rows, vocab] of float32, bfloat16 or float16 whose rows are contiguous")
         stride = logits.stride(0) if logits.shape[0] > 1 else logits.shape[1]
-        self._check(self.lib.pie_beam_select(self.ctx, C.byref(b), logits.data_ptr(), types[logits.dtype], stride, logits.shape[1],
-                                             out_beams.data_ptr(), out_tokens.data_ptr(), out_scores.data_ptr()))
+        self._ordered(self.lib.pie_beam_select, self.ctx, C.byref(b), logits.data_ptr(), types[logits.dtype], stride, logits.shape[1],
+                      out_beams.data_ptr(), out_tokens.data_ptr(), out_scores.data_ptr())
 
     def get_next_beams_async(self, embed_ids, group_indptr, n_out: int, out_beams: torch.Tensor, out_tokens: torch.Tensor,
                              out_scores: torch.Tensor, scores: Optional[torch.Tensor] = None, finished: Optional[torch.Tensor] = None,
                              eos_token: int = -1, temperature: float = 1.0):
-        """pie_get_next_beams; arguments as for beam_select_async."""
+        """pie_get_next_beams; arguments and streams as for beam_select_async."""
         ids = _i32(embed_ids)
         b, keep = self._beam_search(group_indptr, n_out, out_beams, out_tokens, out_scores, scores, finished, eos_token, temperature)
         if len(ids) != keep[-1]:
             raise ValueError("get_next_beams: one Embed per row")
-        self._check(self.lib.pie_get_next_beams(self.ctx, C.byref(b), _at(ids), out_beams.data_ptr(), out_tokens.data_ptr(), out_scores.data_ptr()))
+        self._ordered(self.lib.pie_get_next_beams, self.ctx, C.byref(b), _at(ids), out_beams.data_ptr(), out_tokens.data_ptr(), out_scores.data_ptr())
 
     def get_next_beams(self, embed_ids, group_indptr, n_out: int, scores=None, finished=None, eos_token: int = -1, temperature: float = 1.0):
         """The same with host arrays: (beams, tokens, scores) [groups, n_out], after the stream has been waited for."""
