@@ -370,24 +370,23 @@ class Pie:
             raise ValueError("fork_kvpage: one destination per source")
         self._check(self.lib.pie_fork_kvpage(self.ctx, _at(s), _at(d), len(s)))
 
-    def _image(self, page_ids, image: torch.Tensor) -> np.ndarray:
+    def _image(self, page_ids, image: torch.Tensor):
+        """The pages' numbers as bytes, how many there are, and the image's address."""
         ids, m = _i32(page_ids), self.model
-        if tuple(image.shape) != (len(ids), self.n_layers, 2, m.page_size, m.n_kv_heads, m.head_dim) or image.dtype != torch.bfloat16 or \
+        if image.shape != (len(ids), self.n_layers, 2, m.page_size, m.n_kv_heads, m.head_dim) or image.dtype != torch.bfloat16 or \
                 image.device != self._device() or not image.is_contiguous():
             raise ValueError("an image of pages is a contiguous bfloat16 device tensor [pages, layers, 2, page_size, kv heads, head_dim]")
-        return ids
+        return ids.tobytes(), len(ids), image.data_ptr()
 
     def save_kvpage(self, page_ids, image: torch.Tensor):
         """Enqueues the copy of the pages into `image` [pages, layers, 2, page_size, kv heads, head_dim]; torch's current stream sees it
         whole.  The pages' masks are not in it."""
-        ids = self._image(page_ids, image)
-        self._ordered(self.lib.pie_save_kvpage, self.ctx, _at(ids), len(ids), image.data_ptr())
+        self._ordered(self.lib.pie_save_kvpage, self.ctx, *self._image(page_ids, image))
 
     def restore_kvpage(self, page_ids, image: torch.Tensor):
         """Enqueues the copy of `image`, as torch's current stream leaves it, into the pages; that stream may write it again at once.
         The pages keep the masks that they have."""
-        ids = self._image(page_ids, image)
-        self._ordered(self.lib.pie_restore_kvpage, self.ctx, _at(ids), len(ids), image.data_ptr())
+        self._ordered(self.lib.pie_restore_kvpage, self.ctx, *self._image(page_ids, image))
 
     def compact_kvpage(self, page_indptr, page_ids, kv_len, shifts=None, dst_page_indptr=None, dst_page_ids=None) -> np.ndarray:
         """Returns the sequences' new lengths; the moves are enqueued."""
