@@ -477,9 +477,16 @@ class Pie:
         self.synchronize()
         return oi.cpu().numpy(), op.cpu().numpy()
 
-    def _beam_search(self, group_indptr, n_out, out_beams, out_tokens, out_scores, scores, finished, eos_token, temperature):
+    @staticmethod
+    def _searches(group_indptr) -> np.ndarray:
         ip = _i32(group_indptr)
-        G, n, dev = len(ip) - 1, int(ip[-1]) if len(ip) else 0, self._device()
+        if len(ip) < 1:
+            raise ValueError("beam search: group_indptr has one entry more than there are searches")
+        return ip
+
+    def _beam_search(self, group_indptr, n_out, out_beams, out_tokens, out_scores, scores, finished, eos_token, temperature):
+        ip = self._searches(group_indptr)
+        G, n, dev = len(ip) - 1, int(ip[-1]), self._device()
         for t, dt in ((out_beams, torch.int32), (out_tokens, torch.int32), (out_scores, torch.float32)):
             if t.dtype != dt or t.device != dev or not t.is_contiguous() or t.numel() != G * n_out:
                 raise ValueError("beam search: outputs are contiguous device tensors [groups, n_out] of int32, int32 and float32")
@@ -516,9 +523,9 @@ class Pie:
 
     def get_next_beams(self, embed_ids, group_indptr, n_out: int, scores=None, finished=None, eos_token: int = -1, temperature: float = 1.0):
         """The same with host arrays: (beams, tokens, scores) [groups, n_out], after the stream has been waited for."""
+        G = len(self._searches(group_indptr)) - 1
         dev = lambda a, dt: None if a is None else torch.from_numpy(np.array(a, dtype=dt)).to(self.device)
         s, f = dev(scores, np.float32), dev(finished, np.uint8)
-        G = len(_i32(group_indptr)) - 1
         ob, ot = (torch.empty((G, n_out), dtype=torch.int32, device=self.device) for _ in range(2))
         os_ = torch.empty((G, n_out), dtype=torch.float32, device=self.device)
         torch.cuda.synchronize(self.device)
