@@ -153,8 +153,9 @@ pie_status pie_fork_kvpage(pie_ctx* ctx, const int32_t* src_pages, const int32_t
 
 /* Saves pages into the caller's memory, and restores pages from it: image is dev bf16
  * [n][n_layers][2: K, V][page_size][n_kv_heads][head_dim], 16-byte aligned, bits unchanged (K as it is stored: after the rotary
- * step).  The pool pages of a save, and the image of a restore, stay as they are; page masks are neither saved nor changed.  A page
- * may be saved twice by one call, not restored twice (PIE_ECONFLICT).  page_ids: host int32 [n].  May be captured.
+ * step).  The pool pages of a save, and the image of a restore, stay as they are.  Page masks are neither saved nor changed: a program
+ * that brings pages back sets the masks that it had set (pie_mask_kvpage), or tokens hidden before are seen again, and others are not.
+ * A page may be saved twice by one call, not restored twice (PIE_ECONFLICT).  page_ids: host int32 [n].  May be captured.
  * Errors: PIE_EINVAL, PIE_ERANGE, PIE_ECONFLICT, PIE_EHIP. */
 pie_status pie_save_kvpage(pie_ctx* ctx, const int32_t* page_ids, int32_t n, void* image);
 pie_status pie_restore_kvpage(pie_ctx* ctx, const int32_t* page_ids, int32_t n, const void* image);
@@ -165,8 +166,9 @@ pie_status pie_restore_kvpage(pie_ctx* ctx, const int32_t* page_ids, int32_t n, 
  * dst_page_indptr[s] .. dst_page_indptr[s+1]), or, with both destination arrays NULL, its own table: in place.  out_kv_len[s]
  * receives the number of tokens kept; the destination's first ceil(out_kv_len[s] / page_size) pages hold them.  Of these, pages that
  * the call writes have all slots visible afterwards; slots behind the last kept token are left as they were.  The pages behind them
- * (which the caller may now give to others) keep contents and masks, as do source pages that are no destinations.  A sequence that
- * keeps nothing has length 0.
+ * (which the caller may now give to others) keep contents and masks, as do source pages that are no destinations: their masks are to be
+ * set (pie_mask_kvpage) before others write tokens there, or slots of evicted tokens stay hidden from the new owner too.  A
+ * sequence that keeps nothing has length 0.
  * shifts (may be NULL): host int32, one per token of the sequences one after another (sum of kv_len): the key of a kept token
  * is rotated by that many positions more, with the model's rotary frequencies and rounded to bf16 once, as a token needs
  * that keeps its place relative to others when a gap before it is closed; 0 leaves the bits.

@@ -389,7 +389,8 @@ class Pie:
         self._ordered(self.lib.pie_restore_kvpage, self.ctx, *self._image(page_ids, image))
 
     def compact_kvpage(self, page_indptr, page_ids, kv_len, shifts=None, dst_page_indptr=None, dst_page_ids=None) -> np.ndarray:
-        """Returns the sequences' new lengths; the moves are enqueued."""
+        """Returns the sequences' new lengths; the moves are enqueued.  Pages left behind keep the masks that hid the evicted tokens: set
+        them (mask_kvpage) before they are another's."""
         ip, ids, kl = _i32(page_indptr), _i32(page_ids), _i32(kv_len)
         sh = None if shifts is None else _i32(shifts)
         if (dst_page_indptr is None) != (dst_page_ids is None):
