@@ -174,8 +174,10 @@ pie_status pie_restore_kvpage(pie_ctx* ctx, const int32_t* page_ids, int32_t n, 
  * that keeps its place relative to others when a gap before it is closed; 0 leaves the bits.
  * Pages may be shared by several sequences where no sequence of the call writes them (in place, pages in front of the first token
  * that moves or turns are not written).  A page that is written may be no one's source in any other place: PIE_ECONFLICT.
- * All arrays are host int32.  May allocate; refused with PIE_EHIP while the stream is captured.  On an error other than a
- * PIE_EHIP of a failed launch nothing has changed.
+ * All arrays are host int32.  May allocate: the plan (tens of bytes per 16 tokens; with shifts that differ from token to token
+ * 4 * head_dim + 8 bytes a token), and at most 256 MiB of scratch blocks where a sequence of scattered tokens is compacted in place and there
+ * is room for them.  Both, with some more for longer plans, are kept for later calls until pie_destroy.  Refused with PIE_EHIP
+ * while the stream is captured.  On an error other than a PIE_EHIP of a failed launch nothing has changed.
  * Errors: PIE_EINVAL (also: more tokens kept than the destination holds), PIE_ERANGE, PIE_EBATCH (over 2^30 tokens),
  * PIE_ECONFLICT, PIE_ENOMEM, PIE_EHIP. */
 pie_status pie_compact_kvpage(pie_ctx* ctx, int32_t n_seqs, const int32_t* page_indptr, const int32_t* page_ids, const int32_t* kv_len,

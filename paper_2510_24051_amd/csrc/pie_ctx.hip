@@ -1568,6 +1568,7 @@ static pie_status refuse_capture(pie_ctx* c, const char* who) {  // (before the 
   return fail(c, PIE_EHIP, "%s: the context's stream is being captured", who);
 }
 
+#define COMPACT_SCRATCH ((int64_t)256 << 20)  // bytes of scratch blocks that a compaction may use
 // Brings a plan to the front of the context's block for page plans, and behind it (at a multiple of 256) the table [n_turns, D] of the
 // angles that its n_turns shifts (at `turns` of the image) turn by.  Small plans travel as arguments of the kernel that makes the
 // table; long ones are copied from the context's host image, which has to wait for the copy before it.  Behind the table, `more` bytes.
@@ -1580,7 +1581,9 @@ static pie_status send_plan(pie_ctx* c, const PlanImage& plan, size_t turns, int
     if (c->moves_dev) (void)hipFree(c->moves_dev);
     c->moves_dev = nullptr;
     c->moves_cap = 0;
-    const size_t cap = (std::max(need, (size_t)1 << 18) * 3 / 2 + 255) / 256 * 256;
+    // (a plan is small and grows with the contexts; of scratch blocks an eighth more is kept, and no more than a compaction may use)
+    const size_t room = std::max(more, std::min(more + more / 8, (size_t)COMPACT_SCRATCH));
+    const size_t cap = (std::max(o_more, (size_t)1 << 18) * 3 / 2 + room + 255) / 256 * 256;
     const hipError_t e = hipMalloc(reinterpret_cast<void**>(&c->moves_dev), cap);
     if (e != hipSuccess) {
       (void)hipGetLastError();
@@ -1685,7 +1688,6 @@ extern "C" pie_status pie_restore_kvpage(pie_ctx* c, const int32_t* page_ids, in
   return guarded(c, "pie_restore_kvpage", [&]() { return page_image(c, page_ids, n, const_cast<void*>(image), true, "pie_restore_kvpage"); });
 }
 
-#define COMPACT_SCRATCH ((int64_t)256 << 20)  // bytes of scratch blocks that a compaction may use
 struct CompactSeq {  // a sequence of which something moves: its source blocks, kept tokens, destination blocks [first_tile, n_tiles)
   int block0, block1, first, n, first_tile, n_tiles, tile0, step;  // step: destination blocks of a chain
   bool in_order;
