@@ -58,9 +58,9 @@ __global__ __launch_bounds__(FORK_THREADS) void fork_kernel(unsigned char* __res
 // ---------------------------------------------------------------------------------------------
 // save and restore
 // ---------------------------------------------------------------------------------------------
-// (Kernel arguments cost the host time, here and below, so short lists have a small block of their own.  Calls back to back, the host's
+// (Kernel arguments cost the host time, here and above, so short lists have a small block of their own.  Calls back to back, the host's
 // time for each with the large block and with the small one: two pages saved 3.35 and 3.20 us, a fork with the call's checks 4.7 and 4.4,
-// a fork after an append 15.1 and 11.1, a short compaction's plan 13.1 and 12.9.)
+// a fork after an append 15.1 and 11.1.  A short compaction's plan, 13.1 and 12.9, has one block.)
 template <int N>
 struct PageIds { int32_t v[N]; };
 
@@ -273,10 +273,8 @@ __global__ __launch_bounds__(64 * COMPACT_WAVES) void compact_kernel(const bf16_
 }
 
 // A small plan, as kernel arguments, into device memory, and the angles of its shifts (64 bits, rounded once: a shift may be long).
-template <int N>
-struct PlanBytes { uint32_t w[N]; };
-template <int N>
-__global__ void put_plan_kernel(PlanBytes<N> plan, int words, uint32_t* __restrict__ dev, int turn0, int n_turns, const double* __restrict__ inv_freq,
+struct PlanBytes { uint32_t w[PLAN_BY_VALUE / 4]; };
+__global__ void put_plan_kernel(PlanBytes plan, int words, uint32_t* __restrict__ dev, int turn0, int n_turns, const double* __restrict__ inv_freq,
                                 int D, float* __restrict__ angles) {
   const int idx = blockIdx.x * blockDim.x + threadIdx.x, half = D / 2;
   if (idx < words) dev[idx] = plan.w[idx];
@@ -332,13 +330,10 @@ hipError_t launch_put_plan(const unsigned char* plan, size_t size, unsigned char
                            float* angles, hipStream_t s) {
   if (size > PLAN_BY_VALUE || size % 4 || turns % 4 || turns + (size_t)n_turns * 4 > size) return hipErrorInvalidValue;
   const int words = (int)(size / 4), threads = words > n_turns * (D / 2) ? words : n_turns * (D / 2);
-  auto go = [&](auto bytes) {
-    __builtin_memcpy(bytes.w, plan, size);
-    put_plan_kernel<<<dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s>>>(bytes, words, reinterpret_cast<uint32_t*>(dev), (int)(turns / 4), n_turns,
-                                                                                  inv_freq, D, angles);
-  };
-  if (words <= 192) go(PlanBytes<192>());
-  else go(PlanBytes<PLAN_BY_VALUE / 4>());
+  PlanBytes bytes;
+  __builtin_memcpy(bytes.w, plan, size);
+  put_plan_kernel<<<dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s>>>(bytes, words, reinterpret_cast<uint32_t*>(dev), (int)(turns / 4), n_turns,
+                                                                                inv_freq, D, angles);
   return hipGetLastError();
 }
 
