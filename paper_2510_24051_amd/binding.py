@@ -137,8 +137,11 @@ def product_stream(rows: int, n_out: int, k: int, workspace_floats: int, n_cus: 
     return {"tile_rows": int(out[0]), "k_slices": int(out[1]), "splits": int(out[2])}
 
 
+_INT32 = np.dtype(np.int32)
+
+
 def _i32(a) -> np.ndarray:
-    return np.ascontiguousarray(a, dtype=np.int32)
+    return np.ascontiguousarray(a, _INT32)
 
 
 def _ptr(a: Optional[np.ndarray]):
@@ -216,7 +219,7 @@ class Pie:
         self.device = torch.device(device)
         torch.cuda.set_device(self.device)
         self.stream = stream if stream is not None else torch.cuda.Stream(device=self.device)
-        self.model, self.n_layers = model, n_layers
+        self.model, self.n_layers, self._page_image = model, n_layers, self._image_of_page(model, n_layers)
         md = ModelDescC(model.hidden, model.n_q_heads, model.n_kv_heads, model.head_dim, model.mlp_dim, model.vocab,
                         model.page_size, model.rms_eps, model.rope_theta, n_layers)
         pd = PoolDescC(n_kv_pages, n_embeds, max_batch_tokens, max_batch_requests, max_top_k, max_dist_rows,
@@ -226,7 +229,8 @@ class Pie:
         if st != 0:
             raise PieError(st, self.lib.pie_last_error(None).decode())
         self.ctx = h
-        self._raw_stream, self._before, self._after = self.stream.cuda_stream, torch.cuda.Event(), torch.cuda.Event()
+        self._index, self._raw_stream = self.device.index, self.stream.cuda_stream
+        self._before, self._after = torch.cuda.Event(), torch.cuda.Event()
 
     @classmethod
     def planner(cls, model, n_kv_pages: int, n_embeds: int, max_batch_tokens: int, max_batch_requests: int,
@@ -235,7 +239,7 @@ class Pie:
         PieBatch.work / plan_info and mask_kvpage work on it; everything else raises PieError."""
         self = cls.__new__(cls)
         self.lib = load_library()
-        self.device, self.stream, self.model, self.n_layers = None, None, model, n_layers
+        self.device, self.stream, self.model, self.n_layers, self._page_image = None, None, model, n_layers, self._image_of_page(model, n_layers)
         md = ModelDescC(model.hidden, model.n_q_heads, model.n_kv_heads, model.head_dim, model.mlp_dim, model.vocab,
                         model.page_size, model.rms_eps, model.rope_theta, n_layers)
         pd = PoolDescC(n_kv_pages, n_embeds, max_batch_tokens, max_batch_requests, 0, 0, max_adapters, max_lora_rank)
@@ -247,6 +251,10 @@ class Pie:
         return self
 
     # ---- helpers ----
+    @staticmethod
+    def _image_of_page(model, n_layers: int) -> tuple:
+        return (n_layers, 2, model.page_size, model.n_kv_heads, model.head_dim)
+
     def _check(self, st: int):
         if st != 0:
             raise PieError(st, self.lib.pie_last_error(self.ctx).decode())
@@ -254,8 +262,9 @@ class Pie:
     def _ordered(self, call, *args):
         """A call that works on the caller's tensors: on the context's stream, behind what torch's current stream holds (what made them,
         what their memory was used for before), and in front of what that stream gets afterwards."""
-        if torch._C._cuda_getCurrentRawStream(self.device.index) == self._raw_stream:
-            return self._check(call(*args))
+        if torch._C._cuda_getCurrentRawStream(self._index) == self._raw_stream:
+            st = call(*args)
+            return self._check(st) if st != 0 else None
         current = torch.cuda.current_stream(self.device)
         self._before.record(current)
         self.stream.wait_event(self._before)
@@ -370,23 +379,22 @@ class Pie:
             raise ValueError("fork_kvpage: one destination per source")
         self._check(self.lib.pie_fork_kvpage(self.ctx, _at(s), _at(d), len(s)))
 
-    def _image(self, page_ids, image: torch.Tensor):
-        """The pages' numbers as bytes, how many there are, and the image's address."""
-        ids, m = _i32(page_ids), self.model
-        if image.shape != (len(ids), self.n_layers, 2, m.page_size, m.n_kv_heads, m.head_dim) or image.dtype != torch.bfloat16 or \
-                image.device != self._device() or not image.is_contiguous():
+    def _move_image(self, call, page_ids, image: torch.Tensor):
+        ids = np.ascontiguousarray(page_ids, _INT32)
+        n = len(ids)
+        if image.shape != (n, *self._page_image) or image.dtype is not torch.bfloat16 or image.device != self._device() or not image.is_contiguous():
             raise ValueError("an image of pages is a contiguous bfloat16 device tensor [pages, layers, 2, page_size, kv heads, head_dim]")
-        return ids.tobytes(), len(ids), image.data_ptr()
+        self._ordered(call, self.ctx, ids.tobytes(), n, image.data_ptr())
 
     def save_kvpage(self, page_ids, image: torch.Tensor):
         """Enqueues the copy of the pages into `image` [pages, layers, 2, page_size, kv heads, head_dim]; torch's current stream sees it
         whole.  The pages' masks are not in it."""
-        self._ordered(self.lib.pie_save_kvpage, self.ctx, *self._image(page_ids, image))
+        self._move_image(self.lib.pie_save_kvpage, page_ids, image)
 
     def restore_kvpage(self, page_ids, image: torch.Tensor):
         """Enqueues the copy of `image`, as torch's current stream leaves it, into the pages; that stream may write it again at once.
         The pages keep the masks that they have."""
-        self._ordered(self.lib.pie_restore_kvpage, self.ctx, *self._image(page_ids, image))
+        self._move_image(self.lib.pie_restore_kvpage, page_ids, image)
 
     def compact_kvpage(self, page_indptr, page_ids, kv_len, shifts=None, dst_page_indptr=None, dst_page_ids=None) -> np.ndarray:
         """Returns the sequences' new lengths; the moves are enqueued.  Pages left behind keep the masks that hid the evicted tokens: set

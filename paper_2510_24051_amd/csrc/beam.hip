@@ -12,7 +12,8 @@
 // Two kernels.  beam_tiles reads every logit once and leaves, per segment (what a wave loads at once), the largest, and per tile of
 // eight segments the largest and the sum of exponentials.  beam_pick, one workgroup per group, turns the segments' maxima into scores
 // and keeps the n_out best segments by (score, beam, place): no other segment can hold one of the n_out best candidates, as
-// each of those n_out has one that comes before all of its own.  Only these are read again.
+// each of those n_out has one that comes before all of its own.  Only these are read again.  Where groups are small beam_pick does
+// the tiles as well.
 #include "internal.h"
 
 namespace {
@@ -151,7 +152,7 @@ __device__ __forceinline__ float beam_tile(const BeamRow<T>& z, int tile, const 
   return seg;
 }
 
-// A wave per tile.  Bound by HBM: 262 MB of logits (512 rows of 128256) in 41.7 us, 6.3 TB/s, the rate of a streaming read.
+// A wave per tile.  Bound by HBM: 262 MB of logits (512 rows of 128256) in 41 to 43 us, 6.1 to 6.4 TB/s, the rate of a streaming read.
 #define BT_WAVES 4
 template <typename T>
 __global__ __launch_bounds__(64 * BT_WAVES) void beam_tiles_kernel(const T* __restrict__ logits, int64_t stride, int V, int n_tiles, BeamScale scale,

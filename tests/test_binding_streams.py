@@ -44,7 +44,7 @@ def context(monkeypatch, current, status=0):
     p = Pie.__new__(Pie)
     p.lib = SimpleNamespace(pie_last_error=lambda ctx: b"refused", pie_destroy=lambda ctx: 0, **{n: call(n) for n in CALLS})
     p.ctx, p.device, p.stream, p.model, p.n_layers = C.c_void_p(1), torch.device("cpu"), own, MODEL, 1
-    p._raw_stream, p._before, p._after = 7, Event(), Event()
+    p._index, p._raw_stream, p._before, p._after, p._page_image = 0, 7, Event(), Event(), (1, 2, 16, 2, 64)
     monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: {"own": own, "other": other}[current])
     monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda index: {"own": 7, "other": 9}[current], raising=False)
     return p, log
