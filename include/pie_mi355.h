@@ -321,7 +321,8 @@ enum { PIE_F32 = 0, PIE_BF16 = 1, PIE_F16 = 2 };
 /* The selection over logits that the caller has (changed by a grammar, a penalty, a head of its own): dev [rows] of n_vocab
  * (1 .. the model's vocab) elements, row r at logits + r * row_stride elements; any row_stride >= n_vocab, and any alignment that
  * the element type has.  rows <= max_dist_rows.  Outputs dev [n_groups][n_out]: the beam within its group, the token, the new
- * cumulative score (-inf where it is below what 32 bits hold); they must not overlap the inputs.  Enqueues only and allocates nothing; may be captured into a graph.
+ * cumulative score (-inf where it is below what 32 bits hold); they must not overlap the inputs.  Enqueues only and allocates
+ * nothing; may be captured into a graph (graphs of one context share its workspace: one replays behind the other).
  * Errors: PIE_EINVAL, PIE_ERANGE (n_out, n_vocab, eos_token), PIE_EBATCH (rows, beams of a group), PIE_EHIP. */
 pie_status pie_beam_select(pie_ctx* ctx, const pie_beam_search* search, const void* logits, int32_t dtype, int64_t row_stride,
                            int32_t n_vocab, int32_t* out_beams, int32_t* out_tokens, float* out_scores);
