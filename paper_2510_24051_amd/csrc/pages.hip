@@ -88,17 +88,18 @@ __device__ __forceinline__ u32x4 transpose8(u32x4 w, int label) {
   return out;
 }
 
-// The image is [page][layer][K or V][slot][kv head][dim].  A wave takes one head of one 16-token block: D/32 times 1 KiB of K, which in
-// the pool are 16-byte pieces of 8 dims of a token already, and as much of V.  On the pool's side every access is 1 KiB
-// in one piece, on the image's 16 tokens of 64 bytes.
-// Bound by HBM: 64 pages of an 8B-shaped model (134 MB each way) saved in 43 us, restored in 50, 6.2 and 5.4 TB/s.  One thread per 8 dims
-// of a token, V gathered 2 bytes at a time, took 102 and 262.
-// Written plainly.  Read so where the image is a fifth of the 256 MB cache in front of the memory at most, which then often holds the
-// pages, and non-temporally (ONCE) from there on.  Three sets of pages and images in turn, plain and non-temporal: 16.8 MB 6.6 and 8.2 us,
-// 33.6 MB 10.8 and 13.9, 46 MB 18 both, 67 MB 29.2 and 24.2, 134 MB 52 and 50; half of 4830 tokens compacted and their pages
-// (79 MB) saved 96 and 81.  (The same pages again and again: 67 MB 17.9 and 24.2, 134 MB 44.7 and 41.9, 268 MB 102 and 77.)
+// The image is [page][layer][K or V][slot][kv head][dim].  A wave takes one head of one 16-token block.  An access covers 8 tokens and 64
+// dims, so that both sides move whole lines: 128 bytes of each token in the image; in the pool, where 16-byte pieces hold 8 dims of a
+// token (K) or 8 tokens of a dim (V), 128 bytes of each octet of dims.  (16 tokens and 32 dims, a KiB of the pool and 64 bytes of a
+// token: lines of the image that are read past the caches come twice, 64 pages of an 8B-shaped model restored in 54 us for 49, saved in
+// 50 for 47.)  Bound by HBM: those are 134 MB each way, 5.6 TB/s.  One thread per 8 dims of a token, V gathered 2 bytes at a time, took
+// 262 and 102.
+// Written plainly.  Read so where the image is less than a quarter of the 256 MB cache in front of the memory, which then often holds the
+// pages, and non-temporally (ONCE) from there on.  Three sets of pages and images in turn, plain and non-temporal: 16.8 MB 6.5 and 7.6 us,
+// 33.6 MB 10.7 and 12.8, 46 MB 16 both, 57 MB 22 and 18, 67 MB 27 and 21, 134 MB 51 and 47; three sets of pages into one image 57 MB 16
+// and 18, 67 MB 21 both, 134 MB 36 and 35, 188 MB 70 and 47.
 #define IMAGE_WAVES 4
-#define IMAGE_ONCE ((int64_t)48 << 20)
+#define IMAGE_ONCE ((int64_t)64 << 20)
 template <int D, bool TO_POOL, int IDS, bool ONCE>
 __global__ __launch_bounds__(64 * IMAGE_WAVES) void page_image_kernel(bf16_t* __restrict__ kv, int64_t layer_elems, int n_layers, PageIds<IDS> ids, int total,
                                                                       int F, int Hkv, uint16_t* __restrict__ image) {
@@ -111,22 +112,23 @@ __global__ __launch_bounds__(64 * IMAGE_WAVES) void page_image_kernel(bf16_t* __
   const int64_t row = (int64_t)Hkv * D, part = (int64_t)F * PAGE * row;
   uint16_t* img = image + (((int64_t)p * n_layers + layer) * 2) * part + (int64_t)f * PAGE * row + h * D;
   const int label = octet_label(lane & 7);
-  uint16_t* pk = blk + lane * 8;
-  uint16_t* pv = blk + PAGE * D + (lane & ~7) * 8 + label * 8;
-  uint16_t* ik = img + swap23(lane & 15) * row + (lane >> 4) * 8;
-  uint16_t* iv = img + part + ((lane >> 5) * 8 + label) * row + (lane >> 3 & 3) * 8;
+  const int octet = lane >> 3;  // of the 64 dims that an access covers
+  uint16_t* pk = blk + octet * 128 + (lane & 7) * 8;
+  uint16_t* pv = blk + PAGE * D + (octet >> 2) * 512 + (octet & 3) * 64 + label * 8;
+  uint16_t* ik = img + swap23(lane & 7) * row + octet * 8;  // (swap23 of a slot and of that slot 8 further on: 4 apart)
+  uint16_t* iv = img + part + label * row + octet * 8;
   u32x4 k[N], v[N];
 #pragma unroll
-  for (int j = 0; j < N; ++j) {
-    const u32x4* from_k = reinterpret_cast<const u32x4*>(TO_POOL ? ik + j * 32 : pk + j * 512);
-    const u32x4* from_v = reinterpret_cast<const u32x4*>(TO_POOL ? iv + j * 32 : pv + j * 512);
+  for (int j = 0; j < N; ++j) {  // 64 dims j / 2, half j % 2 of the tokens
+    const u32x4* from_k = reinterpret_cast<const u32x4*>(TO_POOL ? ik + (j & 1) * 4 * row + (j >> 1) * 64 : pk + (j >> 1) * 1024 + (j & 1) * 64);
+    const u32x4* from_v = reinterpret_cast<const u32x4*>(TO_POOL ? iv + (j & 1) * 8 * row + (j >> 1) * 64 : pv + (j >> 1) * 1024 + (j & 1) * 256);
     k[j] = ONCE ? load_nt(from_k) : *from_k;
     v[j] = ONCE ? load_nt(from_v) : *from_v;
   }
 #pragma unroll
   for (int j = 0; j < N; ++j) {
-    *reinterpret_cast<u32x4*>(TO_POOL ? pk + j * 512 : ik + j * 32) = k[j];
-    *reinterpret_cast<u32x4*>(TO_POOL ? pv + j * 512 : iv + j * 32) = transpose8(v[j], label);
+    *reinterpret_cast<u32x4*>(TO_POOL ? pk + (j >> 1) * 1024 + (j & 1) * 64 : ik + (j & 1) * 4 * row + (j >> 1) * 64) = k[j];
+    *reinterpret_cast<u32x4*>(TO_POOL ? pv + (j >> 1) * 1024 + (j & 1) * 256 : iv + (j & 1) * 8 * row + (j >> 1) * 64) = transpose8(v[j], label);
   }
 }
 

@@ -8,13 +8,13 @@ from test_gpu_pages import model
 pytestmark = pytest.mark.gpu
 
 
-@pytest.mark.parametrize("D,Hkv,P,layers,n", [(128, 8, 16, 32, 23), (128, 8, 16, 32, 24), (64, 8, 32, 32, 23), (64, 8, 32, 32, 25), (64, 1, 16, 1, 12289)])
-def test_images_of_about_48_mib(D, Hkv, P, layers, n):
+@pytest.mark.parametrize("D,Hkv,P,layers,n", [(128, 8, 16, 32, 31), (128, 8, 16, 32, 32), (64, 8, 32, 32, 31), (64, 8, 32, 32, 33), (64, 1, 16, 1, 16385)])
+def test_images_of_about_64_mib(D, Hkv, P, layers, n):
     from paper_2510_24051_amd import Pie
     ctx = Pie(model(D, Hkv, P), 2 * n + 1, 1, max_batch_tokens=1, max_batch_requests=1, n_layers=layers)
     gen = torch.Generator(device="cuda").manual_seed(n)
     bits = torch.randint(-32768, 32768, (n, layers, 2, P, Hkv, D), generator=gen, device="cuda", dtype=torch.int16)
-    assert abs(bits.nbytes / (48 << 20) - 1) < 0.05  # (give or take a page)
+    assert abs(bits.nbytes / (64 << 20) - 1) < 0.05  # (give or take a page)
     ids = np.random.default_rng(n).permutation(2 * n + 1).astype(np.int32)
     back = torch.zeros_like(bits)
     torch.cuda.synchronize()
