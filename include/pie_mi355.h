@@ -332,6 +332,74 @@ pie_status pie_beam_select(pie_ctx* ctx, const pie_beam_search* search, const vo
 pie_status pie_get_next_beams(pie_ctx* ctx, const pie_beam_search* search, const int32_t* embed_ids, int32_t* out_beams,
                               int32_t* out_tokens, float* out_scores);
 
+/* Microscaled formats (OCP Microscaling Formats v1.0): layers whose weights take 4.25 bits a value and whose products read activations
+ * of 8.25.  A row of k values (a multiple of 32) is cut into blocks of 32; a block has one scale byte b, worth 2^(b - 127) (255: the
+ * block is NaN), and 32 elements: E4M3, a byte each (PIE_MXFP8), or E2M1, two to a byte, the first in the low half (PIE_MXFP4). */
+enum { PIE_MXFP8 = 0, PIE_MXFP4 = 1 };
+typedef struct {
+  int32_t format;
+  void* elements;      /* dev, 16-byte aligned */
+  int64_t row_bytes;   /* from a row's elements to the next row's: a multiple of 16, at least k or k / 2 */
+  uint8_t* scales;     /* dev, 4-byte aligned */
+  int64_t scale_bytes; /* from a row's scales to the next row's: a multiple of 4, at least k / 32 */
+} pie_mx_rows;
+
+/* Rows of plain values: row r starts row_stride elements behind row r - 1; any stride of at least a row's length, and any alignment
+ * that the element type (PIE_F32, PIE_BF16, PIE_F16) has. */
+typedef struct {
+  void* data; /* dev */
+  int32_t dtype;
+  int64_t row_stride;
+} pie_rows;
+
+/* The calls below take k from 32 to 2^20, and 0 to 2^24 rows (0: nothing is done).  They are enqueued on the context's stream, allocate
+ * nothing unless they say so, and may be captured into a graph (graphs of one context share its workspace: one replays behind the
+ * other).  Outputs must not overlap inputs where nothing else is said.  What is behind the last scale of a row, up to a multiple
+ * of 4 bytes, is written as 0 by every call and looked at by none.
+ * Errors of all: PIE_EINVAL (null, a shape, stride, alignment, format or type that is not as above), PIE_EUNSUPPORTED (k or rows
+ * out of range), PIE_EHIP. */
+
+/* out = x in the format of `out`: per block, b - 127 = floor(log2 max|x|) - 8 (MXFP8) or - 2 (MXFP4), at least -127; elements are
+ * x / 2^(b - 127) rounded to nearest, ties to even, and saturated at 448 or 6.  A block that holds a NaN or an infinity has
+ * b = 255 and elements 0; one of zeros b = 0. */
+pie_status pie_mx_quantise(pie_ctx* ctx, const pie_rows* x, int32_t rows, int32_t k, const pie_mx_rows* out);
+/* out = the values that `a` stands for, rounded once (fp32 holds them exactly, except that more than it can hold is infinite). */
+pie_status pie_mx_dequantise(pie_ctx* ctx, const pie_mx_rows* a, int32_t rows, int32_t k, const pie_rows* out);
+
+/* The norm between two blocks of a layer: h = x + delta (delta may be NULL), rounded to x's type and stored where h is given (h may be
+ * x, or delta where that has the same type), and out = h / sqrt(mean(h^2) + rms_eps) * gain, quantised from 32 bits as pie_mx_quantise
+ * does.  It is the rounded h that is normalised.  gain: dev bf16 [k]; h has x's type; rms_eps is the model's.  k <= 8192. */
+pie_status pie_mx_norm(pie_ctx* ctx, const pie_rows* x, const pie_rows* delta, const void* gain, int32_t rows, int32_t k, const pie_rows* h,
+                       const pie_mx_rows* out);
+
+/* Weights in MXFP4 laid out for the products: n_parts matrices [part_rows[i], k] (Linear layout) one below the other, or, with gated
+ * != 0, exactly two of one size, a multiple of 32 rows: gate and up.  The library copies them into its own storage (the caller may free
+ * its tensors afterwards), and on a context's first weight 64 MiB of workspace are allocated; both may not be captured.  Synchronises the
+ * stream.  A weight belongs to the context that made it, is read by its products only, and is freed by pie_mx_weight_destroy (which
+ * waits for the stream) or, at the latest, by pie_destroy.
+ * Errors: PIE_EINVAL, PIE_EUNSUPPORTED (k, or over 2^24 rows), PIE_ENOMEM, PIE_EHIP. */
+typedef struct pie_mx_weight pie_mx_weight;
+pie_status pie_mx_weight_create(pie_ctx* ctx, const pie_mx_rows* parts, const int32_t* part_rows, int32_t n_parts, int32_t k, int32_t gated,
+                                pie_mx_weight** out);
+pie_status pie_mx_weight_destroy(pie_ctx* ctx, pie_mx_weight* weight);
+
+/* out[m][n] = sum over k of a[m][k] w[n][k], in bf16 or fp32, for the weight's rows n in the order of its parts.  a is MXFP8 or MXFP4
+ * with the weight's k.  Sums are held in 32 bits, but a matrix instruction with MXFP8 rows adds eight neighbouring products at a
+ * time aligned to the largest of them: of each it drops what is below 2^-13 of the largest's power of two.  That leaves sums about 1e-5
+ * of the result's size off (at most 2^-10 of the eight's largest product, for each eight); MXFP4 rows lose nothing. */
+pie_status pie_mx_product(pie_ctx* ctx, const pie_mx_rows* a, int32_t rows, const pie_mx_weight* weight, const pie_rows* out);
+/* out = silu(a gate^T) * (a up^T), computed in 32 bits and quantised as pie_mx_quantise does, for a gated weight; out's rows are as
+ * long as the gate has rows. */
+pie_status pie_mx_swiglu(pie_ctx* ctx, const pie_mx_rows* a, int32_t rows, const pie_mx_weight* weight, const pie_mx_rows* out);
+
+/* pie_load_layer for weights in MXFP4: weights[PIE_PROJ_Q .. PIE_PROJ_DOWN], [out, in] each.  A layer loaded so runs with activations in
+ * MXFP8 in front of every product: the norms and the SwiGLU write them, the attention output is quantised; the residual stays in fp32.
+ * pie_forward, pie_forward_all and pie_forward_dist take such layers as others, and layers of both kinds in one model; adapters
+ * that carry a pair in such a layer are refused there (PIE_EUNSUPPORTED, before anything is launched), and PIE_TAP_ACT gives the values that its activations
+ * stand for.  The layer's previous weights are freed.  Synchronises the stream.
+ * Errors: PIE_EINVAL, PIE_ERANGE (layer), PIE_ENOMEM, PIE_EHIP. */
+pie_status pie_load_layer_mx(pie_ctx* ctx, int32_t layer, const void* g1, const void* g2, const pie_mx_rows* weights);
+
 /* Waits for the context's stream (Table 1, `synchronize`: completion of the calls issued so far). */
 pie_status pie_synchronize(pie_ctx* ctx);
 

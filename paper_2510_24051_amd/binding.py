@@ -51,6 +51,14 @@ class BeamSearchC(C.Structure):
                 ("eos_token", C.c_int32), ("n_out", C.c_int32), ("temperature", C.c_float)]
 
 
+class RowsC(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("dtype", C.c_int32), ("row_stride", C.c_int64)]
+
+
+class MxRowsC(C.Structure):
+    _fields_ = [("format", C.c_int32), ("elements", C.c_void_p), ("row_bytes", C.c_int64), ("scales", C.c_void_p), ("scale_bytes", C.c_int64)]
+
+
 def lib_path() -> str:
     return os.path.join(HERE, _LIB_NAME)
 
@@ -93,6 +101,14 @@ def load_library():
         "pie_compact_kvpage": [vp, i32] + [vp] * 7,
         "pie_beam_select": [vp, C.POINTER(BeamSearchC), vp, i32, i64, i32, vp, vp, vp],
         "pie_get_next_beams": [vp, C.POINTER(BeamSearchC), vp, vp, vp, vp],
+        "pie_mx_quantise": [vp, C.POINTER(RowsC), i32, i32, C.POINTER(MxRowsC)],
+        "pie_mx_dequantise": [vp, C.POINTER(MxRowsC), i32, i32, C.POINTER(RowsC)],
+        "pie_mx_norm": [vp, C.POINTER(RowsC), C.POINTER(RowsC), vp, i32, i32, C.POINTER(RowsC), C.POINTER(MxRowsC)],
+        "pie_mx_weight_create": [vp, C.POINTER(MxRowsC), vp, i32, i32, i32, C.POINTER(vp)],
+        "pie_mx_weight_destroy": [vp, vp],
+        "pie_mx_product": [vp, C.POINTER(MxRowsC), i32, vp, C.POINTER(RowsC)],
+        "pie_mx_swiglu": [vp, C.POINTER(MxRowsC), i32, vp, C.POINTER(MxRowsC)],
+        "pie_load_layer_mx": [vp, i32, vp, vp, C.POINTER(MxRowsC)],
         "pie_forward_host": [vp, i32, C.POINTER(ForwardBatchC), i32],
         "pie_get_next_dist": [vp, vp, i32, i32, f32, vp, vp],
         "pie_get_next_dist_static": [vp, vp, i32, i32, f32, vp, vp],
@@ -161,6 +177,61 @@ def _at(a):
         return C.addressof(C.c_char.from_buffer(a))
     except TypeError:  # a read-only array
         return a.__array_interface__["data"][0]
+
+
+def _row_types() -> dict:
+    return {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+
+MX_FORMATS = {"mxfp8": 0, "mxfp4": 1}
+
+
+class MxRows:
+    """Rows in a microscaled format: `elements` [rows, k] ("mxfp8", one byte each: uint8 or float8_e4m3fn) or [rows, k / 2] ("mxfp4", uint8, the
+    first of two in the low half), `scales` (uint8 or float8_e8m0fnu) [rows, k / 32 up to the next multiple of 4].  Rows may be strided
+    (elements by multiples of 16 bytes, scales of 4)."""
+
+    def __init__(self, format: str, elements: torch.Tensor, scales: torch.Tensor):
+        if format not in MX_FORMATS:
+            raise ValueError(f"microscaled rows: format {format!r} is none of {', '.join(MX_FORMATS)}")
+        for t, types in ((elements, (torch.uint8, torch.float8_e4m3fn) if format == "mxfp8" else (torch.uint8,)),
+                         (scales, (torch.uint8, torch.float8_e8m0fnu))):
+            if t.dtype not in types or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+                raise ValueError("microscaled rows: elements and scales are tensors [rows, bytes] of 8-bit types whose rows are contiguous")
+        self.format, self.elements, self.scales = format, elements, scales
+        self.rows, self.k = elements.shape[0], elements.shape[1] * (1 if format == "mxfp8" else 2)
+        if self.k == 0 or self.k % 32 or scales.shape != (self.rows, (self.k // 32 + 3) // 4 * 4):
+            raise ValueError("microscaled rows: k is a multiple of 32, and scales are [rows, k / 32 up to the next multiple of 4]")
+        self._c = MxRowsC(MX_FORMATS[format], elements.data_ptr(), self._stride(elements), scales.data_ptr(), self._stride(scales))
+
+    @staticmethod
+    def _stride(t: torch.Tensor) -> int:
+        return t.stride(0) if t.shape[0] > 1 else (t.shape[1] + 15) // 16 * 16
+
+    @classmethod
+    def empty(cls, rows: int, k: int, format: str, device="cuda") -> "MxRows":
+        if k <= 0 or k % 32:
+            raise ValueError("microscaled rows: k is a multiple of 32")
+        return cls(format, torch.empty((rows, k // (2 if format == "mxfp4" else 1)), dtype=torch.uint8, device=device),
+                   torch.empty((rows, (k // 32 + 3) // 4 * 4), dtype=torch.uint8, device=device))
+
+
+class MxWeight:
+    """Weights of products (pie_mx_weight_create): `n` output rows (of a gated weight: the gate's), `k` inputs."""
+
+    def __init__(self, owner: "Pie", handle, n: int, k: int, gated: bool):
+        self.owner, self.handle, self.n, self.k, self.gated = owner, handle, n, k, gated
+
+    def destroy(self):
+        if self.handle is not None and self.owner.ctx is not None:
+            self.owner._check(self.owner.lib.pie_mx_weight_destroy(self.owner.ctx, self.handle))
+        self.handle = None
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
 
 
 class PieBatch:
@@ -305,6 +376,22 @@ class Pie:
         torch.cuda.synchronize(self.device)
         self._check(self.lib.pie_load_layer(self.ctx, layer, *[C.c_void_p(t.data_ptr()) for t in ts]))
         del ts
+
+    def load_layer_mx(self, layer: int, w):
+        """pie_load_layer_mx: w.g1 and w.g2 as for load_layer, w.wq, w.wk, w.wv, w.wo, w.wgate, w.wup and w.wdown MxRows in MXFP4."""
+        m, dev = self.model, self._device()
+        q, kv = m.n_q_heads * m.head_dim, m.n_kv_heads * m.head_dim
+        shapes = {"wq": (q, m.hidden), "wk": (kv, m.hidden), "wv": (kv, m.hidden), "wo": (m.hidden, q), "wgate": (m.mlp_dim, m.hidden),
+                  "wup": (m.mlp_dim, m.hidden), "wdown": (m.hidden, m.mlp_dim)}
+        parts = [getattr(w, n) for n in self.PROJECTIONS]
+        for n, p in zip(self.PROJECTIONS, parts):
+            if not isinstance(p, MxRows) or p.format != "mxfp4" or (p.rows, p.k) != shapes[n] or p.elements.device != dev or p.scales.device != dev:
+                raise ValueError(f"load_layer_mx: {n} is {shapes[n]} in mxfp4 on the context's device")
+        g = [self._dev_bf16(x) for x in (w.g1, w.g2)]
+        if any(x.numel() != m.hidden for x in g):
+            raise ValueError("load_layer_mx: gains have one value per hidden dimension")
+        torch.cuda.synchronize(dev)
+        self._check(self.lib.pie_load_layer_mx(self.ctx, layer, g[0].data_ptr(), g[1].data_ptr(), (MxRowsC * 7)(*[p._c for p in parts])))
 
     def load_head(self, head):
         g = None if head.g_final is None else self._dev_bf16(head.g_final)
@@ -541,6 +628,71 @@ class Pie:
         self.get_next_beams_async(embed_ids, group_indptr, n_out, ob, ot, os_, s, f, eos_token, temperature)
         self.synchronize()
         return ob.cpu().numpy(), ot.cpu().numpy(), os_.cpu().numpy()
+
+    # ---- microscaled formats ----
+    # Inputs are as torch's current stream leaves them, and what that stream gets afterwards sees the outputs.
+    def _rows(self, t: torch.Tensor, rows: int, k: int, what: str, types=None) -> RowsC:
+        numbers = _row_types()
+        types = numbers if types is None else types
+        if t.dtype not in types or t.device != self._device() or t.shape != (rows, k) or (k > 1 and t.stride(1) != 1):
+            raise ValueError(f"{what} is a tensor [{rows}, {k}] on the context's device whose rows are contiguous, of "
+                             + ", ".join(str(x).replace("torch.", "") for x in types))
+        return RowsC(t.data_ptr(), numbers[t.dtype], t.stride(0) if rows > 1 else k)
+
+    def _mx_rows(self, r: MxRows, rows: int, k: int, what: str) -> MxRowsC:
+        dev = self._device()
+        if not isinstance(r, MxRows) or r.rows != rows or r.k != k or r.elements.device != dev or r.scales.device != dev:
+            raise ValueError(f"{what}: MxRows of {rows} rows of {k} on the context's device")
+        return r._c
+
+    def mx_quantise(self, x: torch.Tensor, out: MxRows):
+        """pie_mx_quantise: out = x [rows, k] (float32, bfloat16 or float16; rows may be strided)."""
+        o = self._mx_rows(out, out.rows, out.k, "mx_quantise")
+        self._ordered(self.lib.pie_mx_quantise, self.ctx, self._rows(x, out.rows, out.k, "mx_quantise: x"), out.rows, out.k, o)
+
+    def mx_dequantise(self, a: MxRows, out: torch.Tensor):
+        """pie_mx_dequantise: out [rows, k] (float32, bfloat16 or float16; rows may be strided) = the values of a."""
+        r = self._mx_rows(a, a.rows, a.k, "mx_dequantise")
+        self._ordered(self.lib.pie_mx_dequantise, self.ctx, r, a.rows, a.k, self._rows(out, a.rows, a.k, "mx_dequantise: out"))
+
+    def mx_norm(self, x: torch.Tensor, gain: torch.Tensor, out: MxRows, delta: Optional[torch.Tensor] = None, h: Optional[torch.Tensor] = None):
+        """pie_mx_norm: h = x + delta, out = rmsnorm(h) * gain.  gain: bfloat16 [k]; h may be x."""
+        rows, k = out.rows, out.k
+        o = self._mx_rows(out, rows, k, "mx_norm")
+        if gain.dtype != torch.bfloat16 or gain.shape != (k,) or gain.device != self.device or not gain.is_contiguous():
+            raise ValueError("mx_norm: gain is a contiguous bfloat16 tensor [k] on the context's device")
+        rx = self._rows(x, rows, k, "mx_norm: x")
+        rd = None if delta is None else self._rows(delta, rows, k, "mx_norm: delta")
+        rh = None if h is None else self._rows(h, rows, k, "mx_norm: h", (x.dtype,))
+        self._ordered(self.lib.pie_mx_norm, self.ctx, rx, rd, gain.data_ptr(), rows, k, rh, o)
+
+    def mx_weight(self, parts, gated: bool = False) -> MxWeight:
+        """pie_mx_weight_create: matrices in MXFP4, one below the other, or gate and up."""
+        parts, dev = list(parts), self._device()
+        if not parts or any(not isinstance(p, MxRows) or p.k != parts[0].k or p.elements.device != dev or p.scales.device != dev for p in parts):
+            raise ValueError("mx_weight: MxRows of one k on the context's device")
+        torch.cuda.synchronize(dev)
+        n = np.array([p.rows for p in parts], _INT32)
+        h = C.c_void_p()
+        self._check(self.lib.pie_mx_weight_create(self.ctx, (MxRowsC * len(parts))(*[p._c for p in parts]), _ptr(n), len(parts), parts[0].k, int(gated),
+                                                  C.byref(h)))
+        return MxWeight(self, h, int(n[0] if gated else n.sum()), parts[0].k, gated)
+
+    def _mx_weight(self, w: MxWeight, a: MxRows, what: str) -> MxRowsC:
+        if not isinstance(w, MxWeight) or w.handle is None:
+            raise ValueError(f"{what}: the weight is an MxWeight that has not been destroyed")
+        return self._mx_rows(a, a.rows, w.k, f"{what}: a")
+
+    def mx_product(self, a: MxRows, w: MxWeight, out: torch.Tensor):
+        """pie_mx_product: out [rows, n] (bfloat16 or float32; rows may be strided) = a w^T."""
+        r = self._mx_weight(w, a, "mx_product")
+        self._ordered(self.lib.pie_mx_product, self.ctx, r, a.rows, w.handle,
+                      self._rows(out, a.rows, w.n, "mx_product: out", (torch.bfloat16, torch.float32)))
+
+    def mx_swiglu(self, a: MxRows, w: MxWeight, out: MxRows):
+        """pie_mx_swiglu: out [rows, n] = silu(a gate^T) * (a up^T) for a gated weight."""
+        r = self._mx_weight(w, a, "mx_swiglu")
+        self._ordered(self.lib.pie_mx_swiglu, self.ctx, r, a.rows, w.handle, self._mx_rows(out, a.rows, w.n, "mx_swiglu: out"))
 
     def synchronize(self):
         self._check(self.lib.pie_synchronize(self.ctx))

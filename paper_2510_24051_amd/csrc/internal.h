@@ -21,11 +21,25 @@ struct PackedWeight {
   int NB = 0;  // number of 32-row blocks stored (N rounded up)
 };
 
+struct MxPacked {  // MXFP4 weights, tiled (see mx_pack_kernel)
+  uint8_t* data = nullptr;     // [NB][KT][64 lanes][16 bytes]
+  uint32_t* scales = nullptr;  // [NB][KQ][64 lanes], behind the data
+  int N = 0, K = 0;            // rows, inputs
+  int NB = 0, KT = 0, KQ = 0;  // blocks of 32 rows, steps of 64 inputs, groups of four steps
+};
+struct pie_mx_weight {
+  const pie_ctx* owner = nullptr;
+  MxPacked w;
+  bool gated = false;
+};
+
 struct LayerWeights {
   bool loaded = false;
+  bool mx = false;  // the weights are mqkv, mo, mgu and mdown
   bf16_t* g1 = nullptr;
   bf16_t* g2 = nullptr;
   PackedWeight wqkv, wo, wgu, wdown;  // wgu: gate/up interleaved in 32-row blocks
+  MxPacked mqkv, mo, mgu, mdown;      // the same in MXFP4
 };
 
 // ---- KvPage pool layout ----------------------------------------------------------------------
@@ -168,6 +182,9 @@ struct pie_ctx {
   float *h = nullptr, *splitk = nullptr, *logits = nullptr, *topk_stats = nullptr;
   unsigned long long* topk_cand = nullptr;
   size_t splitk_elems = 0;
+  std::vector<pie_mx_weight*> mx_weights;  // the caller's
+  float* mx_ws = nullptr;                  // workspace of the products with them, MX_WS_FLOATS
+  uint8_t* mx_act = nullptr;               // microscaled activations of a layer (pie_load_layer_mx): see MxActs
   // device blocks of destroyed batches, kept for the next pie_batch_create (a serving loop creates and destroys a
   // batch per step; hipMalloc + hipFree cost more than the deserialisation itself)
   std::vector<std::pair<void*, size_t>> blob_pool;
@@ -193,6 +210,7 @@ struct pie_ctx {
   int32_t* ids_dev = nullptr;  // staging for id lists of the small resource calls
   size_t ids_cap = 0;
   int last_T = 0, last_dist_n = 0;
+  bool last_mx = false;        // the last layer that ran had microscaled weights
   const float* last_logits = nullptr;  // logits of the last get_next_dist call (workspace or static scratch)
   unsigned char* static_scratch = nullptr;  // device address of this GPU's static scratch array (pie_get_next_dist_static)
   // timing
@@ -401,3 +419,56 @@ struct CompactPlan {
 hipError_t launch_put_plan(const unsigned char* plan, size_t size, unsigned char* dev, size_t turns, int n_turns, const double* inv_freq, int D,
                            float* angles, hipStream_t s);
 hipError_t launch_compact(const CompactPlan& plan, int n_chains, int n_layers, int Hkv, int D, hipStream_t s);
+
+// Microscaled rows, weights and products (mx.hip)
+#define MX_WS_FLOATS ((size_t)16 << 20)
+struct MxRowsView {  // pie_mx_rows without its format
+  uint8_t* elements;
+  int64_t row_bytes;
+  uint8_t* scales;
+  int64_t scale_bytes;
+};
+struct RowsView {  // pie_rows
+  const void* p;
+  int64_t stride;
+  int dtype;
+  int vec;  // base and stride are multiples of 16 bytes
+};
+RowsView mx_view(const void* p, int dtype, int64_t stride);
+struct MxNormArgs {
+  RowsView x, delta, h;      // delta.p, h.p may be null; h.dtype is x's
+  const int32_t* ids;        // x's row of each row, or null: its own
+  const float* part;         // split sums added to x: [splits][rows][part_stride], split_stride apart
+  int64_t part_stride, split_stride;
+  int splits;
+  const bf16_t* gain;
+  int gain_vec;              // 16-byte aligned
+  float eps;
+};
+hipError_t launch_mx_quantise(const RowsView& x, int rows, int k, int format, const MxRowsView& out, hipStream_t s);
+hipError_t launch_mx_dequantise(const MxRowsView& a, int format, int rows, int k, const RowsView& out, hipStream_t s);
+hipError_t launch_mx_norm(const MxNormArgs& a, int rows, int k, int format, const MxRowsView& out, hipStream_t s);
+// rows of `src` become rows [first, first + rows) of the weight; interleave: its 32-row blocks become blocks 2 b + first
+hipError_t launch_mx_pack(const MxRowsView& src, int rows, int k, int first, int interleave, const MxPacked& w, hipStream_t s);
+enum MxMode {
+  MX_BF16 = 0,         // out bf16 [M, ldo]
+  MX_F32 = 1,          // out fp32 [M, ldo]
+  MX_RESID_EMBED = 2,  // out fp32 = embeds[ids[m]] + sum, or resid[m] + sum where resid is given
+  MX_RESID_OUT = 3,    // embeds[ids[m]] = bf16(resid[m] + sum) where ids[m] >= 0, or out fp32 = resid[m] + sum where out is given
+  MX_SWIGLU8 = 4,      // out, scales: MXFP8 rows of silu(gate) * up
+  MX_SWIGLU4 = 5       // the same in MXFP4
+};
+struct MxEpi {
+  int mode;
+  void* out;
+  int64_t ldo;  // elements, or bytes of the SwiGLU's rows
+  uint8_t* scales;
+  int64_t lds;
+  int N;    // columns stored
+  int vec;  // rows of whole groups of eight (bf16) or four (fp32), 16-byte aligned
+  bf16_t* embeds;
+  const int32_t* ids;
+  const float* resid;
+  int H;
+};
+hipError_t launch_mx_product(const MxRowsView& a, int format, int M, const MxPacked& w, const MxEpi& epi, hipStream_t s);

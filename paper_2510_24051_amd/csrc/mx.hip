@@ -1,0 +1,469 @@
+// Microscaled rows (blocks of 32 values, a power of two as scale, elements E4M3 or E2M1): quantisation, the norm that adds the residual
+// and writes them, the layout of 4-bit weights, and the products of both on the scaled matrix instructions.
+#include <algorithm>
+
+#include "internal.h"
+
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+// ---------------------------------------------------------------------------------------------
+// A block's scale and elements
+// ---------------------------------------------------------------------------------------------
+// Magnitudes are compared as the bits they are: finite < infinity < NaN.
+__device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+// floor(log2 max) - EMAX + 127, at least 0.  (A denormal maximum has exponent field 0 and a scale of 2^-127, as its logarithm asks for.)
+template <int FMT>
+__device__ __forceinline__ uint32_t scale_byte(uint32_t most) {
+  constexpr int EMAX = FMT == PIE_MXFP8 ? 8 : 2;
+  return most >= 0x7f800000u ? 255u : (uint32_t)max((int)(most >> 23) - EMAX, 0);
+}
+// 2^(127 - byte), by which elements are multiplied (exactly: what becomes denormal rounds to 0 in either format); 0 for a NaN block.
+__device__ __forceinline__ float unscale(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
+__device__ __forceinline__ float element(float v, float un, bool nan) { return nan ? 0.f : v * un; }
+
+// Four values -> four E4M3, nearest even.  (The conversion itself saturates up to 464 and then gives NaN, so it is fed at most 448.)
+__device__ __forceinline__ uint32_t to_fp8x4(float a, float b, float c, float d) {
+  auto sat = [](float v) { return __builtin_amdgcn_fmed3f(v, 448.f, -448.f); };
+  int r = __builtin_amdgcn_cvt_pk_fp8_f32(sat(a), sat(b), 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(sat(c), sat(d), r, true);
+}
+// Eight values -> eight E2M1, nearest even, saturating (the conversion does).
+__device__ __forceinline__ uint32_t to_fp4x8(const float (&v)[8]) {
+  uint32_t r = 0;
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, v[0], v[1], 1.f, 0);
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, v[2], v[3], 1.f, 1);
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, v[4], v[5], 1.f, 2);
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, v[6], v[7], 1.f, 3);
+  return r;
+}
+
+// Eight values of a lane, four neighbouring lanes to a block: elements and, by the first of the four, the scale.
+template <int FMT>
+__device__ __forceinline__ void put_eight(const float (&v)[8], uint8_t* elements, uint8_t* scales, int c) {
+  uint32_t most = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) most = max(most, magnitude(v[e]));
+  most = max(most, (uint32_t)__shfl_xor((int)most, 1));
+  most = max(most, (uint32_t)__shfl_xor((int)most, 2));
+  const uint32_t byte = scale_byte<FMT>(most);
+  const bool nan = byte == 255u;
+  const float un = unscale(byte);
+  float s[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) s[e] = element(v[e], un, nan);
+  if (FMT == PIE_MXFP8) {
+    const u32x2 r = {to_fp8x4(s[0], s[1], s[2], s[3]), to_fp8x4(s[4], s[5], s[6], s[7])};
+    *reinterpret_cast<u32x2*>(elements + c) = r;
+  } else {
+    *reinterpret_cast<uint32_t*>(elements + (c >> 1)) = to_fp4x8(s);
+  }
+  if ((c & 31) == 0) scales[c >> 5] = (uint8_t)byte;
+}
+// The bytes behind a row's last scale, up to a multiple of four.
+__device__ __forceinline__ void pad_scales(uint8_t* scales, int k) {
+  for (int b = k >> 5; b & 3; ++b) scales[b] = 0;
+}
+
+// ---------------------------------------------------------------------------------------------
+// Rows of plain values
+// ---------------------------------------------------------------------------------------------
+RowsView mx_view(const void* p, int dtype, int64_t stride) {
+  const int size = dtype == PIE_F32 ? 4 : 2;
+  return RowsView{p, stride, dtype, reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride * size % 16 == 0};
+}
+__device__ __forceinline__ void load8(const RowsView& r, int64_t row, int c, float (&v)[8]) {
+  const int64_t at = row * r.stride + c;
+  if (r.dtype == PIE_F32) {
+    const float* p = reinterpret_cast<const float*>(r.p) + at;
+    if (r.vec) {
+      const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) { v[e] = a[e]; v[4 + e] = b[e]; }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = p[e];
+    }
+    return;
+  }
+  const uint16_t* p = reinterpret_cast<const uint16_t*>(r.p) + at;
+  Pack16 k;
+  if (r.vec) {
+    k.u = *reinterpret_cast<const u32x4*>(p);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) k.s[e] = p[e];
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = r.dtype == PIE_BF16 ? bf16_bits_to_f32(k.s[e]) : (float)__builtin_bit_cast(_Float16, k.s[e]);
+}
+// Rounds v to r's type (v becomes what is stored) and, where r.p is given, stores it.
+__device__ __forceinline__ void store8(const RowsView& r, int64_t row, int c, float (&v)[8]) {
+  const int64_t at = row * r.stride + c;
+  if (r.dtype == PIE_F32) {
+    float* p = const_cast<float*>(reinterpret_cast<const float*>(r.p)) + at;
+    if (r.p == nullptr) return;
+    if (r.vec) {
+      *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
+      *reinterpret_cast<f32x4*>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) p[e] = v[e];
+    }
+    return;
+  }
+  Pack16 k;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    k.s[e] = r.dtype == PIE_BF16 ? __builtin_bit_cast(uint16_t, f32_to_bf16(v[e])) : __builtin_bit_cast(uint16_t, (_Float16)v[e]);
+    v[e] = r.dtype == PIE_BF16 ? bf16_bits_to_f32(k.s[e]) : (float)__builtin_bit_cast(_Float16, k.s[e]);
+  }
+  if (r.p == nullptr) return;
+  uint16_t* p = const_cast<uint16_t*>(reinterpret_cast<const uint16_t*>(r.p)) + at;
+  if (r.vec) {
+    *reinterpret_cast<u32x4*>(p) = k.u;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) p[e] = k.s[e];
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// Quantisation and its inverse: eight values a lane
+// ---------------------------------------------------------------------------------------------
+template <int FMT>
+__global__ __launch_bounds__(256) void mx_quantise_kernel(RowsView x, int64_t pieces, int k, MxRowsView out) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= pieces) return;  // (a row's pieces are a multiple of four: the lanes of a block stay together)
+  const int per_row = k >> 3;
+  const int64_t row = i / per_row;
+  const int c = (int)(i - row * per_row) * 8;
+  float v[8];
+  load8(x, row, c, v);
+  uint8_t* scales = out.scales + row * out.scale_bytes;
+  put_eight<FMT>(v, out.elements + row * out.row_bytes, scales, c);
+  if (c == 0) pad_scales(scales, k);
+}
+
+__global__ __launch_bounds__(256) void mx_dequantise_kernel(MxRowsView a, int fmt, int64_t pieces, int k, RowsView out) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= pieces) return;
+  const int per_row = k >> 3;
+  const int64_t row = i / per_row;
+  const int c = (int)(i - row * per_row) * 8;
+  const uint32_t byte = a.scales[row * a.scale_bytes + (c >> 5)];
+  // 2^(byte - 127): a denormal for byte 0
+  const float scale = byte == 255u ? __uint_as_float(0x7fc00000u) : byte == 0 ? __uint_as_float(0x00400000u) : __uint_as_float(byte << 23);
+  float v[8];
+  if (fmt == PIE_MXFP8) {
+    const u32x2 e = *reinterpret_cast<const u32x2*>(a.elements + row * a.row_bytes + c);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)e[j], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)e[j], true);
+      v[4 * j] = lo[0] * scale; v[4 * j + 1] = lo[1] * scale; v[4 * j + 2] = hi[0] * scale; v[4 * j + 3] = hi[1] * scale;
+    }
+  } else {
+    const uint32_t e = *reinterpret_cast<const uint32_t*>(a.elements + row * a.row_bytes + (c >> 1));
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t n = e >> (4 * j), m = n & 7;  // 0, 1/2, then 1.f * 2^(e - 1): the exponent and fraction bits moved into place
+      const float f = m < 2 ? 0.5f * (float)m : __uint_as_float((m << 22) + (126u << 23));
+      v[j] = (n & 8 ? -f : f) * scale;
+    }
+  }
+  store8(out, row, c, v);
+}
+
+static dim3 pieces_grid(int64_t pieces) { return dim3((unsigned)((pieces + 255) / 256)); }
+
+hipError_t launch_mx_quantise(const RowsView& x, int rows, int k, int format, const MxRowsView& out, hipStream_t s) {
+  const int64_t pieces = (int64_t)rows * (k / 8);
+  if (pieces <= 0) return hipSuccess;
+  if (format == PIE_MXFP8) mx_quantise_kernel<PIE_MXFP8><<<pieces_grid(pieces), dim3(256), 0, s>>>(x, pieces, k, out);
+  else mx_quantise_kernel<PIE_MXFP4><<<pieces_grid(pieces), dim3(256), 0, s>>>(x, pieces, k, out);
+  return hipGetLastError();
+}
+
+hipError_t launch_mx_dequantise(const MxRowsView& a, int format, int rows, int k, const RowsView& out, hipStream_t s) {
+  const int64_t pieces = (int64_t)rows * (k / 8);
+  if (pieces <= 0) return hipSuccess;
+  mx_dequantise_kernel<<<pieces_grid(pieces), dim3(256), 0, s>>>(a, format, pieces, k, out);
+  return hipGetLastError();
+}
+
+// ---------------------------------------------------------------------------------------------
+// Norm: one workgroup per row, eight columns a thread, as rmsnorm_row in elementwise.hip
+// ---------------------------------------------------------------------------------------------
+template <int FMT, int THREADS>
+__global__ __launch_bounds__(THREADS) void mx_norm_kernel(MxNormArgs a, int k, MxRowsView out) {
+  __shared__ float red[THREADS / 64];
+  const int64_t row = blockIdx.x;
+  const int tid = threadIdx.x, c = tid * 8;
+  float v[8], ss = 0.f;
+  Pack16 g;
+  if (c < k) {
+    if (a.gain_vec) {
+      g.u = *reinterpret_cast<const u32x4*>(a.gain + c);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) g.h[e] = a.gain[c + e];
+    }
+    const int64_t from = a.ids ? a.ids[row] : row;
+    load8(a.x, from, c, v);
+    if (a.delta.p) {
+      float d[8];
+      load8(a.delta, row, c, d);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] += d[e];
+    }
+    if (a.splits > 0) {  // partial sums of the product before, in their order, then what they are added to
+      f32x4 p = {0.f, 0.f, 0.f, 0.f}, q = p;
+      const float* at = a.part + row * a.part_stride + c;
+      for (int i = 0; i < a.splits; ++i) {
+        p += *reinterpret_cast<const f32x4*>(at + i * a.split_stride);
+        q += *reinterpret_cast<const f32x4*>(at + i * a.split_stride + 4);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) { v[e] += p[e]; v[4 + e] += q[e]; }
+    }
+    store8(a.h, row, c, v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ss += v[e] * v[e];
+  }
+  ss = wave_sum(ss);
+  if constexpr (THREADS > 64) {
+    if ((tid & 63) == 0) red[tid >> 6] = ss;
+    __syncthreads();
+    ss = 0.f;
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) ss += red[w];
+  }
+  const float r = 1.0f / sqrtf(ss / (float)k + a.eps);
+  if (c < k) {  // (k is a multiple of 32: the four lanes of a block go the same way)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = v[e] * r * bf16_to_f32(g.h[e]);
+    uint8_t* scales = out.scales + row * out.scale_bytes;
+    put_eight<FMT>(v, out.elements + row * out.row_bytes, scales, c);
+    if (c == 0) pad_scales(scales, k);
+  }
+}
+
+hipError_t launch_mx_norm(const MxNormArgs& a, int rows, int k, int format, const MxRowsView& out, hipStream_t s) {
+  if (rows <= 0) return hipSuccess;
+  if (k > 8192) return hipErrorInvalidValue;
+  auto go = [&](auto threads_c) {
+    constexpr int T = decltype(threads_c)::value;
+    if (format == PIE_MXFP8) mx_norm_kernel<PIE_MXFP8, T><<<dim3(rows), dim3(T), 0, s>>>(a, k, out);
+    else mx_norm_kernel<PIE_MXFP4, T><<<dim3(rows), dim3(T), 0, s>>>(a, k, out);
+    return hipGetLastError();
+  };
+  using std::integral_constant;
+  if (k <= 512) return go(integral_constant<int, 64>{});
+  if (k <= 2048) return go(integral_constant<int, 256>{});
+  if (k <= 4096) return go(integral_constant<int, 512>{});
+  return go(integral_constant<int, 1024>{});
+}
+
+// ---------------------------------------------------------------------------------------------
+// Weights: tiles of 32 rows x 64 inputs, 1 KiB each, stored [N/32][K/64]; lane l = h * 32 + n of a tile holds the 32 elements of row n
+// and block h (16 bytes): the operand of mfma_scale 32x32x64.  Their scales: [N/32][K/256][64] dwords, byte t of lane l's dword being the
+// scale of its block in tile 4 q + t: one load for four steps, of which the instruction picks the byte.  What is behind the last row
+// or block is 0.
+// ---------------------------------------------------------------------------------------------
+__global__ __launch_bounds__(256) void mx_pack_kernel(MxRowsView src, int rows, int k, int first, int interleave, MxPacked w) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;  // one per (32-row block of the part, k step, lane)
+  const int KT = w.KT;
+  const int64_t total = (int64_t)((rows + 31) / 32) * KT * 64;
+  if (i >= total) return;
+  const int lane = (int)(i & 63), kt = (int)((i >> 6) % KT), sb = (int)((i >> 6) / KT);
+  const int r = sb * 32 + (lane & 31), b = kt * 2 + (lane >> 5);
+  if (r >= rows) return;
+  const int n = interleave ? (2 * sb + first) * 32 + (lane & 31) : first + r;  // row of the stacked (or interleaved) weight
+  const int nb = n >> 5, l = (lane & 32) + (n & 31);
+  const bool real = b < k / 32;
+  u32x4 e = {0, 0, 0, 0};
+  if (real) e = *reinterpret_cast<const u32x4*>(src.elements + r * src.row_bytes + b * 16);
+  *reinterpret_cast<u32x4*>(w.data + (((int64_t)nb * KT + kt) * 64 + l) * 16) = e;
+  reinterpret_cast<uint8_t*>(w.scales)[(((int64_t)nb * w.KQ + (kt >> 2)) * 64 + l) * 4 + (kt & 3)] = real ? src.scales[r * src.scale_bytes + b] : 0;
+}
+
+hipError_t launch_mx_pack(const MxRowsView& src, int rows, int k, int first, int interleave, const MxPacked& w, hipStream_t s) {
+  const int64_t total = (int64_t)((rows + 31) / 32) * w.KT * 64;
+  if (total <= 0) return hipSuccess;
+  mx_pack_kernel<<<pieces_grid(total), dim3(256), 0, s>>>(src, rows, k, first, interleave, w);
+  return hipGetLastError();
+}
+
+// ---------------------------------------------------------------------------------------------
+// Epilogues.  An accumulator tile has a token per lane (l % 32) and weight rows in its registers: v is row (v / 4) * 8 + (l / 32) * 4 + v % 4
+// of the 32, so a lane's four groups are four consecutive columns of its token's row.
+// ---------------------------------------------------------------------------------------------
+__device__ __forceinline__ void swap_halves(uint32_t& a, uint32_t& b) {  // lower lanes: a, a of lane + 32; upper: b of lane - 32, b
+  const auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+  a = r[0];
+  b = r[1];
+}
+
+// Columns [n0, n0 + 32) of token m; `up` is read by the SwiGLU modes alone.
+template <int MODE>
+__device__ __forceinline__ void mx_epilogue(const MxEpi& e, const f32x16& acc, const f32x16& up, int64_t m, int M, int n0, int lane) {
+  const int h = lane >> 5;
+  if constexpr (MODE == MX_SWIGLU8 || MODE == MX_SWIGLU4) {
+    constexpr int FMT = MODE == MX_SWIGLU8 ? PIE_MXFP8 : PIE_MXFP4;
+    float v[16];
+    uint32_t most = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      v[i] = silu_f(acc[i]) * up[i];
+      most = max(most, magnitude(v[i]));
+    }
+    const auto both = __builtin_amdgcn_permlane32_swap(most, most, false, false);
+    const uint32_t byte = scale_byte<FMT>(max((uint32_t)both[0], (uint32_t)both[1]));
+    const bool nan = byte == 255u;
+    const float un = unscale(byte);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = element(v[i], un, nan);
+    const int c = n0 >> 1;  // (n0: the gate block's packed column)
+    uint8_t* row = reinterpret_cast<uint8_t*>(e.out) + m * e.ldo;
+    if (FMT == PIE_MXFP8) {
+      uint32_t g[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) g[i] = to_fp8x4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+      swap_halves(g[0], g[2]);
+      swap_halves(g[1], g[3]);
+      if (m < M) *reinterpret_cast<u32x4*>(row + c + h * 16) = u32x4{g[0], g[2], g[1], g[3]};
+    } else {
+      const float a[8] = {v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]}, b[8] = {v[8], v[9], v[10], v[11], v[12], v[13], v[14], v[15]};
+      uint32_t p = to_fp4x8(a), q = to_fp4x8(b);
+      swap_halves(p, q);
+      if (m < M) *reinterpret_cast<u32x2*>(row + (c >> 1) + h * 8) = u32x2{(p & 0xffffu) | (q << 16), (p >> 16) | (q & 0xffff0000u)};
+    }
+    if (m < M && h == 0) {
+      uint8_t* scales = e.scales + m * e.lds;
+      scales[c >> 5] = (uint8_t)byte;
+      if (c + 32 >= e.N) pad_scales(scales, e.N);
+    }
+  } else if constexpr (MODE == MX_BF16) {
+    bf16_t* row = reinterpret_cast<bf16_t*>(e.out) + m * e.ldo;
+    if (e.vec) {  // rows of whole, aligned groups of eight
+      uint32_t g[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const bf16x2 b = {f32_to_bf16(acc[2 * i]), f32_to_bf16(acc[2 * i + 1])};
+        g[i] = __builtin_bit_cast(uint32_t, b);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) swap_halves(g[i], g[i + 4]);
+      const int n = n0 + h * 16;
+      if (m < M && n < e.N) *reinterpret_cast<u32x4*>(row + n) = u32x4{g[0], g[1], g[4], g[5]};
+      if (m < M && n + 8 < e.N) *reinterpret_cast<u32x4*>(row + n + 8) = u32x4{g[2], g[3], g[6], g[7]};
+    } else if (m < M) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int n = n0 + (i >> 2) * 8 + h * 4 + (i & 3);
+        if (n < e.N) row[n] = f32_to_bf16(acc[i]);
+      }
+    }
+  } else {  // fp32 sums, alone or on a residual
+    if (m >= M) return;
+    const int64_t id = MODE == MX_RESID_EMBED ? (e.resid ? m : (int64_t)e.ids[m]) : MODE == MX_RESID_OUT && !e.out ? e.ids[m] : m;
+    if (MODE == MX_RESID_OUT && id < 0) return;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int n = n0 + i * 8 + h * 4;
+      f32x4 y = {acc[4 * i], acc[4 * i + 1], acc[4 * i + 2], acc[4 * i + 3]};
+      if (n >= e.N) break;
+      if constexpr (MODE == MX_RESID_EMBED || MODE == MX_RESID_OUT) {  // (rows of whole, aligned groups of four)
+        if (MODE == MX_RESID_EMBED && !e.resid) {
+          const bf16x4 r = *reinterpret_cast<const bf16x4*>(e.embeds + id * e.H + n);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) y[j] += bf16_to_f32(r[j]);
+        } else {
+          y += *reinterpret_cast<const f32x4*>(e.resid + m * e.H + n);
+        }
+        if (MODE == MX_RESID_OUT && !e.out) {
+          bf16x4 o;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) o[j] = f32_to_bf16(y[j]);
+          *reinterpret_cast<bf16x4*>(e.embeds + id * e.H + n) = o;
+          continue;
+        }
+      }
+      float* p = reinterpret_cast<float*>(e.out) + m * e.ldo + n;
+      if (e.vec) {
+        *reinterpret_cast<f32x4*>(p) = y;
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (n + j < e.N) p[j] = y[j];
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// Product.  D[weight row][token] = W x A^T on v_mfma_scale_f32_32x32x64_f8f6f4: a lane of the weight operand has 32 elements of one block; a
+// lane of an MXFP8 operand has bytes [16 h, 16 h + 16) and [32 + 16 h, 48 + 16 h) of its row's 64, and in either case the scale of block
+// h of its row.  A wave takes 32 weight rows (SwiGLU: a gate and an up block) and 32 tokens.
+// ---------------------------------------------------------------------------------------------
+template <int MODE, int FMT>
+__global__ __launch_bounds__(256) void mx_product_kernel(MxRowsView a, int M, MxPacked w, MxEpi epi, int tiles_m) {
+  constexpr int NJ = MODE == MX_SWIGLU8 || MODE == MX_SWIGLU4 ? 2 : 1;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
+  const int nb0 = ((int)(blockIdx.x / tiles_m) * 4 + wave) * NJ;
+  if (nb0 >= w.NB) return;
+  const int64_t m = (int64_t)(blockIdx.x % tiles_m) * 32 + (lane & 31);
+  const int64_t row = m < M ? m : M - 1;  // rows past M re-read a valid row; their results are not stored
+  const uint8_t* ap = a.elements + row * a.row_bytes;
+  const uint8_t* as = a.scales + row * a.scale_bytes;
+  const int blocks = w.K / 32;
+  f32x16 acc[NJ];
+#pragma unroll
+  for (int j = 0; j < NJ; ++j)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) acc[j][v] = 0.f;
+  for (int kt = 0; kt < w.KT; ++kt) {
+    const int b = kt * 2;
+    u32x4 lo = {0, 0, 0, 0}, hi = lo;
+    if (FMT == PIE_MXFP8) {
+      lo = *reinterpret_cast<const u32x4*>(ap + b * 32 + h * 16);
+      if (b + 1 < blocks) hi = *reinterpret_cast<const u32x4*>(ap + b * 32 + 32 + h * 16);
+    } else if (b + h < blocks) {
+      lo = *reinterpret_cast<const u32x4*>(ap + (b + h) * 16);
+    }
+    const int sb = b + h < blocks ? as[b + h] : 0;
+    const i32x8 bo = {(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      const u32x4 e = *reinterpret_cast<const u32x4*>(w.data + (((int64_t)(nb0 + j) * w.KT + kt) * 64 + lane) * 16);
+      const int sa = (int)(w.scales[((int64_t)(nb0 + j) * w.KQ + (kt >> 2)) * 64 + lane] >> (8 * (kt & 3)));
+      const i32x8 ao = {(int)e[0], (int)e[1], (int)e[2], (int)e[3], 0, 0, 0, 0};
+      acc[j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ao, bo, acc[j], 4, FMT == PIE_MXFP8 ? 0 : 4, 0, sa, 0, sb);
+    }
+  }
+  mx_epilogue<MODE>(epi, acc[0], acc[NJ - 1], m, M, nb0 * 32, lane);
+}
+
+template <int MODE>
+static hipError_t run_product(const MxRowsView& a, int format, int M, const MxPacked& w, const MxEpi& epi, hipStream_t s) {
+  const int cols = MODE == MX_SWIGLU8 || MODE == MX_SWIGLU4 ? w.NB / 2 : w.NB;
+  const int tiles_m = (M + 31) / 32;
+  const int64_t tiles = (int64_t)((cols + 3) / 4) * tiles_m;
+  if (tiles > INT32_MAX) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)tiles);
+  if (format == PIE_MXFP8) mx_product_kernel<MODE, PIE_MXFP8><<<grid, dim3(256), 0, s>>>(a, M, w, epi, tiles_m);
+  else mx_product_kernel<MODE, PIE_MXFP4><<<grid, dim3(256), 0, s>>>(a, M, w, epi, tiles_m);
+  return hipGetLastError();
+}
+
+hipError_t launch_mx_product(const MxRowsView& a, int format, int M, const MxPacked& w, const MxEpi& e, hipStream_t s) {
+  if (M <= 0) return hipSuccess;
+  switch (e.mode) {
+    case MX_BF16: return run_product<MX_BF16>(a, format, M, w, e, s);
+    case MX_F32: return run_product<MX_F32>(a, format, M, w, e, s);
+    case MX_RESID_EMBED: return run_product<MX_RESID_EMBED>(a, format, M, w, e, s);
+    case MX_RESID_OUT: return run_product<MX_RESID_OUT>(a, format, M, w, e, s);
+    case MX_SWIGLU8: return run_product<MX_SWIGLU8>(a, format, M, w, e, s);
+    case MX_SWIGLU4: return run_product<MX_SWIGLU4>(a, format, M, w, e, s);
+  }
+  return hipErrorInvalidValue;
+}

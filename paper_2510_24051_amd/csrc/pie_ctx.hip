@@ -206,6 +206,16 @@ static void free_packed(PackedWeight& w) {
   w = PackedWeight();
 }
 
+static void free_packed(MxPacked& w) {
+  if (w.data) (void)hipFree(w.data);
+  w = MxPacked();
+}
+
+static void free_weights(LayerWeights& L) {
+  free_packed(L.wqkv); free_packed(L.wo); free_packed(L.wgu); free_packed(L.wdown);
+  free_packed(L.mqkv); free_packed(L.mo); free_packed(L.mgu); free_packed(L.mdown);
+}
+
 extern "C" pie_status pie_destroy(pie_ctx* c) {
   if (!c) return PIE_OK;
   if (c->host_only) {  // nothing lives on a device
@@ -217,11 +227,15 @@ extern "C" pie_status pie_destroy(pie_ctx* c) {
   for (auto& L : c->layers) {
     if (L.g1) (void)hipFree(L.g1);
     if (L.g2) (void)hipFree(L.g2);
-    free_packed(L.wqkv); free_packed(L.wo); free_packed(L.wgu); free_packed(L.wdown);
+    free_weights(L);
   }
   free_packed(c->wlm);
+  for (pie_mx_weight* w : c->mx_weights) {
+    free_packed(w->w);
+    delete w;
+  }
   void* bufs[] = {c->embeds, c->kv, c->xn, c->qkv, c->attn, c->h, c->act, c->splitk, c->logits, c->en,
-                  c->ids_dev, c->inv_freq, c->g_final, c->topk_cand, c->topk_stats, c->beam_ws, c->moves_dev, c->table, c->x32, c->lora_dev, c->lora_z, c->gu32};
+                  c->ids_dev, c->inv_freq, c->g_final, c->topk_cand, c->topk_stats, c->beam_ws, c->moves_dev, c->table, c->x32, c->lora_dev, c->lora_z, c->gu32, c->mx_ws, c->mx_act};
   for (LoraPair& lp : c->lora) {
     if (lp.A) (void)hipFree(lp.A);
     if (lp.B) (void)hipFree(lp.B);
@@ -265,8 +279,12 @@ extern "C" pie_status pie_load_layer(pie_ctx* c, int32_t layer, const void* g1, 
   if (layer < 0 || layer >= c->m.n_layers) return fail(c, PIE_ERANGE, "pie_load_layer: layer %d of %d", layer, c->m.n_layers);
   const int H = c->m.hidden, QD = c->m.n_q_heads * c->m.head_dim, KD = c->m.n_kv_heads * c->m.head_dim, I = c->m.mlp_dim;
   LayerWeights& L = c->layers[layer];
-  L.loaded = false;
+  L.loaded = L.mx = false;
   pie_status st;
+  if (L.mqkv.data) {  // (the layer may be in use by what is enqueued)
+    HIP_TRY(c, hipStreamSynchronize(c->stream));
+    free_weights(L);
+  }
   if ((st = copy_gain(c, &L.g1, g1, H)) != PIE_OK) return st;
   if ((st = copy_gain(c, &L.g2, g2, H)) != PIE_OK) return st;
   if ((st = pack_into(c, L.wqkv, QD + 2 * KD, H, wq, QD, wk, KD, wv, KD, 0)) != PIE_OK) return st;
@@ -1924,6 +1942,249 @@ extern "C" pie_status pie_compact_kvpage(pie_ctx* c, int32_t n_seqs, const int32
 }
 
 // ---------------------------------------------------------------------------------------------
+// microscaled formats
+// ---------------------------------------------------------------------------------------------
+#define MX_MAX_K (1 << 20)
+#define MX_MAX_ROWS (1 << 24)
+
+static MxRowsView mx_rows_view(const pie_mx_rows* r) {
+  return MxRowsView{reinterpret_cast<uint8_t*>(r->elements), r->row_bytes, r->scales, r->scale_bytes};
+}
+static int64_t mx_row_size(int format, int64_t k) { return format == PIE_MXFP8 ? k : k / 2; }
+
+static pie_status check_mx_shape(pie_ctx* c, int32_t rows, int32_t k, const char* who) {
+  if (!c) return PIE_EINVAL;
+  if (c->host_only) return fail(c, PIE_EINVAL, "%s: the context only plans batches (pie_create_planner)", who);
+  if (rows < 0 || k <= 0 || k % 32) return fail(c, PIE_EINVAL, "%s: %d rows of %d values: k has to be a multiple of 32", who, rows, k);
+  if (k > MX_MAX_K || rows > MX_MAX_ROWS) return fail(c, PIE_EUNSUPPORTED, "%s: %d rows of %d values: at most %d of %d", who, rows, k, MX_MAX_ROWS, MX_MAX_K);
+  return PIE_OK;
+}
+static pie_status check_mx_rows(pie_ctx* c, const pie_mx_rows* r, int32_t k, const char* who) {
+  if (!r || !r->elements || !r->scales) return fail(c, PIE_EINVAL, "%s: null microscaled rows", who);
+  if (r->format != PIE_MXFP8 && r->format != PIE_MXFP4) return fail(c, PIE_EINVAL, "%s: format %d", who, r->format);
+  if (reinterpret_cast<uintptr_t>(r->elements) % 16 || r->row_bytes % 16 || r->row_bytes < mx_row_size(r->format, k))
+    return fail(c, PIE_EINVAL, "%s: elements have to be 16-byte aligned, their rows a multiple of 16 bytes apart and at least %lld", who, (long long)mx_row_size(r->format, k));
+  if (reinterpret_cast<uintptr_t>(r->scales) % 4 || r->scale_bytes % 4 || r->scale_bytes < k / 32)
+    return fail(c, PIE_EINVAL, "%s: scales have to be 4-byte aligned, their rows a multiple of 4 bytes apart and at least %d", who, k / 32);
+  return PIE_OK;
+}
+static pie_status check_rows(pie_ctx* c, const pie_rows* r, int32_t k, const char* what, const char* who) {
+  if (!r || !r->data) return fail(c, PIE_EINVAL, "%s: null %s", who, what);
+  if (r->dtype != PIE_F32 && r->dtype != PIE_BF16 && r->dtype != PIE_F16) return fail(c, PIE_EINVAL, "%s: type %d of %s", who, r->dtype, what);
+  if (r->row_stride < k) return fail(c, PIE_EINVAL, "%s: rows of %s overlap (stride %lld, %d values)", who, what, (long long)r->row_stride, k);
+  if (reinterpret_cast<uintptr_t>(r->data) % (r->dtype == PIE_F32 ? 4 : 2)) return fail(c, PIE_EINVAL, "%s: %s is not aligned to its type", who, what);
+  return PIE_OK;
+}
+static RowsView rows_view(const pie_rows* r) { return r ? mx_view(r->data, r->dtype, r->row_stride) : mx_view(nullptr, PIE_F32, 0); }
+
+extern "C" pie_status pie_mx_quantise(pie_ctx* c, const pie_rows* x, int32_t rows, int32_t k, const pie_mx_rows* out) {
+  const char* who = "pie_mx_quantise";
+  if (pie_status st = check_mx_shape(c, rows, k, who)) return st;
+  if (rows == 0) return PIE_OK;
+  if (pie_status st = check_rows(c, x, k, "x", who)) return st;
+  if (pie_status st = check_mx_rows(c, out, k, who)) return st;
+  HIP_TRY(c, launch_mx_quantise(rows_view(x), rows, k, out->format, mx_rows_view(out), c->stream));
+  return PIE_OK;
+}
+
+extern "C" pie_status pie_mx_dequantise(pie_ctx* c, const pie_mx_rows* a, int32_t rows, int32_t k, const pie_rows* out) {
+  const char* who = "pie_mx_dequantise";
+  if (pie_status st = check_mx_shape(c, rows, k, who)) return st;
+  if (rows == 0) return PIE_OK;
+  if (pie_status st = check_mx_rows(c, a, k, who)) return st;
+  if (pie_status st = check_rows(c, out, k, "out", who)) return st;
+  HIP_TRY(c, launch_mx_dequantise(mx_rows_view(a), a->format, rows, k, rows_view(out), c->stream));
+  return PIE_OK;
+}
+
+extern "C" pie_status pie_mx_norm(pie_ctx* c, const pie_rows* x, const pie_rows* delta, const void* gain, int32_t rows, int32_t k, const pie_rows* h,
+                                  const pie_mx_rows* out) {
+  const char* who = "pie_mx_norm";
+  if (pie_status st = check_mx_shape(c, rows, k, who)) return st;
+  if (k > 8192) return fail(c, PIE_EUNSUPPORTED, "%s: rows of %d values, at most 8192", who, k);
+  if (rows == 0) return PIE_OK;
+  if (pie_status st = check_rows(c, x, k, "x", who)) return st;
+  if (delta)
+    if (pie_status st = check_rows(c, delta, k, "delta", who)) return st;
+  if (h) {
+    if (pie_status st = check_rows(c, h, k, "h", who)) return st;
+    if (h->dtype != x->dtype) return fail(c, PIE_EINVAL, "%s: h has to be of x's type", who);
+  }
+  if (!gain || reinterpret_cast<uintptr_t>(gain) % 2) return fail(c, PIE_EINVAL, "%s: null or unaligned gain", who);
+  if (pie_status st = check_mx_rows(c, out, k, who)) return st;
+  MxNormArgs a{};
+  a.x = rows_view(x); a.delta = rows_view(delta);
+  a.h = h ? rows_view(h) : mx_view(nullptr, x->dtype, 0);
+  a.gain = reinterpret_cast<const bf16_t*>(gain); a.gain_vec = reinterpret_cast<uintptr_t>(gain) % 16 == 0; a.eps = c->m.rms_eps;
+  HIP_TRY(c, launch_mx_norm(a, rows, k, out->format, mx_rows_view(out), c->stream));
+  return PIE_OK;
+}
+
+// Room for N rows of K inputs, all 0.
+static pie_status mx_alloc(pie_ctx* c, MxPacked& w, int N, int K) {
+  free_packed(w);
+  w.N = N; w.K = K;
+  w.NB = (N + 31) / 32; w.KT = (K + 63) / 64; w.KQ = (w.KT + 3) / 4;
+  const size_t data = (size_t)w.NB * w.KT * 1024, scales = (size_t)w.NB * w.KQ * 256;
+  if (hipError_t e = hipMalloc(reinterpret_cast<void**>(&w.data), data + scales); e != hipSuccess) {
+    w = MxPacked();
+    return fail(c, e == hipErrorOutOfMemory ? PIE_ENOMEM : PIE_EHIP, "microscaled weights: %s", hipGetErrorString(e));
+  }
+  w.scales = reinterpret_cast<uint32_t*>(w.data + data);
+  HIP_TRY(c, hipMemsetAsync(w.data, 0, data + scales, c->stream));
+  return PIE_OK;
+}
+static pie_status mx_pack(pie_ctx* c, MxPacked& w, const pie_mx_rows* parts, const int32_t* rows, int n_parts, int K, bool gated) {
+  int64_t N = 0;
+  for (int i = 0; i < n_parts; ++i) N += rows[i];
+  if (pie_status st = mx_alloc(c, w, (int)N, K)) return st;
+  int first = 0;
+  for (int i = 0; i < n_parts; ++i) {
+    HIP_TRY(c, launch_mx_pack(mx_rows_view(&parts[i]), rows[i], K, gated ? i : first, gated, w, c->stream));
+    first += rows[i];
+  }
+  return PIE_OK;
+}
+
+static pie_status pie_mx_weight_create_impl(pie_ctx* c, const pie_mx_rows* parts, const int32_t* part_rows, int32_t n_parts, int32_t k, int32_t gated,
+                                            pie_mx_weight** out) {
+  const char* who = "pie_mx_weight_create";
+  if (!c) return PIE_EINVAL;
+  if (!out) return fail(c, PIE_EINVAL, "%s: null argument", who);
+  *out = nullptr;
+  if (pie_status st = check_mx_shape(c, 0, k, who)) return st;
+  if (!parts || !part_rows || n_parts <= 0) return fail(c, PIE_EINVAL, "%s: no parts", who);
+  if (gated && (n_parts != 2 || part_rows[0] != part_rows[1] || part_rows[0] % 32))
+    return fail(c, PIE_EINVAL, "%s: a gated weight has two parts of one number of rows, a multiple of 32", who);
+  int64_t N = 0;
+  for (int i = 0; i < n_parts; ++i) {
+    if (part_rows[i] <= 0) return fail(c, PIE_EINVAL, "%s: part %d has %d rows", who, i, part_rows[i]);
+    if (pie_status st = check_mx_rows(c, &parts[i], k, who)) return st;
+    if (parts[i].format != PIE_MXFP4) return fail(c, PIE_EINVAL, "%s: part %d is not MXFP4", who, i);
+    N += part_rows[i];
+  }
+  if (N > MX_MAX_ROWS) return fail(c, PIE_EUNSUPPORTED, "%s: %lld rows, at most %d", who, (long long)N, MX_MAX_ROWS);
+  if (pie_status st = refuse_capture(c, who)) return st;
+  c->mx_weights.reserve(c->mx_weights.size() + 1);
+  if (!c->mx_ws) HIP_TRY(c, hipMalloc(reinterpret_cast<void**>(&c->mx_ws), MX_WS_FLOATS * sizeof(float)));
+  pie_mx_weight* w = new pie_mx_weight();
+  w->owner = c;
+  w->gated = gated != 0;
+  pie_status st = mx_pack(c, w->w, parts, part_rows, n_parts, k, w->gated);
+  if (st == PIE_OK && hipStreamSynchronize(c->stream) != hipSuccess) st = fail(c, PIE_EHIP, "%s: the copy of the weights failed", who);
+  if (st != PIE_OK) {
+    free_packed(w->w);
+    delete w;
+    return st;
+  }
+  c->mx_weights.push_back(w);
+  *out = w;
+  return PIE_OK;
+}
+extern "C" pie_status pie_mx_weight_create(pie_ctx* c, const pie_mx_rows* parts, const int32_t* part_rows, int32_t n_parts, int32_t k, int32_t gated,
+                                           pie_mx_weight** out) {
+  return guarded(c, "pie_mx_weight_create", [&]() { return pie_mx_weight_create_impl(c, parts, part_rows, n_parts, k, gated, out); });
+}
+
+extern "C" pie_status pie_mx_weight_destroy(pie_ctx* c, pie_mx_weight* weight) {
+  if (!c) return PIE_EINVAL;
+  if (!weight) return PIE_OK;
+  const auto at = std::find(c->mx_weights.begin(), c->mx_weights.end(), weight);
+  if (at == c->mx_weights.end()) return fail(c, PIE_EINVAL, "pie_mx_weight_destroy: not a weight of this context");
+  if (pie_status st = refuse_capture(c, "pie_mx_weight_destroy")) return st;
+  HIP_TRY(c, hipStreamSynchronize(c->stream));
+  c->mx_weights.erase(at);
+  free_packed(weight->w);
+  delete weight;
+  return PIE_OK;
+}
+
+static pie_status check_mx_weight(pie_ctx* c, const pie_mx_weight* w, bool gated, const char* who) {
+  if (!c) return PIE_EINVAL;
+  if (c->host_only) return fail(c, PIE_EINVAL, "%s: the context only plans batches (pie_create_planner)", who);
+  if (!w) return fail(c, PIE_EINVAL, "%s: null weight", who);
+  if (w->owner != c) return fail(c, PIE_EINVAL, "%s: the weight was made by another context", who);
+  if (w->gated != gated) return fail(c, PIE_EINVAL, gated ? "%s: the weight is not gated" : "%s: the weight is gated", who);
+  return PIE_OK;
+}
+
+extern "C" pie_status pie_mx_product(pie_ctx* c, const pie_mx_rows* a, int32_t rows, const pie_mx_weight* weight, const pie_rows* out) {
+  const char* who = "pie_mx_product";
+  if (pie_status st = check_mx_weight(c, weight, false, who)) return st;
+  const MxPacked& w = weight->w;
+  if (pie_status st = check_mx_shape(c, rows, w.K, who)) return st;
+  if (rows == 0) return PIE_OK;
+  if (pie_status st = check_mx_rows(c, a, w.K, who)) return st;
+  if (pie_status st = check_rows(c, out, w.N, "out", who)) return st;
+  if (out->dtype == PIE_F16) return fail(c, PIE_EINVAL, "%s: out is bf16 or fp32", who);
+  const RowsView o = rows_view(out);
+  const bool f32 = out->dtype == PIE_F32;
+  const MxEpi e{f32 ? MX_F32 : MX_BF16, out->data, out->row_stride, nullptr, 0, w.N, o.vec && w.N % (f32 ? 4 : 8) == 0, nullptr, nullptr, nullptr, 0};
+  HIP_TRY(c, launch_mx_product(mx_rows_view(a), a->format, rows, w, e, c->stream));
+  return PIE_OK;
+}
+
+extern "C" pie_status pie_mx_swiglu(pie_ctx* c, const pie_mx_rows* a, int32_t rows, const pie_mx_weight* weight, const pie_mx_rows* out) {
+  const char* who = "pie_mx_swiglu";
+  if (pie_status st = check_mx_weight(c, weight, true, who)) return st;
+  const MxPacked& w = weight->w;
+  if (pie_status st = check_mx_shape(c, rows, w.K, who)) return st;
+  if (rows == 0) return PIE_OK;
+  if (pie_status st = check_mx_rows(c, a, w.K, who)) return st;
+  if (pie_status st = check_mx_rows(c, out, w.N / 2, who)) return st;
+  const MxRowsView o = mx_rows_view(out);
+  const MxEpi e{out->format == PIE_MXFP8 ? MX_SWIGLU8 : MX_SWIGLU4, o.elements, o.row_bytes, o.scales, o.scale_bytes, w.N / 2, 1, nullptr, nullptr, nullptr, 0};
+  HIP_TRY(c, launch_mx_product(mx_rows_view(a), a->format, rows, w, e, c->stream));
+  return PIE_OK;
+}
+
+// A layer's microscaled activations, in one block of the context: the rows in front of q, k, v and of gate and up, the attention output (in
+// the same place), and the rows in front of the down projection.
+namespace {
+struct MxActs { MxRowsView rows, attn, act; size_t bytes; };
+}
+static MxActs mx_acts(const pie_ctx* c) {
+  const size_t T = (size_t)c->p.max_batch_tokens;
+  const int64_t H = c->m.hidden, Q = (int64_t)c->m.n_q_heads * c->m.head_dim, I = c->m.mlp_dim;
+  auto scales = [](int64_t k) { return (k / 32 + 3) / 4 * 4; };
+  auto up = [](size_t x) { return (x + 255) / 256 * 256; };
+  const size_t e0 = 0, s0 = up(e0 + T * std::max(H, Q)), e1 = up(s0 + T * scales(std::max(H, Q))), s1 = up(e1 + T * I), end = up(s1 + T * scales(I));
+  uint8_t* p = c->mx_act;
+  return MxActs{MxRowsView{p + e0, H, p + s0, scales(H)}, MxRowsView{p + e0, Q, p + s0, scales(Q)}, MxRowsView{p + e1, I, p + s1, scales(I)}, end};
+}
+
+extern "C" pie_status pie_load_layer_mx(pie_ctx* c, int32_t layer, const void* g1, const void* g2, const pie_mx_rows* weights) {
+  const char* who = "pie_load_layer_mx";
+  if (!c) return PIE_EINVAL;
+  if (c->host_only) return fail(c, PIE_EINVAL, "%s: the context only plans batches (pie_create_planner)", who);
+  if (!g1 || !g2 || !weights) return fail(c, PIE_EINVAL, "%s: null weight", who);
+  if (layer < 0 || layer >= c->m.n_layers) return fail(c, PIE_ERANGE, "%s: layer %d of %d", who, layer, c->m.n_layers);
+  const int H = c->m.hidden, QD = c->m.n_q_heads * c->m.head_dim, KD = c->m.n_kv_heads * c->m.head_dim, I = c->m.mlp_dim;
+  for (int pj = 0; pj < PIE_N_PROJ; ++pj) {
+    if (pie_status st = check_mx_rows(c, &weights[pj], pj == PIE_PROJ_O ? QD : pj == PIE_PROJ_DOWN ? I : H, who)) return st;
+    if (weights[pj].format != PIE_MXFP4) return fail(c, PIE_EINVAL, "%s: projection %d is not MXFP4", who, pj);
+  }
+  if (pie_status st = refuse_capture(c, who)) return st;
+  if (!c->mx_act) HIP_TRY(c, hipMalloc(reinterpret_cast<void**>(&c->mx_act), mx_acts(c).bytes));
+  if (!c->mx_ws) HIP_TRY(c, hipMalloc(reinterpret_cast<void**>(&c->mx_ws), MX_WS_FLOATS * sizeof(float)));
+  LayerWeights& L = c->layers[layer];
+  HIP_TRY(c, hipStreamSynchronize(c->stream));  // (the layer may be in use by what is enqueued)
+  L.loaded = L.mx = false;
+  free_weights(L);
+  pie_status st;
+  if ((st = copy_gain(c, &L.g1, g1, H)) != PIE_OK) return st;
+  if ((st = copy_gain(c, &L.g2, g2, H)) != PIE_OK) return st;
+  const int32_t qkv[] = {QD, KD, KD}, o[] = {H}, gu[] = {I, I}, down[] = {H};
+  if ((st = mx_pack(c, L.mqkv, weights + PIE_PROJ_Q, qkv, 3, H, false)) != PIE_OK) return st;
+  if ((st = mx_pack(c, L.mo, weights + PIE_PROJ_O, o, 1, QD, false)) != PIE_OK) return st;
+  if ((st = mx_pack(c, L.mgu, weights + PIE_PROJ_GATE, gu, 2, H, true)) != PIE_OK) return st;
+  if ((st = mx_pack(c, L.mdown, weights + PIE_PROJ_DOWN, down, 1, I, false)) != PIE_OK) return st;
+  HIP_TRY(c, hipStreamSynchronize(c->stream));
+  L.loaded = L.mx = true;
+  return PIE_OK;
+}
+
+// ---------------------------------------------------------------------------------------------
 // forward
 // ---------------------------------------------------------------------------------------------
 namespace {
@@ -1947,94 +2208,10 @@ static pie_status check_batch(pie_ctx* c, const pie_batch* b, const char* who) {
   return PIE_OK;
 }
 
-// One decoder layer.  x_in: wide [T, H] layer input, or null to read the batch's input Embeds; y_out: wide
-// [T, H] destination of the layer output, or null to store it as bf16 into the batch's output Embeds.
-// carry (optional): on entry, the number of split-K partial copies of the previous layer's down projection
-// still waiting in the workspace (x_in = previous residual c->h + their sum has not been formed yet: the first
-// norm does it); on return, the same for this layer's down projection (only when y_out is given).
-static pie_status run_layer(pie_ctx* c, int32_t layer, const pie_batch* b, float* x_in, float* y_out, bool timed,
-                            int* carry = nullptr) {
-  const LayerWeights& L = c->layers[layer];
-  const pie_model_desc& m = c->m;
-  const int T = b->T, H = m.hidden, Hq = m.n_q_heads, Hkv = m.n_kv_heads, D = m.head_dim, I = m.mlp_dim;
-  const int QKV = (Hq + 2 * Hkv) * D;
+// Attention of a batch over one layer's pool: rotated queries in c->qkv, result in c->attn.
+static pie_status run_attention(pie_ctx* c, const pie_batch* b, bf16_t* kv_layer, StageTimer& tm) {
+  const int Hq = c->m.n_q_heads, Hkv = c->m.n_kv_heads, D = c->m.head_dim, QKV = (Hq + 2 * Hkv) * D;
   hipStream_t s = c->stream;
-  bf16_t* kv_layer = c->kv + (size_t)layer * c->kv_layer_elems;
-  const bool was_timing = c->timing;
-  if (!timed) c->timing = false;
-  StageTimer tm(c, PIE_STAGE_NORM1, PIE_STAGE_DOWN);
-  struct Restore { pie_ctx* c; bool v; ~Restore() { c->timing = v; } } restore{c, was_timing};
-  EpiArgs e{};
-
-  // LoRA pairs the batch's adapters carry in this layer, per projection
-  auto adapted = [&](int l, int pj) {
-    if (b->n_lora_tiles > 0)
-      for (int ad : b->used_adapters)
-        if (c->lora[((size_t)ad * m.n_layers + l) * PIE_N_PROJ + pj].rank > 0) return true;
-    return false;
-  };
-  bool lora[PIE_N_PROJ];
-  for (int pj = 0; pj < PIE_N_PROJ; ++pj) lora[pj] = adapted(layer, pj);
-  const int RM = round_up(c->p.max_lora_rank, 16), NL = m.n_layers, LT = b->n_lora_tiles;
-  const bool lora_qkv = lora[PIE_PROJ_Q] || lora[PIE_PROJ_K] || lora[PIE_PROJ_V];
-  // Small batches split their projections along K.  Where the next kernel reads the projection's output row by
-  // row anyway, it sums the partial copies itself and the separate epilogue launch is saved: the rotary step
-  // after QKV, the second norm after the output projection, the next layer's first norm after the down
-  // projection.  An adapter's update of q, k, v or o joins the partial copies before they are summed, one of the
-  // down projection the residual that is added to them.
-  const int carried = (carry && x_in) ? *carry : 0;
-  if (carry) *carry = 0;
-
-  // Up to FEW_ROWS tokens: the norms, the rotary step and the epilogues are part of the products (few.hip), where nothing else
-  // reads what lies between them (an adapter's pair reads the normalised rows and joins the sums before the next step).
-  const int n_cus = c->wave_slots / 8;
-  const int wide_or_embed = x_in ? FEW_F32 : FEW_EMBED;
-  const bool few_qkv = !lora_qkv && carried == 0 && few_rows_ok(T, L.wqkv, EPI_STORE_BF16, wide_or_embed);
-  const bool gu_norms = !lora[PIE_PROJ_GATE] && !lora[PIE_PROJ_UP] && few_rows_ok(T, L.wgu, EPI_SWIGLU, FEW_F32);
-  const bool few_o = !lora[PIE_PROJ_O] && few_resid_ok(T, Hq * D, L.wo) && few_resid_pays(T, L.wo, n_cus, gu_norms ? SUMS_KEEP_NORM : SUMS_JOIN_NORM);
-  // (reads the rows of c->h, which the general output product may leave as partial sums for the second norm to sum)
-  const bool few_gu = few_o && gu_norms;
-  const bool next_layer = carry && y_out && layer + 1 < m.n_layers;  // its first norm sums what this layer's down product leaves ..
-  const bool next_norms = next_layer && !adapted(layer + 1, PIE_PROJ_Q) && !adapted(layer + 1, PIE_PROJ_K) && !adapted(layer + 1, PIE_PROJ_V) &&
-                          few_rows_ok(T, c->layers[layer + 1].wqkv, EPI_STORE_BF16, FEW_F32);  // .. unless it has none of its own
-  const bool few_down = few_resid_ok(T, I, L.wdown) && few_resid_pays(T, L.wdown, n_cus, next_norms ? SUMS_KEEP_NORM : next_layer ? SUMS_JOIN_NORM : SUMS_KERNEL);
-
-  // (a stage that a product takes in is not bracketed: it reports 0)
-  if (!few_qkv) {
-    tm.begin(PIE_STAGE_NORM1);
-    if (x_in && carried > 0)
-      HIP_TRY(c, launch_splitk_resid_norm(c->splitk, carried, L.wdown.NB * 32, c->h, nullptr, nullptr, x_in, L.g1, c->xn, T, H, m.rms_eps, s));
-    else if (x_in) HIP_TRY(c, launch_rmsnorm_f32(x_in, L.g1, c->xn, T, H, m.rms_eps, s));
-    else HIP_TRY(c, launch_rmsnorm_embed(c->embeds, b->in_ids, L.g1, c->xn, T, H, m.rms_eps, s));
-    tm.end(PIE_STAGE_NORM1);
-  }
-
-  tm.begin(PIE_STAGE_QKV);
-  int qkv_splits = 0;
-  e = EpiArgs{EPI_STORE_BF16, c->qkv, QKV, nullptr, nullptr, nullptr, 0};
-  if (few_qkv) {
-    const FewSource src{wide_or_embed, x_in ? (const void*)x_in : c->embeds, H, b->in_ids, L.g1, m.rms_eps};
-    HIP_TRY(c, launch_few_qkv(src, T, L.wqkv, c->qkv, FewRope{b->rope_angles, b->tok_page, b->tok_slot, kv_layer, Hq, Hkv, D}, n_cus, s));
-  } else {
-    HIP_TRY(c, launch_gemm(c->xn, H, T, L.wqkv, e, c->splitk, c->splitk_elems, n_cus, s, &qkv_splits));
-  }
-  tm.end(PIE_STAGE_QKV);
-
-  if (lora_qkv) {  // q, k, v share the normalised input
-    const int KD = Hkv * D;
-    const int ks = lora_ksplits(LT, 3, H, RM, c->lora_z_rows);
-    HIP_TRY(c, launch_lora_down(c->xn, H, H, LT, 3, b->lora_rows, b->lora_tile_ad, c->lora_dev, layer, NL, PIE_PROJ_Q, c->lora_z, RM, ks, s));
-    const bool split = qkv_splits > 0;  // the update goes into the partial sums that the rotary step takes
-    HIP_TRY(c, launch_lora_up(split ? (void*)c->splitk : c->qkv, split ? L.wqkv.NB * 32 : QKV, QKV, split ? 4 : 3, Hq * D, KD, LT, b->lora_rows, b->lora_tile_ad, c->lora_dev, layer, NL, PIE_PROJ_Q, 0, c->lora_z, RM, ks, s, qkv_splits, (int64_t)T * L.wqkv.NB * 32));
-  }
-
-  if (!few_qkv) {
-    tm.begin(PIE_STAGE_ROPE_APPEND);
-    HIP_TRY(c, launch_rope_append(c->qkv, T, Hq, Hkv, D, b->pos, b->tok_page, b->tok_slot, b->rope_angles, kv_layer, b->n_pitems > 0,
-                                  c->splitk, qkv_splits, L.wqkv.NB * 32, s));
-    tm.end(PIE_STAGE_ROPE_APPEND);
-  }
-
   AttnArgs a{};
   a.q = c->qkv; a.q_stride = QKV; a.kv = kv_layer; a.out = c->attn; a.Hq = Hq; a.Hkv = Hkv; a.D = D;
   a.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)D));
@@ -2078,6 +2255,161 @@ static pie_status run_layer(pie_ctx* c, int32_t layer, const pie_batch* b, float
     HIP_TRY(c, launch_attn_merge(a, b->dec_reqs, b->n_dec_reqs, b->mref_indptr, b->mrefs, b->dec_rows, b->part_o, b->part_ml, s));
     tm.end(PIE_STAGE_ATTN_MERGE);
   }
+  return PIE_OK;
+}
+
+// The layer in microscaled formats (pie_load_layer_mx); arguments as for run_layer.  Every product's rows are MXFP8: the norms write them, the
+// attention output is quantised, the SwiGLU writes what the down projection reads.
+static pie_status run_layer_mx(pie_ctx* c, int32_t layer, const pie_batch* b, float* x_in, float* y_out, bool timed, int* carry) {
+  const LayerWeights& L = c->layers[layer];
+  const pie_model_desc& m = c->m;
+  const int T = b->T, H = m.hidden, Hq = m.n_q_heads, Hkv = m.n_kv_heads, D = m.head_dim, I = m.mlp_dim, QKV = (Hq + 2 * Hkv) * D;
+  hipStream_t s = c->stream;
+  bf16_t* kv_layer = c->kv + (size_t)layer * c->kv_layer_elems;
+  const bool was_timing = c->timing;
+  if (!timed) c->timing = false;
+  StageTimer tm(c, PIE_STAGE_NORM1, PIE_STAGE_DOWN);
+  struct Restore { pie_ctx* c; bool v; ~Restore() { c->timing = v; } } restore{c, was_timing};
+  const int carried = (carry && x_in) ? *carry : 0;
+  if (carry) *carry = 0;
+  const MxActs acts = mx_acts(c);
+
+  // a layer of bf16 before may have left its down projection as partial sums on c->h
+  tm.begin(PIE_STAGE_NORM1);
+  MxNormArgs n{};
+  n.x = carried > 0 ? mx_view(c->h, PIE_F32, H) : x_in ? mx_view(x_in, PIE_F32, H) : mx_view(c->embeds, PIE_BF16, H);
+  n.ids = x_in ? nullptr : b->in_ids;
+  n.h = mx_view(carried > 0 ? x_in : nullptr, n.x.dtype, H);
+  n.part = c->splitk; n.splits = carried; n.part_stride = round_up(H, 32); n.split_stride = (int64_t)T * n.part_stride;
+  n.gain = L.g1; n.gain_vec = 1; n.eps = m.rms_eps;
+  HIP_TRY(c, launch_mx_norm(n, T, H, PIE_MXFP8, acts.rows, s));
+  tm.end(PIE_STAGE_NORM1);
+
+  tm.begin(PIE_STAGE_QKV);
+  HIP_TRY(c, launch_mx_product(acts.rows, PIE_MXFP8, T, L.mqkv, MxEpi{MX_BF16, c->qkv, QKV, nullptr, 0, QKV, 1, nullptr, nullptr, nullptr, 0}, s));
+  tm.end(PIE_STAGE_QKV);
+
+  tm.begin(PIE_STAGE_ROPE_APPEND);
+  HIP_TRY(c, launch_rope_append(c->qkv, T, Hq, Hkv, D, b->pos, b->tok_page, b->tok_slot, b->rope_angles, kv_layer, b->n_pitems > 0, c->splitk, 0, QKV, s));
+  tm.end(PIE_STAGE_ROPE_APPEND);
+
+  if (pie_status st = run_attention(c, b, kv_layer, tm)) return st;
+
+  tm.begin(PIE_STAGE_OPROJ);
+  HIP_TRY(c, launch_mx_quantise(mx_view(c->attn, PIE_BF16, Hq * D), T, Hq * D, PIE_MXFP8, acts.attn, s));
+  HIP_TRY(c, launch_mx_product(acts.attn, PIE_MXFP8, T, L.mo, MxEpi{MX_RESID_EMBED, c->h, H, nullptr, 0, H, 1, c->embeds, b->in_ids, x_in, H}, s));
+  tm.end(PIE_STAGE_OPROJ);
+
+  tm.begin(PIE_STAGE_NORM2);
+  MxNormArgs n2{};
+  n2.x = mx_view(c->h, PIE_F32, H); n2.h = mx_view(nullptr, PIE_F32, H);
+  n2.gain = L.g2; n2.gain_vec = 1; n2.eps = m.rms_eps;
+  HIP_TRY(c, launch_mx_norm(n2, T, H, PIE_MXFP8, acts.rows, s));
+  tm.end(PIE_STAGE_NORM2);
+
+  tm.begin(PIE_STAGE_GATEUP);
+  HIP_TRY(c, launch_mx_product(acts.rows, PIE_MXFP8, T, L.mgu,
+                               MxEpi{MX_SWIGLU8, acts.act.elements, acts.act.row_bytes, acts.act.scales, acts.act.scale_bytes, I, 1, nullptr, nullptr, nullptr, 0}, s));
+  tm.end(PIE_STAGE_GATEUP);
+
+  tm.begin(PIE_STAGE_DOWN);
+  HIP_TRY(c, launch_mx_product(acts.act, PIE_MXFP8, T, L.mdown, MxEpi{MX_RESID_OUT, y_out, H, nullptr, 0, H, 1, c->embeds, b->out_ids, c->h, H}, s));
+  tm.end(PIE_STAGE_DOWN);
+  c->last_T = T;
+  c->last_mx = true;
+  return PIE_OK;
+}
+
+// One decoder layer.  x_in: wide [T, H] layer input, or null to read the batch's input Embeds; y_out: wide
+// [T, H] destination of the layer output, or null to store it as bf16 into the batch's output Embeds.
+// carry (optional): on entry, the number of split-K partial copies of the previous layer's down projection
+// still waiting in the workspace (x_in = previous residual c->h + their sum has not been formed yet: the first
+// norm does it); on return, the same for this layer's down projection (only when y_out is given).
+static pie_status run_layer(pie_ctx* c, int32_t layer, const pie_batch* b, float* x_in, float* y_out, bool timed,
+                            int* carry = nullptr) {
+  const LayerWeights& L = c->layers[layer];
+  if (L.mx) return run_layer_mx(c, layer, b, x_in, y_out, timed, carry);
+  const pie_model_desc& m = c->m;
+  const int T = b->T, H = m.hidden, Hq = m.n_q_heads, Hkv = m.n_kv_heads, D = m.head_dim, I = m.mlp_dim;
+  const int QKV = (Hq + 2 * Hkv) * D;
+  hipStream_t s = c->stream;
+  bf16_t* kv_layer = c->kv + (size_t)layer * c->kv_layer_elems;
+  const bool was_timing = c->timing;
+  if (!timed) c->timing = false;
+  StageTimer tm(c, PIE_STAGE_NORM1, PIE_STAGE_DOWN);
+  struct Restore { pie_ctx* c; bool v; ~Restore() { c->timing = v; } } restore{c, was_timing};
+  EpiArgs e{};
+
+  // LoRA pairs the batch's adapters carry in this layer, per projection
+  auto adapted = [&](int l, int pj) {
+    if (b->n_lora_tiles > 0)
+      for (int ad : b->used_adapters)
+        if (c->lora[((size_t)ad * m.n_layers + l) * PIE_N_PROJ + pj].rank > 0) return true;
+    return false;
+  };
+  bool lora[PIE_N_PROJ];
+  for (int pj = 0; pj < PIE_N_PROJ; ++pj) lora[pj] = adapted(layer, pj);
+  const int RM = round_up(c->p.max_lora_rank, 16), NL = m.n_layers, LT = b->n_lora_tiles;
+  const bool lora_qkv = lora[PIE_PROJ_Q] || lora[PIE_PROJ_K] || lora[PIE_PROJ_V];
+  // Small batches split their projections along K.  Where the next kernel reads the projection's output row by
+  // row anyway, it sums the partial copies itself and the separate epilogue launch is saved: the rotary step
+  // after QKV, the second norm after the output projection, the next layer's first norm after the down
+  // projection.  An adapter's update of q, k, v or o joins the partial copies before they are summed, one of the
+  // down projection the residual that is added to them.
+  const int carried = (carry && x_in) ? *carry : 0;
+  if (carry) *carry = 0;
+
+  // Up to FEW_ROWS tokens: the norms, the rotary step and the epilogues are part of the products (few.hip), where nothing else
+  // reads what lies between them (an adapter's pair reads the normalised rows and joins the sums before the next step).
+  const int n_cus = c->wave_slots / 8;
+  const int wide_or_embed = x_in ? FEW_F32 : FEW_EMBED;
+  const bool few_qkv = !lora_qkv && carried == 0 && few_rows_ok(T, L.wqkv, EPI_STORE_BF16, wide_or_embed);
+  const bool gu_norms = !lora[PIE_PROJ_GATE] && !lora[PIE_PROJ_UP] && few_rows_ok(T, L.wgu, EPI_SWIGLU, FEW_F32);
+  const bool few_o = !lora[PIE_PROJ_O] && few_resid_ok(T, Hq * D, L.wo) && few_resid_pays(T, L.wo, n_cus, gu_norms ? SUMS_KEEP_NORM : SUMS_JOIN_NORM);
+  // (reads the rows of c->h, which the general output product may leave as partial sums for the second norm to sum)
+  const bool few_gu = few_o && gu_norms;
+  const bool next_layer = carry && y_out && layer + 1 < m.n_layers;  // its first norm sums what this layer's down product leaves ..
+  const bool next_norms = next_layer && !c->layers[layer + 1].mx && !adapted(layer + 1, PIE_PROJ_Q) && !adapted(layer + 1, PIE_PROJ_K) && !adapted(layer + 1, PIE_PROJ_V) &&
+                          few_rows_ok(T, c->layers[layer + 1].wqkv, EPI_STORE_BF16, FEW_F32);  // .. unless it has none of its own
+  const bool few_down = few_resid_ok(T, I, L.wdown) && few_resid_pays(T, L.wdown, n_cus, next_norms ? SUMS_KEEP_NORM : next_layer ? SUMS_JOIN_NORM : SUMS_KERNEL);
+
+  // (a stage that a product takes in is not bracketed: it reports 0)
+  if (!few_qkv) {
+    tm.begin(PIE_STAGE_NORM1);
+    if (x_in && carried > 0)
+      HIP_TRY(c, launch_splitk_resid_norm(c->splitk, carried, L.wdown.NB * 32, c->h, nullptr, nullptr, x_in, L.g1, c->xn, T, H, m.rms_eps, s));
+    else if (x_in) HIP_TRY(c, launch_rmsnorm_f32(x_in, L.g1, c->xn, T, H, m.rms_eps, s));
+    else HIP_TRY(c, launch_rmsnorm_embed(c->embeds, b->in_ids, L.g1, c->xn, T, H, m.rms_eps, s));
+    tm.end(PIE_STAGE_NORM1);
+  }
+
+  tm.begin(PIE_STAGE_QKV);
+  int qkv_splits = 0;
+  e = EpiArgs{EPI_STORE_BF16, c->qkv, QKV, nullptr, nullptr, nullptr, 0};
+  if (few_qkv) {
+    const FewSource src{wide_or_embed, x_in ? (const void*)x_in : c->embeds, H, b->in_ids, L.g1, m.rms_eps};
+    HIP_TRY(c, launch_few_qkv(src, T, L.wqkv, c->qkv, FewRope{b->rope_angles, b->tok_page, b->tok_slot, kv_layer, Hq, Hkv, D}, n_cus, s));
+  } else {
+    HIP_TRY(c, launch_gemm(c->xn, H, T, L.wqkv, e, c->splitk, c->splitk_elems, n_cus, s, &qkv_splits));
+  }
+  tm.end(PIE_STAGE_QKV);
+
+  if (lora_qkv) {  // q, k, v share the normalised input
+    const int KD = Hkv * D;
+    const int ks = lora_ksplits(LT, 3, H, RM, c->lora_z_rows);
+    HIP_TRY(c, launch_lora_down(c->xn, H, H, LT, 3, b->lora_rows, b->lora_tile_ad, c->lora_dev, layer, NL, PIE_PROJ_Q, c->lora_z, RM, ks, s));
+    const bool split = qkv_splits > 0;  // the update goes into the partial sums that the rotary step takes
+    HIP_TRY(c, launch_lora_up(split ? (void*)c->splitk : c->qkv, split ? L.wqkv.NB * 32 : QKV, QKV, split ? 4 : 3, Hq * D, KD, LT, b->lora_rows, b->lora_tile_ad, c->lora_dev, layer, NL, PIE_PROJ_Q, 0, c->lora_z, RM, ks, s, qkv_splits, (int64_t)T * L.wqkv.NB * 32));
+  }
+
+  if (!few_qkv) {
+    tm.begin(PIE_STAGE_ROPE_APPEND);
+    HIP_TRY(c, launch_rope_append(c->qkv, T, Hq, Hkv, D, b->pos, b->tok_page, b->tok_slot, b->rope_angles, kv_layer, b->n_pitems > 0,
+                                  c->splitk, qkv_splits, L.wqkv.NB * 32, s));
+    tm.end(PIE_STAGE_ROPE_APPEND);
+  }
+
+  if (pie_status st = run_attention(c, b, kv_layer, tm)) return st;
 
   tm.begin(PIE_STAGE_OPROJ);
   int o_splits = 0;
@@ -2130,6 +2462,17 @@ static pie_status run_layer(pie_ctx* c, int32_t layer, const pie_batch* b, float
   else HIP_TRY(c, launch_gemm(c->act, I, T, L.wdown, e, c->splitk, c->splitk_elems, n_cus, s, (carry && y_out) ? carry : nullptr));
   tm.end(PIE_STAGE_DOWN);
   c->last_T = T;
+  c->last_mx = false;
+  return PIE_OK;
+}
+
+// A batch's adapters have no pair in a layer of microscaled weights.
+static pie_status check_mx_adapters(pie_ctx* c, int32_t layer, const pie_batch* b, const char* who) {
+  if (!c->layers[layer].mx || b->n_lora_tiles == 0) return PIE_OK;
+  for (int ad : b->used_adapters)
+    for (int pj = 0; pj < PIE_N_PROJ; ++pj)
+      if (c->lora[((size_t)ad * c->m.n_layers + layer) * PIE_N_PROJ + pj].rank > 0)
+        return fail(c, PIE_EUNSUPPORTED, "%s: adapter %d has a pair in layer %d, whose weights are microscaled", who, ad, layer);
   return PIE_OK;
 }
 
@@ -2139,6 +2482,7 @@ extern "C" pie_status pie_forward(pie_ctx* c, int32_t layer, const pie_batch* b)
   if (pie_status st = check_batch(c, b, "pie_forward")) return st;
   if (layer < 0 || layer >= c->m.n_layers) return fail(c, PIE_ERANGE, "pie_forward: layer %d of %d", layer, c->m.n_layers);
   if (!c->layers[layer].loaded) return fail(c, PIE_EINVAL, "pie_forward: layer %d has no weights", layer);
+  if (pie_status st = check_mx_adapters(c, layer, b, "pie_forward")) return st;
   return run_layer(c, layer, b, nullptr, nullptr, true);
 }
 
@@ -2147,8 +2491,10 @@ extern "C" pie_status pie_forward_all(pie_ctx* c, const pie_batch* b) {
   if (c->host_only) return fail(c, PIE_EINVAL, "pie_forward_all: the context only plans batches (pie_create_planner)");
   if (pie_status st = check_batch(c, b, "pie_forward_all")) return st;
   const int NL = c->m.n_layers;
-  for (int l = 0; l < NL; ++l)
+  for (int l = 0; l < NL; ++l) {
     if (!c->layers[l].loaded) return fail(c, PIE_EINVAL, "pie_forward_all: layer %d has no weights", l);
+    if (pie_status st = check_mx_adapters(c, l, b, "pie_forward_all")) return st;
+  }
   int carry = 0;
   for (int l = 0; l < NL; ++l) {
     // the layer output stays wide between layers; only the last layer stores bf16 Embeds
@@ -2401,7 +2747,12 @@ extern "C" pie_status pie_read_tap(pie_ctx* c, int32_t which, void* dst, int64_t
       break;
     case PIE_TAP_ACT:
       if (n_elements != (int64_t)T * m.mlp_dim) return fail(c, PIE_EINVAL, "tap ACT holds %lld elements", (long long)T * m.mlp_dim);
-      HIP_TRY(c, hipMemcpyAsync(dst, c->act, (size_t)T * m.mlp_dim * 2, hipMemcpyDeviceToDevice, c->stream));
+      if (c->last_mx) {
+        if (reinterpret_cast<uintptr_t>(dst) % 2) return fail(c, PIE_EINVAL, "tap ACT: dst is not aligned to bf16");
+        HIP_TRY(c, launch_mx_dequantise(mx_acts(c).act, PIE_MXFP8, T, m.mlp_dim, mx_view(dst, PIE_BF16, m.mlp_dim), c->stream));
+      } else {
+        HIP_TRY(c, hipMemcpyAsync(dst, c->act, (size_t)T * m.mlp_dim * 2, hipMemcpyDeviceToDevice, c->stream));
+      }
       break;
     case PIE_TAP_LOGITS:
       if (n_elements != (int64_t)c->last_dist_n * m.vocab) return fail(c, PIE_EINVAL, "tap LOGITS holds %lld elements", (long long)c->last_dist_n * m.vocab);
