@@ -339,9 +339,9 @@ enum { PIE_MXFP8 = 0, PIE_MXFP4 = 1 };
 typedef struct {
   int32_t format;
   void* elements;      /* dev, 16-byte aligned */
-  int64_t row_bytes;   /* from a row's elements to the next row's: a multiple of 16, at least k or k / 2 */
+  int64_t row_bytes;   /* from a row's elements to the next row's: a multiple of 16, at least k or k / 2, at most 2^22 */
   uint8_t* scales;     /* dev, 4-byte aligned */
-  int64_t scale_bytes; /* from a row's scales to the next row's: a multiple of 4, at least k / 32 */
+  int64_t scale_bytes; /* from a row's scales to the next row's: a multiple of 4, at least k / 32, at most 2^22 */
 } pie_mx_rows;
 
 /* Rows of plain values: row r starts row_stride elements behind row r - 1; any stride of at least a row's length, and any alignment
@@ -356,8 +356,8 @@ typedef struct {
  * nothing unless they say so, and may be captured into a graph (graphs of one context share its workspace: one replays behind the
  * other).  Outputs must not overlap inputs where nothing else is said.  What is behind the last scale of a row, up to a multiple
  * of 4 bytes, is written as 0 by every call and looked at by none.
- * Errors of all: PIE_EINVAL (null, a shape, stride, alignment, format or type that is not as above), PIE_EUNSUPPORTED (k or rows
- * out of range), PIE_EHIP. */
+ * Errors of all: PIE_EINVAL (null, a shape, stride, alignment, format or type that is not as above), PIE_EUNSUPPORTED (k, rows or
+ * strides out of range), PIE_EHIP. */
 
 /* out = x in the format of `out`: per block, b - 127 = floor(log2 max|x|) - 8 (MXFP8) or - 2 (MXFP4), at least -127; elements are
  * x / 2^(b - 127) rounded to nearest, ties to even, and saturated at 448 or 6.  A block that holds a NaN or an infinity has

@@ -137,3 +137,23 @@ __device__ __forceinline__ void wg_barrier() {
 #define PIE_S_WAIT_VMCNT(n) __builtin_amdgcn_s_waitcnt(((n) & 15) | 0x0F70 | ((((n) >> 4) & 3) << 14))
 // s_waitcnt lgkmcnt(0) alone (LDS and scalar-memory operations done; vector-memory loads stay in flight)
 #define PIE_S_WAIT_LGKMCNT0() __builtin_amdgcn_s_waitcnt(0xC07F)
+
+// Tile order of the products: each XCD (workgroup id % 8) works on a contiguous range of a grouped order, 8 row tiles to a group.
+// Position of workgroup `id` in that order: ids go to the XCDs in turn, XCD x has n / 8 of them and one more when
+// x < n % 8.  A single row of tiles shares no weights between workgroups; where its length is not a multiple of 8 it is
+// left in launch order (128256 x 4096 at 193 rows 257 us, in ranges 262).  With more rows the ranges are what makes the
+// row tiles of a column meet in one L2, whatever the number of tiles: at 129 rows, 501 x 2 tiles of 96 rows, 299 us in
+// launch order (the weights fetched twice), 244 in ranges.
+__host__ __device__ __forceinline__ int xcd_range(int id, int tiles_m, int tiles_n) {
+  const int n = tiles_m * tiles_n, x = id & 7;
+  return tiles_m == 1 && n % 8 != 0 ? id : x * (n >> 3) + (x < (n & 7) ? x : n & 7) + (id >> 3);
+}
+// Row and column tile at a position of the grouped order.
+__host__ __device__ __forceinline__ void tile_at(int pos, int tiles_m, int tiles_n, int& tm, int& tn) {
+  constexpr int GROUP_M = 8;
+  const int width = GROUP_M * tiles_n;
+  const int first_m = (pos / width) * GROUP_M;
+  const int gsz = tiles_m - first_m < GROUP_M ? tiles_m - first_m : GROUP_M;
+  tm = first_m + (pos % width) % gsz;
+  tn = (pos % width) / gsz;
+}

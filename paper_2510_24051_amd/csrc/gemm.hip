@@ -504,27 +504,8 @@ __global__ __launch_bounds__(512) void gemm_large_kernel(const bf16_t* __restric
 // of it).  The matrix pipe went from 62% to 72% busy, of which the lower clock under the higher load gives back a
 // part (8320 x 28672 x 4096: 1.70 -> 1.58 ms on one box).
 // Workgroup ids are remapped so that each XCD (id % 8) works on a contiguous range of a grouped tile order (8 row
-// tiles per group) and its L2 sees a few activation and weight panels at a time.
+// tiles per group) and its L2 sees a few activation and weight panels at a time (xcd_range, tile_at in common.h).
 // ------------------------------------------------------------------------------------------------
-// Position of workgroup `id` in that order: ids go to the XCDs in turn, XCD x has n / 8 of them and one more when
-// x < n % 8.  A single row of tiles shares no weights between workgroups; where its length is not a multiple of 8 it is
-// left in launch order (128256 x 4096 at 193 rows 257 us, in ranges 262).  With more rows the ranges are what makes the
-// row tiles of a column meet in one L2, whatever the number of tiles: at 129 rows, 501 x 2 tiles of 96 rows, 299 us in
-// launch order (the weights fetched twice), 244 in ranges.
-__host__ __device__ __forceinline__ int xcd_range(int id, int tiles_m, int tiles_n) {
-  const int n = tiles_m * tiles_n, x = id & 7;
-  return tiles_m == 1 && n % 8 != 0 ? id : x * (n >> 3) + (x < (n & 7) ? x : n & 7) + (id >> 3);
-}
-// Row and column tile at a position of the grouped order.
-__host__ __device__ __forceinline__ void tile_at(int pos, int tiles_m, int tiles_n, int& tm, int& tn) {
-  constexpr int GROUP_M = 8;
-  const int width = GROUP_M * tiles_n;
-  const int first_m = (pos / width) * GROUP_M;
-  const int gsz = tiles_m - first_m < GROUP_M ? tiles_m - first_m : GROUP_M;
-  tm = first_m + (pos % width) % gsz;
-  tn = (pos % width) / gsz;
-}
-
 template <int MODE, bool PARTIAL>
 __global__ __launch_bounds__(512) void gemm_large_async_kernel(const bf16_t* __restrict__ A, int lda, int M,
                                                                const bf16_t* __restrict__ Wp, int N, int NB, int K,

@@ -25,7 +25,7 @@ struct MxPacked {  // MXFP4 weights, tiled (see mx_pack_kernel)
   uint8_t* data = nullptr;     // [NB][KT][64 lanes][16 bytes]
   uint32_t* scales = nullptr;  // [NB][KQ][64 lanes], behind the data
   int N = 0, K = 0;            // rows, inputs
-  int NB = 0, KT = 0, KQ = 0;  // blocks of 32 rows, steps of 64 inputs, groups of four steps
+  int NB = 0, KT = 0, KQ = 0;  // blocks of 32 rows, steps of 64 inputs (a multiple of four), groups of four steps
 };
 struct pie_mx_weight {
   const pie_ctx* owner = nullptr;

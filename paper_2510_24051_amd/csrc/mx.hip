@@ -421,7 +421,7 @@ __global__ __launch_bounds__(256) void mx_product_kernel(MxRowsView a, int M, Mx
   for (int j = 0; j < NJ; ++j)
 #pragma unroll
     for (int v = 0; v < 16; ++v) acc[j][v] = 0.f;
-  for (int kt = 0; kt < w.KT; ++kt) {
+  for (int kt = 0; kt < (w.K + 63) / 64; ++kt) {
     const int b = kt * 2;
     u32x4 lo = {0, 0, 0, 0}, hi = lo;
     if (FMT == PIE_MXFP8) {
@@ -443,8 +443,207 @@ __global__ __launch_bounds__(256) void mx_product_kernel(MxRowsView a, int M, Mx
   mx_epilogue<MODE>(epi, acc[0], acc[NJ - 1], m, M, nb0 * 32, lane);
 }
 
+// ---------------------------------------------------------------------------------------------
+// Tiles of 256 tokens x 256 weight rows: many rows, bound by the matrix cores.
+// Eight waves, two along the tokens and four along the weight rows, of 4 x 2 accumulator tiles each.  Activations go to LDS by direct copies, 128 bytes of
+// a row (SK steps of 64) and their scales a stage, three stages; weights go from memory to registers, each set refilled for the next
+// stage right behind the instructions that used it (as in gemm_large_async_kernel, whose order of requests, waits and barriers this is).
+// The 16-byte pieces of a row are swizzled by its number: piece c of row r is stored at c ^ (r / 2 % 8), so that the 32 rows of an operand
+// read from all banks.  What is behind K is read from the row's first piece instead: its weights are 0, and so is its scale.
+// ---------------------------------------------------------------------------------------------
+constexpr int MX_TM = 256, MX_TN = 256;
+
+template <int MODE, int FMT>
+__global__ __launch_bounds__(512, 2) void mx_tiles_kernel(MxRowsView a, int M, MxPacked w, MxEpi epi, int tiles_m, int tiles_n) {
+  constexpr int SK = FMT == PIE_MXFP8 ? 2 : 4;  // steps of 64 a stage
+  constexpr int SD = SK / 2;                    // dwords of scales a row and stage
+  constexpr int MI = 4, NJ = 2;
+  [[maybe_unused]] constexpr int UI = FMT == PIE_MXFP8 ? 2 : 4, UN = MI / UI;  // accumulator blocks whose operands are read at a time, and such units of a step
+  [[maybe_unused]] __shared__ __align__(16) uint8_t As0[MX_TM * 128], As1[MX_TM * 128], As2[MX_TM * 128];
+  [[maybe_unused]] __shared__ uint32_t Ss0[MX_TM * SD], Ss1[MX_TM * SD], Ss2[MX_TM * SD];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  [[maybe_unused]] const int h = lane >> 5;
+  const int wm = wave >> 2, wn = wave & 3;
+  int tm, tn;
+  tile_at(xcd_range(blockIdx.x, tiles_m, tiles_n), tiles_m, tiles_n, tm, tn);
+  const int64_t m0 = (int64_t)tm * MX_TM;
+  const int nb0 = tn * (MX_TN / 32) + wn * NJ;
+  f32x16 acc[MI][NJ];
+#pragma unroll
+  for (int i = 0; i < MI; ++i)
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
+  {
+#if __HIP_DEVICE_COMPILE__  // (buffer descriptors: see gemm_large_async_kernel)
+    constexpr int RSRC_FLAGS = 0x00020000;
+    const int rows = (int)(M - m0 < MX_TM ? M - m0 : MX_TM);
+    const int row_len = FMT == PIE_MXFP8 ? w.K : w.K / 2, NS = (row_len + 127) / 128;
+    const __amdgpu_buffer_rsrc_t rsrc_a = __builtin_amdgcn_make_buffer_rsrc(a.elements + m0 * a.row_bytes, 0, (int)((rows - 1) * a.row_bytes) + row_len, RSRC_FLAGS);
+    const __amdgpu_buffer_rsrc_t rsrc_s =
+        __builtin_amdgcn_make_buffer_rsrc(a.scales + m0 * a.scale_bytes, 0, (int)((rows - 1) * a.scale_bytes) + (w.K / 32 + 3) / 4 * 4, RSRC_FLAGS);
+    const int nbw = nb0 < w.NB ? nb0 : w.NB - NJ;  // (blocks past the matrix re-read valid ones; their results are dropped)
+    const int nbx = nbw + 1 < w.NB ? nbw + 1 : w.NB - 1;
+    const __amdgpu_buffer_rsrc_t rsrc_w = __builtin_amdgcn_make_buffer_rsrc(w.data + (int64_t)max(nbw, 0) * w.KT * 1024, 0, NJ * w.KT * 1024, RSRC_FLAGS);
+    const __amdgpu_buffer_rsrc_t rsrc_x = __builtin_amdgcn_make_buffer_rsrc(w.scales + (int64_t)max(nbw, 0) * w.KQ * 64, 0, NJ * w.KQ * 256, RSRC_FLAGS);
+    // copy instruction jj of a wave and stage: rows (wave * MI + jj) * 8 .. + 7, lane -> row lane / 8 of them, stored piece lane % 8
+    int aoff[MI];
+#pragma unroll
+    for (int jj = 0; jj < MI; ++jj) aoff[jj] = (int)(min((wave * MI + jj) * 8 + (lane >> 3), rows - 1) * a.row_bytes);
+    const int akc = ((lane & 7) ^ (lane >> 4)) * 16;  // byte of the row's 128 in instruction 0 and 2; in 1 and 3 its bit 6 is turned
+    // scales: dword d of row r is stored at d * 256 + r; instruction `wave` of 4 (MXFP8: twice) or 8 covers 64 rows of one d
+    const int srow = (wave & 3) * 64 + lane, sd = SD == 2 ? wave >> 2 : 0;
+    const int soff = (int)(min(srow, rows - 1) * a.scale_bytes);
+    const int last_dword = (w.K / 32 - 1) / 4;
+    int woff[NJ], xoff[NJ];
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      const int nb = (j == 0 ? max(nbw, 0) : nbx) - max(nbw, 0);
+      woff[j] = nb * w.KT * 1024 + lane * 16;
+      xoff[j] = nb * w.KQ * 256 + lane * 4;
+    }
+    auto issue_a = [&](uint8_t* As, uint32_t* Ss, int kt) {
+      const int k = kt < NS ? kt : NS - 1;  // past the end: a copy nobody reads, so that the wait counts stay uniform
+#pragma unroll
+      for (int jj = 0; jj < MI; ++jj) {
+        const int at = k * 128 + (akc ^ (jj & 1) * 64);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc_a, (__attribute__((address_space(3))) void*)(As + (wave * MI + jj) * 1024), 16,
+                                                 aoff[jj] + (at < row_len ? at : 0), 0, 0, 0);
+      }
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc_s, (__attribute__((address_space(3))) void*)(Ss + sd * MX_TM + (wave & 3) * 64), 4,
+                                               soff + min(k * SD + sd, last_dword) * 4, 0, 0, 0);
+    };
+    u32x4 wreg[SK][NJ];
+    int xreg[2][NJ];  // the weights' scales, a dword for four steps
+    auto load_w = [&](int kt, int s) {
+      const int k = kt < NS ? kt : NS - 1;
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) wreg[s][j] = __builtin_amdgcn_raw_buffer_load_b128(rsrc_w, woff[j], (k * SK + s) * 1024, 0);
+    };
+    auto load_x = [&](int kt, int slot) {
+      const int k = kt < NS ? kt : NS - 1;
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) xreg[slot][j] = __builtin_amdgcn_raw_buffer_load_b32(rsrc_x, xoff[j], (k * SK >> 2) * 256, 0);
+    };
+    auto load_a = [&](const uint8_t* As, int unit, i32x8 (&af)[UI]) {
+      const int s = unit / UN;
+#pragma unroll
+      for (int i = 0; i < UI; ++i) {
+        const int r = wm * (MX_TM / 2) + (unit % UN * UI + i) * 32 + (lane & 31), z = (r >> 1) & 7;
+        const uint8_t* row = As + r * 128;
+        if (FMT == PIE_MXFP8) {
+          const u32x4 lo = *reinterpret_cast<const u32x4*>(row + (((s * 4 + h) ^ z) << 4)), hi = *reinterpret_cast<const u32x4*>(row + (((s * 4 + 2 + h) ^ z) << 4));
+          af[i] = i32x8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+        } else {
+          const u32x4 lo = *reinterpret_cast<const u32x4*>(row + (((s * 2 + h) ^ z) << 4));
+          af[i] = i32x8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], 0, 0, 0, 0};
+        }
+      }
+    };
+    auto load_s = [&](const uint32_t* Ss, int kt, int (&sc)[SD][MI]) {
+#pragma unroll
+      for (int d = 0; d < SD; ++d) {
+        const int left = w.K / 32 - (kt * SD + d) * 4;  // blocks from here on
+        const uint32_t mask = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1;
+#pragma unroll
+        for (int i = 0; i < MI; ++i) sc[d][i] = (int)((Ss[d * MX_TM + wm * (MX_TM / 2) + i * 32 + (lane & 31)] & mask) >> (8 * h));
+      }
+    };
+    i32x8 af[2][UI];
+    int sc[SD][MI];
+    auto step = [&](const uint8_t* Acur, const uint8_t* Anext, const uint32_t* Snext, uint8_t* Afill, uint32_t* Sfill, int kt) {
+      issue_a(Afill, Sfill, kt + 2);
+      __builtin_amdgcn_sched_barrier(0);
+      load_x(kt + 1, 1);
+      const int shift = FMT == PIE_MXFP8 ? (kt & 1) * 16 : 0;
+      int xs[NJ], nsc[SD][MI];
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) xs[j] = (int)((uint32_t)xreg[0][j] >> shift);
+#pragma unroll
+      for (int u = 0; u < SK * UN; ++u) {
+        const int s = u / UN;
+        if (u + 1 < SK * UN) {
+          load_a(Acur, u + 1, af[(u + 1) & 1]);
+        } else {
+          PIE_S_WAIT_LGKMCNT0();  // this wave's last reads of Acur have returned
+          // newer than the copies of stage kt + 1: the copies, scales and weights requested in this step
+          PIE_S_WAIT_VMCNT(MI + 1 + NJ + (SK - 1) * NJ);
+          wg_barrier();
+          load_a(Anext, 0, af[(u + 1) & 1]);
+          load_s(Snext, kt + 1, nsc);
+        }
+#pragma unroll
+        for (int i = 0; i < UI; ++i)
+#pragma unroll
+          for (int j = 0; j < NJ; ++j) {
+            const u32x4 e = wreg[s][j];
+            const i32x8 wo = {(int)e[0], (int)e[1], (int)e[2], (int)e[3], 0, 0, 0, 0};
+            const int ii = u % UN * UI + i;
+            constexpr int F = FMT == PIE_MXFP8 ? 0 : 4;
+            switch (s) {  // (the byte of the scales is part of the instruction)
+              case 0: acc[ii][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wo, af[u & 1][i], acc[ii][j], 4, F, 0, xs[j], 0, sc[0][ii]); break;
+              case 1: acc[ii][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wo, af[u & 1][i], acc[ii][j], 4, F, 1, xs[j], 2, sc[0][ii]); break;
+              case 2: acc[ii][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wo, af[u & 1][i], acc[ii][j], 4, F, 2, xs[j], 0, sc[SD - 1][ii]); break;
+              case 3: acc[ii][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wo, af[u & 1][i], acc[ii][j], 4, F, 3, xs[j], 2, sc[SD - 1][ii]); break;
+            }
+          }
+        if (u % UN == UN - 1) load_w(kt + 1, s);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) xreg[0][j] = xreg[1][j];
+#pragma unroll
+      for (int d = 0; d < SD; ++d)
+#pragma unroll
+        for (int i = 0; i < MI; ++i) sc[d][i] = nsc[d][i];
+    };
+    issue_a(As0, Ss0, 0);
+    issue_a(As1, Ss1, 1);
+    __builtin_amdgcn_sched_barrier(0);
+    load_x(0, 0);
+#pragma unroll
+    for (int s = 0; s < SK; ++s) load_w(0, s);
+    __builtin_amdgcn_sched_barrier(0);
+    PIE_S_WAIT_VMCNT(MI + 1 + NJ + SK * NJ);  // the first stage has arrived
+    wg_barrier();
+    load_a(As0, 0, af[0]);
+    load_s(Ss0, 0, sc);
+    int kt = 0;
+    for (; kt + 3 <= NS; kt += 3) {
+      step(As0, As1, Ss1, As2, Ss2, kt);
+      step(As1, As2, Ss2, As0, Ss0, kt + 1);
+      step(As2, As0, Ss0, As1, Ss1, kt + 2);
+    }
+    if (kt < NS) {
+      step(As0, As1, Ss1, As2, Ss2, kt);
+      if (kt + 1 < NS) step(As1, As2, Ss2, As0, Ss0, kt + 1);
+    }
+    PIE_S_WAIT_VMCNT(0);  // the surplus copies of the last steps land before the workgroup gives up its LDS
+#endif
+  }
+#pragma unroll
+  for (int i = 0; i < MI; ++i) {
+    const int64_t m = m0 + wm * (MX_TM / 2) + i * 32 + (lane & 31);
+    if constexpr (MODE == MX_SWIGLU8 || MODE == MX_SWIGLU4) {
+      if (nb0 < w.NB) mx_epilogue<MODE>(epi, acc[i][0], acc[i][1], m, M, nb0 * 32, lane);
+    } else {
+#pragma unroll
+      for (int j = 0; j < NJ; ++j)
+        if (nb0 + j < w.NB) mx_epilogue<MODE>(epi, acc[i][j], acc[i][j], m, M, (nb0 + j) * 32, lane);
+    }
+  }
+}
+
 template <int MODE>
 static hipError_t run_product(const MxRowsView& a, int format, int M, const MxPacked& w, const MxEpi& epi, hipStream_t s) {
+  if (M > 128) {
+    const int tiles_m = (M + MX_TM - 1) / MX_TM, tiles_n = (w.NB + MX_TN / 32 - 1) / (MX_TN / 32);
+    const dim3 grid((unsigned)((int64_t)tiles_m * tiles_n));
+    if (format == PIE_MXFP8) mx_tiles_kernel<MODE, PIE_MXFP8><<<grid, dim3(512), 0, s>>>(a, M, w, epi, tiles_m, tiles_n);
+    else mx_tiles_kernel<MODE, PIE_MXFP4><<<grid, dim3(512), 0, s>>>(a, M, w, epi, tiles_m, tiles_n);
+    return hipGetLastError();
+  }
   const int cols = MODE == MX_SWIGLU8 || MODE == MX_SWIGLU4 ? w.NB / 2 : w.NB;
   const int tiles_m = (M + 31) / 32;
   const int64_t tiles = (int64_t)((cols + 3) / 4) * tiles_m;

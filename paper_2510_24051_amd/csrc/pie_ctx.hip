@@ -1945,6 +1945,7 @@ extern "C" pie_status pie_compact_kvpage(pie_ctx* c, int32_t n_seqs, const int32
 // microscaled formats
 // ---------------------------------------------------------------------------------------------
 #define MX_MAX_K (1 << 20)
+#define MX_MAX_STRIDE (1 << 22)  // bytes between rows: 256 of them are within reach of 32-bit offsets
 #define MX_MAX_ROWS (1 << 24)
 
 static MxRowsView mx_rows_view(const pie_mx_rows* r) {
@@ -1966,6 +1967,8 @@ static pie_status check_mx_rows(pie_ctx* c, const pie_mx_rows* r, int32_t k, con
     return fail(c, PIE_EINVAL, "%s: elements have to be 16-byte aligned, their rows a multiple of 16 bytes apart and at least %lld", who, (long long)mx_row_size(r->format, k));
   if (reinterpret_cast<uintptr_t>(r->scales) % 4 || r->scale_bytes % 4 || r->scale_bytes < k / 32)
     return fail(c, PIE_EINVAL, "%s: scales have to be 4-byte aligned, their rows a multiple of 4 bytes apart and at least %d", who, k / 32);
+  if (r->row_bytes > MX_MAX_STRIDE || r->scale_bytes > MX_MAX_STRIDE)
+    return fail(c, PIE_EUNSUPPORTED, "%s: rows are %lld bytes apart, scales %lld: at most %d", who, (long long)r->row_bytes, (long long)r->scale_bytes, MX_MAX_STRIDE);
   return PIE_OK;
 }
 static pie_status check_rows(pie_ctx* c, const pie_rows* r, int32_t k, const char* what, const char* who) {
@@ -2024,7 +2027,7 @@ extern "C" pie_status pie_mx_norm(pie_ctx* c, const pie_rows* x, const pie_rows*
 static pie_status mx_alloc(pie_ctx* c, MxPacked& w, int N, int K) {
   free_packed(w);
   w.N = N; w.K = K;
-  w.NB = (N + 31) / 32; w.KT = (K + 63) / 64; w.KQ = (w.KT + 3) / 4;
+  w.NB = (N + 31) / 32; w.KQ = (K + 255) / 256; w.KT = w.KQ * 4;
   const size_t data = (size_t)w.NB * w.KT * 1024, scales = (size_t)w.NB * w.KQ * 256;
   if (hipError_t e = hipMalloc(reinterpret_cast<void**>(&w.data), data + scales); e != hipSuccess) {
     w = MxPacked();
