@@ -471,4 +471,5 @@ struct MxEpi {
   const float* resid;
   int H;
 };
-hipError_t launch_mx_product(const MxRowsView& a, int format, int M, const MxPacked& w, const MxEpi& epi, hipStream_t s);
+// ws: MX_WS_FLOATS of workspace
+hipError_t launch_mx_product(const MxRowsView& a, int format, int M, const MxPacked& w, const MxEpi& epi, float* ws, int n_cus, hipStream_t s);

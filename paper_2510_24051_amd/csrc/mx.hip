@@ -400,49 +400,27 @@ __device__ __forceinline__ void mx_epilogue(const MxEpi& e, const f32x16& acc, c
   }
 }
 
-// ---------------------------------------------------------------------------------------------
-// Product.  D[weight row][token] = W x A^T on v_mfma_scale_f32_32x32x64_f8f6f4: a lane of the weight operand has 32 elements of one block; a
-// lane of an MXFP8 operand has bytes [16 h, 16 h + 16) and [32 + 16 h, 48 + 16 h) of its row's 64, and in either case the scale of block
-// h of its row.  A wave takes 32 weight rows (SwiGLU: a gate and an up block) and 32 tokens.
-// ---------------------------------------------------------------------------------------------
-template <int MODE, int FMT>
-__global__ __launch_bounds__(256) void mx_product_kernel(MxRowsView a, int M, MxPacked w, MxEpi epi, int tiles_m) {
-  constexpr int NJ = MODE == MX_SWIGLU8 || MODE == MX_SWIGLU4 ? 2 : 1;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
-  const int nb0 = ((int)(blockIdx.x / tiles_m) * 4 + wave) * NJ;
-  if (nb0 >= w.NB) return;
-  const int64_t m = (int64_t)(blockIdx.x % tiles_m) * 32 + (lane & 31);
-  const int64_t row = m < M ? m : M - 1;  // rows past M re-read a valid row; their results are not stored
-  const uint8_t* ap = a.elements + row * a.row_bytes;
-  const uint8_t* as = a.scales + row * a.scale_bytes;
-  const int blocks = w.K / 32;
-  f32x16 acc[NJ];
-#pragma unroll
-  for (int j = 0; j < NJ; ++j)
-#pragma unroll
-    for (int v = 0; v < 16; ++v) acc[j][v] = 0.f;
-  for (int kt = 0; kt < (w.K + 63) / 64; ++kt) {
-    const int b = kt * 2;
-    u32x4 lo = {0, 0, 0, 0}, hi = lo;
-    if (FMT == PIE_MXFP8) {
-      lo = *reinterpret_cast<const u32x4*>(ap + b * 32 + h * 16);
-      if (b + 1 < blocks) hi = *reinterpret_cast<const u32x4*>(ap + b * 32 + 32 + h * 16);
-    } else if (b + h < blocks) {
-      lo = *reinterpret_cast<const u32x4*>(ap + (b + h) * 16);
-    }
-    const int sb = b + h < blocks ? as[b + h] : 0;
-    const i32x8 bo = {(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
-#pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-      const u32x4 e = *reinterpret_cast<const u32x4*>(w.data + (((int64_t)(nb0 + j) * w.KT + kt) * 64 + lane) * 16);
-      const int sa = (int)(w.scales[((int64_t)(nb0 + j) * w.KQ + (kt >> 2)) * 64 + lane] >> (8 * (kt & 3)));
-      const i32x8 ao = {(int)e[0], (int)e[1], (int)e[2], (int)e[3], 0, 0, 0, 0};
-      acc[j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ao, bo, acc[j], 4, FMT == PIE_MXFP8 ? 0 : 4, 0, sa, 0, sb);
-    }
+// The epilogue of a product that is not gated, by the mode of its arguments (uniform).
+__device__ __forceinline__ void mx_plain_epilogue(const MxEpi& e, const f32x16& acc, int64_t m, int M, int n0, int lane) {
+  switch (e.mode) {
+    case MX_BF16: mx_epilogue<MX_BF16>(e, acc, acc, m, M, n0, lane); break;
+    case MX_F32: mx_epilogue<MX_F32>(e, acc, acc, m, M, n0, lane); break;
+    case MX_RESID_EMBED: mx_epilogue<MX_RESID_EMBED>(e, acc, acc, m, M, n0, lane); break;
+    case MX_RESID_OUT: mx_epilogue<MX_RESID_OUT>(e, acc, acc, m, M, n0, lane); break;
   }
-  mx_epilogue<MODE>(epi, acc[0], acc[NJ - 1], m, M, nb0 * 32, lane);
+}
+__device__ __forceinline__ void mx_gated_epilogue(const MxEpi& e, const f32x16& gate, const f32x16& up, int64_t m, int M, int n0, int lane) {
+  if (e.mode == MX_SWIGLU8) mx_epilogue<MX_SWIGLU8>(e, gate, up, m, M, n0, lane);
+  else mx_epilogue<MX_SWIGLU4>(e, gate, up, m, M, n0, lane);
 }
 
+// ---------------------------------------------------------------------------------------------
+// Products.  D[weight row][token] = W x A^T on v_mfma_scale_f32_32x32x64_f8f6f4: a lane of the weight operand has 32 elements of one block; a
+// lane of an MXFP8 operand has bytes [16 h, 16 h + 16) and [32 + 16 h, 48 + 16 h) of its row's 64, and in either case the scale of block
+// h of its row.  With an MXFP8 operand the instruction aligns each eight neighbouring products to the largest and drops what is below
+// 2^-13 of its power of two: 1.5e-5 of a sum's size on rows whose channels differ in size as a model's do, and nothing that 8 bits of activations, 4
+// of weights or bf16 results would show; the way around it, bf16 operands, has half of the rate.  Sums are fp32.
+// ---------------------------------------------------------------------------------------------
 // ---------------------------------------------------------------------------------------------
 // Tiles of 256 tokens x 256 weight rows: many rows, bound by the matrix cores.
 // Eight waves, two along the tokens and four along the weight rows, of 4 x 2 accumulator tiles each.  Activations go to LDS by direct copies, 128 bytes of
@@ -453,12 +431,16 @@ __global__ __launch_bounds__(256) void mx_product_kernel(MxRowsView a, int M, Mx
 // ---------------------------------------------------------------------------------------------
 constexpr int MX_TM = 256, MX_TN = 256;
 
-template <int MODE, int FMT>
+// Byte offset of a tile's row for its copies.  Rows past the matrix are out of the descriptor's range: nothing is fetched for them (rows of
+// one token that copied the last row 32 times took ?), and what their lanes compute is not stored.
+__device__ __forceinline__ int mx_row_offset(int r, int rows, int64_t stride) { return r < rows ? (int)(r * stride) : 0x7f000000; }
+
+template <bool GATED, int FMT>
 __global__ __launch_bounds__(512, 2) void mx_tiles_kernel(MxRowsView a, int M, MxPacked w, MxEpi epi, int tiles_m, int tiles_n) {
   constexpr int SK = FMT == PIE_MXFP8 ? 2 : 4;  // steps of 64 a stage
   constexpr int SD = SK / 2;                    // dwords of scales a row and stage
   constexpr int MI = 4, NJ = 2;
-  [[maybe_unused]] constexpr int UI = FMT == PIE_MXFP8 ? 2 : 4, UN = MI / UI;  // accumulator blocks whose operands are read at a time, and such units of a step
+  [[maybe_unused]] constexpr int UI = 2, UN = MI / UI;  // accumulator blocks whose operands are read at a time, and such units of a step
   [[maybe_unused]] __shared__ __align__(16) uint8_t As0[MX_TM * 128], As1[MX_TM * 128], As2[MX_TM * 128];
   [[maybe_unused]] __shared__ uint32_t Ss0[MX_TM * SD], Ss1[MX_TM * SD], Ss2[MX_TM * SD];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -490,11 +472,11 @@ __global__ __launch_bounds__(512, 2) void mx_tiles_kernel(MxRowsView a, int M, M
     // copy instruction jj of a wave and stage: rows (wave * MI + jj) * 8 .. + 7, lane -> row lane / 8 of them, stored piece lane % 8
     int aoff[MI];
 #pragma unroll
-    for (int jj = 0; jj < MI; ++jj) aoff[jj] = (int)(min((wave * MI + jj) * 8 + (lane >> 3), rows - 1) * a.row_bytes);
+    for (int jj = 0; jj < MI; ++jj) aoff[jj] = mx_row_offset((wave * MI + jj) * 8 + (lane >> 3), rows, a.row_bytes);
     const int akc = ((lane & 7) ^ (lane >> 4)) * 16;  // byte of the row's 128 in instruction 0 and 2; in 1 and 3 its bit 6 is turned
     // scales: dword d of row r is stored at d * 256 + r; instruction `wave` of 4 (MXFP8: twice) or 8 covers 64 rows of one d
     const int srow = (wave & 3) * 64 + lane, sd = SD == 2 ? wave >> 2 : 0;
-    const int soff = (int)(min(srow, rows - 1) * a.scale_bytes);
+    const int soff = mx_row_offset(srow, rows, a.scale_bytes);
     const int last_dword = (w.K / 32 - 1) / 4;
     int woff[NJ], xoff[NJ];
 #pragma unroll
@@ -625,44 +607,482 @@ __global__ __launch_bounds__(512, 2) void mx_tiles_kernel(MxRowsView a, int M, M
 #pragma unroll
   for (int i = 0; i < MI; ++i) {
     const int64_t m = m0 + wm * (MX_TM / 2) + i * 32 + (lane & 31);
-    if constexpr (MODE == MX_SWIGLU8 || MODE == MX_SWIGLU4) {
-      if (nb0 < w.NB) mx_epilogue<MODE>(epi, acc[i][0], acc[i][1], m, M, nb0 * 32, lane);
+    if constexpr (GATED) {
+      if (nb0 < w.NB) mx_gated_epilogue(epi, acc[i][0], acc[i][1], m, M, nb0 * 32, lane);
     } else {
 #pragma unroll
       for (int j = 0; j < NJ; ++j)
-        if (nb0 + j < w.NB) mx_epilogue<MODE>(epi, acc[i][j], acc[i][j], m, M, (nb0 + j) * 32, lane);
+        if (nb0 + j < w.NB) mx_plain_epilogue(epi, acc[i][j], m, M, (nb0 + j) * 32, lane);
     }
   }
 }
 
-template <int MODE>
-static hipError_t run_product(const MxRowsView& a, int format, int M, const MxPacked& w, const MxEpi& epi, hipStream_t s) {
-  if (M > 128) {
-    const int tiles_m = (M + MX_TM - 1) / MX_TM, tiles_n = (w.NB + MX_TN / 32 - 1) / (MX_TN / 32);
-    const dim3 grid((unsigned)((int64_t)tiles_m * tiles_n));
-    if (format == PIE_MXFP8) mx_tiles_kernel<MODE, PIE_MXFP8><<<grid, dim3(512), 0, s>>>(a, M, w, epi, tiles_m, tiles_n);
-    else mx_tiles_kernel<MODE, PIE_MXFP4><<<grid, dim3(512), 0, s>>>(a, M, w, epi, tiles_m, tiles_n);
-    return hipGetLastError();
+// ---------------------------------------------------------------------------------------------
+// Few rows: bound by the stream of weights, or by its latency.
+// Eight waves; KS slices of the contraction (or parts of them, where the product is split over workgroups as well) with 8 / KS waves each, a
+// wave with MB x NJ accumulator tiles: 32 weight rows (SwiGLU: a gate and an up block) by 32 MB tokens.  Each wave keeps SW stages of
+// weights in registers (stages as in mx_tiles_kernel, requested non-temporally), each slice SA stages of its activations in LDS.  A slice's
+// stages are NS p / parts .. NS (p + 1) / parts; all walk as many as the longest has, the others doing nothing in the last.  The slices'
+// sums meet in LDS, in their order.
+// ---------------------------------------------------------------------------------------------
+constexpr int mx_stages_a(int mb, int ks) { return mb * ks <= 8 ? 4 : mb * ks <= 12 ? 3 : 2; }
+// weights in flight: 64 to 128 KiB of a compute unit, less where the registers hold accumulators
+constexpr int mx_stages_w(int fmt, int nj, int mb, int ks) {
+  const int room = mb == 1 ? 128 : mb == 2 ? 64 : 48 + 16 * (mb == 4 && nj == 1), stage = (fmt == PIE_MXFP8 ? 8 : 16) * nj;  // registers
+  const int fit = room / stage;
+  return mx_stages_a(mb, ks) == 3 ? (fit >= 6 ? 6 : fit >= 3 ? 3 : fit >= 2 ? 2 : 1) : fit >= 8 ? 8 : fit >= 4 ? 4 : fit >= 2 ? 2 : 1;
+}
+constexpr int mx_stages_round(int sa, int sw) { return sw % sa == 0 ? sw : sa % sw == 0 ? sa : sa * sw; }
+
+template <bool GATED, int FMT, int MB, int KS, int NJ>
+__global__ __launch_bounds__(512, 2) void mx_stream_kernel(MxRowsView a, int M, MxPacked w, MxEpi epi, int tiles_m, int tiles_n, int splits, float* part) {
+  static_assert(!GATED || NJ == 2, "a gate and an up block");
+  constexpr int WN = 8 / KS, BM = 32 * MB;
+  [[maybe_unused]] constexpr int SK = FMT == PIE_MXFP8 ? 2 : 4, SD = SK / 2;
+  constexpr int SA = mx_stages_a(MB, KS);
+  [[maybe_unused]] constexpr int SW = mx_stages_w(FMT, NJ, MB, KS), RS = mx_stages_round(SA, SW);  // (RS: steps of a round of both rings)
+  [[maybe_unused]] constexpr int UI = MB == 4 ? 2 : MB, UN = MB / UI;                              // (see mx_tiles_kernel)
+  constexpr int STAGE = KS * BM * 128;
+  [[maybe_unused]] constexpr int PIECES = STAGE / 1024, CP = (PIECES + 7) / 8;              // copy instructions of a stage, and of a wave
+  [[maybe_unused]] constexpr int SPIECES = (KS * BM * SD + 63) / 64, SP = (SPIECES + 7) / 8;  // the same of the scales
+  __shared__ __align__(16) uint8_t As[SA][STAGE];
+  [[maybe_unused]] __shared__ uint32_t Ss[SA][SPIECES * 64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  [[maybe_unused]] const int h = lane >> 5;
+  const int ks = wave / WN;
+  int tm, tn;
+  tile_at(xcd_range(blockIdx.x, tiles_m, tiles_n), tiles_m, tiles_n, tm, tn);
+  const int64_t m0 = (int64_t)tm * BM;
+  const int nb0 = (tn * WN + wave % WN) * NJ;
+  f32x16 acc[MB][NJ];
+#pragma unroll
+  for (int i = 0; i < MB; ++i)
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
+  {
+#if __HIP_DEVICE_COMPILE__
+    constexpr int RSRC_FLAGS = 0x00020000;
+    const int rows = (int)(M - m0 < BM ? M - m0 : BM);
+    const int row_len = FMT == PIE_MXFP8 ? w.K : w.K / 2, NS = (row_len + 127) / 128;
+    const int parts = KS * splits;
+    auto first_of = [&](int sl) { return (int)((int64_t)NS * ((int)blockIdx.y * KS + sl) / parts); };
+    const int first = first_of(ks), n = first_of(ks + 1) - first;  // this slice's stages
+    const int nmax = (NS + parts - 1) / parts;
+    const __amdgpu_buffer_rsrc_t rsrc_a = __builtin_amdgcn_make_buffer_rsrc(a.elements + m0 * a.row_bytes, 0, (int)((rows - 1) * a.row_bytes) + row_len, RSRC_FLAGS);
+    const __amdgpu_buffer_rsrc_t rsrc_s =
+        __builtin_amdgcn_make_buffer_rsrc(a.scales + m0 * a.scale_bytes, 0, (int)((rows - 1) * a.scale_bytes) + (w.K / 32 + 3) / 4 * 4, RSRC_FLAGS);
+    // blocks past the matrix are out of the descriptors' range: nothing is fetched for them, and their results are dropped
+    const int held = max(0, min(NJ, w.NB - nb0)), nbw = held > 0 ? nb0 : 0;
+    const __amdgpu_buffer_rsrc_t rsrc_w = __builtin_amdgcn_make_buffer_rsrc(w.data + (int64_t)nbw * w.KT * 1024, 0, held * w.KT * 1024, RSRC_FLAGS);
+    const __amdgpu_buffer_rsrc_t rsrc_x = __builtin_amdgcn_make_buffer_rsrc(w.scales + (int64_t)nbw * w.KQ * 64, 0, held * w.KQ * 256, RSRC_FLAGS);
+    // copy piece p covers eight rows of a slice's tile: lane -> row lane / 8 of them, stored piece lane % 8; past the last one a wave copies
+    // that one again (same bytes)
+    int aoff[CP], akc[CP], afirst[CP], soff[SP], sdw[SP];
+#pragma unroll
+    for (int jj = 0; jj < CP; ++jj) {
+      const int p = min(wave * CP + jj, PIECES - 1), sl = p / (BM / 8), r = p % (BM / 8) * 8 + (lane >> 3);
+      akc[jj] = ((lane & 7) ^ ((r >> 1) & 7)) * 16;
+      aoff[jj] = mx_row_offset(r, rows, a.row_bytes);
+      afirst[jj] = first_of(sl);
+    }
+    // scales: dword d of row r of slice sl is stored at (sl * SD + d) * BM + r
+#pragma unroll
+    for (int jj = 0; jj < SP; ++jj) {
+      const int p = min(wave * SP + jj, SPIECES - 1), at = min(p * 64 + lane, KS * BM * SD - 1), sl = at / (BM * SD), d = at / BM % SD, r = at % BM;
+      soff[jj] = mx_row_offset(r, rows, a.scale_bytes);
+      sdw[jj] = first_of(sl) * SD + d;
+    }
+    const int last_dword = (w.K / 32 - 1) / 4;
+    auto issue_a = [&](int st, int kt) {
+      const int k = min(kt, nmax - 1);  // past the end: a copy nobody reads, so that the wait counts stay uniform
+#pragma unroll
+      for (int jj = 0; jj < CP; ++jj) {
+        const int p = min(wave * CP + jj, PIECES - 1);
+        const int at = min(afirst[jj] + k, NS - 1) * 128 + akc[jj];
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc_a, (__attribute__((address_space(3))) void*)(&As[st][p * 1024]), 16, aoff[jj] + (at < row_len ? at : 0), 0, 0, 0);
+      }
+#pragma unroll
+      for (int jj = 0; jj < SP; ++jj) {
+        const int p = min(wave * SP + jj, SPIECES - 1);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc_s, (__attribute__((address_space(3))) void*)(&Ss[st][p * 64]), 4, soff[jj] + min(sdw[jj] + k * SD, last_dword) * 4, 0, 0, 0);
+      }
+    };
+    u32x4 wreg[SW][SK][NJ];
+    int xreg[SW][NJ];
+    const int stage_last = min(first + max(n, 1), NS) - 1;
+    auto load_x = [&](int slot, int kt) {
+      const int k = min(first + kt, stage_last);
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) xreg[slot][j] = __builtin_amdgcn_raw_buffer_load_b32(rsrc_x, j * w.KQ * 256 + lane * 4, (k * SK >> 2) * 256, 0);
+    };
+    auto load_w = [&](int slot, int kt, int s) {
+      const int k = min(first + kt, stage_last);
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) wreg[slot][s][j] = __builtin_amdgcn_raw_buffer_load_b128(rsrc_w, j * w.KT * 1024 + lane * 16, (k * SK + s) * 1024, 2);  // (2: non-temporal)
+    };
+    auto load_a = [&](int st, int unit, i32x8 (&af)[UI]) {
+      const int s = unit / UN;
+#pragma unroll
+      for (int i = 0; i < UI; ++i) {
+        const int r = (unit % UN * UI + i) * 32 + (lane & 31), z = (r >> 1) & 7;
+        const uint8_t* row = &As[st][(ks * BM + r) * 128];
+        if (FMT == PIE_MXFP8) {
+          const u32x4 lo = *reinterpret_cast<const u32x4*>(row + (((s * 4 + h) ^ z) << 4)), hi = *reinterpret_cast<const u32x4*>(row + (((s * 4 + 2 + h) ^ z) << 4));
+          af[i] = i32x8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+        } else {
+          const u32x4 lo = *reinterpret_cast<const u32x4*>(row + (((s * 2 + h) ^ z) << 4));
+          af[i] = i32x8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], 0, 0, 0, 0};
+        }
+      }
+    };
+    auto load_s = [&](int st, int kt, int (&sc)[SD][MB]) {
+#pragma unroll
+      for (int d = 0; d < SD; ++d) {
+        const int left = w.K / 32 - ((first + kt) * SD + d) * 4;  // blocks from here on
+        const uint32_t mask = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1;
+#pragma unroll
+        for (int i = 0; i < MB; ++i) sc[d][i] = (int)((Ss[st][(ks * SD + d) * BM + i * 32 + (lane & 31)] & mask) >> (8 * h));
+      }
+    };
+    i32x8 af[2][UI];
+    int sc[SD][MB];
+    // Step kt from weight slot `slot` and activation stage slot % SA; the order of requests and waits is that of mx_tiles_kernel, with the copies
+    // SA - 1 steps ahead and the weights SW.  TAIL: no weights are requested any more, and only the copies are counted.
+    auto step = [&](auto tail_c, auto slot_c, int kt) {
+      constexpr int SLOT = decltype(slot_c)::value % SW, AT = decltype(slot_c)::value, CUR = AT % SA, NEXT = (AT + 1) % SA, FILL = (AT + SA - 1) % SA;
+      constexpr bool TAIL = decltype(tail_c)::value;
+      issue_a(FILL, kt + SA - 1);
+      __builtin_amdgcn_sched_barrier(0);
+      const int shift = FMT == PIE_MXFP8 ? ((first + kt) & 1) * 16 : 0;
+      int xs[NJ], nsc[SD][MB];
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) xs[j] = (int)((uint32_t)xreg[SLOT][j] >> shift);
+      if constexpr (!TAIL) load_x(SLOT, kt + SW);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int u = 0; u < SK * UN; ++u) {
+        const int s = u / UN;
+        if (u + 1 < SK * UN) {
+          load_a(CUR, u + 1, af[(u + 1) & 1]);
+        } else {
+          PIE_S_WAIT_LGKMCNT0();  // this wave's last reads of the stage have returned
+          if constexpr (TAIL) PIE_S_WAIT_VMCNT((SA - 2) * (CP + SP));
+          else PIE_S_WAIT_VMCNT((SA - 2) * (CP + SP) + (SW < SA - 2 ? SW : SA - 2) * (SK + 1) * NJ + SK * NJ);  // (the prologue has SW steps' weights)
+          wg_barrier();
+          load_a(NEXT, 0, af[(u + 1) & 1]);
+          load_s(NEXT, kt + 1, nsc);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if (kt < n) {  // (uniform; a slice that is one stage shorter than the longest)
+#pragma unroll
+          for (int i = 0; i < UI; ++i)
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+              const u32x4 e = wreg[SLOT][s][j];
+              const i32x8 wo = {(int)e[0], (int)e[1], (int)e[2], (int)e[3], 0, 0, 0, 0};
+              const int ii = u % UN * UI + i;
+              constexpr int F = FMT == PIE_MXFP8 ? 0 : 4;
+              switch (s) {  // (the byte of the scales is part of the instruction)
+                case 0: acc[ii][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wo, af[u & 1][i], acc[ii][j], 4, F, 0, xs[j], 0, sc[0][ii]); break;
+                case 1: acc[ii][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wo, af[u & 1][i], acc[ii][j], 4, F, 1, xs[j], 2, sc[0][ii]); break;
+                case 2: acc[ii][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wo, af[u & 1][i], acc[ii][j], 4, F, 2, xs[j], 0, sc[SD - 1][ii]); break;
+                case 3: acc[ii][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wo, af[u & 1][i], acc[ii][j], 4, F, 3, xs[j], 2, sc[SD - 1][ii]); break;
+              }
+            }
+        }
+        if constexpr (!TAIL)
+          if (u % UN == UN - 1) load_w(SLOT, kt + SW, s);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int d = 0; d < SD; ++d)
+#pragma unroll
+        for (int i = 0; i < MB; ++i) sc[d][i] = nsc[d][i];
+    };
+    // Prologue: copies of stages 0 .. SA - 2 first, then the weights of SW steps.
+#pragma unroll
+    for (int j = 0; j < SA - 1; ++j) issue_a(j, j);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int j = 0; j < SW; ++j) {
+      load_x(j, j);
+#pragma unroll
+      for (int s = 0; s < SK; ++s) load_w(j, j, s);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    constexpr int NEWER = (SA - 2) * (CP + SP) + SW * (SK + 1) * NJ;
+    PIE_S_WAIT_VMCNT(NEWER < 63 ? NEWER : 63);  // the first stage has arrived
+    wg_barrier();
+    load_a(0, 0, af[0]);
+    load_s(0, 0, sc);
+    int kt = 0;
+    using std::integral_constant;
+    // a round, or its first `left` steps, which request no weights
+    auto round = [&](auto tail_c, int left) {
+      constexpr bool TAIL = decltype(tail_c)::value;
+      auto one = [&](auto slot_c) {
+        constexpr int AT = decltype(slot_c)::value;
+        if constexpr (AT < (TAIL ? SW : RS)) {
+          if (!TAIL || AT < left) step(tail_c, slot_c, kt + AT);
+        }
+      };
+      one(integral_constant<int, 0>{}); one(integral_constant<int, 1>{}); one(integral_constant<int, 2>{}); one(integral_constant<int, 3>{});
+      one(integral_constant<int, 4>{}); one(integral_constant<int, 5>{}); one(integral_constant<int, 6>{}); one(integral_constant<int, 7>{});
+    };
+    static_assert(RS <= 8 && RS >= SW, "a round is written out");
+    for (; kt + SW < nmax; kt += RS) round(std::false_type{}, RS);  // (steps past the last do nothing)
+    round(std::true_type{}, nmax - kt);
+    PIE_S_WAIT_VMCNT(0);  // the surplus copies of the last steps land before the stages are used for anything else
+#endif
   }
-  const int cols = MODE == MX_SWIGLU8 || MODE == MX_SWIGLU4 ? w.NB / 2 : w.NB;
-  const int tiles_m = (M + 31) / 32;
-  const int64_t tiles = (int64_t)((cols + 3) / 4) * tiles_m;
-  if (tiles > INT32_MAX) return hipErrorInvalidValue;
-  const dim3 grid((unsigned)tiles);
-  if (format == PIE_MXFP8) mx_product_kernel<MODE, PIE_MXFP8><<<grid, dim3(256), 0, s>>>(a, M, w, epi, tiles_m);
-  else mx_product_kernel<MODE, PIE_MXFP4><<<grid, dim3(256), 0, s>>>(a, M, w, epi, tiles_m);
+  // The slices' sums meet one row of token blocks at a time: wave (ks, column) of block i's turn adds those of the others to its own, in
+  // slice order, and finishes it.
+  auto finish = [&](int i) {
+    const int64_t m = m0 + i * 32 + (lane & 31);
+    if (part != nullptr) {
+      if (m >= M) return;
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        if (nb0 + j >= w.NB) continue;
+        float* p = part + (((int64_t)blockIdx.y * M + m) * w.NB + nb0 + j) * 32 + (lane >> 5) * 4;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) *reinterpret_cast<f32x4*>(p + 8 * g) = f32x4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
+      }
+    } else if constexpr (GATED) {
+      if (nb0 < w.NB) mx_gated_epilogue(epi, acc[i][0], acc[i][1], m, M, nb0 * 32, lane);
+    } else {
+#pragma unroll
+      for (int j = 0; j < NJ; ++j)
+        if (nb0 + j < w.NB) mx_plain_epilogue(epi, acc[i][j], m, M, (nb0 + j) * 32, lane);
+    }
+  };
+  if constexpr (KS == 1) {
+#pragma unroll
+    for (int i = 0; i < MB; ++i) finish(i);
+    return;
+  }
+  constexpr int OTHERS = (KS - 1) * WN;  // waves whose sums a block's owners read
+  constexpr int FIT = SA * STAGE / ((OTHERS ? OTHERS : 1) * NJ * 4096), ROUND = FIT < MB ? FIT : MB;  // token blocks whose sums fit the stages
+  static_assert(ROUND >= 1, "a block of every wave fits the stages");
+  auto sums_of = [&](int i, int sl, int j) {  // of slice sl (not the owner i % KS), block i of a round
+    const int other = sl < i % KS ? sl : sl - 1;
+    return reinterpret_cast<float*>(&As[0][0]) + ((i % ROUND * OTHERS + other * WN + wave % WN) * NJ + j) * 1024 + lane * 4;
+  };
+#pragma unroll
+  for (int i0 = 0; i0 < MB; i0 += ROUND) {
+    __syncthreads();
+#pragma unroll
+    for (int i = i0; i < (i0 + ROUND < MB ? i0 + ROUND : MB); ++i)
+      if (i % KS != ks) {
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+          for (int v = 0; v < 16; v += 4)
+            *reinterpret_cast<f32x4*>(sums_of(i, ks, j) + v * 64) = f32x4{acc[i][j][v], acc[i][j][v + 1], acc[i][j][v + 2], acc[i][j][v + 3]};
+      }
+    __syncthreads();
+#pragma unroll
+    for (int i = i0; i < (i0 + ROUND < MB ? i0 + ROUND : MB); ++i)
+      if (i % KS == ks) {
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+          f32x16 t;
+#pragma unroll
+          for (int v = 0; v < 16; ++v) t[v] = 0.f;
+#pragma unroll
+          for (int sl = 0; sl < KS; ++sl) {
+            if (sl == ks) {
+              t += acc[i][j];
+            } else {
+#pragma unroll
+              for (int v = 0; v < 16; v += 4) {
+                const f32x4 o = *reinterpret_cast<const f32x4*>(sums_of(i, sl, j) + v * 64);
+#pragma unroll
+                for (int u = 0; u < 4; ++u) t[v + u] += o[u];
+              }
+            }
+          }
+          acc[i][j] = t;
+        }
+        finish(i);
+      }
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// Joins the sums [splits][M][NB * 32] of a product that was split over workgroups, in their order: eight columns a lane.
+// ---------------------------------------------------------------------------------------------
+template <bool GATED>
+__global__ __launch_bounds__(256) void mx_join_kernel(const float* __restrict__ part, int splits, int M, int NB, MxEpi e) {
+  const int cols8 = GATED ? NB * 2 : NB * 4;  // pieces of eight columns (of the result) a row
+  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (at >= (int64_t)M * cols8) return;
+  const int64_t m = at / cols8;
+  const int c = (int)(at % cols8) * 8;
+  const int64_t stride = (int64_t)M * NB * 32;
+  auto total = [&](int n, float (&v)[8]) {
+    f32x4 a = {0.f, 0.f, 0.f, 0.f}, b = a;
+    const float* p = part + m * NB * 32 + n;
+    for (int k = 0; k < splits; ++k) {
+      a += *reinterpret_cast<const f32x4*>(p + k * stride);
+      b += *reinterpret_cast<const f32x4*>(p + k * stride + 4);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
+  };
+  float v[8];
+  if constexpr (GATED) {
+    const int n = (c >> 5) * 64 + (c & 31);
+    float u[8];
+    total(n, v);
+    total(n + 32, u);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = silu_f(v[i]) * u[i];
+    uint8_t* row = reinterpret_cast<uint8_t*>(e.out) + m * e.ldo;
+    uint8_t* scales = e.scales + m * e.lds;
+    if (e.mode == MX_SWIGLU8) put_eight<PIE_MXFP8>(v, row, scales, c);
+    else put_eight<PIE_MXFP4>(v, row, scales, c);
+    if (c == 0) pad_scales(scales, e.N);
+    return;
+  }
+  if (c >= e.N) return;
+  total(c, v);
+  if (e.mode == MX_RESID_EMBED || e.mode == MX_RESID_OUT) {
+    float r[8];
+    if (e.mode == MX_RESID_EMBED && !e.resid) load8(RowsView{e.embeds, e.H, PIE_BF16, 1}, e.ids[m], c, r);
+    else load8(RowsView{e.resid, e.H, PIE_F32, 1}, m, c, r);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] += r[i];
+    if (e.mode == MX_RESID_OUT && !e.out) {
+      const int id = e.ids[m];
+      if (id >= 0) store8(RowsView{e.embeds, e.H, PIE_BF16, 1}, id, c, v);
+      return;
+    }
+  }
+  const RowsView out{e.out, e.ldo, e.mode == MX_BF16 ? PIE_BF16 : PIE_F32, 1};
+  if (e.vec && c + 8 <= e.N) {
+    store8(out, m, c, v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (c + i >= e.N) break;
+      if (e.mode == MX_BF16) reinterpret_cast<bf16_t*>(e.out)[m * e.ldo + c + i] = f32_to_bf16(v[i]);
+      else reinterpret_cast<float*>(e.out)[m * e.ldo + c + i] = v[i];
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// dispatch
+// ---------------------------------------------------------------------------------------------
+// How a product is taken: tiles of 256 x 256 (mb 0), or mx_stream_kernel of mb token blocks, ks slices and nj weight blocks a wave, split over
+// `splits` workgroups along K; of the leading `rows` rows, the rest being a product of its own.
+struct MxForm { int mb, ks, nj; };
+struct MxPlan { MxForm form; int splits, rows; double us; };
+static constexpr MxForm MX_TILES = {0, 1, 2};
+// The forms that a sweep of all (1 to 4 blocks, 1 to 8 slices, 110 products of 1 to 2100 rows, up to 8 splits) needs to come within 1% of its best.
+static constexpr MxForm MX_PLAIN[] = {{1, 2, 1}, {1, 4, 1}, {1, 8, 1}, {2, 4, 1}, {2, 8, 1}, {3, 2, 1}, {3, 4, 1}, {1, 4, 2}, {2, 4, 2}, {3, 2, 2}, {4, 2, 2}, {4, 4, 2}};
+static constexpr MxForm MX_GATED[] = {{1, 2, 2}, {1, 4, 2}, {2, 2, 2}, {2, 4, 2}, {3, 2, 2}, {3, 4, 2}, {4, 2, 2}, {4, 4, 2}};
+
+// Estimated microseconds, fitted to that sweep (weights from HBM, calls in a graph): workgroups go in rounds of one to a compute unit, a round
+// costs its start (4 us: first requests, the slices' sums, the epilogue) and its stages, a stage the longest of its matrix instructions (118 ns per
+// accumulator tile of a wave), of what it fetches (34 bytes a nanosecond) and of its reads of LDS.  The form that this picks takes 1.9% more
+// time than the best of the sweep on average, 14% at most (333 rows of 4096 onto 4096: 17.5 us, 15.4).  Examples, best and next form:
+// 28672 x 4096 gated at 1 row (1, 4) 17.2, tiles 43; at 64 rows (2, 4) 20.7, (1, 2) 22.5; at 333 (3, 2) 53.5, tiles 55; at 1400 tiles 161, (4, 2) 184.
+// 4096 x 14336 at 64 rows (1, 4, 2) in 4 splits 19.4, (1, 8, 1) whole 20.3; at 900 rows (4, 4, 2) 74, tiles 150.
+static double mx_tiles_us(int M, int NB, int NS, bool fp8, int n_cus) {
+  const int64_t wgs = (int64_t)((M + MX_TM - 1) / MX_TM) * ((NB + MX_TN / 32 - 1) / (MX_TN / 32));
+  const double stages = NS * (fp8 ? 1.0 : 1.56);
+  auto round = [&](int64_t busy) { return 4.1 + stages * (1.07 + 0.42 * (double)busy / n_cus); };
+  return 0.9 + (double)(wgs / n_cus) * round(n_cus) + (wgs % n_cus ? round(wgs % n_cus) : 0.0);
+}
+static double mx_stream_us(const MxForm& f, int splits, int M, int NB, int64_t K, int NS, bool fp8, int n_cus) {
+  const int WN = 8 / f.ks, tiles_m = (M + 32 * f.mb - 1) / (32 * f.mb), tiles_n = (NB + f.nj * WN - 1) / (f.nj * WN);
+  const int64_t wgs = (int64_t)tiles_m * tiles_n * splits, rounds = (wgs + n_cus - 1) / n_cus;
+  const int steps = (NS + f.ks * splits - 1) / (f.ks * splits);
+  const double kib = f.ks * std::min(32 * f.mb, M) / 8.0 + (fp8 ? 16 : 32) * f.nj;
+  const double stage = std::max({0.118 * f.mb * f.nj, kib / 34.0, 0.15 * f.mb}) + 0.057;
+  const double t = 0.9 + (double)rounds * (4.2 + 0.08 * f.mb * f.nj + steps * stage);
+  const double least = 0.9 + (double)NB * 32 * (double)K * 0.53e-6 / 3.83;  // (the weights' bytes)
+  return std::max(t, least) + (splits > 1 ? 3.3 + (double)splits * M * NB * 32 * 8e-6 / 3.5 : 0.0);
+}
+// The best of one form for all rows, and of tiles for whole rounds with another form behind them (8320 rows of 14336 onto 4096: 33 x 16 tiles
+// took 503 us, 32 x 16 and 128 rows in another form ? us).
+static MxPlan mx_plan_whole(int M, const MxPacked& w, bool gated, bool fp8, int n_cus) {
+  const int row = fp8 ? w.K : w.K / 2, NS = (row + 127) / 128;
+  MxPlan best{MX_TILES, 1, M, mx_tiles_us(M, w.NB, NS, fp8, n_cus)};
+  auto look = [&](const MxForm& f) {
+    for (int splits = 1; splits <= 8; ++splits) {
+      if (splits > 1 && ((size_t)splits * M * w.NB * 32 > MX_WS_FLOATS || f.ks * splits * 2 > NS)) break;
+      const double us = mx_stream_us(f, splits, M, w.NB, w.K, NS, fp8, n_cus);
+      if (us < best.us) best = MxPlan{f, splits, M, us};
+    }
+  };
+  if (gated) for (const MxForm& f : MX_GATED) look(f);
+  else for (const MxForm& f : MX_PLAIN) look(f);
+  return best;
+}
+static MxPlan mx_plan(int M, const MxPacked& w, bool gated, bool fp8, int n_cus) {
+  MxPlan best = mx_plan_whole(M, w, gated, fp8, n_cus);
+  const int tiles_m = (M + MX_TM - 1) / MX_TM, NS = ((fp8 ? w.K : w.K / 2) + 127) / 128;
+  for (int cut = tiles_m - 1; cut >= 1 && cut >= tiles_m - 4; --cut) {
+    const int rows = cut * MX_TM;
+    const double us = mx_tiles_us(rows, w.NB, NS, fp8, n_cus) + mx_plan_whole(M - rows, w, gated, fp8, n_cus).us;
+    if (us < best.us) best = MxPlan{MX_TILES, 1, rows, us};
+  }
+  return best;
+}
+
+template <bool GATED, int FMT, int MB, int KS, int NJ>
+static hipError_t run_stream_form(const MxRowsView& a, int M, const MxPacked& w, const MxEpi& e, int splits, float* ws, hipStream_t s) {
+  constexpr int WN = 8 / KS;
+  const int tiles_m = (M + MB * 32 - 1) / (MB * 32), tiles_n = (w.NB + NJ * WN - 1) / (NJ * WN);
+  if ((int64_t)tiles_m * tiles_n > INT32_MAX) return hipErrorInvalidValue;
+  mx_stream_kernel<GATED, FMT, MB, KS, NJ><<<dim3(tiles_m * tiles_n, splits), dim3(512), 0, s>>>(a, M, w, e, tiles_m, tiles_n, splits, splits > 1 ? ws : nullptr);
+  if (splits > 1) {
+    const int64_t pieces = (int64_t)M * w.NB * (GATED ? 2 : 4);
+    mx_join_kernel<GATED><<<pieces_grid(pieces), dim3(256), 0, s>>>(ws, splits, M, w.NB, e);
+  }
   return hipGetLastError();
 }
 
-hipError_t launch_mx_product(const MxRowsView& a, int format, int M, const MxPacked& w, const MxEpi& e, hipStream_t s) {
-  if (M <= 0) return hipSuccess;
-  switch (e.mode) {
-    case MX_BF16: return run_product<MX_BF16>(a, format, M, w, e, s);
-    case MX_F32: return run_product<MX_F32>(a, format, M, w, e, s);
-    case MX_RESID_EMBED: return run_product<MX_RESID_EMBED>(a, format, M, w, e, s);
-    case MX_RESID_OUT: return run_product<MX_RESID_OUT>(a, format, M, w, e, s);
-    case MX_SWIGLU8: return run_product<MX_SWIGLU8>(a, format, M, w, e, s);
-    case MX_SWIGLU4: return run_product<MX_SWIGLU4>(a, format, M, w, e, s);
+template <bool GATED, int FMT>
+static hipError_t run_product(const MxRowsView& a, int M, const MxPacked& w, const MxEpi& e, const MxPlan& p, float* ws, hipStream_t s) {
+  const MxForm& f = p.form;
+  if (f.mb == 0) {
+    const int tiles_m = (M + MX_TM - 1) / MX_TM, tiles_n = (w.NB + MX_TN / 32 - 1) / (MX_TN / 32);
+    if ((int64_t)tiles_m * tiles_n > INT32_MAX) return hipErrorInvalidValue;
+    mx_tiles_kernel<GATED, FMT><<<dim3(tiles_m * tiles_n), dim3(512), 0, s>>>(a, M, w, e, tiles_m, tiles_n);
+    return hipGetLastError();
   }
+#define MX_FORM(MB, KS, NJ) \
+  if (f.mb == MB && f.ks == KS && f.nj == NJ) return run_stream_form<GATED, FMT, MB, KS, NJ>(a, M, w, e, p.splits, ws, s);
+  MX_FORM(1, 4, 2) MX_FORM(2, 4, 2) MX_FORM(3, 2, 2) MX_FORM(4, 2, 2) MX_FORM(4, 4, 2)
+  if constexpr (GATED) {
+    MX_FORM(1, 2, 2) MX_FORM(2, 2, 2) MX_FORM(3, 4, 2)
+  } else {
+    MX_FORM(1, 2, 1) MX_FORM(1, 4, 1) MX_FORM(1, 8, 1) MX_FORM(2, 4, 1) MX_FORM(2, 8, 1) MX_FORM(3, 2, 1) MX_FORM(3, 4, 1)
+  }
+#undef MX_FORM
   return hipErrorInvalidValue;
+}
+
+hipError_t launch_mx_product(const MxRowsView& a, int format, int M, const MxPacked& w, const MxEpi& e, float* ws, int n_cus, hipStream_t s) {
+  if (M <= 0) return hipSuccess;
+  const bool gated = e.mode == MX_SWIGLU8 || e.mode == MX_SWIGLU4, fp8 = format == PIE_MXFP8;
+  const MxPlan p = mx_plan(M, w, gated, fp8, n_cus);
+  const hipError_t err = gated ? (fp8 ? run_product<true, PIE_MXFP8>(a, p.rows, w, e, p, ws, s) : run_product<true, PIE_MXFP4>(a, p.rows, w, e, p, ws, s))
+                               : (fp8 ? run_product<false, PIE_MXFP8>(a, p.rows, w, e, p, ws, s) : run_product<false, PIE_MXFP4>(a, p.rows, w, e, p, ws, s));
+  if (err != hipSuccess || p.rows == M) return err;
+  MxRowsView rest = a;
+  rest.elements += p.rows * a.row_bytes;
+  rest.scales += p.rows * a.scale_bytes;
+  MxEpi r = e;
+  if (e.out) r.out = reinterpret_cast<uint8_t*>(e.out) + p.rows * e.ldo * (gated ? 1 : e.mode == MX_BF16 ? 2 : 4);
+  if (e.scales) r.scales = e.scales + p.rows * e.lds;
+  if (e.ids) r.ids = e.ids + p.rows;
+  if (e.resid) r.resid = e.resid + (int64_t)p.rows * e.H;
+  return launch_mx_product(rest, format, M - p.rows, w, r, ws, n_cus, s);
 }

@@ -2123,7 +2123,7 @@ extern "C" pie_status pie_mx_product(pie_ctx* c, const pie_mx_rows* a, int32_t r
   const RowsView o = rows_view(out);
   const bool f32 = out->dtype == PIE_F32;
   const MxEpi e{f32 ? MX_F32 : MX_BF16, out->data, out->row_stride, nullptr, 0, w.N, o.vec && w.N % (f32 ? 4 : 8) == 0, nullptr, nullptr, nullptr, 0};
-  HIP_TRY(c, launch_mx_product(mx_rows_view(a), a->format, rows, w, e, c->stream));
+  HIP_TRY(c, launch_mx_product(mx_rows_view(a), a->format, rows, w, e, c->mx_ws, c->wave_slots / 8, c->stream));
   return PIE_OK;
 }
 
@@ -2137,7 +2137,7 @@ extern "C" pie_status pie_mx_swiglu(pie_ctx* c, const pie_mx_rows* a, int32_t ro
   if (pie_status st = check_mx_rows(c, out, w.N / 2, who)) return st;
   const MxRowsView o = mx_rows_view(out);
   const MxEpi e{out->format == PIE_MXFP8 ? MX_SWIGLU8 : MX_SWIGLU4, o.elements, o.row_bytes, o.scales, o.scale_bytes, w.N / 2, 1, nullptr, nullptr, nullptr, 0};
-  HIP_TRY(c, launch_mx_product(mx_rows_view(a), a->format, rows, w, e, c->stream));
+  HIP_TRY(c, launch_mx_product(mx_rows_view(a), a->format, rows, w, e, c->mx_ws, c->wave_slots / 8, c->stream));
   return PIE_OK;
 }
 
@@ -2289,7 +2289,7 @@ static pie_status run_layer_mx(pie_ctx* c, int32_t layer, const pie_batch* b, fl
   tm.end(PIE_STAGE_NORM1);
 
   tm.begin(PIE_STAGE_QKV);
-  HIP_TRY(c, launch_mx_product(acts.rows, PIE_MXFP8, T, L.mqkv, MxEpi{MX_BF16, c->qkv, QKV, nullptr, 0, QKV, 1, nullptr, nullptr, nullptr, 0}, s));
+  HIP_TRY(c, launch_mx_product(acts.rows, PIE_MXFP8, T, L.mqkv, MxEpi{MX_BF16, c->qkv, QKV, nullptr, 0, QKV, 1, nullptr, nullptr, nullptr, 0}, c->mx_ws, c->wave_slots / 8, s));
   tm.end(PIE_STAGE_QKV);
 
   tm.begin(PIE_STAGE_ROPE_APPEND);
@@ -2300,7 +2300,7 @@ static pie_status run_layer_mx(pie_ctx* c, int32_t layer, const pie_batch* b, fl
 
   tm.begin(PIE_STAGE_OPROJ);
   HIP_TRY(c, launch_mx_quantise(mx_view(c->attn, PIE_BF16, Hq * D), T, Hq * D, PIE_MXFP8, acts.attn, s));
-  HIP_TRY(c, launch_mx_product(acts.attn, PIE_MXFP8, T, L.mo, MxEpi{MX_RESID_EMBED, c->h, H, nullptr, 0, H, 1, c->embeds, b->in_ids, x_in, H}, s));
+  HIP_TRY(c, launch_mx_product(acts.attn, PIE_MXFP8, T, L.mo, MxEpi{MX_RESID_EMBED, c->h, H, nullptr, 0, H, 1, c->embeds, b->in_ids, x_in, H}, c->mx_ws, c->wave_slots / 8, s));
   tm.end(PIE_STAGE_OPROJ);
 
   tm.begin(PIE_STAGE_NORM2);
@@ -2312,11 +2312,11 @@ static pie_status run_layer_mx(pie_ctx* c, int32_t layer, const pie_batch* b, fl
 
   tm.begin(PIE_STAGE_GATEUP);
   HIP_TRY(c, launch_mx_product(acts.rows, PIE_MXFP8, T, L.mgu,
-                               MxEpi{MX_SWIGLU8, acts.act.elements, acts.act.row_bytes, acts.act.scales, acts.act.scale_bytes, I, 1, nullptr, nullptr, nullptr, 0}, s));
+                               MxEpi{MX_SWIGLU8, acts.act.elements, acts.act.row_bytes, acts.act.scales, acts.act.scale_bytes, I, 1, nullptr, nullptr, nullptr, 0}, c->mx_ws, c->wave_slots / 8, s));
   tm.end(PIE_STAGE_GATEUP);
 
   tm.begin(PIE_STAGE_DOWN);
-  HIP_TRY(c, launch_mx_product(acts.act, PIE_MXFP8, T, L.mdown, MxEpi{MX_RESID_OUT, y_out, H, nullptr, 0, H, 1, c->embeds, b->out_ids, c->h, H}, s));
+  HIP_TRY(c, launch_mx_product(acts.act, PIE_MXFP8, T, L.mdown, MxEpi{MX_RESID_OUT, y_out, H, nullptr, 0, H, 1, c->embeds, b->out_ids, c->h, H}, c->mx_ws, c->wave_slots / 8, s));
   tm.end(PIE_STAGE_DOWN);
   c->last_T = T;
   c->last_mx = true;
