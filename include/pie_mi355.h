@@ -479,6 +479,12 @@ pie_status pie_product_plan(int32_t rows, int32_t n_out, int32_t k, int64_t work
  * Computes on the host only.  Host int64[3]. */
 pie_status pie_product_stream(int32_t rows, int32_t n_out, int32_t k, int64_t workspace_floats, int32_t n_cus, int64_t* out);
 
+/* How a product of microscaled rows [rows, k] (format PIE_MXFP8 or PIE_MXFP4) with n weight rows (gated: n of the gate and n of the up) is taken on
+ * n_cus compute units: out[0] = rows of a tile, out[1] = weight rows of a tile, out[2] = slices of the contraction inside a workgroup, out[3] =
+ * workgroups that the contraction is split over, out[4] = leading rows that go this way; the rest is a product of its own.
+ * Computes on the host only.  Host int64[5]. */
+pie_status pie_mx_product_plan(int32_t rows, int32_t n, int32_t k, int32_t gated, int32_t format, int32_t n_cus, int64_t* out);
+
 #ifdef __cplusplus
 }
 #endif

@@ -108,6 +108,7 @@ def load_library():
         "pie_mx_weight_destroy": [vp, vp],
         "pie_mx_product": [vp, C.POINTER(MxRowsC), i32, vp, C.POINTER(RowsC)],
         "pie_mx_swiglu": [vp, C.POINTER(MxRowsC), i32, vp, C.POINTER(MxRowsC)],
+        "pie_mx_product_plan": [i32, i32, i32, i32, i32, i32, vp],
         "pie_load_layer_mx": [vp, i32, vp, vp, C.POINTER(MxRowsC)],
         "pie_forward_host": [vp, i32, C.POINTER(ForwardBatchC), i32],
         "pie_get_next_dist": [vp, vp, i32, i32, f32, vp, vp],
@@ -151,6 +152,15 @@ def product_stream(rows: int, n_out: int, k: int, workspace_floats: int, n_cus: 
     if st != 0:
         raise PieError(st, "pie_product_stream: bad argument")
     return {"tile_rows": int(out[0]), "k_slices": int(out[1]), "splits": int(out[2])}
+
+
+def mx_product_plan(rows: int, n: int, k: int, gated: bool = False, format: str = "mxfp8", n_cus: int = 256) -> dict:
+    """pie_mx_product_plan: how a product of microscaled rows is taken."""
+    out = np.zeros(5, dtype=np.int64)
+    st = load_library().pie_mx_product_plan(rows, n, k, int(gated), MX_FORMATS.get(format, -1), n_cus, _ptr(out))
+    if st != 0:
+        raise PieError(st, "pie_mx_product_plan: bad argument")
+    return {"tile_rows": int(out[0]), "tile_columns": int(out[1]), "k_slices": int(out[2]), "splits": int(out[3]), "rows": int(out[4])}
 
 
 _INT32 = np.dtype(np.int32)

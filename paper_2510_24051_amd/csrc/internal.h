@@ -473,3 +473,4 @@ struct MxEpi {
 };
 // ws: MX_WS_FLOATS of workspace
 hipError_t launch_mx_product(const MxRowsView& a, int format, int M, const MxPacked& w, const MxEpi& epi, float* ws, int n_cus, hipStream_t s);
+void mx_product_plan(int M, const MxPacked& w, bool gated, int format, int n_cus, int64_t out[5]);  // see pie_mx_product_plan

@@ -1012,7 +1012,7 @@ static double mx_stream_us(const MxForm& f, int splits, int M, int NB, int64_t K
 // took 503 us, 32 x 16 and 128 rows in another form ? us).
 static MxPlan mx_plan_whole(int M, const MxPacked& w, bool gated, bool fp8, int n_cus) {
   const int row = fp8 ? w.K : w.K / 2, NS = (row + 127) / 128;
-  MxPlan best{MX_TILES, 1, M, mx_tiles_us(M, w.NB, NS, fp8, n_cus)};
+  MxPlan best{MX_TILES, 1, M, M > 128 ? mx_tiles_us(M, w.NB, NS, fp8, n_cus) : 1e30};  // (the sweep has no product of up to 128 rows for them)
   auto look = [&](const MxForm& f) {
     for (int splits = 1; splits <= 8; ++splits) {
       if (splits > 1 && ((size_t)splits * M * w.NB * 32 > MX_WS_FLOATS || f.ks * splits * 2 > NS)) break;
@@ -1085,4 +1085,13 @@ hipError_t launch_mx_product(const MxRowsView& a, int format, int M, const MxPac
   if (e.ids) r.ids = e.ids + p.rows;
   if (e.resid) r.resid = e.resid + (int64_t)p.rows * e.H;
   return launch_mx_product(rest, format, M - p.rows, w, r, ws, n_cus, s);
+}
+
+void mx_product_plan(int M, const MxPacked& w, bool gated, int format, int n_cus, int64_t out[5]) {
+  const MxPlan p = mx_plan(M, w, gated, format == PIE_MXFP8, n_cus);
+  out[0] = p.form.mb ? 32 * p.form.mb : MX_TM;
+  out[1] = p.form.mb ? 32 * p.form.nj * (8 / p.form.ks) : MX_TN;
+  out[2] = p.form.ks;
+  out[3] = p.splits;
+  out[4] = p.rows;
 }

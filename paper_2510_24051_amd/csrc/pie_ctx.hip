@@ -2023,11 +2023,24 @@ extern "C" pie_status pie_mx_norm(pie_ctx* c, const pie_rows* x, const pie_rows*
   return PIE_OK;
 }
 
+static MxPacked mx_shape(int N, int K) {
+  MxPacked w;
+  w.N = N; w.K = K;
+  w.NB = (N + 31) / 32; w.KQ = (K + 255) / 256; w.KT = w.KQ * 4;
+  return w;
+}
+
+extern "C" pie_status pie_mx_product_plan(int32_t rows, int32_t n, int32_t k, int32_t gated, int32_t format, int32_t n_cus, int64_t* out) {
+  if (rows <= 0 || n <= 0 || k <= 0 || k % 32 || (gated && n % 32) || (format != PIE_MXFP8 && format != PIE_MXFP4) || n_cus <= 0 || !out) return PIE_EINVAL;
+  if (k > MX_MAX_K || rows > MX_MAX_ROWS || n > MX_MAX_ROWS / (gated ? 2 : 1)) return PIE_EUNSUPPORTED;
+  mx_product_plan(rows, mx_shape(gated ? 2 * n : n, k), gated != 0, format, n_cus, out);
+  return PIE_OK;
+}
+
 // Room for N rows of K inputs, all 0.
 static pie_status mx_alloc(pie_ctx* c, MxPacked& w, int N, int K) {
   free_packed(w);
-  w.N = N; w.K = K;
-  w.NB = (N + 31) / 32; w.KQ = (K + 255) / 256; w.KT = w.KQ * 4;
+  w = mx_shape(N, K);
   const size_t data = (size_t)w.NB * w.KT * 1024, scales = (size_t)w.NB * w.KQ * 256;
   if (hipError_t e = hipMalloc(reinterpret_cast<void**>(&w.data), data + scales); e != hipSuccess) {
     w = MxPacked();

@@ -14,6 +14,7 @@ import torch
 import workloads as W
 from oracle import mx
 from oracle import pie_oracle as O
+from test_host_mx import FORM_SIZES
 
 pytestmark = pytest.mark.gpu
 
@@ -207,24 +208,28 @@ WHOLE = [(1, 32, 1), (1, 64, 32), (3, 96, 5), (17, 128, 33), (32, 160, 64), (33,
          (257, 2080, 520), (300, 320, 1000), (520, 96, 40), (700, 640, 260), (1030, 288, 515)]
 
 
+def whole_rows(rng, rows, k, vals, form, gap, low=126):
+    """Rows of elements out of vals and scales of 2^(low - 127) to four times that, with what could be read by mistake behind and between them."""
+    e = rng.choice(np.array(vals, dtype=np.float64), size=(rows, k))
+    b = rng.integers(low, low + 3, size=(rows, k // 32)).astype(np.uint8)
+    r = rows_of(form, rows, k, fill=0x7F, gap=gap)  # (0x7F: NaN in E4M3, a huge scale behind the last one)
+    r.elements.copy_(torch.from_numpy(mx.encode(e, form)))
+    r.scales[:, :k // 32] = torch.from_numpy(b).cuda()
+    r.scales[:, k // 32:] = 0xFF
+    return r, mx.values(e, b)
+
+
+ACTS, WEIGHTS = [0, 1, -1, 2, -2, 3, 4, -4], [0, 0, 1, -1, 2, -3, 4]
+
+
 @pytest.mark.parametrize("form", ["mxfp8", "mxfp4"])
 @pytest.mark.parametrize("m,k,n", WHOLE)
 def test_product_of_whole_numbers(ctx, form, m, k, n):
     """Small whole numbers and scales of 1/2 to 2: every sum is exact, so every bit of an fp32 result is the oracle's, whatever the order."""
     rng = np.random.default_rng(m * k + n)
     from paper_2510_24051_amd import MxRows
-
-    def made(rows, vals, form, gap):
-        e = rng.choice(vals, size=(rows, k))
-        b = rng.integers(126, 129, size=(rows, k // 32)).astype(np.uint8)
-        r = rows_of(form, rows, k, fill=0x7F, gap=gap)  # (0x7F: NaN in E4M3, a huge scale behind the last one)
-        r.elements.copy_(torch.from_numpy(mx.encode(e, form)))
-        r.scales[:, :k // 32] = torch.from_numpy(b).cuda()
-        r.scales[:, k // 32:] = 0xFF
-        return r, mx.values(e, b)
-
-    a, av = made(m, [0, 1, -1, 2, -2, 3, 4, -4], form, 1)
-    w, wv = made(n, [0, 0, 1, -1, 2, -3, 4], "mxfp4", 2)
+    a, av = whole_rows(rng, m, k, ACTS, form, 1)
+    w, wv = whole_rows(rng, n, k, WEIGHTS, "mxfp4", 2)
     want = mx.product(av, wv)
     assert np.abs(av).max() * np.abs(wv).max() * k < 2 ** 22
     parts = [w] if n <= 40 else [MxRows("mxfp4", w.elements[i:j], w.scales[i:j]) for i, j in ((0, 7), (7, n - 33), (n - 33, n))]
@@ -238,6 +243,28 @@ def test_product_of_whole_numbers(ctx, form, m, k, n):
         bad = got != wanted
         assert not bad.any(), f"{bad.sum()} of {bad.size} differ, first at {np.argwhere(bad)[0]}: {got[bad][0]} not {wanted[bad][0]}"
         assert (c[:, n:] == -9.0).all() and (flat[:offset] == -9.0).all(), "bytes outside the result were written"
+
+
+@pytest.mark.parametrize("gated,form,m,k,n", FORM_SIZES)
+def test_every_form(ctx, gated, form, m, k, n):
+    """Every form that a product is taken in (test_host_mx.py has the list and sees that it is whole): exact sums as above."""
+    rng = np.random.default_rng(m + k + n)
+    a, av = whole_rows(rng, m, k, ACTS, form, 1)
+    parts = [whole_rows(rng, n, k, WEIGHTS, "mxfp4", 1, 126 if not gated else 120) for _ in range(2 if gated else 1)]
+    weight = ctx.mx_weight([p[0] for p in parts], gated=gated)
+    sums = [mx.product(av, p[1]) for p in parts]
+    if gated:
+        r = rows_of("mxfp8", m, n, gap=1)
+        ctx.mx_swiglu(a, weight, r)
+        check_computed(r, O.silu(sums[0]) * sums[1], 2.0 ** -21 * (1 + np.abs(sums[0])), f"gated {m} x {k} x {n}")
+        check_gaps(r)
+    else:
+        c = torch.full((m, n + 4), -9.0, device="cuda")
+        ctx.mx_product(a, weight, c[:, :n])
+        assert np.array_equal(c[:, :n].cpu().numpy(), sums[0].astype(np.float32)) and (c[:, n:] == -9.0).all()
+        h = torch.empty((m, n), dtype=torch.bfloat16, device="cuda")
+        ctx.mx_product(a, weight, h)
+        assert np.array_equal(h.double().cpu().numpy(), O.bf16_round(sums[0]))
 
 
 @pytest.mark.parametrize("form", ["mxfp8", "mxfp4"])

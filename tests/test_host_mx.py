@@ -16,6 +16,30 @@ F32, BF16, F16 = 0, 1, 2
 ROOM = np.zeros(1 << 20, np.uint8)
 A = (ROOM.ctypes.data + 255) // 256 * 256  # (copies and fills of the stand-in may touch it; kernels do nothing)
 
+# (gated, format, rows, k, n): products that between them go through every form (test_gpu_mx.py computes them)
+FORM_SIZES = [
+    (False, "mxfp4", 1, 2048, 20000), (False, "mxfp4", 1, 1056, 32), (False, "mxfp4", 2050, 8192, 32), (False, "mxfp4", 1, 544, 32), (False, "mxfp4", 1030, 8192, 32),
+    (False, "mxfp4", 1, 32, 32), (False, "mxfp4", 17, 8192, 32), (False, "mxfp4", 33, 1056, 8192), (False, "mxfp4", 2050, 544, 200),
+    (False, "mxfp4", 33, 8192, 4096), (False, "mxfp4", 200, 544, 8192), (False, "mxfp4", 1030, 544, 1000), (False, "mxfp4", 257, 8192, 1000),
+    (False, "mxfp4", 1030, 512, 1000), (False, "mxfp4", 515, 8192, 1000), (False, "mxfp4", 400, 512, 8192), (False, "mxfp4", 400, 544, 8192),
+    (False, "mxfp4", 900, 512, 8192), (False, "mxfp4", 1030, 32, 1000), (False, "mxfp8", 1, 544, 32), (False, "mxfp8", 1030, 8192, 32),
+    (False, "mxfp8", 1, 512, 32), (False, "mxfp8", 1, 8192, 32), (False, "mxfp8", 1, 32, 32), (False, "mxfp8", 31, 4096, 32),
+    (False, "mxfp8", 130, 8192, 1000), (False, "mxfp8", 33, 544, 8192), (False, "mxfp8", 515, 4096, 1000), (False, "mxfp8", 65, 8192, 1000),
+    (False, "mxfp8", 200, 512, 8192), (False, "mxfp8", 257, 8192, 1000), (False, "mxfp8", 1030, 512, 1000), (False, "mxfp8", 700, 8192, 200),
+    (False, "mxfp8", 1030, 256, 1000), (False, "mxfp8", 130, 8192, 2048), (False, "mxfp8", 400, 256, 8192), (False, "mxfp8", 400, 512, 8192),
+    (False, "mxfp8", 900, 512, 8192), (False, "mxfp8", 1030, 32, 1000), (False, "mxfp8", 2050, 256, 8192), (True, "mxfp4", 1, 544, 32),
+    (True, "mxfp4", 1, 4096, 2048), (True, "mxfp4", 1, 32, 32), (True, "mxfp4", 1, 4096, 32), (True, "mxfp4", 2050, 544, 224),
+    (True, "mxfp4", 2050, 8192, 32), (True, "mxfp4", 2050, 512, 512), (True, "mxfp4", 2050, 544, 512), (True, "mxfp4", 1030, 8192, 224),
+    (True, "mxfp4", 257, 544, 8192), (True, "mxfp4", 200, 544, 8192), (True, "mxfp4", 97, 8192, 4096), (True, "mxfp4", 400, 512, 8192),
+    (True, "mxfp4", 130, 32, 32), (True, "mxfp4", 2050, 512, 4096), (True, "mxfp8", 1, 512, 32), (True, "mxfp8", 1, 8192, 32),
+    (True, "mxfp8", 1, 32, 32), (True, "mxfp8", 1, 4096, 32), (True, "mxfp8", 2050, 512, 224), (True, "mxfp8", 2050, 4096, 32),
+    (True, "mxfp8", 2050, 256, 512), (True, "mxfp8", 200, 8192, 2048), (True, "mxfp8", 2050, 512, 512), (True, "mxfp8", 2050, 8192, 32),
+    (True, "mxfp8", 2050, 256, 1024), (True, "mxfp8", 2050, 8192, 224), (True, "mxfp8", 97, 8192, 4096), (True, "mxfp8", 400, 512, 8192),
+    (True, "mxfp8", 130, 32, 32), (True, "mxfp8", 2050, 256, 4096)]
+FORMS = {False: {(32, 128, 2), (32, 64, 4), (32, 32, 8), (64, 64, 4), (64, 32, 8), (96, 128, 2), (96, 64, 4), (32, 128, 4), (64, 128, 4), (96, 256, 2), (128, 256, 2),
+                 (128, 128, 4), (256, 256, 1)},
+         True: {(32, 256, 2), (32, 128, 4), (64, 256, 2), (64, 128, 4), (96, 256, 2), (96, 128, 4), (128, 256, 2), (128, 128, 4), (256, 256, 1)}}
+
 
 class Calls:
     def __init__(self, c, ctx):
@@ -49,10 +73,11 @@ def rows_refused(c):
         assert f(None) == INVALID and f(out=None) == INVALID
         mx, plain = (lambda v: f(out=v)) if f is q else f, f if f is q else (lambda v: f(out=v))  # noqa: E731
         for v in (m.mx(format=2), m.mx(format=-1), m.mx(elements=None), m.mx(scales=None), m.mx(elements=A + 8), m.mx(scales=A + 2), m.mx(row_bytes=48),
-                  m.mx(row_bytes=72), m.mx(scale_bytes=2), m.mx(scale_bytes=6), m.mx(scale_bytes=0), m.mx(FP4, row_bytes=16), m.mx(row_bytes=-64)):
+                  m.mx(row_bytes=72), m.mx(scale_bytes=2), m.mx(row_bytes=-(1 << 23)), m.mx(scale_bytes=-4), m.mx(scale_bytes=6), m.mx(scale_bytes=0), m.mx(FP4, row_bytes=16), m.mx(row_bytes=-64)):
             assert mx(v) == INVALID
         for v in (m.rows(data=None), m.rows(dtype=3), m.rows(dtype=-1), m.rows(stride=63), m.rows(stride=-64), m.rows(data=A + 2), m.rows(data=A + 1, dtype=BF16)):
             assert plain(v) == INVALID
+        assert mx(m.mx(row_bytes=(1 << 22) + 16)) == UNSUPPORTED and mx(m.mx(scale_bytes=(1 << 22) + 4)) == UNSUPPORTED
         assert c.launches() == []
         for v in (m.mx(), m.mx(FP4, row_bytes=32), m.mx(row_bytes=80, scale_bytes=8)):
             assert mx(v) == 0
@@ -233,3 +258,39 @@ def test_rows_in_the_binding():
             MxRows(*bad)
     with pytest.raises(ValueError):
         MxRows.empty(3, 40, "mxfp8", "cpu")
+
+
+def test_every_form_is_listed():
+    """Which forms the listed products go through, by the library's own rule; some split over workgroups, some cut behind whole rounds of tiles."""
+    from paper_2510_24051_amd import mx_product_plan
+    for gated in (False, True):
+        for form in ("mxfp8", "mxfp4"):
+            plans = [mx_product_plan(m, n, k, g, f) for g, f, m, k, n in FORM_SIZES if (g, f) == (gated, form)]
+            assert {(p["tile_rows"], p["tile_columns"], p["k_slices"]) for p in plans} == FORMS[gated]
+            assert any(p["splits"] > 1 for p in plans) and any(p["rows"] < r[2] for p, r in zip(plans, [s for s in FORM_SIZES if s[:2] == (gated, form)])) or not gated
+    assert any(mx_product_plan(m, n, k, g, f)["rows"] < m for g, f, m, k, n in FORM_SIZES if not g)
+
+
+def test_plans():
+    """What a plan may be: parts no more than stages, sums that fit the workspace, whole rounds of whole tiles; and what is refused."""
+    from paper_2510_24051_amd import PieError, mx_product_plan
+    rng = np.random.default_rng(0)
+    for _ in range(3000):
+        m, n, k = (int(2 ** rng.uniform(0, b)) for b in (14, 15, 10))
+        k, gated, form = 32 * k, bool(rng.integers(2)), ["mxfp8", "mxfp4"][rng.integers(2)]
+        n = (n + 31) // 32 * 32 if gated else n
+        p = mx_product_plan(m, n, k, gated, form, int(rng.choice([256, 64, 304])))
+        assert (p["tile_rows"], p["tile_columns"], p["k_slices"]) in FORMS[gated] and 1 <= p["rows"] <= m and 1 <= p["splits"] <= 8
+        assert p["tile_rows"] < 256 or (m > 128 and p["splits"] == 1)
+        assert p["rows"] == m or (p["tile_rows"] == 256 and p["rows"] % 256 == 0)
+        if p["splits"] > 1:
+            assert p["splits"] * m * (n + 31) // 32 * 32 * (2 if gated else 1) <= 1 << 24
+            assert p["splits"] * p["k_slices"] * 2 <= -(-k // (128 if form == "mxfp8" else 256))
+    for bad in ((0, 32, 32), (1, 0, 32), (1, 32, 0), (1, 32, 48), (1, 33, 32, True), (1, 32, 32, False, "mxfp6"), (1, 32, 32, False, "mxfp8", 0)):
+        with pytest.raises(PieError) as e:
+            mx_product_plan(*bad)
+        assert e.value.status == INVALID
+    for bad in ((1 << 25, 32, 32), (1, 1 << 25, 32), (1, 1 << 24, 32, True), (1, 32, 1 << 21)):
+        with pytest.raises(PieError) as e:
+            mx_product_plan(*bad)
+        assert e.value.status == UNSUPPORTED
