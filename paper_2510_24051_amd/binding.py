@@ -5,6 +5,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Optional
 
 import numpy as np
@@ -51,8 +52,7 @@ class BeamSearchC(C.Structure):
                 ("eos_token", C.c_int32), ("n_out", C.c_int32), ("temperature", C.c_float)]
 
 
-class RowsC(C.Structure):
-    _fields_ = [("data", C.c_void_p), ("dtype", C.c_int32), ("row_stride", C.c_int64)]
+_ROWS = struct.Struct("@Pi4xq")  # pie_rows: data, dtype, row_stride
 
 
 class MxRowsC(C.Structure):
@@ -101,13 +101,13 @@ def load_library():
         "pie_compact_kvpage": [vp, i32] + [vp] * 7,
         "pie_beam_select": [vp, C.POINTER(BeamSearchC), vp, i32, i64, i32, vp, vp, vp],
         "pie_get_next_beams": [vp, C.POINTER(BeamSearchC), vp, vp, vp, vp],
-        "pie_mx_quantise": [vp, C.POINTER(RowsC), i32, i32, C.POINTER(MxRowsC)],
-        "pie_mx_dequantise": [vp, C.POINTER(MxRowsC), i32, i32, C.POINTER(RowsC)],
-        "pie_mx_norm": [vp, C.POINTER(RowsC), C.POINTER(RowsC), vp, i32, i32, C.POINTER(RowsC), C.POINTER(MxRowsC)],
+        "pie_mx_quantise": [vp, vp, i32, i32, vp],
+        "pie_mx_dequantise": [vp, vp, i32, i32, vp],
+        "pie_mx_norm": [vp, vp, vp, vp, i32, i32, vp, vp],
         "pie_mx_weight_create": [vp, C.POINTER(MxRowsC), vp, i32, i32, i32, C.POINTER(vp)],
         "pie_mx_weight_destroy": [vp, vp],
-        "pie_mx_product": [vp, C.POINTER(MxRowsC), i32, vp, C.POINTER(RowsC)],
-        "pie_mx_swiglu": [vp, C.POINTER(MxRowsC), i32, vp, C.POINTER(MxRowsC)],
+        "pie_mx_product": [vp, vp, i32, vp, vp],
+        "pie_mx_swiglu": [vp, vp, i32, vp, vp],
         "pie_mx_product_plan": [i32, i32, i32, i32, i32, i32, vp],
         "pie_load_layer_mx": [vp, i32, vp, vp, C.POINTER(MxRowsC)],
         "pie_forward_host": [vp, i32, C.POINTER(ForwardBatchC), i32],
@@ -189,8 +189,13 @@ def _at(a):
         return a.__array_interface__["data"][0]
 
 
-def _row_types() -> dict:
-    return {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+_row_types = {}  # numbers of the element types that rows may have, and of those that a product may leave
+
+
+def _types(which: str) -> dict:
+    if not _row_types:
+        _row_types.update(any={torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}, product={torch.float32: 0, torch.bfloat16: 1})
+    return _row_types[which]
 
 
 MX_FORMATS = {"mxfp8": 0, "mxfp4": 1}
@@ -213,6 +218,8 @@ class MxRows:
         if self.k == 0 or self.k % 32 or scales.shape != (self.rows, (self.k // 32 + 3) // 4 * 4):
             raise ValueError("microscaled rows: k is a multiple of 32, and scales are [rows, k / 32 up to the next multiple of 4]")
         self._c = MxRowsC(MX_FORMATS[format], elements.data_ptr(), self._stride(elements), scales.data_ptr(), self._stride(scales))
+        self._at = C.addressof(self._c)
+        self._index = elements.get_device() if elements.device == scales.device else -1
 
     @staticmethod
     def _stride(t: torch.Tensor) -> int:
@@ -395,7 +402,7 @@ class Pie:
                   "wup": (m.mlp_dim, m.hidden), "wdown": (m.hidden, m.mlp_dim)}
         parts = [getattr(w, n) for n in self.PROJECTIONS]
         for n, p in zip(self.PROJECTIONS, parts):
-            if not isinstance(p, MxRows) or p.format != "mxfp4" or (p.rows, p.k) != shapes[n] or p.elements.device != dev or p.scales.device != dev:
+            if not isinstance(p, MxRows) or p.format != "mxfp4" or (p.rows, p.k) != shapes[n] or p._index != self._index:
                 raise ValueError(f"load_layer_mx: {n} is {shapes[n]} in mxfp4 on the context's device")
         g = [self._dev_bf16(x) for x in (w.g1, w.g2)]
         if any(x.numel() != m.hidden for x in g):
@@ -641,45 +648,50 @@ class Pie:
 
     # ---- microscaled formats ----
     # Inputs are as torch's current stream leaves them, and what that stream gets afterwards sees the outputs.
-    def _rows(self, t: torch.Tensor, rows: int, k: int, what: str, types=None) -> RowsC:
-        numbers = _row_types()
-        types = numbers if types is None else types
-        if t.dtype not in types or t.device != self._device() or t.shape != (rows, k) or (k > 1 and t.stride(1) != 1):
+    def _rows(self, t: torch.Tensor, rows: int, k: int, what: str, types: dict) -> bytes:
+        """pie_rows of a tensor."""
+        number, shape, strides = types.get(t.dtype), t.shape, t.stride()
+        if number is None or len(shape) != 2 or shape[0] != rows or shape[1] != k or strides[1] != 1 or t.get_device() != self._index:
             raise ValueError(f"{what} is a tensor [{rows}, {k}] on the context's device whose rows are contiguous, of "
                              + ", ".join(str(x).replace("torch.", "") for x in types))
-        return RowsC(t.data_ptr(), numbers[t.dtype], t.stride(0) if rows > 1 else k)
+        return _ROWS.pack(t.data_ptr(), number, strides[0] if rows > 1 else k)
 
-    def _mx_rows(self, r: MxRows, rows: int, k: int, what: str) -> MxRowsC:
-        dev = self._device()
-        if not isinstance(r, MxRows) or r.rows != rows or r.k != k or r.elements.device != dev or r.scales.device != dev:
+    def _mx_rows(self, r: MxRows, rows: int, k: int, what: str) -> int:
+        """Address of r's pie_mx_rows."""
+        if self.device is None:
+            self._device()  # (says why)
+        if not isinstance(r, MxRows) or r.rows != rows or r.k != k or r._index != self._index:
             raise ValueError(f"{what}: MxRows of {rows} rows of {k} on the context's device")
-        return r._c
+        return r._at
 
     def mx_quantise(self, x: torch.Tensor, out: MxRows):
         """pie_mx_quantise: out = x [rows, k] (float32, bfloat16 or float16; rows may be strided)."""
-        o = self._mx_rows(out, out.rows, out.k, "mx_quantise")
-        self._ordered(self.lib.pie_mx_quantise, self.ctx, self._rows(x, out.rows, out.k, "mx_quantise: x"), out.rows, out.k, o)
+        rows, k = out.rows, out.k
+        o = self._mx_rows(out, rows, k, "mx_quantise")
+        self._ordered(self.lib.pie_mx_quantise, self.ctx, self._rows(x, rows, k, "mx_quantise: x", _types("any")), rows, k, o)
 
     def mx_dequantise(self, a: MxRows, out: torch.Tensor):
         """pie_mx_dequantise: out [rows, k] (float32, bfloat16 or float16; rows may be strided) = the values of a."""
         r = self._mx_rows(a, a.rows, a.k, "mx_dequantise")
-        self._ordered(self.lib.pie_mx_dequantise, self.ctx, r, a.rows, a.k, self._rows(out, a.rows, a.k, "mx_dequantise: out"))
+        self._ordered(self.lib.pie_mx_dequantise, self.ctx, r, a.rows, a.k, self._rows(out, a.rows, a.k, "mx_dequantise: out", _types("any")))
 
     def mx_norm(self, x: torch.Tensor, gain: torch.Tensor, out: MxRows, delta: Optional[torch.Tensor] = None, h: Optional[torch.Tensor] = None):
         """pie_mx_norm: h = x + delta, out = rmsnorm(h) * gain.  gain: bfloat16 [k]; h may be x."""
-        rows, k = out.rows, out.k
+        rows, k, types = out.rows, out.k, _types("any")
         o = self._mx_rows(out, rows, k, "mx_norm")
-        if gain.dtype != torch.bfloat16 or gain.shape != (k,) or gain.device != self.device or not gain.is_contiguous():
+        if gain.dtype is not torch.bfloat16 or gain.shape != (k,) or gain.get_device() != self._index or not gain.is_contiguous():
             raise ValueError("mx_norm: gain is a contiguous bfloat16 tensor [k] on the context's device")
-        rx = self._rows(x, rows, k, "mx_norm: x")
-        rd = None if delta is None else self._rows(delta, rows, k, "mx_norm: delta")
-        rh = None if h is None else self._rows(h, rows, k, "mx_norm: h", (x.dtype,))
+        rx = self._rows(x, rows, k, "mx_norm: x", types)
+        rd = None if delta is None else self._rows(delta, rows, k, "mx_norm: delta", types)
+        if h is not None and h.dtype is not x.dtype:
+            raise ValueError("mx_norm: h has x's type")
+        rh = None if h is None else rx if h is x else self._rows(h, rows, k, "mx_norm: h", types)
         self._ordered(self.lib.pie_mx_norm, self.ctx, rx, rd, gain.data_ptr(), rows, k, rh, o)
 
     def mx_weight(self, parts, gated: bool = False) -> MxWeight:
         """pie_mx_weight_create: matrices in MXFP4, one below the other, or gate and up."""
         parts, dev = list(parts), self._device()
-        if not parts or any(not isinstance(p, MxRows) or p.k != parts[0].k or p.elements.device != dev or p.scales.device != dev for p in parts):
+        if not parts or any(not isinstance(p, MxRows) or p.k != parts[0].k or p._index != self._index for p in parts):
             raise ValueError("mx_weight: MxRows of one k on the context's device")
         torch.cuda.synchronize(dev)
         n = np.array([p.rows for p in parts], _INT32)
@@ -688,16 +700,16 @@ class Pie:
                                                   C.byref(h)))
         return MxWeight(self, h, int(n[0] if gated else n.sum()), parts[0].k, gated)
 
-    def _mx_weight(self, w: MxWeight, a: MxRows, what: str) -> MxRowsC:
+    def _mx_weight(self, w: MxWeight, a: MxRows, what: str) -> int:
         if not isinstance(w, MxWeight) or w.handle is None:
             raise ValueError(f"{what}: the weight is an MxWeight that has not been destroyed")
-        return self._mx_rows(a, a.rows, w.k, f"{what}: a")
+        return self._mx_rows(a, a.rows, w.k, what)
 
     def mx_product(self, a: MxRows, w: MxWeight, out: torch.Tensor):
         """pie_mx_product: out [rows, n] (bfloat16 or float32; rows may be strided) = a w^T."""
         r = self._mx_weight(w, a, "mx_product")
         self._ordered(self.lib.pie_mx_product, self.ctx, r, a.rows, w.handle,
-                      self._rows(out, a.rows, w.n, "mx_product: out", (torch.bfloat16, torch.float32)))
+                      self._rows(out, a.rows, w.n, "mx_product: out", _types("product")))
 
     def mx_swiglu(self, a: MxRows, w: MxWeight, out: MxRows):
         """pie_mx_swiglu: out [rows, n] = silu(a gate^T) * (a up^T) for a gated weight."""

@@ -32,30 +32,6 @@ __device__ __forceinline__ float beam_score(const float* scores, int row) {  // 
   return s != s ? -INFINITY : fminf(s, 3.402823466e38f);
 }
 
-// The sum of a wave's values in every lane, without LDS: halves, then rows of 16 change places, then the lanes of a row turn
-// (one search of four beams of 1024 tokens: 10.7 us a call, 11.3 with shuffles through LDS).
-template <int CTRL>
-__device__ __forceinline__ double dpp_f64(double v) {
-  return __hiloint2double(__builtin_amdgcn_mov_dpp(__double2hiint(v), CTRL, 0xF, 0xF, true), __builtin_amdgcn_mov_dpp(__double2loint(v), CTRL, 0xF, 0xF, true));
-}
-__device__ __forceinline__ double wave_sum_f64(double v) {
-  {
-    const auto lo = __builtin_amdgcn_permlane32_swap(__double2loint(v), __double2loint(v), false, false);
-    const auto hi = __builtin_amdgcn_permlane32_swap(__double2hiint(v), __double2hiint(v), false, false);
-    v = __hiloint2double(hi[0], lo[0]) + __hiloint2double(hi[1], lo[1]);
-  }
-  {
-    const auto lo = __builtin_amdgcn_permlane16_swap(__double2loint(v), __double2loint(v), false, false);
-    const auto hi = __builtin_amdgcn_permlane16_swap(__double2hiint(v), __double2hiint(v), false, false);
-    v = __hiloint2double(hi[0], lo[0]) + __hiloint2double(hi[1], lo[1]);
-  }
-  v += dpp_f64<0x128>(v);
-  v += dpp_f64<0x124>(v);
-  v += dpp_f64<0x122>(v);
-  v += dpp_f64<0x121>(v);
-  return v;
-}
-
 #define BT_SEGS 8  // segments of a tile
 typedef u32x4 u32x4_at2 __attribute__((aligned(2)));
 // A row cut into segments by its tokens, wherever it lies in memory: equal rows then have equal sums, bit for bit, and so

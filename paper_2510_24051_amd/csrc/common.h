@@ -98,6 +98,30 @@ __device__ __forceinline__ float wave_max(float v) {
   return v;
 }
 
+// The sum of a wave's values in every lane, without LDS: halves, then rows of 16 change places, then the lanes of a row turn
+// (one search of four beams of 1024 tokens: 10.7 us a call, 11.3 with shuffles through LDS).
+template <int CTRL>
+__device__ __forceinline__ double dpp_f64(double v) {
+  return __hiloint2double(__builtin_amdgcn_mov_dpp(__double2hiint(v), CTRL, 0xF, 0xF, true), __builtin_amdgcn_mov_dpp(__double2loint(v), CTRL, 0xF, 0xF, true));
+}
+__device__ __forceinline__ double wave_sum_f64(double v) {
+  {
+    const auto lo = __builtin_amdgcn_permlane32_swap(__double2loint(v), __double2loint(v), false, false);
+    const auto hi = __builtin_amdgcn_permlane32_swap(__double2hiint(v), __double2hiint(v), false, false);
+    v = __hiloint2double(hi[0], lo[0]) + __hiloint2double(hi[1], lo[1]);
+  }
+  {
+    const auto lo = __builtin_amdgcn_permlane16_swap(__double2loint(v), __double2loint(v), false, false);
+    const auto hi = __builtin_amdgcn_permlane16_swap(__double2hiint(v), __double2hiint(v), false, false);
+    v = __hiloint2double(hi[0], lo[0]) + __hiloint2double(hi[1], lo[1]);
+  }
+  v += dpp_f64<0x128>(v);
+  v += dpp_f64<0x124>(v);
+  v += dpp_f64<0x122>(v);
+  v += dpp_f64<0x121>(v);
+  return v;
+}
+
 // Sum of the eight bf16 values of a packed MFMA operand added to `acc` in fp32 (v_dot2c_f32_bf16 against a pair of
 // ones: two values per instruction, the products by 1 are exact).  The softmax normaliser is summed from the
 // rounded weights that the PV product multiplies by, so the weights applied and their sum carry the same rounding:

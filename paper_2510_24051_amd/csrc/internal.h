@@ -25,6 +25,9 @@ struct MxPacked {  // MXFP4 weights, tiled (see mx_pack_kernel)
   uint8_t* data = nullptr;     // [NB][KT][64 lanes][16 bytes]
   uint32_t* scales = nullptr;  // [NB][KQ][64 lanes], behind the data
   int N = 0, K = 0;            // rows, inputs
+  // how the last product was taken, for the next of as many rows (the estimates of a plan take the host microseconds)
+  struct Plan { int key = -1, mb, ks, nj, splits, rows; };
+  mutable Plan plan;
   int NB = 0, KT = 0, KQ = 0;  // blocks of 32 rows, steps of 64 inputs (a multiple of four), groups of four steps
 };
 struct pie_mx_weight {
@@ -432,7 +435,6 @@ struct RowsView {  // pie_rows
   const void* p;
   int64_t stride;
   int dtype;
-  int vec;  // base and stride are multiples of 16 bytes
 };
 RowsView mx_view(const void* p, int dtype, int64_t stride);
 struct MxNormArgs {
@@ -442,7 +444,6 @@ struct MxNormArgs {
   int64_t part_stride, split_stride;
   int splits;
   const bf16_t* gain;
-  int gain_vec;              // 16-byte aligned
   float eps;
 };
 hipError_t launch_mx_quantise(const RowsView& x, int rows, int k, int format, const MxRowsView& out, hipStream_t s);
@@ -465,7 +466,6 @@ struct MxEpi {
   uint8_t* scales;
   int64_t lds;
   int N;    // columns stored
-  int vec;  // rows of whole groups of eight (bf16) or four (fp32), 16-byte aligned
   bf16_t* embeds;
   const int32_t* ids;
   const float* resid;

@@ -1,6 +1,7 @@
 // Microscaled rows (blocks of 32 values, a power of two as scale, elements E4M3 or E2M1): quantisation, the norm that adds the residual
 // and writes them, the layout of 4-bit weights, and the products of both on the scaled matrix instructions.
 #include <algorithm>
+#include <type_traits>
 
 #include "internal.h"
 
@@ -17,9 +18,8 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t most) {
   constexpr int EMAX = FMT == PIE_MXFP8 ? 8 : 2;
   return most >= 0x7f800000u ? 255u : (uint32_t)max((int)(most >> 23) - EMAX, 0);
 }
-// 2^(127 - byte), by which elements are multiplied (exactly: what becomes denormal rounds to 0 in either format); 0 for a NaN block.
+// 2^(127 - byte), by which elements are multiplied (exactly: what becomes denormal rounds to 0 in either format).
 __device__ __forceinline__ float unscale(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
-__device__ __forceinline__ float element(float v, float un, bool nan) { return nan ? 0.f : v * un; }
 
 // Four values -> four E4M3, nearest even.  (The conversion itself saturates up to 464 and then gives NaN, so it is fed at most 448.)
 __device__ __forceinline__ uint32_t to_fp8x4(float a, float b, float c, float d) {
@@ -46,16 +46,16 @@ __device__ __forceinline__ void put_eight(const float (&v)[8], uint8_t* elements
   most = max(most, (uint32_t)__shfl_xor((int)most, 1));
   most = max(most, (uint32_t)__shfl_xor((int)most, 2));
   const uint32_t byte = scale_byte<FMT>(most);
-  const bool nan = byte == 255u;
+  const uint32_t held = byte == 255u ? 0u : ~0u;  // (a NaN block's elements are 0)
   const float un = unscale(byte);
   float s[8];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) s[e] = element(v[e], un, nan);
+  for (int e = 0; e < 8; ++e) s[e] = v[e] * un;
   if (FMT == PIE_MXFP8) {
-    const u32x2 r = {to_fp8x4(s[0], s[1], s[2], s[3]), to_fp8x4(s[4], s[5], s[6], s[7])};
+    const u32x2 r = {to_fp8x4(s[0], s[1], s[2], s[3]) & held, to_fp8x4(s[4], s[5], s[6], s[7]) & held};
     *reinterpret_cast<u32x2*>(elements + c) = r;
   } else {
-    *reinterpret_cast<uint32_t*>(elements + (c >> 1)) = to_fp4x8(s);
+    *reinterpret_cast<uint32_t*>(elements + (c >> 1)) = to_fp4x8(s) & held;
   }
   if ((c & 31) == 0) scales[c >> 5] = (uint8_t)byte;
 }
@@ -67,48 +67,33 @@ __device__ __forceinline__ void pad_scales(uint8_t* scales, int k) {
 // ---------------------------------------------------------------------------------------------
 // Rows of plain values
 // ---------------------------------------------------------------------------------------------
-RowsView mx_view(const void* p, int dtype, int64_t stride) {
-  const int size = dtype == PIE_F32 ? 4 : 2;
-  return RowsView{p, stride, dtype, reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride * size % 16 == 0};
-}
+RowsView mx_view(const void* p, int dtype, int64_t stride) { return RowsView{p, stride, dtype}; }
+// (Vector accesses at addresses that are aligned to the elements only are ordinary on this chip; they touch a line more now and then.)
+typedef f32x4 f32x4_at4 __attribute__((aligned(4)));
+typedef u32x4 u32x4_at2 __attribute__((aligned(2)));
 __device__ __forceinline__ void load8(const RowsView& r, int64_t row, int c, float (&v)[8]) {
   const int64_t at = row * r.stride + c;
   if (r.dtype == PIE_F32) {
     const float* p = reinterpret_cast<const float*>(r.p) + at;
-    if (r.vec) {
-      const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
+    const f32x4 a = *reinterpret_cast<const f32x4_at4*>(p), b = *reinterpret_cast<const f32x4_at4*>(p + 4);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) { v[e] = a[e]; v[4 + e] = b[e]; }
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = p[e];
-    }
+    for (int e = 0; e < 4; ++e) { v[e] = a[e]; v[4 + e] = b[e]; }
     return;
   }
-  const uint16_t* p = reinterpret_cast<const uint16_t*>(r.p) + at;
   Pack16 k;
-  if (r.vec) {
-    k.u = *reinterpret_cast<const u32x4*>(p);
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) k.s[e] = p[e];
-  }
+  k.u = *reinterpret_cast<const u32x4_at2*>(reinterpret_cast<const uint16_t*>(r.p) + at);
 #pragma unroll
   for (int e = 0; e < 8; ++e) v[e] = r.dtype == PIE_BF16 ? bf16_bits_to_f32(k.s[e]) : (float)__builtin_bit_cast(_Float16, k.s[e]);
 }
 // Rounds v to r's type (v becomes what is stored) and, where r.p is given, stores it.
 __device__ __forceinline__ void store8(const RowsView& r, int64_t row, int c, float (&v)[8]) {
   const int64_t at = row * r.stride + c;
+  void* to = const_cast<void*>(r.p);
   if (r.dtype == PIE_F32) {
-    float* p = const_cast<float*>(reinterpret_cast<const float*>(r.p)) + at;
-    if (r.p == nullptr) return;
-    if (r.vec) {
-      *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
-      *reinterpret_cast<f32x4*>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) p[e] = v[e];
-    }
+    if (to == nullptr) return;
+    float* p = reinterpret_cast<float*>(to) + at;
+    *reinterpret_cast<f32x4_at4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
+    *reinterpret_cast<f32x4_at4*>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
     return;
   }
   Pack16 k;
@@ -117,105 +102,155 @@ __device__ __forceinline__ void store8(const RowsView& r, int64_t row, int c, fl
     k.s[e] = r.dtype == PIE_BF16 ? __builtin_bit_cast(uint16_t, f32_to_bf16(v[e])) : __builtin_bit_cast(uint16_t, (_Float16)v[e]);
     v[e] = r.dtype == PIE_BF16 ? bf16_bits_to_f32(k.s[e]) : (float)__builtin_bit_cast(_Float16, k.s[e]);
   }
-  if (r.p == nullptr) return;
-  uint16_t* p = const_cast<uint16_t*>(reinterpret_cast<const uint16_t*>(r.p)) + at;
-  if (r.vec) {
-    *reinterpret_cast<u32x4*>(p) = k.u;
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) p[e] = k.s[e];
-  }
+  if (to != nullptr) *reinterpret_cast<u32x4_at2*>(reinterpret_cast<uint16_t*>(to) + at) = k.u;
 }
 
 // ---------------------------------------------------------------------------------------------
-// Quantisation and its inverse: eight values a lane
+// Quantisation and its inverse: eight values a lane and piece, MX_PIECES pieces of a thread requested together.  Bound by HBM: 28672 x 4096 of bf16 to
+// 4 bits 59 us (5.1 TB/s), with one piece a thread and 64-bit divisions 75; 64 x 4096 to 8 bits 3.3 us, a launch.
 // ---------------------------------------------------------------------------------------------
-template <int FMT>
+constexpr int MX_PIECES = 4;
+// Row and column of piece i of rows of k values; SMALL: pieces fit 32 bits, where a division is a few instructions.
+template <bool SMALL>
+__device__ __forceinline__ void piece_at(int64_t i, int per_row, int64_t& row, int& c) {
+  if (SMALL) {
+    const uint32_t r = (uint32_t)i / (uint32_t)per_row;
+    row = r;
+    c = (int)((uint32_t)i - r * (uint32_t)per_row) * 8;
+  } else {
+    row = i / per_row;
+    c = (int)(i - row * per_row) * 8;
+  }
+}
+
+template <int FMT, bool SMALL, int P>
 __global__ __launch_bounds__(256) void mx_quantise_kernel(RowsView x, int64_t pieces, int k, MxRowsView out) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= pieces) return;  // (a row's pieces are a multiple of four: the lanes of a block stay together)
-  const int per_row = k >> 3;
-  const int64_t row = i / per_row;
-  const int c = (int)(i - row * per_row) * 8;
-  float v[8];
-  load8(x, row, c, v);
-  uint8_t* scales = out.scales + row * out.scale_bytes;
-  put_eight<FMT>(v, out.elements + row * out.row_bytes, scales, c);
-  if (c == 0) pad_scales(scales, k);
+  const int64_t first = (int64_t)blockIdx.x * (256 * P) + threadIdx.x;
+  float v[P][8];
+  int64_t row[P];
+  int c[P];
+#pragma unroll
+  for (int j = 0; j < P; ++j) {
+    if (first + j * 256 >= pieces) break;  // (a row's pieces are a multiple of four: the lanes of a block stay together)
+    piece_at<SMALL>(first + j * 256, k >> 3, row[j], c[j]);
+    load8(x, row[j], c[j], v[j]);
+  }
+#pragma unroll
+  for (int j = 0; j < P; ++j) {
+    if (first + j * 256 >= pieces) break;
+    uint8_t* scales = out.scales + row[j] * out.scale_bytes;
+    put_eight<FMT>(v[j], out.elements + row[j] * out.row_bytes, scales, c[j]);
+    if (c[j] == 0) pad_scales(scales, k);
+  }
 }
 
+template <bool SMALL, int P>
 __global__ __launch_bounds__(256) void mx_dequantise_kernel(MxRowsView a, int fmt, int64_t pieces, int k, RowsView out) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= pieces) return;
-  const int per_row = k >> 3;
-  const int64_t row = i / per_row;
-  const int c = (int)(i - row * per_row) * 8;
-  const uint32_t byte = a.scales[row * a.scale_bytes + (c >> 5)];
-  // 2^(byte - 127): a denormal for byte 0
-  const float scale = byte == 255u ? __uint_as_float(0x7fc00000u) : byte == 0 ? __uint_as_float(0x00400000u) : __uint_as_float(byte << 23);
-  float v[8];
-  if (fmt == PIE_MXFP8) {
-    const u32x2 e = *reinterpret_cast<const u32x2*>(a.elements + row * a.row_bytes + c);
+  const int64_t first = (int64_t)blockIdx.x * (256 * P) + threadIdx.x;
+  int64_t row[P];
+  int c[P];
+  u32x2 e[P];
+  uint32_t byte[P];
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)e[j], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)e[j], true);
-      v[4 * j] = lo[0] * scale; v[4 * j + 1] = lo[1] * scale; v[4 * j + 2] = hi[0] * scale; v[4 * j + 3] = hi[1] * scale;
-    }
-  } else {
-    const uint32_t e = *reinterpret_cast<const uint32_t*>(a.elements + row * a.row_bytes + (c >> 1));
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const uint32_t n = e >> (4 * j), m = n & 7;  // 0, 1/2, then 1.f * 2^(e - 1): the exponent and fraction bits moved into place
-      const float f = m < 2 ? 0.5f * (float)m : __uint_as_float((m << 22) + (126u << 23));
-      v[j] = (n & 8 ? -f : f) * scale;
-    }
+  for (int j = 0; j < P; ++j) {
+    if (first + j * 256 >= pieces) break;
+    piece_at<SMALL>(first + j * 256, k >> 3, row[j], c[j]);
+    byte[j] = a.scales[row[j] * a.scale_bytes + (c[j] >> 5)];
+    const uint8_t* p = a.elements + row[j] * a.row_bytes;
+    if (fmt == PIE_MXFP8) e[j] = *reinterpret_cast<const u32x2*>(p + c[j]);
+    else e[j][0] = *reinterpret_cast<const uint32_t*>(p + (c[j] >> 1));
   }
-  store8(out, row, c, v);
+#pragma unroll
+  for (int j = 0; j < P; ++j) {
+    if (first + j * 256 >= pieces) break;
+    // 2^(byte - 127): a denormal for byte 0
+    const float scale = byte[j] == 255u ? __uint_as_float(0x7fc00000u) : byte[j] == 0 ? __uint_as_float(0x00400000u) : __uint_as_float(byte[j] << 23);
+    float v[8];
+    if (fmt == PIE_MXFP8) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)e[j][i], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)e[j][i], true);
+        v[4 * i] = lo[0] * scale; v[4 * i + 1] = lo[1] * scale; v[4 * i + 2] = hi[0] * scale; v[4 * i + 3] = hi[1] * scale;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t n = e[j][0] >> (4 * i), m = n & 7;  // 0, 1/2, then 1.f * 2^(e - 1): the exponent and fraction bits moved into place
+        const float f = m < 2 ? 0.5f * (float)m : __uint_as_float((m << 22) + (126u << 23));
+        v[i] = (n & 8 ? -f : f) * scale;
+      }
+    }
+    store8(out, row[j], c[j], v);
+  }
 }
 
 static dim3 pieces_grid(int64_t pieces) { return dim3((unsigned)((pieces + 255) / 256)); }
 
+// One piece a thread while that leaves fewer than eight workgroups to a compute unit.
+template <typename F>
+static void with_pieces(int64_t pieces, F&& go) {
+  using std::integral_constant;
+  if (pieces < 256 * 2048) go(std::true_type{}, integral_constant<int, 1>{});
+  else if (pieces < INT32_MAX) go(std::true_type{}, integral_constant<int, MX_PIECES>{});
+  else go(std::false_type{}, integral_constant<int, MX_PIECES>{});
+}
+
 hipError_t launch_mx_quantise(const RowsView& x, int rows, int k, int format, const MxRowsView& out, hipStream_t s) {
   const int64_t pieces = (int64_t)rows * (k / 8);
   if (pieces <= 0) return hipSuccess;
-  if (format == PIE_MXFP8) mx_quantise_kernel<PIE_MXFP8><<<pieces_grid(pieces), dim3(256), 0, s>>>(x, pieces, k, out);
-  else mx_quantise_kernel<PIE_MXFP4><<<pieces_grid(pieces), dim3(256), 0, s>>>(x, pieces, k, out);
+  with_pieces(pieces, [&](auto small_c, auto p_c) {
+    constexpr bool SMALL = decltype(small_c)::value;
+    constexpr int P = decltype(p_c)::value;
+    const dim3 grid = pieces_grid((pieces + P - 1) / P);
+    if (format == PIE_MXFP8) mx_quantise_kernel<PIE_MXFP8, SMALL, P><<<grid, dim3(256), 0, s>>>(x, pieces, k, out);
+    else mx_quantise_kernel<PIE_MXFP4, SMALL, P><<<grid, dim3(256), 0, s>>>(x, pieces, k, out);
+  });
   return hipGetLastError();
 }
 
 hipError_t launch_mx_dequantise(const MxRowsView& a, int format, int rows, int k, const RowsView& out, hipStream_t s) {
   const int64_t pieces = (int64_t)rows * (k / 8);
   if (pieces <= 0) return hipSuccess;
-  mx_dequantise_kernel<<<pieces_grid(pieces), dim3(256), 0, s>>>(a, format, pieces, k, out);
+  with_pieces(pieces, [&](auto small_c, auto p_c) {
+    constexpr bool SMALL = decltype(small_c)::value;
+    constexpr int P = decltype(p_c)::value;
+    mx_dequantise_kernel<SMALL, P><<<pieces_grid((pieces + P - 1) / P), dim3(256), 0, s>>>(a, format, pieces, k, out);
+  });
   return hipGetLastError();
 }
 
 // ---------------------------------------------------------------------------------------------
-// Norm: one workgroup per row, eight columns a thread, as rmsnorm_row in elementwise.hip
+// Norm: a workgroup per row, eight columns a thread (as rmsnorm_row in elementwise.hip).  Bound by HBM for many rows, by latency for few.
+// An element that rounds the other way is off by a step, an eighth of it, so the normalised values are off by their last rounding to fp32 alone:
+// squares are summed eight to a thread in fp32 and beyond in 64 bits, and gain over root enters as a pair of fp32.  (Root and quotient in 64 bits
+// by every wave cost more than the rest of the kernel: 8320 x 4096 of bf16 42 us; the fp32 reciprocal root and one step of Newton's method in 64
+// bits, good to 2^-44: 29 us.  Several rows to a workgroup, the next one's values requested ahead, gained nothing.  8320 x 4096 of fp32 with the
+// residual's addition, 444 MB: 80 us, 5.6 TB/s; one row 3.6 us.)
 // ---------------------------------------------------------------------------------------------
-template <int FMT, int THREADS>
-__global__ __launch_bounds__(THREADS) void mx_norm_kernel(MxNormArgs a, int k, MxRowsView out) {
-  __shared__ float red[THREADS / 64];
+__device__ __forceinline__ double rsqrt_f64(double m) {
+  if (!(m > 1e-30 && m < 1e30)) return m == INFINITY ? 0.0 : 1.0 / sqrt(m);  // (uniform; beyond what fp32 holds well)
+  const double r = (double)__builtin_amdgcn_rsqf((float)m);
+  return r * (1.5 - 0.5 * m * r * r);
+}
+
+template <int FMT, int THREADS, bool SUMS>
+__global__ __launch_bounds__(THREADS) void mx_norm_kernel(MxNormArgs a, double inv_k, int k, MxRowsView out) {
+  __shared__ double red[THREADS / 64];
   const int64_t row = blockIdx.x;
   const int tid = threadIdx.x, c = tid * 8;
+  const bool in = c < k;  // (k is a multiple of 32: the four lanes of a block go the same way)
   float v[8], ss = 0.f;
   Pack16 g;
-  if (c < k) {
-    if (a.gain_vec) {
-      g.u = *reinterpret_cast<const u32x4*>(a.gain + c);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) g.h[e] = a.gain[c + e];
-    }
-    const int64_t from = a.ids ? a.ids[row] : row;
-    load8(a.x, from, c, v);
+  if (in) {
+    g.u = *reinterpret_cast<const u32x4_at2*>(reinterpret_cast<const uint16_t*>(a.gain) + c);
+    load8(a.x, a.ids ? a.ids[row] : row, c, v);
     if (a.delta.p) {
       float d[8];
       load8(a.delta, row, c, d);
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] += d[e];
     }
-    if (a.splits > 0) {  // partial sums of the product before, in their order, then what they are added to
+    if constexpr (SUMS) {  // partial sums of the product before, in their order, then what they are added to
       f32x4 p = {0.f, 0.f, 0.f, 0.f}, q = p;
       const float* at = a.part + row * a.part_stride + c;
       for (int i = 0; i < a.splits; ++i) {
@@ -229,18 +264,22 @@ __global__ __launch_bounds__(THREADS) void mx_norm_kernel(MxNormArgs a, int k, M
 #pragma unroll
     for (int e = 0; e < 8; ++e) ss += v[e] * v[e];
   }
-  ss = wave_sum(ss);
+  double sum = wave_sum_f64(ss);
   if constexpr (THREADS > 64) {
-    if ((tid & 63) == 0) red[tid >> 6] = ss;
+    if ((tid & 63) == 0) red[tid >> 6] = sum;
     __syncthreads();
-    ss = 0.f;
+    sum = 0.0;
 #pragma unroll
-    for (int w = 0; w < THREADS / 64; ++w) ss += red[w];
+    for (int w = 0; w < THREADS / 64; ++w) sum += red[w];
   }
-  const float r = 1.0f / sqrtf(ss / (float)k + a.eps);
-  if (c < k) {  // (k is a multiple of 32: the four lanes of a block go the same way)
+  const double r = rsqrt_f64(sum * inv_k + (double)a.eps);
+  const float rh = (float)r, rl = rh < INFINITY ? (float)(r - (double)rh) : 0.f;
+  if (in) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = v[e] * r * bf16_to_f32(g.h[e]);
+    for (int e = 0; e < 8; ++e) {
+      const float ge = bf16_to_f32(g.h[e]), hi = rh * ge, lo = __builtin_fmaf(rh, ge, -hi) + rl * ge;
+      v[e] = __builtin_fmaf(v[e], hi, v[e] * lo);
+    }
     uint8_t* scales = out.scales + row * out.scale_bytes;
     put_eight<FMT>(v, out.elements + row * out.row_bytes, scales, c);
     if (c == 0) pad_scales(scales, k);
@@ -252,8 +291,9 @@ hipError_t launch_mx_norm(const MxNormArgs& a, int rows, int k, int format, cons
   if (k > 8192) return hipErrorInvalidValue;
   auto go = [&](auto threads_c) {
     constexpr int T = decltype(threads_c)::value;
-    if (format == PIE_MXFP8) mx_norm_kernel<PIE_MXFP8, T><<<dim3(rows), dim3(T), 0, s>>>(a, k, out);
-    else mx_norm_kernel<PIE_MXFP4, T><<<dim3(rows), dim3(T), 0, s>>>(a, k, out);
+    if (a.splits > 0) mx_norm_kernel<PIE_MXFP8, T, true><<<dim3(rows), dim3(T), 0, s>>>(a, 1.0 / k, k, out);  // (a layer's)
+    else if (format == PIE_MXFP8) mx_norm_kernel<PIE_MXFP8, T, false><<<dim3(rows), dim3(T), 0, s>>>(a, 1.0 / k, k, out);
+    else mx_norm_kernel<PIE_MXFP4, T, false><<<dim3(rows), dim3(T), 0, s>>>(a, 1.0 / k, k, out);
     return hipGetLastError();
   };
   using std::integral_constant;
@@ -318,22 +358,22 @@ __device__ __forceinline__ void mx_epilogue(const MxEpi& e, const f32x16& acc, c
     }
     const auto both = __builtin_amdgcn_permlane32_swap(most, most, false, false);
     const uint32_t byte = scale_byte<FMT>(max((uint32_t)both[0], (uint32_t)both[1]));
-    const bool nan = byte == 255u;
+    const uint32_t held = byte == 255u ? 0u : ~0u;
     const float un = unscale(byte);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = element(v[i], un, nan);
+    for (int i = 0; i < 16; ++i) v[i] *= un;
     const int c = n0 >> 1;  // (n0: the gate block's packed column)
     uint8_t* row = reinterpret_cast<uint8_t*>(e.out) + m * e.ldo;
     if (FMT == PIE_MXFP8) {
       uint32_t g[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) g[i] = to_fp8x4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+      for (int i = 0; i < 4; ++i) g[i] = to_fp8x4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]) & held;
       swap_halves(g[0], g[2]);
       swap_halves(g[1], g[3]);
       if (m < M) *reinterpret_cast<u32x4*>(row + c + h * 16) = u32x4{g[0], g[2], g[1], g[3]};
     } else {
       const float a[8] = {v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]}, b[8] = {v[8], v[9], v[10], v[11], v[12], v[13], v[14], v[15]};
-      uint32_t p = to_fp4x8(a), q = to_fp4x8(b);
+      uint32_t p = to_fp4x8(a) & held, q = to_fp4x8(b) & held;
       swap_halves(p, q);
       if (m < M) *reinterpret_cast<u32x2*>(row + (c >> 1) + h * 8) = u32x2{(p & 0xffffu) | (q << 16), (p >> 16) | (q & 0xffff0000u)};
     }
@@ -344,7 +384,7 @@ __device__ __forceinline__ void mx_epilogue(const MxEpi& e, const f32x16& acc, c
     }
   } else if constexpr (MODE == MX_BF16) {
     bf16_t* row = reinterpret_cast<bf16_t*>(e.out) + m * e.ldo;
-    if (e.vec) {  // rows of whole, aligned groups of eight
+    if (n0 + 32 <= e.N) {
       uint32_t g[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
@@ -353,9 +393,11 @@ __device__ __forceinline__ void mx_epilogue(const MxEpi& e, const f32x16& acc, c
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) swap_halves(g[i], g[i + 4]);
-      const int n = n0 + h * 16;
-      if (m < M && n < e.N) *reinterpret_cast<u32x4*>(row + n) = u32x4{g[0], g[1], g[4], g[5]};
-      if (m < M && n + 8 < e.N) *reinterpret_cast<u32x4*>(row + n + 8) = u32x4{g[2], g[3], g[6], g[7]};
+      uint16_t* to = reinterpret_cast<uint16_t*>(row) + n0 + h * 16;
+      if (m < M) {
+        *reinterpret_cast<u32x4_at2*>(to) = u32x4{g[0], g[1], g[4], g[5]};
+        *reinterpret_cast<u32x4_at2*>(to + 8) = u32x4{g[2], g[3], g[6], g[7]};
+      }
     } else if (m < M) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
@@ -389,8 +431,8 @@ __device__ __forceinline__ void mx_epilogue(const MxEpi& e, const f32x16& acc, c
         }
       }
       float* p = reinterpret_cast<float*>(e.out) + m * e.ldo + n;
-      if (e.vec) {
-        *reinterpret_cast<f32x4*>(p) = y;
+      if (n + 4 <= e.N) {
+        *reinterpret_cast<f32x4_at4*>(p) = y;
       } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
@@ -951,18 +993,18 @@ __global__ __launch_bounds__(256) void mx_join_kernel(const float* __restrict__ 
   total(c, v);
   if (e.mode == MX_RESID_EMBED || e.mode == MX_RESID_OUT) {
     float r[8];
-    if (e.mode == MX_RESID_EMBED && !e.resid) load8(RowsView{e.embeds, e.H, PIE_BF16, 1}, e.ids[m], c, r);
-    else load8(RowsView{e.resid, e.H, PIE_F32, 1}, m, c, r);
+    if (e.mode == MX_RESID_EMBED && !e.resid) load8(RowsView{e.embeds, e.H, PIE_BF16}, e.ids[m], c, r);
+    else load8(RowsView{e.resid, e.H, PIE_F32}, m, c, r);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] += r[i];
     if (e.mode == MX_RESID_OUT && !e.out) {
       const int id = e.ids[m];
-      if (id >= 0) store8(RowsView{e.embeds, e.H, PIE_BF16, 1}, id, c, v);
+      if (id >= 0) store8(RowsView{e.embeds, e.H, PIE_BF16}, id, c, v);
       return;
     }
   }
-  const RowsView out{e.out, e.ldo, e.mode == MX_BF16 ? PIE_BF16 : PIE_F32, 1};
-  if (e.vec && c + 8 <= e.N) {
+  const RowsView out{e.out, e.ldo, e.mode == MX_BF16 ? PIE_BF16 : PIE_F32};
+  if (c + 8 <= e.N) {
     store8(out, m, c, v);
   } else {
 #pragma unroll
@@ -1072,10 +1114,16 @@ static hipError_t run_product(const MxRowsView& a, int M, const MxPacked& w, con
 hipError_t launch_mx_product(const MxRowsView& a, int format, int M, const MxPacked& w, const MxEpi& e, float* ws, int n_cus, hipStream_t s) {
   if (M <= 0) return hipSuccess;
   const bool gated = e.mode == MX_SWIGLU8 || e.mode == MX_SWIGLU4, fp8 = format == PIE_MXFP8;
-  const MxPlan p = mx_plan(M, w, gated, fp8, n_cus);
+  MxPacked::Plan& kept = w.plan;  // (gated or not, and the number of compute units, do not change from call to call)
+  if (kept.key != 2 * M + fp8) {
+    const MxPlan q = mx_plan(M, w, gated, fp8, n_cus);
+    kept = MxPacked::Plan{2 * M + fp8, q.form.mb, q.form.ks, q.form.nj, q.splits, q.rows};
+  }
+  const MxPlan p{{kept.mb, kept.ks, kept.nj}, kept.splits, kept.rows, 0.0};
   const hipError_t err = gated ? (fp8 ? run_product<true, PIE_MXFP8>(a, p.rows, w, e, p, ws, s) : run_product<true, PIE_MXFP4>(a, p.rows, w, e, p, ws, s))
                                : (fp8 ? run_product<false, PIE_MXFP8>(a, p.rows, w, e, p, ws, s) : run_product<false, PIE_MXFP4>(a, p.rows, w, e, p, ws, s));
   if (err != hipSuccess || p.rows == M) return err;
+  MxPacked tail = w;  // (with a plan of its own)
   MxRowsView rest = a;
   rest.elements += p.rows * a.row_bytes;
   rest.scales += p.rows * a.scale_bytes;
@@ -1084,7 +1132,7 @@ hipError_t launch_mx_product(const MxRowsView& a, int format, int M, const MxPac
   if (e.scales) r.scales = e.scales + p.rows * e.lds;
   if (e.ids) r.ids = e.ids + p.rows;
   if (e.resid) r.resid = e.resid + (int64_t)p.rows * e.H;
-  return launch_mx_product(rest, format, M - p.rows, w, r, ws, n_cus, s);
+  return launch_mx_product(rest, format, M - p.rows, tail, r, ws, n_cus, s);
 }
 
 void mx_product_plan(int M, const MxPacked& w, bool gated, int format, int n_cus, int64_t out[5]) {

@@ -2018,7 +2018,7 @@ extern "C" pie_status pie_mx_norm(pie_ctx* c, const pie_rows* x, const pie_rows*
   MxNormArgs a{};
   a.x = rows_view(x); a.delta = rows_view(delta);
   a.h = h ? rows_view(h) : mx_view(nullptr, x->dtype, 0);
-  a.gain = reinterpret_cast<const bf16_t*>(gain); a.gain_vec = reinterpret_cast<uintptr_t>(gain) % 16 == 0; a.eps = c->m.rms_eps;
+  a.gain = reinterpret_cast<const bf16_t*>(gain); a.eps = c->m.rms_eps;
   HIP_TRY(c, launch_mx_norm(a, rows, k, out->format, mx_rows_view(out), c->stream));
   return PIE_OK;
 }
@@ -2133,9 +2133,8 @@ extern "C" pie_status pie_mx_product(pie_ctx* c, const pie_mx_rows* a, int32_t r
   if (pie_status st = check_mx_rows(c, a, w.K, who)) return st;
   if (pie_status st = check_rows(c, out, w.N, "out", who)) return st;
   if (out->dtype == PIE_F16) return fail(c, PIE_EINVAL, "%s: out is bf16 or fp32", who);
-  const RowsView o = rows_view(out);
   const bool f32 = out->dtype == PIE_F32;
-  const MxEpi e{f32 ? MX_F32 : MX_BF16, out->data, out->row_stride, nullptr, 0, w.N, o.vec && w.N % (f32 ? 4 : 8) == 0, nullptr, nullptr, nullptr, 0};
+  const MxEpi e{f32 ? MX_F32 : MX_BF16, out->data, out->row_stride, nullptr, 0, w.N, nullptr, nullptr, nullptr, 0};
   HIP_TRY(c, launch_mx_product(mx_rows_view(a), a->format, rows, w, e, c->mx_ws, c->wave_slots / 8, c->stream));
   return PIE_OK;
 }
@@ -2149,7 +2148,7 @@ extern "C" pie_status pie_mx_swiglu(pie_ctx* c, const pie_mx_rows* a, int32_t ro
   if (pie_status st = check_mx_rows(c, a, w.K, who)) return st;
   if (pie_status st = check_mx_rows(c, out, w.N / 2, who)) return st;
   const MxRowsView o = mx_rows_view(out);
-  const MxEpi e{out->format == PIE_MXFP8 ? MX_SWIGLU8 : MX_SWIGLU4, o.elements, o.row_bytes, o.scales, o.scale_bytes, w.N / 2, 1, nullptr, nullptr, nullptr, 0};
+  const MxEpi e{out->format == PIE_MXFP8 ? MX_SWIGLU8 : MX_SWIGLU4, o.elements, o.row_bytes, o.scales, o.scale_bytes, w.N / 2, nullptr, nullptr, nullptr, 0};
   HIP_TRY(c, launch_mx_product(mx_rows_view(a), a->format, rows, w, e, c->mx_ws, c->wave_slots / 8, c->stream));
   return PIE_OK;
 }
@@ -2297,12 +2296,12 @@ static pie_status run_layer_mx(pie_ctx* c, int32_t layer, const pie_batch* b, fl
   n.ids = x_in ? nullptr : b->in_ids;
   n.h = mx_view(carried > 0 ? x_in : nullptr, n.x.dtype, H);
   n.part = c->splitk; n.splits = carried; n.part_stride = round_up(H, 32); n.split_stride = (int64_t)T * n.part_stride;
-  n.gain = L.g1; n.gain_vec = 1; n.eps = m.rms_eps;
+  n.gain = L.g1; n.eps = m.rms_eps;
   HIP_TRY(c, launch_mx_norm(n, T, H, PIE_MXFP8, acts.rows, s));
   tm.end(PIE_STAGE_NORM1);
 
   tm.begin(PIE_STAGE_QKV);
-  HIP_TRY(c, launch_mx_product(acts.rows, PIE_MXFP8, T, L.mqkv, MxEpi{MX_BF16, c->qkv, QKV, nullptr, 0, QKV, 1, nullptr, nullptr, nullptr, 0}, c->mx_ws, c->wave_slots / 8, s));
+  HIP_TRY(c, launch_mx_product(acts.rows, PIE_MXFP8, T, L.mqkv, MxEpi{MX_BF16, c->qkv, QKV, nullptr, 0, QKV, nullptr, nullptr, nullptr, 0}, c->mx_ws, c->wave_slots / 8, s));
   tm.end(PIE_STAGE_QKV);
 
   tm.begin(PIE_STAGE_ROPE_APPEND);
@@ -2313,23 +2312,23 @@ static pie_status run_layer_mx(pie_ctx* c, int32_t layer, const pie_batch* b, fl
 
   tm.begin(PIE_STAGE_OPROJ);
   HIP_TRY(c, launch_mx_quantise(mx_view(c->attn, PIE_BF16, Hq * D), T, Hq * D, PIE_MXFP8, acts.attn, s));
-  HIP_TRY(c, launch_mx_product(acts.attn, PIE_MXFP8, T, L.mo, MxEpi{MX_RESID_EMBED, c->h, H, nullptr, 0, H, 1, c->embeds, b->in_ids, x_in, H}, c->mx_ws, c->wave_slots / 8, s));
+  HIP_TRY(c, launch_mx_product(acts.attn, PIE_MXFP8, T, L.mo, MxEpi{MX_RESID_EMBED, c->h, H, nullptr, 0, H, c->embeds, b->in_ids, x_in, H}, c->mx_ws, c->wave_slots / 8, s));
   tm.end(PIE_STAGE_OPROJ);
 
   tm.begin(PIE_STAGE_NORM2);
   MxNormArgs n2{};
   n2.x = mx_view(c->h, PIE_F32, H); n2.h = mx_view(nullptr, PIE_F32, H);
-  n2.gain = L.g2; n2.gain_vec = 1; n2.eps = m.rms_eps;
+  n2.gain = L.g2; n2.eps = m.rms_eps;
   HIP_TRY(c, launch_mx_norm(n2, T, H, PIE_MXFP8, acts.rows, s));
   tm.end(PIE_STAGE_NORM2);
 
   tm.begin(PIE_STAGE_GATEUP);
   HIP_TRY(c, launch_mx_product(acts.rows, PIE_MXFP8, T, L.mgu,
-                               MxEpi{MX_SWIGLU8, acts.act.elements, acts.act.row_bytes, acts.act.scales, acts.act.scale_bytes, I, 1, nullptr, nullptr, nullptr, 0}, c->mx_ws, c->wave_slots / 8, s));
+                               MxEpi{MX_SWIGLU8, acts.act.elements, acts.act.row_bytes, acts.act.scales, acts.act.scale_bytes, I, nullptr, nullptr, nullptr, 0}, c->mx_ws, c->wave_slots / 8, s));
   tm.end(PIE_STAGE_GATEUP);
 
   tm.begin(PIE_STAGE_DOWN);
-  HIP_TRY(c, launch_mx_product(acts.act, PIE_MXFP8, T, L.mdown, MxEpi{MX_RESID_OUT, y_out, H, nullptr, 0, H, 1, c->embeds, b->out_ids, c->h, H}, c->mx_ws, c->wave_slots / 8, s));
+  HIP_TRY(c, launch_mx_product(acts.act, PIE_MXFP8, T, L.mdown, MxEpi{MX_RESID_OUT, y_out, H, nullptr, 0, H, c->embeds, b->out_ids, c->h, H}, c->mx_ws, c->wave_slots / 8, s));
   tm.end(PIE_STAGE_DOWN);
   c->last_T = T;
   c->last_mx = true;

@@ -50,7 +50,7 @@ class Calls:
         return C.byref(self.b.MxRowsC(format, elements, row_bytes, scales, scale_bytes))
 
     def rows(self, data=A, dtype=F32, stride=64):
-        return C.byref(self.b.RowsC(data, dtype, stride))
+        return self.b._ROWS.pack(data or 0, dtype, stride)
 
     def call(self, name, *args):
         return getattr(self.c.lib, name)(self.ctx.ctx, *args)
@@ -258,6 +258,20 @@ def test_rows_in_the_binding():
             MxRows(*bad)
     with pytest.raises(ValueError):
         MxRows.empty(3, 40, "mxfp8", "cpu")
+
+
+def test_contexts_that_only_plan_refuse_in_the_binding():
+    import torch
+    from types import SimpleNamespace
+    from paper_2510_24051_amd import MxRows, MxWeight, Pie, PieError
+    p = Pie.planner(MODEL, 32, 16, 8, 4)
+    r, x = MxRows.empty(2, 64, "mxfp8", "cpu"), torch.zeros((2, 64))
+    w = MxWeight(SimpleNamespace(ctx=None), 1, 64, 64, False)
+    for call in (lambda: p.mx_quantise(x, r), lambda: p.mx_dequantise(r, x), lambda: p.mx_norm(x, x[0].bfloat16(), r), lambda: p.mx_product(r, w, x),
+                 lambda: p.mx_swiglu(r, w, r), lambda: p.mx_weight([r]), lambda: p.load_layer_mx(0, None)):
+        with pytest.raises(PieError) as e:
+            call()
+        assert e.value.status == INVALID and "only plans" in str(e.value)
 
 
 def test_every_form_is_listed():
