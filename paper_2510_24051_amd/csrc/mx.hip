@@ -343,117 +343,109 @@ __device__ __forceinline__ void swap_halves(uint32_t& a, uint32_t& b) {  // lowe
   b = r[1];
 }
 
-// Columns [n0, n0 + 32) of token m; `up` is read by the SwiGLU modes alone.
-template <int MODE>
-__device__ __forceinline__ void mx_epilogue(const MxEpi& e, const f32x16& acc, const f32x16& up, int64_t m, int M, int n0, int lane) {
+// Gate and up columns [n0, n0 + 32) of token m (n0: the gate block's packed column) -> 32 columns of activations.
+template <int FMT>
+__device__ __forceinline__ void mx_gated_columns(const MxEpi& e, const f32x16& gate, const f32x16& up, int64_t m, int M, int n0, int lane) {
   const int h = lane >> 5;
-  if constexpr (MODE == MX_SWIGLU8 || MODE == MX_SWIGLU4) {
-    constexpr int FMT = MODE == MX_SWIGLU8 ? PIE_MXFP8 : PIE_MXFP4;
-    float v[16];
-    uint32_t most = 0;
+  float v[16];
+  uint32_t most = 0;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      v[i] = silu_f(acc[i]) * up[i];
-      most = max(most, magnitude(v[i]));
-    }
-    const auto both = __builtin_amdgcn_permlane32_swap(most, most, false, false);
-    const uint32_t byte = scale_byte<FMT>(max((uint32_t)both[0], (uint32_t)both[1]));
-    const uint32_t held = byte == 255u ? 0u : ~0u;
-    const float un = unscale(byte);
-#pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] *= un;
-    const int c = n0 >> 1;  // (n0: the gate block's packed column)
-    uint8_t* row = reinterpret_cast<uint8_t*>(e.out) + m * e.ldo;
-    if (FMT == PIE_MXFP8) {
-      uint32_t g[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) g[i] = to_fp8x4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]) & held;
-      swap_halves(g[0], g[2]);
-      swap_halves(g[1], g[3]);
-      if (m < M) *reinterpret_cast<u32x4*>(row + c + h * 16) = u32x4{g[0], g[2], g[1], g[3]};
-    } else {
-      const float a[8] = {v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]}, b[8] = {v[8], v[9], v[10], v[11], v[12], v[13], v[14], v[15]};
-      uint32_t p = to_fp4x8(a) & held, q = to_fp4x8(b) & held;
-      swap_halves(p, q);
-      if (m < M) *reinterpret_cast<u32x2*>(row + (c >> 1) + h * 8) = u32x2{(p & 0xffffu) | (q << 16), (p >> 16) | (q & 0xffff0000u)};
-    }
-    if (m < M && h == 0) {
-      uint8_t* scales = e.scales + m * e.lds;
-      scales[c >> 5] = (uint8_t)byte;
-      if (c + 32 >= e.N) pad_scales(scales, e.N);
-    }
-  } else if constexpr (MODE == MX_BF16) {
-    bf16_t* row = reinterpret_cast<bf16_t*>(e.out) + m * e.ldo;
-    if (n0 + 32 <= e.N) {
-      uint32_t g[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const bf16x2 b = {f32_to_bf16(acc[2 * i]), f32_to_bf16(acc[2 * i + 1])};
-        g[i] = __builtin_bit_cast(uint32_t, b);
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) swap_halves(g[i], g[i + 4]);
-      uint16_t* to = reinterpret_cast<uint16_t*>(row) + n0 + h * 16;
-      if (m < M) {
-        *reinterpret_cast<u32x4_at2*>(to) = u32x4{g[0], g[1], g[4], g[5]};
-        *reinterpret_cast<u32x4_at2*>(to + 8) = u32x4{g[2], g[3], g[6], g[7]};
-      }
-    } else if (m < M) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int n = n0 + (i >> 2) * 8 + h * 4 + (i & 3);
-        if (n < e.N) row[n] = f32_to_bf16(acc[i]);
-      }
-    }
-  } else {  // fp32 sums, alone or on a residual
-    if (m >= M) return;
-    const int64_t id = MODE == MX_RESID_EMBED ? (e.resid ? m : (int64_t)e.ids[m]) : MODE == MX_RESID_OUT && !e.out ? e.ids[m] : m;
-    if (MODE == MX_RESID_OUT && id < 0) return;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int n = n0 + i * 8 + h * 4;
-      f32x4 y = {acc[4 * i], acc[4 * i + 1], acc[4 * i + 2], acc[4 * i + 3]};
-      if (n >= e.N) break;
-      if constexpr (MODE == MX_RESID_EMBED || MODE == MX_RESID_OUT) {  // (rows of whole, aligned groups of four)
-        if (MODE == MX_RESID_EMBED && !e.resid) {
-          const bf16x4 r = *reinterpret_cast<const bf16x4*>(e.embeds + id * e.H + n);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) y[j] += bf16_to_f32(r[j]);
-        } else {
-          y += *reinterpret_cast<const f32x4*>(e.resid + m * e.H + n);
-        }
-        if (MODE == MX_RESID_OUT && !e.out) {
-          bf16x4 o;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) o[j] = f32_to_bf16(y[j]);
-          *reinterpret_cast<bf16x4*>(e.embeds + id * e.H + n) = o;
-          continue;
-        }
-      }
-      float* p = reinterpret_cast<float*>(e.out) + m * e.ldo + n;
-      if (n + 4 <= e.N) {
-        *reinterpret_cast<f32x4_at4*>(p) = y;
-      } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (n + j < e.N) p[j] = y[j];
-      }
-    }
+  for (int i = 0; i < 16; ++i) {
+    v[i] = silu_f(gate[i]) * up[i];
+    most = max(most, magnitude(v[i]));
   }
-}
-
-// The epilogue of a product that is not gated, by the mode of its arguments (uniform).
-__device__ __forceinline__ void mx_plain_epilogue(const MxEpi& e, const f32x16& acc, int64_t m, int M, int n0, int lane) {
-  switch (e.mode) {
-    case MX_BF16: mx_epilogue<MX_BF16>(e, acc, acc, m, M, n0, lane); break;
-    case MX_F32: mx_epilogue<MX_F32>(e, acc, acc, m, M, n0, lane); break;
-    case MX_RESID_EMBED: mx_epilogue<MX_RESID_EMBED>(e, acc, acc, m, M, n0, lane); break;
-    case MX_RESID_OUT: mx_epilogue<MX_RESID_OUT>(e, acc, acc, m, M, n0, lane); break;
+  const auto both = __builtin_amdgcn_permlane32_swap(most, most, false, false);
+  const uint32_t byte = scale_byte<FMT>(max((uint32_t)both[0], (uint32_t)both[1]));
+  const uint32_t held = byte == 255u ? 0u : ~0u;
+  const float un = unscale(byte);
+#pragma unroll
+  for (int i = 0; i < 16; ++i) v[i] *= un;
+  const int c = n0 >> 1;
+  uint8_t* row = reinterpret_cast<uint8_t*>(e.out) + m * e.ldo;
+  if (FMT == PIE_MXFP8) {
+    uint32_t g[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) g[i] = to_fp8x4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]) & held;
+    swap_halves(g[0], g[2]);
+    swap_halves(g[1], g[3]);
+    if (m < M) *reinterpret_cast<u32x4*>(row + c + h * 16) = u32x4{g[0], g[2], g[1], g[3]};
+  } else {
+    const float a[8] = {v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]}, b[8] = {v[8], v[9], v[10], v[11], v[12], v[13], v[14], v[15]};
+    uint32_t p = to_fp4x8(a) & held, q = to_fp4x8(b) & held;
+    swap_halves(p, q);
+    if (m < M) *reinterpret_cast<u32x2*>(row + (c >> 1) + h * 8) = u32x2{(p & 0xffffu) | (q << 16), (p >> 16) | (q & 0xffff0000u)};
+  }
+  if (m < M && h == 0) {
+    uint8_t* scales = e.scales + m * e.lds;
+    scales[c >> 5] = (uint8_t)byte;
+    if (c + 32 >= e.N) pad_scales(scales, e.N);
   }
 }
 __device__ __forceinline__ void mx_gated_epilogue(const MxEpi& e, const f32x16& gate, const f32x16& up, int64_t m, int M, int n0, int lane) {
-  if (e.mode == MX_SWIGLU8) mx_epilogue<MX_SWIGLU8>(e, gate, up, m, M, n0, lane);
-  else mx_epilogue<MX_SWIGLU4>(e, gate, up, m, M, n0, lane);
+  if (e.mode == MX_SWIGLU8) mx_gated_columns<PIE_MXFP8>(e, gate, up, m, M, n0, lane);
+  else mx_gated_columns<PIE_MXFP4>(e, gate, up, m, M, n0, lane);
+}
+
+// Columns [n0, n0 + 32) of token m of a product that is not gated: a residual or none, then bf16 or fp32 (uniform; rows of residuals are whole blocks).
+__device__ __forceinline__ void mx_plain_epilogue(const MxEpi& e, const f32x16& acc, int64_t m, int M, int n0, int lane) {
+  const int h = lane >> 5;
+  if (m >= M) return;  // (lanes l and l + 32 have the same token)
+  float y[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) y[i] = acc[i];
+  if (e.mode == MX_RESID_EMBED && !e.resid) {
+    const bf16_t* r = e.embeds + (int64_t)e.ids[m] * e.H + n0 + h * 4;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const bf16x4 v = *reinterpret_cast<const bf16x4*>(r + 8 * i);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) y[4 * i + j] += bf16_to_f32(v[j]);
+    }
+  } else if (e.mode == MX_RESID_EMBED || e.mode == MX_RESID_OUT) {
+    const float* r = e.resid + m * e.H + n0 + h * 4;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const f32x4 v = *reinterpret_cast<const f32x4*>(r + 8 * i);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) y[4 * i + j] += v[j];
+    }
+  }
+  const bool to_embed = e.mode == MX_RESID_OUT && !e.out, whole = n0 + 32 <= e.N;
+  if (e.mode == MX_BF16 || to_embed) {
+    const int64_t id = to_embed ? e.ids[m] : m;
+    if (id < 0) return;
+    uint16_t* row = reinterpret_cast<uint16_t*>(to_embed ? e.embeds : e.out) + id * (to_embed ? e.H : e.ldo) + n0;
+    uint32_t g[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const bf16x2 b = {f32_to_bf16(y[2 * i]), f32_to_bf16(y[2 * i + 1])};
+      g[i] = __builtin_bit_cast(uint32_t, b);
+    }
+    if (whole) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) swap_halves(g[i], g[i + 4]);
+      *reinterpret_cast<u32x4_at2*>(row + h * 16) = u32x4{g[0], g[1], g[4], g[5]};
+      *reinterpret_cast<u32x4_at2*>(row + h * 16 + 8) = u32x4{g[2], g[3], g[6], g[7]};
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int n = (i >> 2) * 8 + h * 4 + (i & 3);
+        if (n0 + n < e.N) row[n] = (uint16_t)(g[i >> 1] >> (16 * (i & 1)));
+      }
+    }
+  } else {
+    float* row = reinterpret_cast<float*>(e.out) + m * e.ldo + n0;
+    if (whole) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) *reinterpret_cast<f32x4_at4*>(row + 8 * i + h * 4) = f32x4{y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]};
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int n = (i >> 2) * 8 + h * 4 + (i & 3);
+        if (n0 + n < e.N) row[n] = y[i];
+      }
+    }
+  }
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -473,9 +465,24 @@ __device__ __forceinline__ void mx_gated_epilogue(const MxEpi& e, const f32x16& 
 // ---------------------------------------------------------------------------------------------
 constexpr int MX_TM = 256, MX_TN = 256;
 
-// Byte offset of a tile's row for its copies.  Rows past the matrix are out of the descriptor's range: nothing is fetched for them (rows of
-// one token that copied the last row 32 times took ?), and what their lanes compute is not stored.
+// Byte offset of a tile's row for its copies.  Rows past the matrix are out of the descriptor's range: nothing is fetched for them, and
+// what their lanes compute is not stored.
 __device__ __forceinline__ int mx_row_offset(int r, int rows, int64_t stride) { return r < rows ? (int)(r * stride) : 0x7f000000; }
+#if __HIP_DEVICE_COMPILE__
+// Copy piece p of a tile of rows: 1 KiB, rows 8 p .. 8 p + 7, lane -> row lane / 8 of them, stored piece lane % 8.  Byte of its row's 128 that a
+// lane brings:
+__device__ __forceinline__ int mx_piece_byte(int p, int lane) { return (((lane & 7) ^ (lane >> 4)) * 16) ^ (p & 1) * 64; }
+// How far the bytes of the last stage that are behind a row's end are moved, for pieces of p's parity: to the stage's first bytes.
+__device__ __forceinline__ int mx_piece_back(int p, int lane, int row_len) {
+  const int byte = mx_piece_byte(p, lane), held = row_len & 127;
+  return held && byte >= held ? byte : 0;
+}
+// From stage k to `to`; off: byte offset of the lane's row plus mx_piece_byte.  (Without a branch: one around the last stage's copies made the compiler
+// wait for weights at every step, 8192 rows of 14336 onto 4096 358 -> 391 us.)
+__device__ __forceinline__ void mx_copy_piece(__amdgpu_buffer_rsrc_t rsrc, int off, uint8_t* to, int k, int back, bool last) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)to, 16, off - (back & (last ? -1 : 0)), k * 128, 0, 0);
+}
+#endif
 
 template <bool GATED, int FMT>
 __global__ __launch_bounds__(512, 2) void mx_tiles_kernel(MxRowsView a, int M, MxPacked w, MxEpi epi, int tiles_m, int tiles_n) {
@@ -507,36 +514,31 @@ __global__ __launch_bounds__(512, 2) void mx_tiles_kernel(MxRowsView a, int M, M
     const __amdgpu_buffer_rsrc_t rsrc_a = __builtin_amdgcn_make_buffer_rsrc(a.elements + m0 * a.row_bytes, 0, (int)((rows - 1) * a.row_bytes) + row_len, RSRC_FLAGS);
     const __amdgpu_buffer_rsrc_t rsrc_s =
         __builtin_amdgcn_make_buffer_rsrc(a.scales + m0 * a.scale_bytes, 0, (int)((rows - 1) * a.scale_bytes) + (w.K / 32 + 3) / 4 * 4, RSRC_FLAGS);
-    const int nbw = nb0 < w.NB ? nb0 : w.NB - NJ;  // (blocks past the matrix re-read valid ones; their results are dropped)
-    const int nbx = nbw + 1 < w.NB ? nbw + 1 : w.NB - 1;
-    const __amdgpu_buffer_rsrc_t rsrc_w = __builtin_amdgcn_make_buffer_rsrc(w.data + (int64_t)max(nbw, 0) * w.KT * 1024, 0, NJ * w.KT * 1024, RSRC_FLAGS);
-    const __amdgpu_buffer_rsrc_t rsrc_x = __builtin_amdgcn_make_buffer_rsrc(w.scales + (int64_t)max(nbw, 0) * w.KQ * 64, 0, NJ * w.KQ * 256, RSRC_FLAGS);
-    // copy instruction jj of a wave and stage: rows (wave * MI + jj) * 8 .. + 7, lane -> row lane / 8 of them, stored piece lane % 8
-    int aoff[MI];
+    // blocks past the matrix are out of the descriptors' range: nothing is fetched for them, and their results are dropped
+    // (readfirstlane: the compiler takes their number for a lane's own, and rebuilt the descriptors at every load: 7% of the kernel's time)
+    const int held_w = __builtin_amdgcn_readfirstlane(max(0, min(NJ, w.NB - nb0))), nbw = held_w > 0 ? nb0 : 0;
+    const __amdgpu_buffer_rsrc_t rsrc_w = __builtin_amdgcn_make_buffer_rsrc(w.data + (int64_t)nbw * w.KT * 1024, 0, held_w * w.KT * 1024, RSRC_FLAGS);
+    const __amdgpu_buffer_rsrc_t rsrc_x = __builtin_amdgcn_make_buffer_rsrc(w.scales + (int64_t)nbw * w.KQ * 64, 0, held_w * w.KQ * 256, RSRC_FLAGS);
+    const int back[2] = {mx_piece_back(0, lane, row_len), mx_piece_back(1, lane, row_len)};
+    int aoff[MI];  // (a wave copies pieces wave * MI .. wave * MI + MI - 1)
 #pragma unroll
-    for (int jj = 0; jj < MI; ++jj) aoff[jj] = mx_row_offset((wave * MI + jj) * 8 + (lane >> 3), rows, a.row_bytes);
-    const int akc = ((lane & 7) ^ (lane >> 4)) * 16;  // byte of the row's 128 in instruction 0 and 2; in 1 and 3 its bit 6 is turned
+    for (int jj = 0; jj < MI; ++jj)
+      aoff[jj] = mx_row_offset((wave * MI + jj) * 8 + (lane >> 3), rows, a.row_bytes) + mx_piece_byte(jj, lane);
     // scales: dword d of row r is stored at d * 256 + r; instruction `wave` of 4 (MXFP8: twice) or 8 covers 64 rows of one d
-    const int srow = (wave & 3) * 64 + lane, sd = SD == 2 ? wave >> 2 : 0;
-    const int soff = mx_row_offset(srow, rows, a.scale_bytes);
-    const int last_dword = (w.K / 32 - 1) / 4;
+    const int sd = SD == 2 ? wave >> 2 : 0;
+    const int soff = mx_row_offset((wave & 3) * 64 + lane, rows, a.scale_bytes) + sd * 4;
     int woff[NJ], xoff[NJ];
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
-      const int nb = (j == 0 ? max(nbw, 0) : nbx) - max(nbw, 0);
-      woff[j] = nb * w.KT * 1024 + lane * 16;
-      xoff[j] = nb * w.KQ * 256 + lane * 4;
+      woff[j] = j * w.KT * 1024 + lane * 16;
+      xoff[j] = j * w.KQ * 256 + lane * 4;
     }
     auto issue_a = [&](uint8_t* As, uint32_t* Ss, int kt) {
       const int k = kt < NS ? kt : NS - 1;  // past the end: a copy nobody reads, so that the wait counts stay uniform
 #pragma unroll
-      for (int jj = 0; jj < MI; ++jj) {
-        const int at = k * 128 + (akc ^ (jj & 1) * 64);
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc_a, (__attribute__((address_space(3))) void*)(As + (wave * MI + jj) * 1024), 16,
-                                                 aoff[jj] + (at < row_len ? at : 0), 0, 0, 0);
-      }
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc_s, (__attribute__((address_space(3))) void*)(Ss + sd * MX_TM + (wave & 3) * 64), 4,
-                                               soff + min(k * SD + sd, last_dword) * 4, 0, 0, 0);
+      for (int jj = 0; jj < MI; ++jj) mx_copy_piece(rsrc_a, aoff[jj], As + (wave * MI + jj) * 1024, k, back[jj & 1], k == NS - 1);
+      // (behind the last scale of a row: others, or out of range; masked when they are read)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc_s, (__attribute__((address_space(3))) void*)(Ss + sd * MX_TM + (wave & 3) * 64), 4, soff, k * SD * 4, 0, 0);
     };
     u32x4 wreg[SK][NJ];
     int xreg[2][NJ];  // the weights' scales, a dword for four steps
@@ -716,39 +718,37 @@ __global__ __launch_bounds__(512, 2) void mx_stream_kernel(MxRowsView a, int M, 
     const __amdgpu_buffer_rsrc_t rsrc_s =
         __builtin_amdgcn_make_buffer_rsrc(a.scales + m0 * a.scale_bytes, 0, (int)((rows - 1) * a.scale_bytes) + (w.K / 32 + 3) / 4 * 4, RSRC_FLAGS);
     // blocks past the matrix are out of the descriptors' range: nothing is fetched for them, and their results are dropped
-    const int held = max(0, min(NJ, w.NB - nb0)), nbw = held > 0 ? nb0 : 0;
+    const int held = __builtin_amdgcn_readfirstlane(max(0, min(NJ, w.NB - nb0))), nbw = held > 0 ? nb0 : 0;  // (see mx_tiles_kernel)
     const __amdgpu_buffer_rsrc_t rsrc_w = __builtin_amdgcn_make_buffer_rsrc(w.data + (int64_t)nbw * w.KT * 1024, 0, held * w.KT * 1024, RSRC_FLAGS);
     const __amdgpu_buffer_rsrc_t rsrc_x = __builtin_amdgcn_make_buffer_rsrc(w.scales + (int64_t)nbw * w.KQ * 64, 0, held * w.KQ * 256, RSRC_FLAGS);
-    // copy piece p covers eight rows of a slice's tile: lane -> row lane / 8 of them, stored piece lane % 8; past the last one a wave copies
-    // that one again (same bytes)
-    int aoff[CP], akc[CP], afirst[CP], soff[SP], sdw[SP];
+    // a wave copies pieces wave * CP .. of the slices' tiles one after the other; past the last one it copies that one again (same bytes)
+    const int back[2] = {mx_piece_back(0, lane, row_len), mx_piece_back(1, lane, row_len)};
+    int aoff[CP], afirst[CP], soff[SP], sfirst[SP];
 #pragma unroll
     for (int jj = 0; jj < CP; ++jj) {
-      const int p = min(wave * CP + jj, PIECES - 1), sl = p / (BM / 8), r = p % (BM / 8) * 8 + (lane >> 3);
-      akc[jj] = ((lane & 7) ^ ((r >> 1) & 7)) * 16;
-      aoff[jj] = mx_row_offset(r, rows, a.row_bytes);
-      afirst[jj] = first_of(sl);
+      const int p = min(wave * CP + jj, PIECES - 1);
+      aoff[jj] = mx_row_offset(p % (BM / 8) * 8 + (lane >> 3), rows, a.row_bytes) + mx_piece_byte(p, lane);
+      afirst[jj] = first_of(p / (BM / 8));
     }
-    // scales: dword d of row r of slice sl is stored at (sl * SD + d) * BM + r
+    // scales: dword d of row r of slice sl is stored at (sl * SD + d) * BM + r; where 64 of them are of two slices, the later one's lanes are
+    // further on by what lies between the slices
 #pragma unroll
     for (int jj = 0; jj < SP; ++jj) {
       const int p = min(wave * SP + jj, SPIECES - 1), at = min(p * 64 + lane, KS * BM * SD - 1), sl = at / (BM * SD), d = at / BM % SD, r = at % BM;
-      soff[jj] = mx_row_offset(r, rows, a.scale_bytes);
-      sdw[jj] = first_of(sl) * SD + d;
+      sfirst[jj] = first_of(p * 64 / (BM * SD));
+      soff[jj] = mx_row_offset(r, rows, a.scale_bytes) + ((first_of(sl) - sfirst[jj]) * SD + d) * 4;
     }
-    const int last_dword = (w.K / 32 - 1) / 4;
     auto issue_a = [&](int st, int kt) {
       const int k = min(kt, nmax - 1);  // past the end: a copy nobody reads, so that the wait counts stay uniform
 #pragma unroll
       for (int jj = 0; jj < CP; ++jj) {
-        const int p = min(wave * CP + jj, PIECES - 1);
-        const int at = min(afirst[jj] + k, NS - 1) * 128 + akc[jj];
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc_a, (__attribute__((address_space(3))) void*)(&As[st][p * 1024]), 16, aoff[jj] + (at < row_len ? at : 0), 0, 0, 0);
+        const int p = min(wave * CP + jj, PIECES - 1), at = afirst[jj] + k;  // (at NS, in a shorter slice: never read)
+        mx_copy_piece(rsrc_a, aoff[jj], &As[st][p * 1024], at, back[p & 1], at == NS - 1);
       }
 #pragma unroll
-      for (int jj = 0; jj < SP; ++jj) {
+      for (int jj = 0; jj < SP; ++jj) {  // (behind the last scale of a row: others, or out of range; masked when they are read)
         const int p = min(wave * SP + jj, SPIECES - 1);
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc_s, (__attribute__((address_space(3))) void*)(&Ss[st][p * 64]), 4, soff[jj] + min(sdw[jj] + k * SD, last_dword) * 4, 0, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc_s, (__attribute__((address_space(3))) void*)(&Ss[st][p * 64]), 4, soff[jj], (sfirst[jj] + k) * SD * 4, 0, 0);
       }
     };
     u32x4 wreg[SW][SK][NJ];
