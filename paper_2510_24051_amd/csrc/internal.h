@@ -471,6 +471,8 @@ struct MxEpi {
   const float* resid;
   int H;
 };
-// ws: MX_WS_FLOATS of workspace
-hipError_t launch_mx_product(const MxRowsView& a, int format, int M, const MxPacked& w, const MxEpi& epi, float* ws, int n_cus, hipStream_t s);
+// ws: MX_WS_FLOATS of workspace.  deferred (optional): where the product is split over workgroups its sums are not joined, and *deferred receives
+// the number of copies [split][M][NB * 32] left in ws for a following kernel to add (0: the epilogue has run).
+hipError_t launch_mx_product(const MxRowsView& a, int format, int M, const MxPacked& w, const MxEpi& epi, float* ws, int n_cus, hipStream_t s,
+                             int* deferred = nullptr);
 void mx_product_plan(int M, const MxPacked& w, bool gated, int format, int n_cus, int64_t out[5]);  // see pie_mx_product_plan

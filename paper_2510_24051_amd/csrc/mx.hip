@@ -105,6 +105,39 @@ __device__ __forceinline__ void store8(const RowsView& r, int64_t row, int c, fl
   if (to != nullptr) *reinterpret_cast<u32x4_at2*>(reinterpret_cast<uint16_t*>(to) + at) = k.u;
 }
 
+// Eight columns of split sums, `stride` apart, in their order; up to four splits' loads go out together.
+__device__ __forceinline__ void add_splits(const float* p, int64_t stride, int splits, float (&v)[8]) {
+  f32x4 a = {0.f, 0.f, 0.f, 0.f}, b = a;
+  int i = 0;
+  for (; i + 4 <= splits; i += 4) {
+    f32x4 x[4], y[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      x[u] = *reinterpret_cast<const f32x4*>(p + (i + u) * stride);
+      y[u] = *reinterpret_cast<const f32x4*>(p + (i + u) * stride + 4);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) { a += x[u]; b += y[u]; }
+  }
+  if (i + 2 <= splits) {
+    f32x4 x[2], y[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      x[u] = *reinterpret_cast<const f32x4*>(p + (i + u) * stride);
+      y[u] = *reinterpret_cast<const f32x4*>(p + (i + u) * stride + 4);
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) { a += x[u]; b += y[u]; }
+    i += 2;
+  }
+  if (i < splits) {
+    a += *reinterpret_cast<const f32x4*>(p + i * stride);
+    b += *reinterpret_cast<const f32x4*>(p + i * stride + 4);
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) { v[e] = a[e]; v[4 + e] = b[e]; }
+}
+
 // ---------------------------------------------------------------------------------------------
 // Quantisation and its inverse: eight values a lane and piece, MX_PIECES pieces of a thread requested together.  Bound by HBM: 28672 x 4096 of bf16 to
 // 4 bits 59 us (5.1 TB/s), with one piece a thread and 64-bit divisions 75; 64 x 4096 to 8 bits 3.3 us, a launch.
@@ -251,14 +284,10 @@ __global__ __launch_bounds__(THREADS) void mx_norm_kernel(MxNormArgs a, double i
       for (int e = 0; e < 8; ++e) v[e] += d[e];
     }
     if constexpr (SUMS) {  // partial sums of the product before, in their order, then what they are added to
-      f32x4 p = {0.f, 0.f, 0.f, 0.f}, q = p;
-      const float* at = a.part + row * a.part_stride + c;
-      for (int i = 0; i < a.splits; ++i) {
-        p += *reinterpret_cast<const f32x4*>(at + i * a.split_stride);
-        q += *reinterpret_cast<const f32x4*>(at + i * a.split_stride + 4);
-      }
+      float d[8];
+      add_splits(a.part + row * a.part_stride + c, a.split_stride, a.splits, d);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) { v[e] += p[e]; v[4 + e] += q[e]; }
+      for (int e = 0; e < 8; ++e) v[e] += d[e];
     }
     store8(a.h, row, c, v);
 #pragma unroll
@@ -964,16 +993,7 @@ __global__ __launch_bounds__(256) void mx_join_kernel(const float* __restrict__ 
   const int64_t m = at / cols8;
   const int c = (int)(at % cols8) * 8;
   const int64_t stride = (int64_t)M * NB * 32;
-  auto total = [&](int n, float (&v)[8]) {
-    f32x4 a = {0.f, 0.f, 0.f, 0.f}, b = a;
-    const float* p = part + m * NB * 32 + n;
-    for (int k = 0; k < splits; ++k) {
-      a += *reinterpret_cast<const f32x4*>(p + k * stride);
-      b += *reinterpret_cast<const f32x4*>(p + k * stride + 4);
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
-  };
+  auto total = [&](int n, float (&v)[8]) { add_splits(part + m * NB * 32 + n, stride, splits, v); };
   float v[8];
   if constexpr (GATED) {
     const int n = (c >> 5) * 64 + (c & 31);
@@ -1040,7 +1060,7 @@ static double mx_tiles_us(int M, int NB, int NS, bool fp8, int n_cus) {
   auto round = [&](int64_t busy) { return 4.1 + stages * (1.07 + 0.42 * (double)busy / n_cus); };
   return 0.9 + (double)(wgs / n_cus) * round(n_cus) + (wgs % n_cus ? round(wgs % n_cus) : 0.0);
 }
-static double mx_stream_us(const MxForm& f, int splits, int M, int NB, int64_t K, int NS, bool fp8, int n_cus) {
+static double mx_stream_us(const MxForm& f, int splits, int M, int NB, int64_t K, int NS, bool fp8, bool defer, int n_cus) {
   const int WN = 8 / f.ks, tiles_m = (M + 32 * f.mb - 1) / (32 * f.mb), tiles_n = (NB + f.nj * WN - 1) / (f.nj * WN);
   const int64_t wgs = (int64_t)tiles_m * tiles_n * splits, rounds = (wgs + n_cus - 1) / n_cus;
   const int steps = (NS + f.ks * splits - 1) / (f.ks * splits);
@@ -1048,17 +1068,17 @@ static double mx_stream_us(const MxForm& f, int splits, int M, int NB, int64_t K
   const double stage = std::max({0.118 * f.mb * f.nj, kib / 34.0, 0.15 * f.mb}) + 0.057;
   const double t = 0.9 + (double)rounds * (4.2 + 0.08 * f.mb * f.nj + steps * stage);
   const double least = 0.9 + (double)NB * 32 * (double)K * 0.53e-6 / 3.83;  // (the weights' bytes)
-  return std::max(t, least) + (splits > 1 ? 3.3 + (double)splits * M * NB * 32 * 8e-6 / 3.5 : 0.0);
+  return std::max(t, least) + (splits > 1 ? (defer ? 0.5 : 3.3) + (double)splits * M * NB * 32 * 8e-6 / 3.5 : 0.0);
 }
 // The best of one form for all rows, and of tiles for whole rounds with another form behind them (8320 rows of 14336 onto 4096: 33 x 16 tiles
 // took 503 us, 32 x 16 and 128 rows in another form ? us).
-static MxPlan mx_plan_whole(int M, const MxPacked& w, bool gated, bool fp8, int n_cus) {
+static MxPlan mx_plan_whole(int M, const MxPacked& w, bool gated, bool fp8, bool defer, int n_cus) {
   const int row = fp8 ? w.K : w.K / 2, NS = (row + 127) / 128;
   MxPlan best{MX_TILES, 1, M, M > 128 ? mx_tiles_us(M, w.NB, NS, fp8, n_cus) : 1e30};  // (the sweep has no product of up to 128 rows for them)
   auto look = [&](const MxForm& f) {
     for (int splits = 1; splits <= 8; ++splits) {
       if (splits > 1 && ((size_t)splits * M * w.NB * 32 > MX_WS_FLOATS || f.ks * splits * 2 > NS)) break;
-      const double us = mx_stream_us(f, splits, M, w.NB, w.K, NS, fp8, n_cus);
+      const double us = mx_stream_us(f, splits, M, w.NB, w.K, NS, fp8, defer, n_cus);
       if (us < best.us) best = MxPlan{f, splits, M, us};
     }
   };
@@ -1066,24 +1086,24 @@ static MxPlan mx_plan_whole(int M, const MxPacked& w, bool gated, bool fp8, int 
   else for (const MxForm& f : MX_PLAIN) look(f);
   return best;
 }
-static MxPlan mx_plan(int M, const MxPacked& w, bool gated, bool fp8, int n_cus) {
-  MxPlan best = mx_plan_whole(M, w, gated, fp8, n_cus);
+static MxPlan mx_plan(int M, const MxPacked& w, bool gated, bool fp8, bool defer, int n_cus) {
+  MxPlan best = mx_plan_whole(M, w, gated, fp8, defer, n_cus);
   const int tiles_m = (M + MX_TM - 1) / MX_TM, NS = ((fp8 ? w.K : w.K / 2) + 127) / 128;
   for (int cut = tiles_m - 1; cut >= 1 && cut >= tiles_m - 4; --cut) {
     const int rows = cut * MX_TM;
-    const double us = mx_tiles_us(rows, w.NB, NS, fp8, n_cus) + mx_plan_whole(M - rows, w, gated, fp8, n_cus).us;
+    const double us = mx_tiles_us(rows, w.NB, NS, fp8, n_cus) + mx_plan_whole(M - rows, w, gated, fp8, false, n_cus).us;
     if (us < best.us) best = MxPlan{MX_TILES, 1, rows, us};
   }
   return best;
 }
 
 template <bool GATED, int FMT, int MB, int KS, int NJ>
-static hipError_t run_stream_form(const MxRowsView& a, int M, const MxPacked& w, const MxEpi& e, int splits, float* ws, hipStream_t s) {
+static hipError_t run_stream_form(const MxRowsView& a, int M, const MxPacked& w, const MxEpi& e, int splits, bool defer, float* ws, hipStream_t s) {
   constexpr int WN = 8 / KS;
   const int tiles_m = (M + MB * 32 - 1) / (MB * 32), tiles_n = (w.NB + NJ * WN - 1) / (NJ * WN);
   if ((int64_t)tiles_m * tiles_n > INT32_MAX) return hipErrorInvalidValue;
   mx_stream_kernel<GATED, FMT, MB, KS, NJ><<<dim3(tiles_m * tiles_n, splits), dim3(512), 0, s>>>(a, M, w, e, tiles_m, tiles_n, splits, splits > 1 ? ws : nullptr);
-  if (splits > 1) {
+  if (splits > 1 && !defer) {
     const int64_t pieces = (int64_t)M * w.NB * (GATED ? 2 : 4);
     mx_join_kernel<GATED><<<pieces_grid(pieces), dim3(256), 0, s>>>(ws, splits, M, w.NB, e);
   }
@@ -1091,7 +1111,7 @@ static hipError_t run_stream_form(const MxRowsView& a, int M, const MxPacked& w,
 }
 
 template <bool GATED, int FMT>
-static hipError_t run_product(const MxRowsView& a, int M, const MxPacked& w, const MxEpi& e, const MxPlan& p, float* ws, hipStream_t s) {
+static hipError_t run_product(const MxRowsView& a, int M, const MxPacked& w, const MxEpi& e, const MxPlan& p, bool defer, float* ws, hipStream_t s) {
   const MxForm& f = p.form;
   if (f.mb == 0) {
     const int tiles_m = (M + MX_TM - 1) / MX_TM, tiles_n = (w.NB + MX_TN / 32 - 1) / (MX_TN / 32);
@@ -1100,7 +1120,7 @@ static hipError_t run_product(const MxRowsView& a, int M, const MxPacked& w, con
     return hipGetLastError();
   }
 #define MX_FORM(MB, KS, NJ) \
-  if (f.mb == MB && f.ks == KS && f.nj == NJ) return run_stream_form<GATED, FMT, MB, KS, NJ>(a, M, w, e, p.splits, ws, s);
+  if (f.mb == MB && f.ks == KS && f.nj == NJ) return run_stream_form<GATED, FMT, MB, KS, NJ>(a, M, w, e, p.splits, defer, ws, s);
   MX_FORM(1, 4, 2) MX_FORM(2, 4, 2) MX_FORM(3, 2, 2) MX_FORM(4, 2, 2) MX_FORM(4, 4, 2)
   if constexpr (GATED) {
     MX_FORM(1, 2, 2) MX_FORM(2, 2, 2) MX_FORM(3, 4, 2)
@@ -1111,17 +1131,20 @@ static hipError_t run_product(const MxRowsView& a, int M, const MxPacked& w, con
   return hipErrorInvalidValue;
 }
 
-hipError_t launch_mx_product(const MxRowsView& a, int format, int M, const MxPacked& w, const MxEpi& e, float* ws, int n_cus, hipStream_t s) {
+hipError_t launch_mx_product(const MxRowsView& a, int format, int M, const MxPacked& w, const MxEpi& e, float* ws, int n_cus, hipStream_t s, int* deferred) {
+  if (deferred) *deferred = 0;
   if (M <= 0) return hipSuccess;
-  const bool gated = e.mode == MX_SWIGLU8 || e.mode == MX_SWIGLU4, fp8 = format == PIE_MXFP8;
+  const bool gated = e.mode == MX_SWIGLU8 || e.mode == MX_SWIGLU4, fp8 = format == PIE_MXFP8, defer = deferred != nullptr;
   MxPacked::Plan& kept = w.plan;  // (gated or not, and the number of compute units, do not change from call to call)
-  if (kept.key != 2 * M + fp8) {
-    const MxPlan q = mx_plan(M, w, gated, fp8, n_cus);
-    kept = MxPacked::Plan{2 * M + fp8, q.form.mb, q.form.ks, q.form.nj, q.splits, q.rows};
+  const int key = 4 * M + 2 * defer + fp8;
+  if (kept.key != key) {
+    const MxPlan q = mx_plan(M, w, gated, fp8, defer, n_cus);
+    kept = MxPacked::Plan{key, q.form.mb, q.form.ks, q.form.nj, q.splits, q.rows};
   }
   const MxPlan p{{kept.mb, kept.ks, kept.nj}, kept.splits, kept.rows, 0.0};
-  const hipError_t err = gated ? (fp8 ? run_product<true, PIE_MXFP8>(a, p.rows, w, e, p, ws, s) : run_product<true, PIE_MXFP4>(a, p.rows, w, e, p, ws, s))
-                               : (fp8 ? run_product<false, PIE_MXFP8>(a, p.rows, w, e, p, ws, s) : run_product<false, PIE_MXFP4>(a, p.rows, w, e, p, ws, s));
+  const hipError_t err = gated ? (fp8 ? run_product<true, PIE_MXFP8>(a, p.rows, w, e, p, defer, ws, s) : run_product<true, PIE_MXFP4>(a, p.rows, w, e, p, defer, ws, s))
+                               : (fp8 ? run_product<false, PIE_MXFP8>(a, p.rows, w, e, p, defer, ws, s) : run_product<false, PIE_MXFP4>(a, p.rows, w, e, p, defer, ws, s));
+  if (deferred && p.splits > 1) *deferred = p.splits;
   if (err != hipSuccess || p.rows == M) return err;
   MxPacked tail = w;  // (with a plan of its own)
   MxRowsView rest = a;
@@ -1136,7 +1159,7 @@ hipError_t launch_mx_product(const MxRowsView& a, int format, int M, const MxPac
 }
 
 void mx_product_plan(int M, const MxPacked& w, bool gated, int format, int n_cus, int64_t out[5]) {
-  const MxPlan p = mx_plan(M, w, gated, format == PIE_MXFP8, n_cus);
+  const MxPlan p = mx_plan(M, w, gated, format == PIE_MXFP8, false, n_cus);
   out[0] = p.form.mb ? 32 * p.form.mb : MX_TM;
   out[1] = p.form.mb ? 32 * p.form.nj * (8 / p.form.ks) : MX_TN;
   out[2] = p.form.ks;

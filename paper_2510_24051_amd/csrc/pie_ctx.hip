@@ -2289,13 +2289,13 @@ static pie_status run_layer_mx(pie_ctx* c, int32_t layer, const pie_batch* b, fl
   if (carry) *carry = 0;
   const MxActs acts = mx_acts(c);
 
-  // a layer of bf16 before may have left its down projection as partial sums on c->h
+  // the layer before may have left its down projection as sums to be added to c->h
   tm.begin(PIE_STAGE_NORM1);
   MxNormArgs n{};
   n.x = carried > 0 ? mx_view(c->h, PIE_F32, H) : x_in ? mx_view(x_in, PIE_F32, H) : mx_view(c->embeds, PIE_BF16, H);
   n.ids = x_in ? nullptr : b->in_ids;
   n.h = mx_view(carried > 0 ? x_in : nullptr, n.x.dtype, H);
-  n.part = c->splitk; n.splits = carried; n.part_stride = round_up(H, 32); n.split_stride = (int64_t)T * n.part_stride;
+  n.part = carried > 0 && c->layers[layer - 1].mx ? c->mx_ws : c->splitk; n.splits = carried; n.part_stride = round_up(H, 32); n.split_stride = (int64_t)T * n.part_stride;
   n.gain = L.g1; n.eps = m.rms_eps;
   HIP_TRY(c, launch_mx_norm(n, T, H, PIE_MXFP8, acts.rows, s));
   tm.end(PIE_STAGE_NORM1);
@@ -2312,12 +2312,21 @@ static pie_status run_layer_mx(pie_ctx* c, int32_t layer, const pie_batch* b, fl
 
   tm.begin(PIE_STAGE_OPROJ);
   HIP_TRY(c, launch_mx_quantise(mx_view(c->attn, PIE_BF16, Hq * D), T, Hq * D, PIE_MXFP8, acts.attn, s));
-  HIP_TRY(c, launch_mx_product(acts.attn, PIE_MXFP8, T, L.mo, MxEpi{MX_RESID_EMBED, c->h, H, nullptr, 0, H, c->embeds, b->in_ids, x_in, H}, c->mx_ws, c->wave_slots / 8, s));
+  int o_splits = 0;  // (the second norm adds them)
+  HIP_TRY(c, launch_mx_product(acts.attn, PIE_MXFP8, T, L.mo, MxEpi{MX_RESID_EMBED, c->h, H, nullptr, 0, H, c->embeds, b->in_ids, x_in, H}, c->mx_ws,
+                               c->wave_slots / 8, s, &o_splits));
   tm.end(PIE_STAGE_OPROJ);
 
   tm.begin(PIE_STAGE_NORM2);
   MxNormArgs n2{};
-  n2.x = mx_view(c->h, PIE_F32, H); n2.h = mx_view(nullptr, PIE_F32, H);
+  if (o_splits > 0) {
+    n2.x = x_in ? mx_view(x_in, PIE_F32, H) : mx_view(c->embeds, PIE_BF16, H);
+    n2.ids = x_in ? nullptr : b->in_ids;
+    n2.h = mx_view(c->h, PIE_F32, H);
+    n2.part = c->mx_ws; n2.splits = o_splits; n2.part_stride = round_up(H, 32); n2.split_stride = (int64_t)T * n2.part_stride;
+  } else {
+    n2.x = mx_view(c->h, PIE_F32, H); n2.h = mx_view(nullptr, PIE_F32, H);
+  }
   n2.gain = L.g2; n2.eps = m.rms_eps;
   HIP_TRY(c, launch_mx_norm(n2, T, H, PIE_MXFP8, acts.rows, s));
   tm.end(PIE_STAGE_NORM2);
@@ -2328,7 +2337,8 @@ static pie_status run_layer_mx(pie_ctx* c, int32_t layer, const pie_batch* b, fl
   tm.end(PIE_STAGE_GATEUP);
 
   tm.begin(PIE_STAGE_DOWN);
-  HIP_TRY(c, launch_mx_product(acts.act, PIE_MXFP8, T, L.mdown, MxEpi{MX_RESID_OUT, y_out, H, nullptr, 0, H, c->embeds, b->out_ids, c->h, H}, c->mx_ws, c->wave_slots / 8, s));
+  HIP_TRY(c, launch_mx_product(acts.act, PIE_MXFP8, T, L.mdown, MxEpi{MX_RESID_OUT, y_out, H, nullptr, 0, H, c->embeds, b->out_ids, c->h, H}, c->mx_ws,
+                               c->wave_slots / 8, s, carry && y_out && layer + 1 < m.n_layers && c->layers[layer + 1].mx ? carry : nullptr));
   tm.end(PIE_STAGE_DOWN);
   c->last_T = T;
   c->last_mx = true;
