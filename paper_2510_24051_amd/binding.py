@@ -701,8 +701,9 @@ class Pie:
         return MxWeight(self, h, int(n[0] if gated else n.sum()), parts[0].k, gated)
 
     def _mx_weight(self, w: MxWeight, a: MxRows, what: str) -> int:
-        if not isinstance(w, MxWeight) or w.handle is None:
-            raise ValueError(f"{what}: the weight is an MxWeight that has not been destroyed")
+        self._device()
+        if not isinstance(w, MxWeight) or w.handle is None or w.owner.ctx is None:
+            raise ValueError(f"{what}: the weight is an MxWeight that has not been destroyed, nor its context closed")
         return self._mx_rows(a, a.rows, w.k, what)
 
     def mx_product(self, a: MxRows, w: MxWeight, out: torch.Tensor):

@@ -68,6 +68,10 @@ __device__ __forceinline__ void pad_scales(uint8_t* scales, int k) {
 // Rows of plain values
 // ---------------------------------------------------------------------------------------------
 RowsView mx_view(const void* p, int dtype, int64_t stride) { return RowsView{p, stride, dtype}; }
+static RowsView rows_behind(RowsView r, int64_t rows) {
+  if (r.p) r.p = reinterpret_cast<const uint8_t*>(r.p) + rows * r.stride * (r.dtype == PIE_F32 ? 4 : 2);
+  return r;
+}
 // (Vector accesses at addresses that are aligned to the elements only are ordinary on this chip; they touch a line more now and then.)
 typedef f32x4 f32x4_at4 __attribute__((aligned(4)));
 typedef u32x4 u32x4_at2 __attribute__((aligned(2)));
@@ -258,7 +262,7 @@ hipError_t launch_mx_dequantise(const MxRowsView& a, int format, int rows, int k
 // squares are summed eight to a thread in fp32 and beyond in 64 bits, and gain over root enters as a pair of fp32.  (Root and quotient in 64 bits
 // by every wave cost more than the rest of the kernel: 8320 x 4096 of bf16 42 us; the fp32 reciprocal root and one step of Newton's method in 64
 // bits, good to 2^-44: 29 us.  Several rows to a workgroup, the next one's values requested ahead, gained nothing.  8320 x 4096 of fp32 with the
-// residual's addition, 444 MB: 80 us, 5.6 TB/s; one row 3.6 us.)
+// residual's addition, 444 MB: 77 us, 5.8 TB/s; one row 3.6 us.)
 // ---------------------------------------------------------------------------------------------
 __device__ __forceinline__ double rsqrt_f64(double m) {
   if (!(m > 1e-30 && m < 1e30)) return m == INFINITY ? 0.0 : 1.0 / sqrt(m);  // (uniform; beyond what fp32 holds well)
@@ -293,13 +297,26 @@ __global__ __launch_bounds__(THREADS) void mx_norm_kernel(MxNormArgs a, double i
 #pragma unroll
     for (int e = 0; e < 8; ++e) ss += v[e] * v[e];
   }
-  double sum = wave_sum_f64(ss);
-  if constexpr (THREADS > 64) {
-    if ((tid & 63) == 0) red[tid >> 6] = sum;
-    __syncthreads();
-    sum = 0.0;
+  auto total = [&](double part) {
+    part = wave_sum_f64(part);
+    if constexpr (THREADS > 64) {
+      if ((tid & 63) == 0) red[tid >> 6] = part;
+      __syncthreads();
+      part = 0.0;
 #pragma unroll
-    for (int w = 0; w < THREADS / 64; ++w) sum += red[w];
+      for (int w = 0; w < THREADS / 64; ++w) part += red[w];
+    }
+    return part;
+  };
+  double sum = total(ss);
+  if (!(sum > 1e-25 && sum < 1e37)) {  // (uniform) squares near the ends of what 32 bits hold, or past them; zeros, infinities and NaN
+    double wide = 0.0;
+    if (in) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) wide += (double)v[e] * (double)v[e];
+    }
+    if constexpr (THREADS > 64) __syncthreads();  // (everyone has read the first sums)
+    sum = total(wide);
   }
   const double r = rsqrt_f64(sum * inv_k + (double)a.eps);
   const float rh = (float)r, rl = rh < INFINITY ? (float)(r - (double)rh) : 0.f;
@@ -320,9 +337,22 @@ hipError_t launch_mx_norm(const MxNormArgs& a, int rows, int k, int format, cons
   if (k > 8192) return hipErrorInvalidValue;
   auto go = [&](auto threads_c) {
     constexpr int T = decltype(threads_c)::value;
-    if (a.splits > 0) mx_norm_kernel<PIE_MXFP8, T, true><<<dim3(rows), dim3(T), 0, s>>>(a, 1.0 / k, k, out);  // (a layer's)
-    else if (format == PIE_MXFP8) mx_norm_kernel<PIE_MXFP8, T, false><<<dim3(rows), dim3(T), 0, s>>>(a, 1.0 / k, k, out);
-    else mx_norm_kernel<PIE_MXFP4, T, false><<<dim3(rows), dim3(T), 0, s>>>(a, 1.0 / k, k, out);
+    if (a.splits > 0) {  // (a layer's)
+      mx_norm_kernel<PIE_MXFP8, T, true><<<dim3(rows), dim3(T), 0, s>>>(a, 1.0 / k, k, out);
+      return hipGetLastError();
+    }
+    constexpr int MOST = 1 << 21;  // rows of a launch, which may have fewer than 2^32 threads
+    MxNormArgs p = a;
+    MxRowsView o = out;
+    for (int left = rows; left > 0; left -= MOST) {
+      const dim3 grid(std::min(left, MOST));
+      if (format == PIE_MXFP8) mx_norm_kernel<PIE_MXFP8, T, false><<<grid, dim3(T), 0, s>>>(p, 1.0 / k, k, o);
+      else mx_norm_kernel<PIE_MXFP4, T, false><<<grid, dim3(T), 0, s>>>(p, 1.0 / k, k, o);
+      p.x = rows_behind(p.x, MOST); p.delta = rows_behind(p.delta, MOST); p.h = rows_behind(p.h, MOST);
+      if (p.ids) p.ids += MOST;
+      o.elements += MOST * o.row_bytes;
+      o.scales += MOST * o.scale_bytes;
+    }
     return hipGetLastError();
   };
   using std::integral_constant;
@@ -338,8 +368,8 @@ hipError_t launch_mx_norm(const MxNormArgs& a, int rows, int k, int format, cons
 // scale of its block in tile 4 q + t: one load for four steps, of which the instruction picks the byte.  What is behind the last row
 // or block is 0.
 // ---------------------------------------------------------------------------------------------
-__global__ __launch_bounds__(256) void mx_pack_kernel(MxRowsView src, int rows, int k, int first, int interleave, MxPacked w) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;  // one per (32-row block of the part, k step, lane)
+__global__ __launch_bounds__(256) void mx_pack_kernel(MxRowsView src, int rows, int k, int first, int interleave, MxPacked w, int64_t from) {
+  const int64_t i = from + (int64_t)blockIdx.x * 256 + threadIdx.x;  // one per (32-row block of the part, k step, lane)
   const int KT = w.KT;
   const int64_t total = (int64_t)((rows + 31) / 32) * KT * 64;
   if (i >= total) return;
@@ -357,8 +387,9 @@ __global__ __launch_bounds__(256) void mx_pack_kernel(MxRowsView src, int rows, 
 
 hipError_t launch_mx_pack(const MxRowsView& src, int rows, int k, int first, int interleave, const MxPacked& w, hipStream_t s) {
   const int64_t total = (int64_t)((rows + 31) / 32) * w.KT * 64;
-  if (total <= 0) return hipSuccess;
-  mx_pack_kernel<<<pieces_grid(total), dim3(256), 0, s>>>(src, rows, k, first, interleave, w);
+  constexpr int64_t MOST = 1ll << 31;  // (a launch has fewer than 2^32 threads)
+  for (int64_t from = 0; from < total; from += MOST)
+    mx_pack_kernel<<<pieces_grid(std::min(total - from, MOST)), dim3(256), 0, s>>>(src, rows, k, first, interleave, w, from);
   return hipGetLastError();
 }
 
@@ -1071,7 +1102,7 @@ static double mx_stream_us(const MxForm& f, int splits, int M, int NB, int64_t K
   return std::max(t, least) + (splits > 1 ? (defer ? 0.5 : 3.3) + (double)splits * M * NB * 32 * 8e-6 / 3.5 : 0.0);
 }
 // The best of one form for all rows, and of tiles for whole rounds with another form behind them (8320 rows of 14336 onto 4096: 33 x 16 tiles
-// took 503 us, 32 x 16 and 128 rows in another form ? us).
+// took 503 us, 32 x 16 and the last 128 rows in another form 409).
 static MxPlan mx_plan_whole(int M, const MxPacked& w, bool gated, bool fp8, bool defer, int n_cus) {
   const int row = fp8 ? w.K : w.K / 2, NS = (row + 127) / 128;
   MxPlan best{MX_TILES, 1, M, M > 128 ? mx_tiles_us(M, w.NB, NS, fp8, n_cus) : 1e30};  // (the sweep has no product of up to 128 rows for them)
@@ -1101,7 +1132,6 @@ template <bool GATED, int FMT, int MB, int KS, int NJ>
 static hipError_t run_stream_form(const MxRowsView& a, int M, const MxPacked& w, const MxEpi& e, int splits, bool defer, float* ws, hipStream_t s) {
   constexpr int WN = 8 / KS;
   const int tiles_m = (M + MB * 32 - 1) / (MB * 32), tiles_n = (w.NB + NJ * WN - 1) / (NJ * WN);
-  if ((int64_t)tiles_m * tiles_n > INT32_MAX) return hipErrorInvalidValue;
   mx_stream_kernel<GATED, FMT, MB, KS, NJ><<<dim3(tiles_m * tiles_n, splits), dim3(512), 0, s>>>(a, M, w, e, tiles_m, tiles_n, splits, splits > 1 ? ws : nullptr);
   if (splits > 1 && !defer) {
     const int64_t pieces = (int64_t)M * w.NB * (GATED ? 2 : 4);
@@ -1115,7 +1145,6 @@ static hipError_t run_product(const MxRowsView& a, int M, const MxPacked& w, con
   const MxForm& f = p.form;
   if (f.mb == 0) {
     const int tiles_m = (M + MX_TM - 1) / MX_TM, tiles_n = (w.NB + MX_TN / 32 - 1) / (MX_TN / 32);
-    if ((int64_t)tiles_m * tiles_n > INT32_MAX) return hipErrorInvalidValue;
     mx_tiles_kernel<GATED, FMT><<<dim3(tiles_m * tiles_n), dim3(512), 0, s>>>(a, M, w, e, tiles_m, tiles_n);
     return hipGetLastError();
   }
@@ -1131,10 +1160,29 @@ static hipError_t run_product(const MxRowsView& a, int M, const MxPacked& w, con
   return hipErrorInvalidValue;
 }
 
+// Rows of one launch, which has fewer than 2^32 threads: at most 2^22 tiles, were they of 32 x 32.
+static int mx_rows_at_once(const MxPacked& w) { return std::max((1 << 27) / w.NB / MX_TM * MX_TM, MX_TM); }
+
 hipError_t launch_mx_product(const MxRowsView& a, int format, int M, const MxPacked& w, const MxEpi& e, float* ws, int n_cus, hipStream_t s, int* deferred) {
   if (deferred) *deferred = 0;
   if (M <= 0) return hipSuccess;
-  const bool gated = e.mode == MX_SWIGLU8 || e.mode == MX_SWIGLU4, fp8 = format == PIE_MXFP8, defer = deferred != nullptr;
+  const bool gated = e.mode == MX_SWIGLU8 || e.mode == MX_SWIGLU4, fp8 = format == PIE_MXFP8;
+  auto behind = [&](int rows, const MxPacked& weight) {  // the product of the rows from `rows` on
+    MxRowsView rest = a;
+    rest.elements += rows * a.row_bytes;
+    rest.scales += rows * a.scale_bytes;
+    MxEpi r = e;
+    if (e.out) r.out = reinterpret_cast<uint8_t*>(e.out) + rows * e.ldo * (gated ? 1 : e.mode == MX_BF16 ? 2 : 4);
+    if (e.scales) r.scales = e.scales + rows * e.lds;
+    if (e.ids) r.ids = e.ids + rows;
+    if (e.resid) r.resid = e.resid + (int64_t)rows * e.H;
+    return launch_mx_product(rest, format, M - rows, weight, r, ws, n_cus, s);
+  };
+  if (const int most = mx_rows_at_once(w); M > most) {
+    const hipError_t err = launch_mx_product(a, format, most, w, e, ws, n_cus, s);
+    return err != hipSuccess ? err : behind(most, w);
+  }
+  const bool defer = deferred != nullptr;
   MxPacked::Plan& kept = w.plan;  // (gated or not, and the number of compute units, do not change from call to call)
   const int key = 4 * M + 2 * defer + fp8;
   if (kept.key != key) {
@@ -1146,20 +1194,12 @@ hipError_t launch_mx_product(const MxRowsView& a, int format, int M, const MxPac
                                : (fp8 ? run_product<false, PIE_MXFP8>(a, p.rows, w, e, p, defer, ws, s) : run_product<false, PIE_MXFP4>(a, p.rows, w, e, p, defer, ws, s));
   if (deferred && p.splits > 1) *deferred = p.splits;
   if (err != hipSuccess || p.rows == M) return err;
-  MxPacked tail = w;  // (with a plan of its own)
-  MxRowsView rest = a;
-  rest.elements += p.rows * a.row_bytes;
-  rest.scales += p.rows * a.scale_bytes;
-  MxEpi r = e;
-  if (e.out) r.out = reinterpret_cast<uint8_t*>(e.out) + p.rows * e.ldo * (gated ? 1 : e.mode == MX_BF16 ? 2 : 4);
-  if (e.scales) r.scales = e.scales + p.rows * e.lds;
-  if (e.ids) r.ids = e.ids + p.rows;
-  if (e.resid) r.resid = e.resid + (int64_t)p.rows * e.H;
-  return launch_mx_product(rest, format, M - p.rows, tail, r, ws, n_cus, s);
+  const MxPacked tail = w;  // (with a plan of its own)
+  return behind(p.rows, tail);
 }
 
 void mx_product_plan(int M, const MxPacked& w, bool gated, int format, int n_cus, int64_t out[5]) {
-  const MxPlan p = mx_plan(M, w, gated, format == PIE_MXFP8, false, n_cus);
+  const MxPlan p = mx_plan(std::min(M, mx_rows_at_once(w)), w, gated, format == PIE_MXFP8, false, n_cus);
   out[0] = p.form.mb ? 32 * p.form.mb : MX_TM;
   out[1] = p.form.mb ? 32 * p.form.nj * (8 / p.form.ks) : MX_TN;
   out[2] = p.form.ks;

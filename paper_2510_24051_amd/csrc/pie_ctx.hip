@@ -1986,6 +1986,7 @@ extern "C" pie_status pie_mx_quantise(pie_ctx* c, const pie_rows* x, int32_t row
   if (rows == 0) return PIE_OK;
   if (pie_status st = check_rows(c, x, k, "x", who)) return st;
   if (pie_status st = check_mx_rows(c, out, k, who)) return st;
+  OnDevice on(c);
   HIP_TRY(c, launch_mx_quantise(rows_view(x), rows, k, out->format, mx_rows_view(out), c->stream));
   return PIE_OK;
 }
@@ -1996,6 +1997,7 @@ extern "C" pie_status pie_mx_dequantise(pie_ctx* c, const pie_mx_rows* a, int32_
   if (rows == 0) return PIE_OK;
   if (pie_status st = check_mx_rows(c, a, k, who)) return st;
   if (pie_status st = check_rows(c, out, k, "out", who)) return st;
+  OnDevice on(c);
   HIP_TRY(c, launch_mx_dequantise(mx_rows_view(a), a->format, rows, k, rows_view(out), c->stream));
   return PIE_OK;
 }
@@ -2019,6 +2021,7 @@ extern "C" pie_status pie_mx_norm(pie_ctx* c, const pie_rows* x, const pie_rows*
   a.x = rows_view(x); a.delta = rows_view(delta);
   a.h = h ? rows_view(h) : mx_view(nullptr, x->dtype, 0);
   a.gain = reinterpret_cast<const bf16_t*>(gain); a.eps = c->m.rms_eps;
+  OnDevice on(c);
   HIP_TRY(c, launch_mx_norm(a, rows, k, out->format, mx_rows_view(out), c->stream));
   return PIE_OK;
 }
@@ -2081,6 +2084,7 @@ static pie_status pie_mx_weight_create_impl(pie_ctx* c, const pie_mx_rows* parts
   }
   if (N > MX_MAX_ROWS) return fail(c, PIE_EUNSUPPORTED, "%s: %lld rows, at most %d", who, (long long)N, MX_MAX_ROWS);
   if (pie_status st = refuse_capture(c, who)) return st;
+  OnDevice on(c);
   c->mx_weights.reserve(c->mx_weights.size() + 1);
   if (!c->mx_ws) HIP_TRY(c, hipMalloc(reinterpret_cast<void**>(&c->mx_ws), MX_WS_FLOATS * sizeof(float)));
   pie_mx_weight* w = new pie_mx_weight();
@@ -2108,6 +2112,7 @@ extern "C" pie_status pie_mx_weight_destroy(pie_ctx* c, pie_mx_weight* weight) {
   const auto at = std::find(c->mx_weights.begin(), c->mx_weights.end(), weight);
   if (at == c->mx_weights.end()) return fail(c, PIE_EINVAL, "pie_mx_weight_destroy: not a weight of this context");
   if (pie_status st = refuse_capture(c, "pie_mx_weight_destroy")) return st;
+  OnDevice on(c);
   HIP_TRY(c, hipStreamSynchronize(c->stream));
   c->mx_weights.erase(at);
   free_packed(weight->w);
@@ -2135,6 +2140,7 @@ extern "C" pie_status pie_mx_product(pie_ctx* c, const pie_mx_rows* a, int32_t r
   if (out->dtype == PIE_F16) return fail(c, PIE_EINVAL, "%s: out is bf16 or fp32", who);
   const bool f32 = out->dtype == PIE_F32;
   const MxEpi e{f32 ? MX_F32 : MX_BF16, out->data, out->row_stride, nullptr, 0, w.N, nullptr, nullptr, nullptr, 0};
+  OnDevice on(c);
   HIP_TRY(c, launch_mx_product(mx_rows_view(a), a->format, rows, w, e, c->mx_ws, c->wave_slots / 8, c->stream));
   return PIE_OK;
 }
@@ -2149,6 +2155,7 @@ extern "C" pie_status pie_mx_swiglu(pie_ctx* c, const pie_mx_rows* a, int32_t ro
   if (pie_status st = check_mx_rows(c, out, w.N / 2, who)) return st;
   const MxRowsView o = mx_rows_view(out);
   const MxEpi e{out->format == PIE_MXFP8 ? MX_SWIGLU8 : MX_SWIGLU4, o.elements, o.row_bytes, o.scales, o.scale_bytes, w.N / 2, nullptr, nullptr, nullptr, 0};
+  OnDevice on(c);
   HIP_TRY(c, launch_mx_product(mx_rows_view(a), a->format, rows, w, e, c->mx_ws, c->wave_slots / 8, c->stream));
   return PIE_OK;
 }
@@ -2180,6 +2187,7 @@ extern "C" pie_status pie_load_layer_mx(pie_ctx* c, int32_t layer, const void* g
     if (weights[pj].format != PIE_MXFP4) return fail(c, PIE_EINVAL, "%s: projection %d is not MXFP4", who, pj);
   }
   if (pie_status st = refuse_capture(c, who)) return st;
+  OnDevice on(c);
   if (!c->mx_act) HIP_TRY(c, hipMalloc(reinterpret_cast<void**>(&c->mx_act), mx_acts(c).bytes));
   if (!c->mx_ws) HIP_TRY(c, hipMalloc(reinterpret_cast<void**>(&c->mx_ws), MX_WS_FLOATS * sizeof(float)));
   LayerWeights& L = c->layers[layer];

@@ -27,6 +27,7 @@ size_t n_done = 0;
 struct Event { size_t upto; };
 size_t malloc_limit = ~(size_t)0, largest_malloc = 0;
 int capturing = 0, event_syncs = 0, fail_event_syncs = 0, allocations = 0;
+int current_device = 0, elsewhere = 0;  // the caller's device; launches, allocations and waits while it was not the first
 long news = 0, fail_new_at = 0;
 struct Kernel { const void* stub; const char* name; };
 std::vector<Kernel, Plain<Kernel>> kernels;
@@ -68,6 +69,8 @@ void fake_capturing(int on) { capturing = on; }
 void fake_fail_event_syncs(int n) { fail_event_syncs = n; }
 int fake_event_syncs() { return event_syncs; }
 int fake_allocations() { return allocations; }  // calls that allocate or free, device or pinned
+void fake_set_device(int d) { current_device = d; elsewhere = 0; }
+int fake_elsewhere() { return elsewhere; }
 int fake_copies_done() { return (int)done.size(); }
 size_t fake_copy_size(int i) { return done[i].size(); }
 const char* fake_copy_data(int i) { return done[i].data(); }
@@ -102,24 +105,27 @@ int hipLaunchKernel(const void* stub, dim3, dim3, void** args, size_t, void*) {
       if (watched && strstr(k.name, watched)) snprintf(line, sizeof line, "%s %d\n", k.name, *(const int*)args[watched_arg]);
       else snprintf(line, sizeof line, "%s\n", k.name);
     }
+  elsewhere += current_device != 0;
   launches.insert(launches.end(), line, line + strlen(line));
   return SUCCESS;
 }
 int hipFuncSetAttribute(const void*, int, int) { return SUCCESS; }
-int hipGetDevice(int* d) { *d = 0; return SUCCESS; }
+int hipGetDevice(int* d) { *d = current_device; return SUCCESS; }
+int hipSetDevice(int d) { current_device = d; return SUCCESS; }
 int hipDeviceGetAttribute(int* v, int, int) { *v = 256; return SUCCESS; }
 const char* hipGetErrorString(int) { return "an error of the stand-in runtime"; }
 int hipGetLastError() { return SUCCESS; }
 int hipGetSymbolAddress(void** p, const void*) { static char array[1 << 24]; *p = array; return SUCCESS; }
 int hipMalloc(void** p, size_t n) {
   ++allocations;
+  elsewhere += current_device != 0;
   *p = nullptr;
   if (n > largest_malloc) largest_malloc = n;
   if (n > malloc_limit) return OUT_OF_MEMORY;
   *p = malloc(n ? n : 1);
   return *p ? SUCCESS : OUT_OF_MEMORY;
 }
-int hipFree(void* p) { ++allocations; drain(pending.size()); free(p); return SUCCESS; }  // (waits for the device)
+int hipFree(void* p) { ++allocations; elsewhere += current_device != 0; drain(pending.size()); free(p); return SUCCESS; }  // (waits for the device)
 int hipHostMalloc(void** p, size_t n, unsigned) { ++allocations; *p = malloc(n); return *p ? SUCCESS : OUT_OF_MEMORY; }
 int hipHostFree(void* p) { ++allocations; drain(pending.size()); free(p); return SUCCESS; }
 int hipMemcpyAsync(void* d, const void* s, size_t n, int, void*) { pending.push_back(Copy{d, s, n}); return SUCCESS; }
@@ -127,6 +133,7 @@ int hipMemcpy2DAsync(void*, size_t, const void*, size_t, size_t, size_t, int, vo
 int hipMemsetAsync(void*, int, size_t, void*) { return SUCCESS; }
 int hipStreamSynchronize(void*) {
   if (capturing) return CAPTURE_UNSUPPORTED;
+  elsewhere += current_device != 0;
   drain(pending.size());
   return SUCCESS;
 }

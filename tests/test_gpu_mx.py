@@ -183,6 +183,98 @@ def test_norm_of_zeros_and_nans(ctx):
     assert (b[3] == 119 - 1).all() or (b[3] == 119).all()
 
 
+def test_norm_of_squares_that_32_bits_do_not_hold():
+    """From 2^-70 (with an epsilon below their squares) to 2^120, alone and beside ordinary rows: the root is of the 64-bit mean, and may be a denormal
+    of 32 bits, off by 2^-22 of it."""
+    from paper_2510_24051_amd import Pie
+    from types import SimpleNamespace
+    m = W.model_tiny()
+    own = Pie(SimpleNamespace(**{**{f: getattr(m, f) for f in ("hidden", "n_q_heads", "n_kv_heads", "head_dim", "mlp_dim", "vocab", "page_size", "rope_theta")},
+                                 "rms_eps": 1e-44}), 8, 8, max_batch_tokens=8, max_batch_requests=8)
+    for k in (64, 544, 4096):
+        gen = torch.Generator(device="cuda").manual_seed(k)
+        powers = torch.tensor([-70, -66, -60, -40, 0, 40, 62, 64, 70, 100, 120], device="cuda")
+        x = torch.randn((len(powers), k), generator=gen, device="cuda").clamp(-4, 4) * torch.exp2(powers.float())[:, None]
+        gain = torch.randn(k, generator=gen, device="cuda").bfloat16()
+        r = rows_of("mxfp8", len(powers), k)
+        own.mx_norm(x, gain, r)
+        eps = float(np.float32(1e-44))
+        check_computed(r, mx.norm(x.double().cpu().numpy(), gain.double().cpu().numpy(), eps), NORM_REL, f"norm of {k}")
+
+
+# ---- past 32 bits ----------------------------------------------------------------------------------
+@pytest.fixture
+def large():
+    yield
+    torch.cuda.empty_cache()
+
+
+def test_quantise_past_32_bits(ctx, large):
+    """2^34 values: more than 2^31 pieces of eight, and bytes past 2^32 on both sides."""
+    from paper_2510_24051_amd import MxRows
+    k, n, times = 1 << 20, 1025, 16
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    part = torch.randn((n, k), generator=gen, dtype=torch.bfloat16, device="cuda")
+    want = MxRows.empty(n, k, "mxfp8")
+    ctx.mx_quantise(part, want)
+    x = torch.empty((n * times, k), dtype=torch.bfloat16, device="cuda")
+    for i in range(times):
+        x[i * n:(i + 1) * n] = part
+    r = MxRows.empty(n * times, k, "mxfp8")
+    assert n * times * k // 8 >= 1 << 31
+    ctx.mx_quantise(x, r)
+    back = torch.empty_like(part)
+    ctx.mx_dequantise(want, back)
+    x.zero_()
+    ctx.mx_dequantise(r, x)
+    for i in range(times):
+        rows = slice(i * n, (i + 1) * n)
+        assert torch.equal(r.elements[rows], want.elements) and torch.equal(r.scales[rows], want.scales) and torch.equal(x[rows], back)
+
+
+def test_norm_of_the_most_rows(ctx, large):
+    """2^24 rows of 256 threads each: 2^32."""
+    from paper_2510_24051_amd import MxRows
+    rows, k = 1 << 24, 544
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    part = torch.randn((1 << 14, k), generator=gen, device="cuda").bfloat16()
+    gain = torch.randn(k, generator=gen, device="cuda").bfloat16()
+    want = MxRows.empty(1 << 14, k, "mxfp8")
+    ctx.mx_norm(part, gain, want)
+    x = part.repeat(1 << 10, 1)
+    r = MxRows.empty(rows, k, "mxfp8")
+    h = torch.zeros_like(x)
+    ctx.mx_norm(x, gain, r, h=h)
+    assert torch.equal(h, x)
+    assert (r.elements.view(1 << 10, 1 << 14, k) == want.elements).all() and (r.scales.view(1 << 10, 1 << 14, -1) == want.scales).all()
+
+
+@pytest.mark.parametrize("gated", [False, True])
+def test_product_past_32_bits(ctx, large, gated):
+    """More rows than one launch takes, and results past 2^32 bytes; every row is computed as it is among few others (whole numbers: exactly)."""
+    from paper_2510_24051_amd import MxRows
+    n, k, period = 4096, 32, 1536
+    m = (1 << 20) + 300
+    rng = np.random.default_rng(7)
+    w, _ = weight_of(ctx, [rng.choice(WEIGHTS, size=(n, k)) for _ in range(1 + gated)], gated=gated)
+    a, _ = device_rows(rng.choice([0.0, 1, -1, 2], size=(period, k)), "mxfp4")
+    times = (m + period - 1) // period
+    many = MxRows("mxfp4", a.elements.repeat(times, 1)[:m].contiguous(), a.scales.repeat(times, 1)[:m].contiguous())
+    if gated:
+        want, out = MxRows.empty(period, n, "mxfp8"), MxRows.empty(m, n, "mxfp8")
+        ctx.mx_swiglu(a, w, want)
+        ctx.mx_swiglu(many, w, out)
+        pairs = [(out.elements, want.elements), (out.scales, want.scales)]
+    else:
+        want, out = (torch.empty((r, n), dtype=torch.bfloat16, device="cuda") for r in (period, m))
+        ctx.mx_product(a, w, want)
+        ctx.mx_product(many, w, out)
+        pairs = [(out, want)]
+    for got, one in pairs:
+        whole = m // period * period
+        assert (got[:whole].view(-1, *one.shape) == one).all() and torch.equal(got[whole:], one[:m - whole])
+
+
 # ---- products ------------------------------------------------------------------------------------
 def weight_of(ctx, parts, gated=False, gap=0, pad=0):
     """(handle, values [n, k]) of matrices given as values."""
@@ -243,6 +335,19 @@ def test_product_of_whole_numbers(ctx, form, m, k, n):
         bad = got != wanted
         assert not bad.any(), f"{bad.sum()} of {bad.size} differ, first at {np.argwhere(bad)[0]}: {got[bad][0]} not {wanted[bad][0]}"
         assert (c[:, n:] == -9.0).all() and (flat[:offset] == -9.0).all(), "bytes outside the result were written"
+
+
+@pytest.mark.parametrize("form", ["mxfp8", "mxfp4"])
+@pytest.mark.parametrize("m,k,n", [(2, 1 << 20, 33), (33, (1 << 18) + 32, 40), (300, 1 << 17, 64)])
+def test_product_of_long_rows(ctx, form, m, k, n):
+    """As above; most weights are 0, so that sums stay exact."""
+    rng = np.random.default_rng(m + k)
+    a, av = whole_rows(rng, m, k, ACTS, form, 1)
+    w, wv = whole_rows(rng, n, k, WEIGHTS + [0] * 150, "mxfp4", 0)
+    assert (np.abs(av) @ np.abs(wv).T).max() < 2 ** 22
+    out = torch.empty((m, n), device="cuda")
+    ctx.mx_product(a, ctx.mx_weight([w]), out)
+    assert np.array_equal(out.double().cpu().numpy(), mx.product(av, wv))
 
 
 @pytest.mark.parametrize("gated,form,m,k,n", FORM_SIZES)
@@ -373,9 +478,12 @@ def test_strided_views_streams_and_capture(ctx):
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph, stream=ctx.stream):
         chain(ctx)
-    for s in (1, 0, 2, 1):
+    elsewhere, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.graph(elsewhere, stream=side):  # (the context's stream joins the capture)
+        chain(ctx)
+    for s, g in ((1, graph), (0, elsewhere), (2, graph), (2, elsewhere), (1, elsewhere), (1, graph)):
         fresh(s)
-        graph.replay()
+        g.replay()
         torch.cuda.synchronize()
         for got, w in zip((h, y, act.elements, act.scales), want[s]):
             assert torch.equal(got, w)
@@ -409,6 +517,13 @@ def test_no_rows_and_what_the_binding_refuses(ctx):
         with pytest.raises(PieError) as e:
             call()
         assert e.value.status == -1
+    other = type(ctx)(W.model_tiny(), 8, 8, max_batch_tokens=8, max_batch_requests=8)
+    foreign, _ = weight_of(other, [np.ones((40, 64))])
+    with pytest.raises(PieError) as e:
+        ctx.mx_product(a, foreign, out)
+    assert e.value.status == -1
+    other.close()
     w.destroy()
-    with pytest.raises(ValueError):
-        ctx.mx_product(a, w, out)
+    for gone in (foreign, w):
+        with pytest.raises(ValueError):
+            ctx.mx_product(a, gone, out)

@@ -228,7 +228,27 @@ def adapters(c):
     pb.destroy(), other.destroy()
 
 
-CASES = {f.__name__: f for f in (rows_refused, norm_refused, weights_refused, no_memory, layers, adapters)}
+def another_device(c):
+    """Calls made while the caller's current device is another: everything happens on the context's, and the caller's is current again."""
+    ctx = c.context(m=MODEL)
+    m = Calls(c, ctx)
+    now = C.c_int(-1)
+    c.fake.fake_set_device(1)
+    st, w = m.weight(64)
+    st2, g = m.weight(32, 32, gated=1)
+    assert (st, st2) == (0, 0)
+    assert m.call("pie_mx_quantise", m.rows(), 3, 64, m.mx()) == 0 and m.call("pie_mx_dequantise", m.mx(), 3, 64, m.rows()) == 0
+    assert m.call("pie_mx_norm", m.rows(), None, A, 3, 64, None, m.mx()) == 0
+    assert m.call("pie_mx_product", m.mx(), 3, w, m.rows()) == 0 and m.call("pie_mx_swiglu", m.mx(), 3, g, m.mx()) == 0
+    parts = (m.b.MxRowsC * 7)(*[m.b.MxRowsC(FP4, A, 2048, A, 128)] * 7)
+    assert m.call("pie_load_layer_mx", 0, A, A, parts) == 0
+    assert m.call("pie_mx_weight_destroy", w) == 0
+    assert c.fake.fake_elsewhere() == 0 and len(c.launches()) > 7
+    assert c.fake.hipGetDevice(C.byref(now)) == 0 and now.value == 1
+    c.fake.fake_set_device(0)
+
+
+CASES = {f.__name__: f for f in (another_device, rows_refused, norm_refused, weights_refused, no_memory, layers, adapters)}
 
 if __name__ == "__main__":
     CASES[sys.argv[2]](Child(sys.argv[1]))
