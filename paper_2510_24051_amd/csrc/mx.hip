@@ -89,7 +89,9 @@ __device__ __forceinline__ void load8(const RowsView& r, int64_t row, int c, flo
 #pragma unroll
   for (int e = 0; e < 8; ++e) v[e] = r.dtype == PIE_BF16 ? bf16_bits_to_f32(k.s[e]) : (float)__builtin_bit_cast(_Float16, k.s[e]);
 }
-// Rounds v to r's type (v becomes what is stored) and, where r.p is given, stores it.
+// Rounds v to r's type (v becomes what is stored) and, where r.p is given, stores it.  ONCE: past the caches, for results that they would not hold;
+// 16-bit ones only, of which a lane stores 16 bytes in a row.
+template <bool ONCE = false>
 __device__ __forceinline__ void store8(const RowsView& r, int64_t row, int c, float (&v)[8]) {
   const int64_t at = row * r.stride + c;
   void* to = const_cast<void*>(r.p);
@@ -106,7 +108,10 @@ __device__ __forceinline__ void store8(const RowsView& r, int64_t row, int c, fl
     k.s[e] = r.dtype == PIE_BF16 ? __builtin_bit_cast(uint16_t, f32_to_bf16(v[e])) : __builtin_bit_cast(uint16_t, (_Float16)v[e]);
     v[e] = r.dtype == PIE_BF16 ? bf16_bits_to_f32(k.s[e]) : (float)__builtin_bit_cast(_Float16, k.s[e]);
   }
-  if (to != nullptr) *reinterpret_cast<u32x4_at2*>(reinterpret_cast<uint16_t*>(to) + at) = k.u;
+  if (to == nullptr) return;
+  u32x4_at2* p = reinterpret_cast<u32x4_at2*>(reinterpret_cast<uint16_t*>(to) + at);
+  if (ONCE) __builtin_nontemporal_store((u32x4_at2)k.u, p);
+  else *p = k.u;
 }
 
 // Eight columns of split sums, `stride` apart, in their order; up to four splits' loads go out together.
@@ -144,7 +149,9 @@ __device__ __forceinline__ void add_splits(const float* p, int64_t stride, int s
 
 // ---------------------------------------------------------------------------------------------
 // Quantisation and its inverse: eight values a lane and piece, MX_PIECES pieces of a thread requested together.  Bound by HBM: 28672 x 4096 of bf16 to
-// 4 bits 59 us (5.1 TB/s), with one piece a thread and 64-bit divisions 75; 64 x 4096 to 8 bits 3.3 us, a launch.
+// 4 bits 60 us (5.0 TB/s), with one piece a thread and 64-bit divisions 75; 64 x 4096 to 8 bits 3.3 us, a launch.  Back from 4 bits 53 us, 60 where
+// its stores went through the caches; both in turn, where these are then written back underneath the other, 103 and 120.  (Loads past the caches gain
+// nothing here, and lose what they hold of a smaller input: 8320 x 4096 to 8 bits 21.4 us, 23.4.  fp32's halves of 32 bytes stored past them: 28.5, 52.)
 // ---------------------------------------------------------------------------------------------
 constexpr int MX_PIECES = 4;
 // Row and column of piece i of rows of k values; SMALL: pieces fit 32 bits, where a division is a few instructions.
@@ -217,7 +224,7 @@ __global__ __launch_bounds__(256) void mx_dequantise_kernel(MxRowsView a, int fm
         v[i] = (n & 8 ? -f : f) * scale;
       }
     }
-    store8(out, row[j], c[j], v);
+    store8<(P > 1)>(out, row[j], c[j], v);
   }
 }
 
