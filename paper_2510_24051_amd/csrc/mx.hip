@@ -525,10 +525,13 @@ __device__ __forceinline__ void mx_plain_epilogue(const MxEpi& e, const f32x16& 
 // ---------------------------------------------------------------------------------------------
 // Tiles of 256 tokens x 256 weight rows: many rows, bound by the matrix cores.
 // Eight waves, two along the tokens and four along the weight rows, of 4 x 2 accumulator tiles each.  Activations go to LDS by direct copies, 128 bytes of
-// a row (SK steps of 64) and their scales a stage, three stages; weights go from memory to registers, each set refilled for the next
+// a row (SK steps of 64) a stage, four stages, and every fourth stage the scales of four; weights go from memory to registers, each set refilled for the next
 // stage right behind the instructions that used it (as in gemm_large_async_kernel, whose order of requests, waits and barriers this is).
 // The 16-byte pieces of a row are swizzled by its number: piece c of row r is stored at c ^ (r / 2 % 8), so that the 32 rows of an operand
 // read from all banks.  What is behind K is read from the row's first piece instead: its weights are 0, and so is its scale.
+// A row's scales of a stage are 4 or 8 bytes of a cache line of their own, and the lines that a copy touches are what it costs: with the scales copied every
+// stage 8192 rows of 14336 onto 4096 took 370 us, with four stages' at a time 342, on zeros (no power limit) 295 and 267; SwiGLU of 4096 onto
+// 2 x 14336 755 and 698.  (Weights requested up to two stages earlier, copies two or three stages ahead: the same.)
 // ---------------------------------------------------------------------------------------------
 constexpr int MX_TM = 256, MX_TN = 256;
 
@@ -557,8 +560,8 @@ __global__ __launch_bounds__(512, 2) void mx_tiles_kernel(MxRowsView a, int M, M
   constexpr int SD = SK / 2;                    // dwords of scales a row and stage
   constexpr int MI = 4, NJ = 2;
   [[maybe_unused]] constexpr int UI = 2, UN = MI / UI;  // accumulator blocks whose operands are read at a time, and such units of a step
-  [[maybe_unused]] __shared__ __align__(16) uint8_t As0[MX_TM * 128], As1[MX_TM * 128], As2[MX_TM * 128];
-  [[maybe_unused]] __shared__ uint32_t Ss0[MX_TM * SD], Ss1[MX_TM * SD], Ss2[MX_TM * SD];
+  [[maybe_unused]] __shared__ __align__(16) uint8_t As0[MX_TM * 128], As1[MX_TM * 128], As2[MX_TM * 128], As3[MX_TM * 128];
+  [[maybe_unused]] __shared__ __align__(16) uint8_t Ss[2][MX_TM * SD * 16], spare[SD == 1 ? 1024 : 16];  // scales of four stages: 16 SD bytes a row
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   [[maybe_unused]] const int h = lane >> 5;
   const int wm = wave >> 2, wn = wave & 3;
@@ -591,21 +594,23 @@ __global__ __launch_bounds__(512, 2) void mx_tiles_kernel(MxRowsView a, int M, M
 #pragma unroll
     for (int jj = 0; jj < MI; ++jj)
       aoff[jj] = mx_row_offset((wave * MI + jj) * 8 + (lane >> 3), rows, a.row_bytes) + mx_piece_byte(jj, lane);
-    // scales: dword d of row r is stored at d * 256 + r; instruction `wave` of 4 (MXFP8: twice) or 8 covers 64 rows of one d
-    const int sd = SD == 2 ? wave >> 2 : 0;
-    const int soff = mx_row_offset((wave & 3) * 64 + lane, rows, a.scale_bytes) + sd * 4;
+    // scales: SD lanes a row; with MXFP8 four waves copy them all, the others nothing, elsewhere (so that all count the same copies)
+    const bool scopies = wave < 4 * SD;
+    const int soff = scopies ? mx_row_offset(wave * (64 / SD) + lane / SD, rows, a.scale_bytes) + lane % SD * 16 : 0x7f000000;
     int woff[NJ], xoff[NJ];
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
       woff[j] = j * w.KT * 1024 + lane * 16;
       xoff[j] = j * w.KQ * 256 + lane * 4;
     }
-    auto issue_a = [&](uint8_t* As, uint32_t* Ss, int kt) {
+    // scales of stages 4 g .. 4 g + 3 (behind the last one of a row: others, or out of range, which is checked by the dword; masked when they are read)
+    auto issue_s = [&](int g) {
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc_s, (__attribute__((address_space(3))) void*)(scopies ? &Ss[g & 1][wave * 1024] : spare), 16, soff, g * SD * 16, 0, 0);
+    };
+    auto issue_a = [&](uint8_t* As, int kt) {
       const int k = kt < NS ? kt : NS - 1;  // past the end: a copy nobody reads, so that the wait counts stay uniform
 #pragma unroll
       for (int jj = 0; jj < MI; ++jj) mx_copy_piece(rsrc_a, aoff[jj], As + (wave * MI + jj) * 1024, k, back[jj & 1], k == NS - 1);
-      // (behind the last scale of a row: others, or out of range; masked when they are read)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc_s, (__attribute__((address_space(3))) void*)(Ss + sd * MX_TM + (wave & 3) * 64), 4, soff, k * SD * 4, 0, 0);
     };
     u32x4 wreg[SK][NJ];
     int xreg[2][NJ];  // the weights' scales, a dword for four steps
@@ -634,19 +639,23 @@ __global__ __launch_bounds__(512, 2) void mx_tiles_kernel(MxRowsView a, int M, M
         }
       }
     };
-    auto load_s = [&](const uint32_t* Ss, int kt, int (&sc)[SD][MI]) {
+    auto load_s = [&](int kt, int at, int (&sc)[SD][MI]) {  // (at: kt % 4)
+      const uint32_t* group = reinterpret_cast<const uint32_t*>(&Ss[(kt >> 2) & 1][(wm * (MX_TM / 2) + (lane & 31)) * SD * 16]);
 #pragma unroll
       for (int d = 0; d < SD; ++d) {
         const int left = w.K / 32 - (kt * SD + d) * 4;  // blocks from here on
         const uint32_t mask = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1;
 #pragma unroll
-        for (int i = 0; i < MI; ++i) sc[d][i] = (int)((Ss[d * MX_TM + wm * (MX_TM / 2) + i * 32 + (lane & 31)] & mask) >> (8 * h));
+        for (int i = 0; i < MI; ++i) sc[d][i] = (int)((group[i * 32 * SD * 4 + at * SD + d] & mask) >> (8 * h));
       }
     };
     i32x8 af[2][UI];
     int sc[SD][MI];
-    auto step = [&](const uint8_t* Acur, const uint8_t* Anext, const uint32_t* Snext, uint8_t* Afill, uint32_t* Sfill, int kt) {
-      issue_a(Afill, Sfill, kt + 2);
+    auto step = [&](auto at_c, const uint8_t* Acur, const uint8_t* Anext, uint8_t* Afill, int kt) {
+      constexpr int AT = decltype(at_c)::value;  // kt % 4
+      constexpr int GROUP = (AT + 3) % 4 == 0;
+      if constexpr (GROUP) issue_s((kt + 3) >> 2);
+      issue_a(Afill, kt + 3);
       __builtin_amdgcn_sched_barrier(0);
       load_x(kt + 1, 1);
       const int shift = FMT == PIE_MXFP8 ? (kt & 1) * 16 : 0;
@@ -660,11 +669,11 @@ __global__ __launch_bounds__(512, 2) void mx_tiles_kernel(MxRowsView a, int M, M
           load_a(Acur, u + 1, af[(u + 1) & 1]);
         } else {
           PIE_S_WAIT_LGKMCNT0();  // this wave's last reads of Acur have returned
-          // newer than the copies of stage kt + 1: the copies, scales and weights requested in this step
-          PIE_S_WAIT_VMCNT(MI + 1 + NJ + (SK - 1) * NJ);
+          // all but the copies, scales and weights requested in this stage: the copies of stage kt + 1 are older, and of the others all is needed by now
+          PIE_S_WAIT_VMCNT(GROUP + MI + NJ + (SK - 1) * NJ);
           wg_barrier();
           load_a(Anext, 0, af[(u + 1) & 1]);
-          load_s(Snext, kt + 1, nsc);
+          load_s(kt + 1, (AT + 1) % 4, nsc);
         }
 #pragma unroll
         for (int i = 0; i < UI; ++i)
@@ -691,26 +700,29 @@ __global__ __launch_bounds__(512, 2) void mx_tiles_kernel(MxRowsView a, int M, M
 #pragma unroll
         for (int i = 0; i < MI; ++i) sc[d][i] = nsc[d][i];
     };
-    issue_a(As0, Ss0, 0);
-    issue_a(As1, Ss1, 1);
+    issue_s(0);
+    issue_a(As0, 0);
+    issue_a(As1, 1);
+    issue_a(As2, 2);
     __builtin_amdgcn_sched_barrier(0);
     load_x(0, 0);
 #pragma unroll
     for (int s = 0; s < SK; ++s) load_w(0, s);
     __builtin_amdgcn_sched_barrier(0);
-    PIE_S_WAIT_VMCNT(MI + 1 + NJ + SK * NJ);  // the first stage has arrived
+    PIE_S_WAIT_VMCNT(2 * MI + NJ + SK * NJ);  // the first stage has arrived
     wg_barrier();
     load_a(As0, 0, af[0]);
-    load_s(Ss0, 0, sc);
-    int kt = 0;
-    for (; kt + 3 <= NS; kt += 3) {
-      step(As0, As1, Ss1, As2, Ss2, kt);
-      step(As1, As2, Ss2, As0, Ss0, kt + 1);
-      step(As2, As0, Ss0, As1, Ss1, kt + 2);
-    }
-    if (kt < NS) {
-      step(As0, As1, Ss1, As2, Ss2, kt);
-      if (kt + 1 < NS) step(As1, As2, Ss2, As0, Ss0, kt + 1);
+    load_s(0, 0, sc);
+    using std::integral_constant;
+    for (int kt = 0;;) {
+      step(integral_constant<int, 0>{}, As0, As1, As3, kt);
+      if (++kt >= NS) break;
+      step(integral_constant<int, 1>{}, As1, As2, As0, kt);
+      if (++kt >= NS) break;
+      step(integral_constant<int, 2>{}, As2, As3, As1, kt);
+      if (++kt >= NS) break;
+      step(integral_constant<int, 3>{}, As3, As0, As2, kt);
+      if (++kt >= NS) break;
     }
     PIE_S_WAIT_VMCNT(0);  // the surplus copies of the last steps land before the workgroup gives up its LDS
 #endif
