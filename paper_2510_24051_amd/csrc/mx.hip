@@ -744,7 +744,9 @@ __global__ __launch_bounds__(512, 2) void mx_tiles_kernel(MxRowsView a, int M, M
 // Few rows: bound by the stream of weights, or by its latency.
 // Eight waves; KS slices of the contraction (or parts of them, where the product is split over workgroups as well) with 8 / KS waves each, a
 // wave with MB x NJ accumulator tiles: 32 weight rows (SwiGLU: a gate and an up block) by 32 MB tokens.  Each wave keeps SW stages of
-// weights in registers (stages as in mx_tiles_kernel, requested non-temporally), each slice SA stages of its activations in LDS.  A slice's
+// weights in registers (stages as in mx_tiles_kernel, requested non-temporally), each slice SA stages of its activations in LDS, and the
+// scales of SG stages at a time (one stage's by themselves cost as much as its activations: 333 rows of 4 bits, 4096 onto 6144, 14.8 us for 13.4; 64 of 8
+// bits 10.8 for 9.8; SwiGLU of 64, 4096 onto 2 x 14336, 20.8 for 19.9).  A slice's
 // stages are NS p / parts .. NS (p + 1) / parts; all walk as many as the longest has, the others doing nothing in the last.  The slices'
 // sums meet in LDS, in their order.
 // ---------------------------------------------------------------------------------------------
@@ -764,12 +766,14 @@ __global__ __launch_bounds__(512, 2) void mx_stream_kernel(MxRowsView a, int M, 
   [[maybe_unused]] constexpr int SK = FMT == PIE_MXFP8 ? 2 : 4, SD = SK / 2;
   constexpr int SA = mx_stages_a(MB, KS);
   [[maybe_unused]] constexpr int SW = mx_stages_w(FMT, NJ, MB, KS), RS = mx_stages_round(SA, SW);  // (RS: steps of a round of both rings)
+  [[maybe_unused]] constexpr int SG = SA == 4 ? 4 : SA == 3 && SD == 1 ? 3 : 1, SL = SG == 1 ? 4 : 16, SROW = SD * SL;  // stages whose scales are copied together (as LDS has room), a lane's bytes of a copy, a row's
+  [[maybe_unused]] constexpr int SB = SG == 1 ? SA : 2;  // such groups held
   [[maybe_unused]] constexpr int UI = MB == 4 ? 2 : MB, UN = MB / UI;                              // (see mx_tiles_kernel)
   constexpr int STAGE = KS * BM * 128;
   [[maybe_unused]] constexpr int PIECES = STAGE / 1024, CP = (PIECES + 7) / 8;              // copy instructions of a stage, and of a wave
-  [[maybe_unused]] constexpr int SPIECES = (KS * BM * SD + 63) / 64, SP = (SPIECES + 7) / 8;  // the same of the scales
+  [[maybe_unused]] constexpr int SPIECES = (KS * BM * SD + 63) / 64, SP = (SPIECES + 7) / 8;  // the same of SG stages' scales
   __shared__ __align__(16) uint8_t As[SA][STAGE];
-  [[maybe_unused]] __shared__ uint32_t Ss[SA][SPIECES * 64];
+  [[maybe_unused]] __shared__ __align__(16) uint8_t Ss[SB][SPIECES * 64 * SL];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   [[maybe_unused]] const int h = lane >> 5;
   const int ks = wave / WN;
@@ -802,32 +806,33 @@ __global__ __launch_bounds__(512, 2) void mx_stream_kernel(MxRowsView a, int M, 
     const __amdgpu_buffer_rsrc_t rsrc_x = __builtin_amdgcn_make_buffer_rsrc(w.scales + (int64_t)nbw * w.KQ * 64, 0, held * w.KQ * 256, RSRC_FLAGS);
     // a wave copies pieces wave * CP .. of the slices' tiles one after the other; past the last one it copies that one again (same bytes)
     const int back[2] = {mx_piece_back(0, lane, row_len), mx_piece_back(1, lane, row_len)};
-    int aoff[CP], afirst[CP], soff[SP], sfirst[SP];
+    int aoff[CP], afirst[CP], soff[SP];
 #pragma unroll
     for (int jj = 0; jj < CP; ++jj) {
       const int p = min(wave * CP + jj, PIECES - 1);
       aoff[jj] = mx_row_offset(p % (BM / 8) * 8 + (lane >> 3), rows, a.row_bytes) + mx_piece_byte(p, lane);
       afirst[jj] = first_of(p / (BM / 8));
     }
-    // scales: dword d of row r of slice sl is stored at (sl * SD + d) * BM + r; where 64 of them are of two slices, the later one's lanes are
-    // further on by what lies between the slices
+    // scales: SG stages of a row lie together, SD lanes' copies; row r of slice sl is row sl * BM + r of them
 #pragma unroll
     for (int jj = 0; jj < SP; ++jj) {
-      const int p = min(wave * SP + jj, SPIECES - 1), at = min(p * 64 + lane, KS * BM * SD - 1), sl = at / (BM * SD), d = at / BM % SD, r = at % BM;
-      sfirst[jj] = first_of(p * 64 / (BM * SD));
-      soff[jj] = mx_row_offset(r, rows, a.scale_bytes) + ((first_of(sl) - sfirst[jj]) * SD + d) * 4;
+      const int p = min(wave * SP + jj, SPIECES - 1), at = min(p * 64 + lane, KS * BM * SD - 1), sl = at / (BM * SD), r = at / SD % BM;
+      soff[jj] = mx_row_offset(r, rows, a.scale_bytes) + first_of(sl) * SD * 4 + at % SD * SL;
     }
+    // stages g SG .. of every slice (behind the last scale of a row: others, or out of range, by the dword; masked when they are read)
+    auto issue_s = [&](int g, int buf) {
+#pragma unroll
+      for (int jj = 0; jj < SP; ++jj) {
+        const int p = min(wave * SP + jj, SPIECES - 1);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc_s, (__attribute__((address_space(3))) void*)(&Ss[buf][p * 64 * SL]), SL, soff[jj], g * SG * SD * 4, 0, 0);
+      }
+    };
     auto issue_a = [&](int st, int kt) {
       const int k = min(kt, nmax - 1);  // past the end: a copy nobody reads, so that the wait counts stay uniform
 #pragma unroll
       for (int jj = 0; jj < CP; ++jj) {
         const int p = min(wave * CP + jj, PIECES - 1), at = afirst[jj] + k;  // (at NS, in a shorter slice: never read)
         mx_copy_piece(rsrc_a, aoff[jj], &As[st][p * 1024], at, back[p & 1], at == NS - 1);
-      }
-#pragma unroll
-      for (int jj = 0; jj < SP; ++jj) {  // (behind the last scale of a row: others, or out of range; masked when they are read)
-        const int p = min(wave * SP + jj, SPIECES - 1);
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc_s, (__attribute__((address_space(3))) void*)(&Ss[st][p * 64]), 4, soff[jj], (sfirst[jj] + k) * SD * 4, 0, 0);
       }
     };
     u32x4 wreg[SW][SK][NJ];
@@ -858,13 +863,14 @@ __global__ __launch_bounds__(512, 2) void mx_stream_kernel(MxRowsView a, int M, 
         }
       }
     };
-    auto load_s = [&](int st, int kt, int (&sc)[SD][MB]) {
+    auto load_s = [&](int at, int kt, int buf, int (&sc)[SD][MB]) {  // (at: kt % SG)
+      const uint32_t* group = reinterpret_cast<const uint32_t*>(&Ss[buf][(ks * BM + (lane & 31)) * SROW]) + at * SD;
 #pragma unroll
       for (int d = 0; d < SD; ++d) {
         const int left = w.K / 32 - ((first + kt) * SD + d) * 4;  // blocks from here on
         const uint32_t mask = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1;
 #pragma unroll
-        for (int i = 0; i < MB; ++i) sc[d][i] = (int)((Ss[st][(ks * SD + d) * BM + i * 32 + (lane & 31)] & mask) >> (8 * h));
+        for (int i = 0; i < MB; ++i) sc[d][i] = (int)((group[i * 32 * SROW / 4 + d] & mask) >> (8 * h));
       }
     };
     i32x8 af[2][UI];
@@ -875,6 +881,7 @@ __global__ __launch_bounds__(512, 2) void mx_stream_kernel(MxRowsView a, int M, 
       constexpr int SLOT = decltype(slot_c)::value % SW, AT = decltype(slot_c)::value, CUR = AT % SA, NEXT = (AT + 1) % SA, FILL = (AT + SA - 1) % SA;
       constexpr bool TAIL = decltype(tail_c)::value;
       issue_a(FILL, kt + SA - 1);
+      if constexpr ((AT + SA - 1) % SG == 0) issue_s((kt + SA - 1) / SG, SG == 1 ? FILL : (kt + SA - 1) / SG % SB);  // (behind them: in front 28 us for 26, SwiGLU of 128 rows)
       __builtin_amdgcn_sched_barrier(0);
       const int shift = FMT == PIE_MXFP8 ? ((first + kt) & 1) * 16 : 0;
       int xs[NJ], nsc[SD][MB];
@@ -889,11 +896,13 @@ __global__ __launch_bounds__(512, 2) void mx_stream_kernel(MxRowsView a, int M, 
           load_a(CUR, u + 1, af[(u + 1) & 1]);
         } else {
           PIE_S_WAIT_LGKMCNT0();  // this wave's last reads of the stage have returned
-          if constexpr (TAIL) PIE_S_WAIT_VMCNT((SA - 2) * (CP + SP));
-          else PIE_S_WAIT_VMCNT((SA - 2) * (CP + SP) + (SW < SA - 2 ? SW : SA - 2) * (SK + 1) * NJ + SK * NJ);  // (the prologue has SW steps' weights)
+          // newer than the copies of stage kt + 1: those of stages kt + 2 .. kt + SA - 1, the scales that went out with them, and weights
+          constexpr int COPIES = (SA - 2) * CP + ((SA > 2 && (AT + 2) % SG == 0) + (SA > 3 && (AT + 3) % SG == 0)) * SP;
+          if constexpr (TAIL) PIE_S_WAIT_VMCNT(COPIES);
+          else PIE_S_WAIT_VMCNT(COPIES + (SW < SA - 2 ? SW : SA - 2) * (SK + 1) * NJ + SK * NJ);  // (the prologue has SW steps' weights)
           wg_barrier();
           load_a(NEXT, 0, af[(u + 1) & 1]);
-          load_s(NEXT, kt + 1, nsc);
+          load_s((AT + 1) % SG, kt + 1, SG == 1 ? NEXT : (kt + 1) / SG % SB, nsc);
         }
         __builtin_amdgcn_sched_barrier(0);
         if (kt < n) {  // (uniform; a slice that is one stage shorter than the longest)
@@ -922,7 +931,9 @@ __global__ __launch_bounds__(512, 2) void mx_stream_kernel(MxRowsView a, int M, 
 #pragma unroll
         for (int i = 0; i < MB; ++i) sc[d][i] = nsc[d][i];
     };
-    // Prologue: copies of stages 0 .. SA - 2 first, then the weights of SW steps.
+    // Prologue: the first scales, copies of stages 0 .. SA - 2, then the weights of SW steps.
+#pragma unroll
+    for (int g = 0; g * SG <= SA - 2; ++g) issue_s(g, g);
 #pragma unroll
     for (int j = 0; j < SA - 1; ++j) issue_a(j, j);
     __builtin_amdgcn_sched_barrier(0);
@@ -933,11 +944,11 @@ __global__ __launch_bounds__(512, 2) void mx_stream_kernel(MxRowsView a, int M, 
       for (int s = 0; s < SK; ++s) load_w(j, j, s);
       __builtin_amdgcn_sched_barrier(0);
     }
-    constexpr int NEWER = (SA - 2) * (CP + SP) + SW * (SK + 1) * NJ;
+    constexpr int NEWER = (SA - 2) * CP + SW * (SK + 1) * NJ;
     PIE_S_WAIT_VMCNT(NEWER < 63 ? NEWER : 63);  // the first stage has arrived
     wg_barrier();
     load_a(0, 0, af[0]);
-    load_s(0, 0, sc);
+    load_s(0, 0, 0, sc);
     int kt = 0;
     using std::integral_constant;
     // a round, or its first `left` steps, which request no weights
@@ -952,7 +963,7 @@ __global__ __launch_bounds__(512, 2) void mx_stream_kernel(MxRowsView a, int M, 
       one(integral_constant<int, 0>{}); one(integral_constant<int, 1>{}); one(integral_constant<int, 2>{}); one(integral_constant<int, 3>{});
       one(integral_constant<int, 4>{}); one(integral_constant<int, 5>{}); one(integral_constant<int, 6>{}); one(integral_constant<int, 7>{});
     };
-    static_assert(RS <= 8 && RS >= SW, "a round is written out");
+    static_assert(RS <= 8 && RS >= SW && RS % SG == 0, "a round is written out");
     for (; kt + SW < nmax; kt += RS) round(std::false_type{}, RS);  // (steps past the last do nothing)
     round(std::true_type{}, nmax - kt);
     PIE_S_WAIT_VMCNT(0);  // the surplus copies of the last steps land before the stages are used for anything else
