@@ -1114,7 +1114,8 @@ static constexpr MxForm MX_GATED[] = {{1, 2, 2}, {1, 4, 2}, {2, 2, 2}, {2, 4, 2}
 // accumulator tile of a wave), of what it fetches (34 bytes a nanosecond) and of its reads of LDS.  The form that this picks takes 1.9% more
 // time than the best of the sweep on average, 14% at most (333 rows of 4096 onto 4096: 17.5 us, 15.4).  Examples, best and next form:
 // 28672 x 4096 gated at 1 row (1, 4) 17.2, tiles 43; at 64 rows (2, 4) 20.7, (1, 2) 22.5; at 333 (3, 2) 53.5, tiles 55; at 1400 tiles 161, (4, 2) 184.
-// 4096 x 14336 at 64 rows (1, 4, 2) in 4 splits 19.4, (1, 8, 1) whole 20.3; at 900 rows (4, 4, 2) 74, tiles 150.
+// 4096 x 14336 at 64 rows (1, 4, 2) in 4 splits 19.4, (1, 8, 1) whole 20.3; at 900 rows (4, 4, 2) 74, tiles 150.  (With scales copied several stages
+// at a time, since the sweep, tiles and most forms are 5 to 9% faster; the estimate compares them as before.)
 static double mx_tiles_us(int M, int NB, int NS, bool fp8, int n_cus) {
   const int64_t wgs = (int64_t)((M + MX_TM - 1) / MX_TM) * ((NB + MX_TN / 32 - 1) / (MX_TN / 32));
   const double stages = NS * (fp8 ? 1.0 : 1.56);
@@ -1132,7 +1133,7 @@ static double mx_stream_us(const MxForm& f, int splits, int M, int NB, int64_t K
   return std::max(t, least) + (splits > 1 ? (defer ? 0.5 : 3.3) + (double)splits * M * NB * 32 * 8e-6 / 3.5 : 0.0);
 }
 // The best of one form for all rows, and of tiles for whole rounds with another form behind them (8320 rows of 14336 onto 4096: 33 x 16 tiles
-// took 503 us, 32 x 16 and the last 128 rows in another form 409).
+// took 503 us, 32 x 16 and the last 128 rows in another form 409, and 362 since scales are copied four stages at a time).
 static MxPlan mx_plan_whole(int M, const MxPacked& w, bool gated, bool fp8, bool defer, int n_cus) {
   const int row = fp8 ? w.K : w.K / 2, NS = (row + 127) / 128;
   MxPlan best{MX_TILES, 1, M, M > 128 ? mx_tiles_us(M, w.NB, NS, fp8, n_cus) : 1e30};  // (the sweep has no product of up to 128 rows for them)
