@@ -518,9 +518,14 @@ __device__ __forceinline__ void mx_plain_epilogue(const MxEpi& e, const f32x16& 
 // ---------------------------------------------------------------------------------------------
 // Products.  D[weight row][token] = W x A^T on v_mfma_scale_f32_32x32x64_f8f6f4: a lane of the weight operand has 32 elements of one block; a
 // lane of an MXFP8 operand has bytes [16 h, 16 h + 16) and [32 + 16 h, 48 + 16 h) of its row's 64, and in either case the scale of block
-// h of its row.  With an MXFP8 operand the instruction aligns each eight neighbouring products to the largest and drops what is below
-// 2^-13 of its power of two: 1.5e-5 of a sum's size on rows whose channels differ in size as a model's do, and nothing that 8 bits of activations, 4
-// of weights or bf16 results would show; the way around it, bf16 operands, has half of the rate.  Sums are fp32.
+// h of its row.  Sums are fp32, and whole in between: the instruction adds eight neighbouring products aligned to the largest sum of two operands'
+// exponents, E, and drops what is below 2^(E - 13) (found with all pairs of elements, and eight at a time at random).  Products of two E2M1 elements are multiples of 2^-2
+// with E at most 4 and lose nothing.  Those of E4M3 with E2M1 are multiples of 2^-10 with E up to 10, so MXFP8 rows are multiplied in two parts: elements of at
+// least 2, multiples of 2^-2, whose products are multiples of 2^-3 = 2^(10 - 13), and the smaller ones, whose products have E at most 2.  Each sum of eight is
+// then exact, and is added to the fp32 sum.  That costs a second instruction: 8192 rows of 14336 onto 4096 take 600 us, with one 350, at sums that are 1.5e-5 of their
+// size off where channels differ as a model's do; the parts themselves take 5 to 10% of it.  (bf16 operands have the rate of two such instructions.)
+// Up to 16 rows have their parts side by side instead, as columns c and 16 + c of one instruction, added behind the contraction: SwiGLU of one row, 4096 onto
+// 2 x 14336, 18.2 us for 19.1, 16 rows of 14336 onto 4096 14.9 for 15.4.
 // ---------------------------------------------------------------------------------------------
 // ---------------------------------------------------------------------------------------------
 // Tiles of 256 tokens x 256 weight rows: many rows, bound by the matrix cores.
@@ -538,6 +543,46 @@ constexpr int MX_TM = 256, MX_TN = 256;
 // Byte offset of a tile's row for its copies.  Rows past the matrix are out of the descriptor's range: nothing is fetched for them, and
 // what their lanes compute is not stored.
 __device__ __forceinline__ int mx_row_offset(int r, int rows, int64_t stride) { return r < rows ? (int)(r * stride) : 0x7f000000; }
+#if __HIP_DEVICE_COMPILE__
+// One step of a stage: step S takes byte S of the weights' scales, and byte 0 or 2 of the rows'.
+template <int FMT, int S>
+__device__ __forceinline__ f32x16 mx_mfma(const i32x8& w, const i32x8& a, const f32x16& c, int ws, int as) {
+  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w, a, c, 4, FMT == PIE_MXFP8 ? 0 : 4, S, ws, S % 2 * 2, as);
+}
+// Ones in the bytes of E4M3 codes whose value is at least 2 (bit 6).
+__device__ __forceinline__ uint32_t mx_large(uint32_t codes) { return __builtin_amdgcn_perm(codes << 1, codes << 9, 0x0B090A08u); }
+// acc[first + i][j] += weights j times rows i of a unit, step s of a stage (known at compile time: the bytes of the scales are part of the instruction).
+// flip: with PAIRS, ones in the lanes that have the smaller elements' turn.
+template <int FMT, bool PAIRS, int UI, int NJ, int MI, int SD>
+__device__ __forceinline__ void mx_multiply(f32x16 (&acc)[MI][NJ], const u32x4 (&w)[NJ], const i32x8 (&a)[UI], int first, int s, const int (&xs)[NJ], const int (&sc)[SD][MI],
+                                            uint32_t flip) {
+  constexpr int PARTS = FMT == PIE_MXFP8 && !PAIRS ? 2 : 1;
+#pragma unroll
+  for (int i = 0; i < UI; ++i) {
+    i32x8 part[2] = {a[i], a[i]};
+    if constexpr (FMT == PIE_MXFP8) {
+#pragma unroll
+      for (int d = 0; d < 8; ++d) {
+        const uint32_t u = (uint32_t)a[i][d], large = mx_large(u);
+        part[0][d] = (int)(u & (PAIRS ? large ^ flip : large));
+        part[1][d] = (int)(u & ~large);
+      }
+    }
+#pragma unroll
+    for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        const i32x8 wo = {(int)w[j][0], (int)w[j][1], (int)w[j][2], (int)w[j][3], 0, 0, 0, 0};
+        f32x16& c = acc[first + i][j];
+        const int as = sc[s / 2][first + i];
+        if (s == 0) c = mx_mfma<FMT, 0>(wo, part[p], c, xs[j], as);
+        if (s == 1) c = mx_mfma<FMT, 1>(wo, part[p], c, xs[j], as);
+        if (s == 2) c = mx_mfma<FMT, 2>(wo, part[p], c, xs[j], as);
+        if (s == 3) c = mx_mfma<FMT, 3>(wo, part[p], c, xs[j], as);
+      }
+  }
+}
+#endif
 #if __HIP_DEVICE_COMPILE__
 // Copy piece p of a tile of rows: 1 KiB, rows 8 p .. 8 p + 7, lane -> row lane / 8 of them, stored piece lane % 8.  Byte of its row's 128 that a
 // lane brings:
@@ -675,21 +720,7 @@ __global__ __launch_bounds__(512, 2) void mx_tiles_kernel(MxRowsView a, int M, M
           load_a(Anext, 0, af[(u + 1) & 1]);
           load_s(kt + 1, (AT + 1) % 4, nsc);
         }
-#pragma unroll
-        for (int i = 0; i < UI; ++i)
-#pragma unroll
-          for (int j = 0; j < NJ; ++j) {
-            const u32x4 e = wreg[s][j];
-            const i32x8 wo = {(int)e[0], (int)e[1], (int)e[2], (int)e[3], 0, 0, 0, 0};
-            const int ii = u % UN * UI + i;
-            constexpr int F = FMT == PIE_MXFP8 ? 0 : 4;
-            switch (s) {  // (the byte of the scales is part of the instruction)
-              case 0: acc[ii][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wo, af[u & 1][i], acc[ii][j], 4, F, 0, xs[j], 0, sc[0][ii]); break;
-              case 1: acc[ii][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wo, af[u & 1][i], acc[ii][j], 4, F, 1, xs[j], 2, sc[0][ii]); break;
-              case 2: acc[ii][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wo, af[u & 1][i], acc[ii][j], 4, F, 2, xs[j], 0, sc[SD - 1][ii]); break;
-              case 3: acc[ii][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wo, af[u & 1][i], acc[ii][j], 4, F, 3, xs[j], 2, sc[SD - 1][ii]); break;
-            }
-          }
+        mx_multiply<FMT, false>(acc, wreg[s], af[u & 1], u % UN * UI, s, xs, sc, 0);
         if (u % UN == UN - 1) load_w(kt + 1, s);
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -759,16 +790,17 @@ constexpr int mx_stages_w(int fmt, int nj, int mb, int ks) {
 }
 constexpr int mx_stages_round(int sa, int sw) { return sw % sa == 0 ? sw : sa % sw == 0 ? sa : sa * sw; }
 
-template <bool GATED, int FMT, int MB, int KS, int NJ>
+template <bool GATED, int FMT, int MB, int KS, int NJ, bool PAIRS>
 __global__ __launch_bounds__(512, 2) void mx_stream_kernel(MxRowsView a, int M, MxPacked w, MxEpi epi, int tiles_m, int tiles_n, int splits, float* part) {
   static_assert(!GATED || NJ == 2, "a gate and an up block");
+  static_assert(!PAIRS || (MB == 1 && FMT == PIE_MXFP8), "two lanes' columns to a row");
   constexpr int WN = 8 / KS, BM = 32 * MB;
   [[maybe_unused]] constexpr int SK = FMT == PIE_MXFP8 ? 2 : 4, SD = SK / 2;
   constexpr int SA = mx_stages_a(MB, KS);
   [[maybe_unused]] constexpr int SW = mx_stages_w(FMT, NJ, MB, KS), RS = mx_stages_round(SA, SW);  // (RS: steps of a round of both rings)
   [[maybe_unused]] constexpr int SG = SA == 4 ? 4 : SA == 3 && SD == 1 ? 3 : 1, SL = SG == 1 ? 4 : 16, SROW = SD * SL;  // stages whose scales are copied together (as LDS has room), a lane's bytes of a copy, a row's
   [[maybe_unused]] constexpr int SB = SG == 1 ? SA : 2;  // such groups held
-  [[maybe_unused]] constexpr int UI = MB == 4 ? 2 : MB, UN = MB / UI;                              // (see mx_tiles_kernel)
+  [[maybe_unused]] constexpr int UI = FMT == PIE_MXFP8 && MB > 2 ? 1 : MB == 4 ? 2 : MB, UN = MB / UI;  // (see mx_tiles_kernel; three blocks at a time do not fit the registers beside their halves)
   constexpr int STAGE = KS * BM * 128;
   [[maybe_unused]] constexpr int PIECES = STAGE / 1024, CP = (PIECES + 7) / 8;              // copy instructions of a stage, and of a wave
   [[maybe_unused]] constexpr int SPIECES = (KS * BM * SD + 63) / 64, SP = (SPIECES + 7) / 8;  // the same of SG stages' scales
@@ -852,7 +884,7 @@ __global__ __launch_bounds__(512, 2) void mx_stream_kernel(MxRowsView a, int M, 
       const int s = unit / UN;
 #pragma unroll
       for (int i = 0; i < UI; ++i) {
-        const int r = (unit % UN * UI + i) * 32 + (lane & 31), z = (r >> 1) & 7;
+        const int r = (unit % UN * UI + i) * 32 + (lane & (PAIRS ? 15 : 31)), z = (r >> 1) & 7;
         const uint8_t* row = &As[st][(ks * BM + r) * 128];
         if (FMT == PIE_MXFP8) {
           const u32x4 lo = *reinterpret_cast<const u32x4*>(row + (((s * 4 + h) ^ z) << 4)), hi = *reinterpret_cast<const u32x4*>(row + (((s * 4 + 2 + h) ^ z) << 4));
@@ -864,7 +896,7 @@ __global__ __launch_bounds__(512, 2) void mx_stream_kernel(MxRowsView a, int M, 
       }
     };
     auto load_s = [&](int at, int kt, int buf, int (&sc)[SD][MB]) {  // (at: kt % SG)
-      const uint32_t* group = reinterpret_cast<const uint32_t*>(&Ss[buf][(ks * BM + (lane & 31)) * SROW]) + at * SD;
+      const uint32_t* group = reinterpret_cast<const uint32_t*>(&Ss[buf][(ks * BM + (lane & (PAIRS ? 15 : 31))) * SROW]) + at * SD;
 #pragma unroll
       for (int d = 0; d < SD; ++d) {
         const int left = w.K / 32 - ((first + kt) * SD + d) * 4;  // blocks from here on
@@ -875,6 +907,7 @@ __global__ __launch_bounds__(512, 2) void mx_stream_kernel(MxRowsView a, int M, 
     };
     i32x8 af[2][UI];
     int sc[SD][MB];
+    const uint32_t flip = PAIRS && (lane & 16) ? ~0u : 0u;
     // Step kt from weight slot `slot` and activation stage slot % SA; the order of requests and waits is that of mx_tiles_kernel, with the copies
     // SA - 1 steps ahead and the weights SW.  TAIL: no weights are requested any more, and only the copies are counted.
     auto step = [&](auto tail_c, auto slot_c, int kt) {
@@ -906,21 +939,7 @@ __global__ __launch_bounds__(512, 2) void mx_stream_kernel(MxRowsView a, int M, 
         }
         __builtin_amdgcn_sched_barrier(0);
         if (kt < n) {  // (uniform; a slice that is one stage shorter than the longest)
-#pragma unroll
-          for (int i = 0; i < UI; ++i)
-#pragma unroll
-            for (int j = 0; j < NJ; ++j) {
-              const u32x4 e = wreg[SLOT][s][j];
-              const i32x8 wo = {(int)e[0], (int)e[1], (int)e[2], (int)e[3], 0, 0, 0, 0};
-              const int ii = u % UN * UI + i;
-              constexpr int F = FMT == PIE_MXFP8 ? 0 : 4;
-              switch (s) {  // (the byte of the scales is part of the instruction)
-                case 0: acc[ii][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wo, af[u & 1][i], acc[ii][j], 4, F, 0, xs[j], 0, sc[0][ii]); break;
-                case 1: acc[ii][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wo, af[u & 1][i], acc[ii][j], 4, F, 1, xs[j], 2, sc[0][ii]); break;
-                case 2: acc[ii][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wo, af[u & 1][i], acc[ii][j], 4, F, 2, xs[j], 0, sc[SD - 1][ii]); break;
-                case 3: acc[ii][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wo, af[u & 1][i], acc[ii][j], 4, F, 3, xs[j], 2, sc[SD - 1][ii]); break;
-              }
-            }
+          mx_multiply<FMT, PAIRS>(acc, wreg[SLOT][s], af[u & 1], u % UN * UI, s, xs, sc, flip);
         }
         if constexpr (!TAIL)
           if (u % UN == UN - 1) load_w(SLOT, kt + SW, s);
@@ -973,6 +992,12 @@ __global__ __launch_bounds__(512, 2) void mx_stream_kernel(MxRowsView a, int M, 
   // slice order, and finishes it.
   auto finish = [&](int i) {
     const int64_t m = m0 + i * 32 + (lane & 31);
+    if constexpr (PAIRS) {
+#pragma unroll
+      for (int j = 0; j < NJ; ++j)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) acc[i][j][v] = sum_xor16(acc[i][j][v]);
+    }
     if (part != nullptr) {
       if (m >= M) return;
 #pragma unroll
@@ -1163,7 +1188,12 @@ template <bool GATED, int FMT, int MB, int KS, int NJ>
 static hipError_t run_stream_form(const MxRowsView& a, int M, const MxPacked& w, const MxEpi& e, int splits, bool defer, float* ws, hipStream_t s) {
   constexpr int WN = 8 / KS;
   const int tiles_m = (M + MB * 32 - 1) / (MB * 32), tiles_n = (w.NB + NJ * WN - 1) / (NJ * WN);
-  mx_stream_kernel<GATED, FMT, MB, KS, NJ><<<dim3(tiles_m * tiles_n, splits), dim3(512), 0, s>>>(a, M, w, e, tiles_m, tiles_n, splits, splits > 1 ? ws : nullptr);
+  auto go = [&](auto pairs_c) {
+    mx_stream_kernel<GATED, FMT, MB, KS, NJ, decltype(pairs_c)::value>
+        <<<dim3(tiles_m * tiles_n, splits), dim3(512), 0, s>>>(a, M, w, e, tiles_m, tiles_n, splits, splits > 1 ? ws : nullptr);
+  };
+  if (FMT == PIE_MXFP8 && MB == 1 && M <= 16) go(std::integral_constant<bool, FMT == PIE_MXFP8 && MB == 1>{});
+  else go(std::false_type{});
   if (splits > 1 && !defer) {
     const int64_t pieces = (int64_t)M * w.NB * (GATED ? 2 : 4);
     mx_join_kernel<GATED><<<pieces_grid(pieces), dim3(256), 0, s>>>(ws, splits, M, w.NB, e);
