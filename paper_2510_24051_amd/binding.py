@@ -234,7 +234,9 @@ class MxRows:
 
 
 class MxWeight:
-    """Weights of products (pie_mx_weight_create): `n` output rows (of a gated weight: the gate's), `k` inputs."""
+    """Weights of products (pie_mx_weight_create): `n` output rows (of a gated weight: the gate's), `k` inputs.  destroy() frees it; one that is only
+    dropped is freed when its context next makes a weight, synchronizes or is closed: Python drops things at any time, and freeing waits for the
+    GPU, which ends a capture on whatever stream."""
 
     def __init__(self, owner: "Pie", handle, n: int, k: int, gated: bool):
         self.owner, self.handle, self.n, self.k, self.gated = owner, handle, n, k, gated
@@ -245,10 +247,8 @@ class MxWeight:
         self.handle = None
 
     def __del__(self):
-        try:
-            self.destroy()
-        except Exception:
-            pass
+        if self.handle is not None and getattr(self.owner, "ctx", None) is not None:
+            self.owner.__dict__.setdefault("_dropped", []).append(self.handle)
 
 
 class PieBatch:
@@ -297,6 +297,8 @@ class PieBatch:
 class Pie:
     """One context = one GPU = one stream.  bf16 tensors cross this binding as uint16 numpy arrays (host)
     or torch.bfloat16 CUDA tensors (device)."""
+
+    _dropped = ()  # handles of microscaled weights that nothing names any more (a list, once there is one)
 
     def __init__(self, model, n_kv_pages: int, n_embeds: int, max_batch_tokens: int, max_batch_requests: int,
                  max_top_k: int = 256, max_dist_rows: int = 0, n_layers: int = 1, device: str = "cuda:0",
@@ -694,11 +696,16 @@ class Pie:
         if not parts or any(not isinstance(p, MxRows) or p.k != parts[0].k or p._index != self._index for p in parts):
             raise ValueError("mx_weight: MxRows of one k on the context's device")
         torch.cuda.synchronize(dev)
+        self._free_dropped()
         n = np.array([p.rows for p in parts], _INT32)
         h = C.c_void_p()
         self._check(self.lib.pie_mx_weight_create(self.ctx, (MxRowsC * len(parts))(*[p._c for p in parts]), _ptr(n), len(parts), parts[0].k, int(gated),
                                                   C.byref(h)))
         return MxWeight(self, h, int(n[0] if gated else n.sum()), parts[0].k, gated)
+
+    def _free_dropped(self):
+        while self._dropped:
+            self._check(self.lib.pie_mx_weight_destroy(self.ctx, self._dropped.pop()))
 
     def _mx_weight(self, w: MxWeight, a: MxRows, what: str) -> int:
         self._device()
@@ -719,6 +726,7 @@ class Pie:
 
     def synchronize(self):
         self._check(self.lib.pie_synchronize(self.ctx))
+        self._free_dropped()
 
     # ---- observation ----
     def read_tap(self, which: int, rows: int) -> np.ndarray:
