@@ -266,24 +266,19 @@ hipError_t launch_mx_dequantise(const MxRowsView& a, int format, int rows, int k
 // ---------------------------------------------------------------------------------------------
 // Norm: a workgroup per row, eight columns a thread (as rmsnorm_row in elementwise.hip).  Bound by HBM for many rows, by latency for few.
 // An element that rounds the other way is off by a step, an eighth of it, so the normalised values are off by their last rounding to fp32 alone:
-// squares are summed eight to a thread in fp32 and beyond in 64 bits, and gain over root enters as a pair of fp32.  (Root and quotient in 64 bits
-// by every wave cost more than the rest of the kernel: 8320 x 4096 of bf16 42 us; the fp32 reciprocal root and one step of Newton's method in 64
-// bits, good to 2^-44: 29 us.  Several rows to a workgroup, the next one's values requested ahead, gained nothing.  8320 x 4096 of fp32 with the
-// residual's addition, 444 MB: 77 us, 5.8 TB/s; one row 3.6 us.)
+// squares are summed in 64 bits, and gain over root enters as a pair of fp32.  (8320 x 4096 of bf16 30.0 us; the first eight squares of a thread in
+// fp32 29.6, and rows that its columns dominate two units off; root and quotient in 64 bits by every wave 42: the root is the fp32 reciprocal one and a
+// step of Newton's method in 64 bits, good to 2^-44.  Several rows to a workgroup, the next one's values requested ahead, gained nothing.  8320 x 4096 of
+// fp32 with the residual's addition, 444 MB: 78 us, 5.7 TB/s; one row 3.1 us.  All back to back in a graph.)
 // ---------------------------------------------------------------------------------------------
-__device__ __forceinline__ double rsqrt_f64(double m) {
-  if (!(m > 1e-30 && m < 1e30)) return m == INFINITY ? 0.0 : 1.0 / sqrt(m);  // (uniform; beyond what fp32 holds well)
-  const double r = (double)__builtin_amdgcn_rsqf((float)m);
-  return r * (1.5 - 0.5 * m * r * r);
-}
-
 template <int FMT, int THREADS, bool SUMS>
 __global__ __launch_bounds__(THREADS) void mx_norm_kernel(MxNormArgs a, double inv_k, int k, MxRowsView out) {
   __shared__ double red[THREADS / 64];
   const int64_t row = blockIdx.x;
   const int tid = threadIdx.x, c = tid * 8;
   const bool in = c < k;  // (k is a multiple of 32: the four lanes of a block go the same way)
-  float v[8], ss = 0.f;
+  float v[8];
+  double ss = 0.0;
   Pack16 g;
   if (in) {
     g.u = *reinterpret_cast<const u32x4_at2*>(reinterpret_cast<const uint16_t*>(a.gain) + c);
@@ -302,36 +297,31 @@ __global__ __launch_bounds__(THREADS) void mx_norm_kernel(MxNormArgs a, double i
     }
     store8(a.h, row, c, v);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) ss += v[e] * v[e];
+    for (int e = 0; e < 8; ++e) ss = __builtin_fma((double)v[e], (double)v[e], ss);
   }
-  auto total = [&](double part) {
-    part = wave_sum_f64(part);
-    if constexpr (THREADS > 64) {
-      if ((tid & 63) == 0) red[tid >> 6] = part;
-      __syncthreads();
-      part = 0.0;
+  ss = wave_sum_f64(ss);
+  if constexpr (THREADS > 64) {
+    if ((tid & 63) == 0) red[tid >> 6] = ss;
+    __syncthreads();
+    ss = 0.0;
 #pragma unroll
-      for (int w = 0; w < THREADS / 64; ++w) part += red[w];
-    }
-    return part;
-  };
-  double sum = total(ss);
-  if (!(sum > 1e-25 && sum < 1e37)) {  // (uniform) squares near the ends of what 32 bits hold, or past them; zeros, infinities and NaN
-    double wide = 0.0;
-    if (in) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) wide += (double)v[e] * (double)v[e];
-    }
-    if constexpr (THREADS > 64) __syncthreads();  // (everyone has read the first sums)
-    sum = total(wide);
+    for (int w = 0; w < THREADS / 64; ++w) ss += red[w];
   }
-  const double r = rsqrt_f64(sum * inv_k + (double)a.eps);
-  const float rh = (float)r, rl = rh < INFINITY ? (float)(r - (double)rh) : 0.f;
+  const double m = ss * inv_k + (double)a.eps;
   if (in) {
+    if (m > 1e-30 && m < 1e30) {  // (uniform)
+      double r = (double)__builtin_amdgcn_rsqf((float)m);
+      r = r * (1.5 - 0.5 * m * r * r);
+      const float rh = (float)r, rl = (float)(r - (double)rh);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float ge = bf16_to_f32(g.h[e]), hi = rh * ge, lo = __builtin_fmaf(rh, ge, -hi) + rl * ge;
-      v[e] = __builtin_fmaf(v[e], hi, v[e] * lo);
+      for (int e = 0; e < 8; ++e) {
+        const float ge = bf16_to_f32(g.h[e]), hi = rh * ge, lo = __builtin_fmaf(rh, ge, -hi) + rl * ge;
+        v[e] = __builtin_fmaf(v[e], hi, v[e] * lo);
+      }
+    } else {  // a root that 32 bits hold as a denormal or not at all; an infinity or a NaN in the row
+      const double r = m == INFINITY ? 0.0 : 1.0 / sqrt(m);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = (float)((double)v[e] * (r * (double)bf16_to_f32(g.h[e])));
     }
     uint8_t* scales = out.scales + row * out.scale_bytes;
     put_eight<FMT>(v, out.elements + row * out.row_bytes, scales, c);
