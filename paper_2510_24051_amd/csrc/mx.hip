@@ -774,11 +774,10 @@ __global__ __launch_bounds__(512, 2) void mx_tiles_kernel(MxRowsView a, int M, M
 constexpr int mx_stages_a(int mb, int ks) { return mb * ks <= 8 ? 4 : mb * ks <= 12 ? 3 : 2; }
 // weights in flight: 64 to 128 KiB of a compute unit, less where the registers hold accumulators
 constexpr int mx_stages_w(int fmt, int nj, int mb, int ks) {
-  const int room = mb == 1 ? 128 : mb == 2 ? 64 : 48 + 16 * (mb == 4 && nj == 1), stage = (fmt == PIE_MXFP8 ? 8 : 16) * nj;  // registers
+  const int room = mb == 1 ? 128 : mb == 2 ? 64 : 48, stage = (fmt == PIE_MXFP8 ? 8 : 16) * nj;  // registers
   const int fit = room / stage;
   return mx_stages_a(mb, ks) == 3 ? (fit >= 6 ? 6 : fit >= 3 ? 3 : fit >= 2 ? 2 : 1) : fit >= 8 ? 8 : fit >= 4 ? 4 : fit >= 2 ? 2 : 1;
 }
-constexpr int mx_stages_round(int sa, int sw) { return sw % sa == 0 ? sw : sa % sw == 0 ? sa : sa * sw; }
 
 template <bool GATED, int FMT, int MB, int KS, int NJ, bool PAIRS>
 __global__ __launch_bounds__(512, 2) void mx_stream_kernel(MxRowsView a, int M, MxPacked w, MxEpi epi, int tiles_m, int tiles_n, int splits, float* part) {
@@ -787,7 +786,7 @@ __global__ __launch_bounds__(512, 2) void mx_stream_kernel(MxRowsView a, int M, 
   constexpr int WN = 8 / KS, BM = 32 * MB;
   [[maybe_unused]] constexpr int SK = FMT == PIE_MXFP8 ? 2 : 4, SD = SK / 2;
   constexpr int SA = mx_stages_a(MB, KS);
-  [[maybe_unused]] constexpr int SW = mx_stages_w(FMT, NJ, MB, KS), RS = mx_stages_round(SA, SW);  // (RS: steps of a round of both rings)
+  [[maybe_unused]] constexpr int SW = mx_stages_w(FMT, NJ, MB, KS), RS = SA > SW ? SA : SW;  // (RS: steps of a round of both rings)
   [[maybe_unused]] constexpr int SG = SA == 4 ? 4 : SA == 3 && SD == 1 ? 3 : 1, SL = SG == 1 ? 4 : 16, SROW = SD * SL;  // stages whose scales are copied together (as LDS has room), a lane's bytes of a copy, a row's
   [[maybe_unused]] constexpr int SB = SG == 1 ? SA : 2;  // such groups held
   [[maybe_unused]] constexpr int UI = FMT == PIE_MXFP8 && MB > 2 ? 1 : MB == 4 ? 2 : MB, UN = MB / UI;  // (see mx_tiles_kernel; three blocks at a time do not fit the registers beside their halves)
@@ -972,7 +971,7 @@ __global__ __launch_bounds__(512, 2) void mx_stream_kernel(MxRowsView a, int M, 
       one(integral_constant<int, 0>{}); one(integral_constant<int, 1>{}); one(integral_constant<int, 2>{}); one(integral_constant<int, 3>{});
       one(integral_constant<int, 4>{}); one(integral_constant<int, 5>{}); one(integral_constant<int, 6>{}); one(integral_constant<int, 7>{});
     };
-    static_assert(RS <= 8 && RS >= SW && RS % SG == 0, "a round is written out");
+    static_assert(RS <= 8 && RS % SA == 0 && RS % SW == 0 && RS % SG == 0, "a round is written out");
     for (; kt + SW < nmax; kt += RS) round(std::false_type{}, RS);  // (steps past the last do nothing)
     round(std::true_type{}, nmax - kt);
     PIE_S_WAIT_VMCNT(0);  // the surplus copies of the last steps land before the stages are used for anything else
@@ -1005,13 +1004,9 @@ __global__ __launch_bounds__(512, 2) void mx_stream_kernel(MxRowsView a, int M, 
         if (nb0 + j < w.NB) mx_plain_epilogue(epi, acc[i][j], m, M, (nb0 + j) * 32, lane);
     }
   };
-  if constexpr (KS == 1) {
-#pragma unroll
-    for (int i = 0; i < MB; ++i) finish(i);
-    return;
-  }
+  static_assert(KS > 1, "slices whose sums meet");
   constexpr int OTHERS = (KS - 1) * WN;  // waves whose sums a block's owners read
-  constexpr int FIT = SA * STAGE / ((OTHERS ? OTHERS : 1) * NJ * 4096), ROUND = FIT < MB ? FIT : MB;  // token blocks whose sums fit the stages
+  constexpr int FIT = SA * STAGE / (OTHERS * NJ * 4096), ROUND = FIT < MB ? FIT : MB;  // token blocks whose sums fit the stages
   static_assert(ROUND >= 1, "a block of every wave fits the stages");
   auto sums_of = [&](int i, int sl, int j) {  // of slice sl (not the owner i % KS), block i of a round
     const int other = sl < i % KS ? sl : sl - 1;
