@@ -21,14 +21,18 @@ struct PackedWeight {
   int NB = 0;  // number of 32-row blocks stored (N rounded up)
 };
 
-struct MxPacked {  // MXFP4 weights, tiled (see mx_pack_kernel)
+struct MxTiles {  // MXFP4 weights, tiled (see mx_pack_kernel)
   uint8_t* data = nullptr;     // [NB][KT][64 lanes][16 bytes]
   uint32_t* scales = nullptr;  // [NB][KQ][64 lanes], behind the data
   int N = 0, K = 0;            // rows, inputs
-  // how the last product was taken, for the next of as many rows (the estimates of a plan take the host microseconds)
-  struct Plan { int key = -1, mb, ks, nj, splits, rows; };
-  mutable Plan plan;
   int NB = 0, KT = 0, KQ = 0;  // blocks of 32 rows, steps of 64 inputs (a multiple of four), groups of four steps
+};
+struct MxPacked : MxTiles {
+  // how its last products were taken, for the next ones of as many rows (a plan's estimates take the host 1 to 5 us): decode batches, prompts, and
+  // what is left of their rows behind whole tiles
+  struct Plan { int key = -1, mb, ks, nj, splits, rows; };
+  mutable Plan plans[8];
+  mutable unsigned oldest = 0;
 };
 struct pie_mx_weight {
   const pie_ctx* owner = nullptr;

@@ -1,6 +1,7 @@
 // Microscaled rows (blocks of 32 values, a power of two as scale, elements E4M3 or E2M1): quantisation, the norm that adds the residual
 // and writes them, the layout of 4-bit weights, and the products of both on the scaled matrix instructions.
 #include <algorithm>
+#include <iterator>
 #include <type_traits>
 
 #include "internal.h"
@@ -365,7 +366,7 @@ hipError_t launch_mx_norm(const MxNormArgs& a, int rows, int k, int format, cons
 // scale of its block in tile 4 q + t: one load for four steps, of which the instruction picks the byte.  What is behind the last row
 // or block is 0.
 // ---------------------------------------------------------------------------------------------
-__global__ __launch_bounds__(256) void mx_pack_kernel(MxRowsView src, int rows, int k, int first, int interleave, MxPacked w, int64_t from) {
+__global__ __launch_bounds__(256) void mx_pack_kernel(MxRowsView src, int rows, int k, int first, int interleave, MxTiles w, int64_t from) {
   const int64_t i = from + (int64_t)blockIdx.x * 256 + threadIdx.x;  // one per (32-row block of the part, k step, lane)
   const int KT = w.KT;
   const int64_t total = (int64_t)((rows + 31) / 32) * KT * 64;
@@ -590,7 +591,7 @@ __device__ __forceinline__ void mx_copy_piece(__amdgpu_buffer_rsrc_t rsrc, int o
 #endif
 
 template <bool GATED, int FMT>
-__global__ __launch_bounds__(512, 2) void mx_tiles_kernel(MxRowsView a, int M, MxPacked w, MxEpi epi, int tiles_m, int tiles_n) {
+__global__ __launch_bounds__(512, 2) void mx_tiles_kernel(MxRowsView a, int M, MxTiles w, MxEpi epi, int tiles_m, int tiles_n) {
   constexpr int SK = FMT == PIE_MXFP8 ? 2 : 4;  // steps of 64 a stage
   constexpr int SD = SK / 2;                    // dwords of scales a row and stage
   constexpr int MI = 4, NJ = 2;
@@ -780,7 +781,7 @@ constexpr int mx_stages_w(int fmt, int nj, int mb, int ks) {
 }
 
 template <bool GATED, int FMT, int MB, int KS, int NJ, bool PAIRS>
-__global__ __launch_bounds__(512, 2) void mx_stream_kernel(MxRowsView a, int M, MxPacked w, MxEpi epi, int tiles_m, int tiles_n, int splits, float* part) {
+__global__ __launch_bounds__(512, 2) void mx_stream_kernel(MxRowsView a, int M, MxTiles w, MxEpi epi, int tiles_m, int tiles_n, int splits, float* part) {
   static_assert(!GATED || NJ == 2, "a gate and an up block");
   static_assert(!PAIRS || (MB == 1 && FMT == PIE_MXFP8), "two lanes' columns to a row");
   constexpr int WN = 8 / KS, BM = 32 * MB;
@@ -1213,7 +1214,7 @@ hipError_t launch_mx_product(const MxRowsView& a, int format, int M, const MxPac
   if (deferred) *deferred = 0;
   if (M <= 0) return hipSuccess;
   const bool gated = e.mode == MX_SWIGLU8 || e.mode == MX_SWIGLU4, fp8 = format == PIE_MXFP8;
-  auto behind = [&](int rows, const MxPacked& weight) {  // the product of the rows from `rows` on
+  auto behind = [&](int rows) {  // the product of the rows from `rows` on
     MxRowsView rest = a;
     rest.elements += rows * a.row_bytes;
     rest.scales += rows * a.scale_bytes;
@@ -1222,26 +1223,26 @@ hipError_t launch_mx_product(const MxRowsView& a, int format, int M, const MxPac
     if (e.scales) r.scales = e.scales + rows * e.lds;
     if (e.ids) r.ids = e.ids + rows;
     if (e.resid) r.resid = e.resid + (int64_t)rows * e.H;
-    return launch_mx_product(rest, format, M - rows, weight, r, ws, n_cus, s);
+    return launch_mx_product(rest, format, M - rows, w, r, ws, n_cus, s);
   };
   if (const int most = mx_rows_at_once(w); M > most) {
     const hipError_t err = launch_mx_product(a, format, most, w, e, ws, n_cus, s);
-    return err != hipSuccess ? err : behind(most, w);
+    return err != hipSuccess ? err : behind(most);
   }
   const bool defer = deferred != nullptr;
-  MxPacked::Plan& kept = w.plan;  // (gated or not, and the number of compute units, do not change from call to call)
-  const int key = 4 * M + 2 * defer + fp8;
-  if (kept.key != key) {
+  const int key = 4 * M + 2 * defer + fp8;  // (gated or not, and the number of compute units, do not change from call to call)
+  const MxPacked::Plan* kept = std::find_if(std::begin(w.plans), std::end(w.plans), [&](const MxPacked::Plan& x) { return x.key == key; });
+  if (kept == std::end(w.plans)) {
     const MxPlan q = mx_plan(M, w, gated, fp8, defer, n_cus);
-    kept = MxPacked::Plan{key, q.form.mb, q.form.ks, q.form.nj, q.splits, q.rows};
+    MxPacked::Plan& slot = w.plans[w.oldest++ % std::size(w.plans)];
+    slot = MxPacked::Plan{key, q.form.mb, q.form.ks, q.form.nj, q.splits, q.rows};
+    kept = &slot;
   }
-  const MxPlan p{{kept.mb, kept.ks, kept.nj}, kept.splits, kept.rows, 0.0};
+  const MxPlan p{{kept->mb, kept->ks, kept->nj}, kept->splits, kept->rows, 0.0};
   const hipError_t err = gated ? (fp8 ? run_product<true, PIE_MXFP8>(a, p.rows, w, e, p, defer, ws, s) : run_product<true, PIE_MXFP4>(a, p.rows, w, e, p, defer, ws, s))
                                : (fp8 ? run_product<false, PIE_MXFP8>(a, p.rows, w, e, p, defer, ws, s) : run_product<false, PIE_MXFP4>(a, p.rows, w, e, p, defer, ws, s));
   if (deferred && p.splits > 1) *deferred = p.splits;
-  if (err != hipSuccess || p.rows == M) return err;
-  const MxPacked tail = w;  // (with a plan of its own)
-  return behind(p.rows, tail);
+  return err != hipSuccess || p.rows == M ? err : behind(p.rows);
 }
 
 void mx_product_plan(int M, const MxPacked& w, bool gated, int format, int n_cus, int64_t out[5]) {
