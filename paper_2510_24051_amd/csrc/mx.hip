@@ -1116,42 +1116,48 @@ __global__ __launch_bounds__(256) void mx_join_kernel(const float* __restrict__ 
 struct MxForm { int mb, ks, nj; };
 struct MxPlan { MxForm form; int splits, rows; double us; };
 static constexpr MxForm MX_TILES = {0, 1, 2};
-// The forms that a sweep of all (1 to 4 blocks, 1 to 8 slices, 110 products of 1 to 2100 rows, up to 8 splits) needs to come within 1% of its best.
+// The forms that a sweep of 1 to 4 blocks and 1 to 8 slices needed to come within 1% of its best.
 static constexpr MxForm MX_PLAIN[] = {{1, 2, 1}, {1, 4, 1}, {1, 8, 1}, {2, 4, 1}, {2, 8, 1}, {3, 2, 1}, {3, 4, 1}, {1, 4, 2}, {2, 4, 2}, {3, 2, 2}, {4, 2, 2}, {4, 4, 2}};
 static constexpr MxForm MX_GATED[] = {{1, 2, 2}, {1, 4, 2}, {2, 2, 2}, {2, 4, 2}, {3, 2, 2}, {3, 4, 2}, {4, 2, 2}, {4, 4, 2}};
 
-// Estimated microseconds, fitted to that sweep (weights from HBM, calls in a graph): workgroups go in rounds of one to a compute unit, a round
-// costs its start (4 us: first requests, the slices' sums, the epilogue) and its stages, a stage the longest of its matrix instructions (118 ns per
-// accumulator tile of a wave), of what it fetches (34 bytes a nanosecond) and of its reads of LDS.  The form that this picks takes 1.9% more
-// time than the best of the sweep on average, 14% at most (333 rows of 4096 onto 4096: 17.5 us, 15.4).  Examples, best and next form:
-// 28672 x 4096 gated at 1 row (1, 4) 17.2, tiles 43; at 64 rows (2, 4) 20.7, (1, 2) 22.5; at 333 (3, 2) 53.5, tiles 55; at 1400 tiles 161, (4, 2) 184.
-// 4096 x 14336 at 64 rows (1, 4, 2) in 4 splits 19.4, (1, 8, 1) whole 20.3; at 900 rows (4, 4, 2) 74, tiles 150.  (With scales copied several stages
-// at a time, since the sweep, tiles and most forms are 5 to 9% faster; the estimate compares them as before.)
+// Estimated microseconds.  Workgroups go in rounds of one to a compute unit; a round costs its start (first requests, the slices' sums, the epilogue) and its
+// stages, a stage the longest of its matrix instructions, of what it fetches and of its reads of LDS.  The constants are fitted to every form and
+// split of 207 products of 1 to 2500 rows (weights from HBM, calls in a graph): what this picks takes 1.1% more time than the best form with 8-bit
+// rows on average, 1.9% with 4-bit ones, 2.2% on 35 products outside the fit, and 16% at most (40 rows of 608 onto 4874: 8.1 us, 7.0).
+// Examples, its choice and the next best, 8-bit rows: SwiGLU of 4096 onto 2 x 14336 at one row (1, 4, 2) 18.7 us, (1, 2, 2) in 2 splits 20.7; at 64 rows (2, 4, 2)
+// 24.1, (1, 2, 2) 27.6; at 333 (3, 2, 2) 78.9, tiles 91; at 2100 tiles 369, (3, 2, 2) 408.  14336 onto 4096 at 64 rows (2, 4, 2) in 7 splits 22.8, the best (1, 4, 2) in
+// 4 20.1; at 900 (4, 4, 2) 105, (4, 2, 2) in 2 105.
+struct MxCosts {
+  double round, stage, busy;               // tiles: a round, a stage, and what that costs more on all compute units
+  double mma, bandwidth, reads, step;      // others, a stage: matrix instructions of an accumulator tile, KiB a us, reads of a block of rows; what comes on top
+  double start, tile, join, sums;          // a round, and that of an accumulator tile; a split product's join, GB/ms of its sums
+};
+static constexpr MxCosts MX_COSTS8 = {7.48, 2.06, 0.43, 0.35, 32.2, 0.48, 0.091, 3.59, 0.27, 3.34, 3.2}, MX_COSTS4 = {5.83, 0.93, 1.05, 0.27, 53.6, 0.058, 0.015, 5.77, 0.03, 2.14, 1.75};
 static double mx_tiles_us(int M, int NB, int NS, bool fp8, int n_cus) {
+  const MxCosts& c = fp8 ? MX_COSTS8 : MX_COSTS4;
   const int64_t wgs = (int64_t)((M + MX_TM - 1) / MX_TM) * ((NB + MX_TN / 32 - 1) / (MX_TN / 32));
-  const double stages = NS * (fp8 ? 1.0 : 1.56);
-  auto round = [&](int64_t busy) { return 4.1 + stages * (1.07 + 0.42 * (double)busy / n_cus); };
+  auto round = [&](int64_t busy) { return c.round + NS * (c.stage + c.busy * (double)busy / n_cus); };
   return 0.9 + (double)(wgs / n_cus) * round(n_cus) + (wgs % n_cus ? round(wgs % n_cus) : 0.0);
 }
-static double mx_stream_us(const MxForm& f, int splits, int M, int NB, int64_t K, int NS, bool fp8, bool defer, int n_cus) {
+static double mx_stream_us(const MxForm& f, int splits, int M, int NB, int NS, bool fp8, bool defer, int n_cus) {
+  const MxCosts& c = fp8 ? MX_COSTS8 : MX_COSTS4;
   const int WN = 8 / f.ks, tiles_m = (M + 32 * f.mb - 1) / (32 * f.mb), tiles_n = (NB + f.nj * WN - 1) / (f.nj * WN);
   const int64_t wgs = (int64_t)tiles_m * tiles_n * splits, rounds = (wgs + n_cus - 1) / n_cus;
   const int steps = (NS + f.ks * splits - 1) / (f.ks * splits);
   const double kib = f.ks * std::min(32 * f.mb, M) / 8.0 + (fp8 ? 16 : 32) * f.nj;
-  const double stage = std::max({0.118 * f.mb * f.nj, kib / 34.0, 0.15 * f.mb}) + 0.057;
-  const double t = 0.9 + (double)rounds * (4.2 + 0.08 * f.mb * f.nj + steps * stage);
-  const double least = 0.9 + (double)NB * 32 * (double)K * 0.53e-6 / 3.83;  // (the weights' bytes)
-  return std::max(t, least) + (splits > 1 ? (defer ? 0.5 : 3.3) + (double)splits * M * NB * 32 * 8e-6 / 3.5 : 0.0);
+  const double stage = std::max({c.mma * f.mb * f.nj, kib / c.bandwidth, c.reads * f.mb}) + c.step;
+  const double t = 0.9 + (double)rounds * (c.start + c.tile * f.mb * f.nj + steps * stage);
+  return t + (splits > 1 ? (defer ? 0.5 : c.join) + (double)splits * M * NB * 32 * 8e-6 / c.sums : 0.0);
 }
-// The best of one form for all rows, and of tiles for whole rounds with another form behind them (8320 rows of 14336 onto 4096: 33 x 16 tiles
-// took 503 us, 32 x 16 and the last 128 rows in another form 409, and 362 since scales are copied four stages at a time).
+// The best of one form for all rows, and of tiles for whole rounds with another form behind them (8320 rows of 14336 onto 4096 in 4 bits: 33 x 16 tiles
+// take 285 us, 32 x 16 and the last 128 rows in another form 239; SwiGLU of 8320 rows of 8 bits 1392 and 1348).
 static MxPlan mx_plan_whole(int M, const MxPacked& w, bool gated, bool fp8, bool defer, int n_cus) {
   const int row = fp8 ? w.K : w.K / 2, NS = (row + 127) / 128;
   MxPlan best{MX_TILES, 1, M, M > 128 ? mx_tiles_us(M, w.NB, NS, fp8, n_cus) : 1e30};  // (the sweep has no product of up to 128 rows for them)
   auto look = [&](const MxForm& f) {
     for (int splits = 1; splits <= 8; ++splits) {
       if (splits > 1 && ((size_t)splits * M * w.NB * 32 > MX_WS_FLOATS || f.ks * splits * 2 > NS)) break;
-      const double us = mx_stream_us(f, splits, M, w.NB, w.K, NS, fp8, defer, n_cus);
+      const double us = mx_stream_us(f, splits, M, w.NB, NS, fp8, defer, n_cus);
       if (us < best.us) best = MxPlan{f, splits, M, us};
     }
   };
