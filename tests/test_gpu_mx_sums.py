@@ -61,8 +61,9 @@ def ones(m, k, byte=127):
     return np.full((m, k // 32), byte, np.int64)
 
 
-# (rows, k, n): one row to more than a tile, with ends inside tiles, stages and groups of stages; the small ones in every form of few rows
-SIZES = [(1, 32, 1), (1, 64, 40), (1, 512, 256), (5, 96, 33), (15, 1056, 64), (16, 2080, 96), (16, 4096, 700), (17, 1056, 64), (3, 8192, 32), (9, 4096, 8192), (31, 256, 130),
+# (rows, k, n): one row to more than a tile, with ends inside tiles, stages and groups of stages; up to 16 rows in every form that they are taken in, split
+# over workgroups and whole (test_host_mx_plans.py sees to it)
+SIZES = [(1, 12288, 32), (9, 8192, 2816), (1, 1536, 16896), (1, 12288, 3296), (1, 32, 1), (1, 64, 40), (1, 512, 256), (5, 96, 33), (15, 1056, 64), (16, 2080, 96), (16, 4096, 700), (17, 1056, 64), (3, 8192, 32), (9, 4096, 8192), (31, 256, 130),
          (33, 544, 257), (64, 4096, 96), (129, 1056, 300), (300, 320, 520), (700, 640, 260), (1030, 288, 515)]
 LISTED = [(m, k, n) for gated, form, m, k, n in FORM_SIZES if not gated and form == "mxfp8"]
 
@@ -83,6 +84,21 @@ def test_sums_of_few_elements_are_whole(ctx, m, k, n):
     half = torch.empty((m, n), dtype=torch.bfloat16, device="cuda")
     ctx.mx_product(a, weight, half)
     assert np.array_equal(half.double().cpu().numpy(), O.bf16_round(want))
+
+
+# 4-bit rows: tiles with a rest behind them, and products split over workgroups
+SIZES4 = [(2050, 512, 8192), (1, 8192, 32), (40, 14336, 512), (333, 14336, 96), (16, 4096, 700)]
+
+
+@pytest.mark.parametrize("m,k,n", SIZES4)
+def test_sums_of_4_bit_rows_are_whole(ctx, m, k, n):
+    """Any elements: products are multiples of 1/4 and at most 36, sums of 14336 of them below 2^19."""
+    rng = np.random.default_rng(m + k + n)
+    a, av = device(codes(rng, (m, k), "mxfp4"), "mxfp4", ones(m, k))
+    w, wv = device(codes(rng, (n, k), "mxfp4"), "mxfp4", ones(n, k))
+    out = torch.full((m, n + 3), -9.0, device="cuda")
+    ctx.mx_product(a, ctx.mx_weight([w]), out[:, :n])
+    assert np.array_equal(out[:, :n].cpu().numpy(), mx.product(av, wv).astype(np.float32)) and (out[:, n:] == -9.0).all()
 
 
 GATED_SIZES = [(1, 32, 32), (4, 512, 64), (16, 4096, 96), (16, 256, 4096), (17, 544, 64), (64, 1024, 288), (300, 416, 320), (600, 64, 256)]

@@ -7,7 +7,7 @@ import sys
 import numpy as np
 import pytest
 
-from test_host_mx import FORM_SIZES, FP4, FP8, Calls
+from test_host_mx import FORM_SIZES, FORMS, FP4, FP8, Calls
 from test_host_runtime_paths import Child, fake  # noqa: F401  (the fixture builds the stand-in)
 
 K, N = 2048, 4096
@@ -57,3 +57,48 @@ if __name__ == "__main__":
 def test_host_path(fake, case):  # noqa: F811
     r = subprocess.run([sys.executable, os.path.abspath(__file__), fake, case], capture_output=True, text=True, timeout=120)
     assert r.returncode == 0 and "case passed" in r.stdout, f"exit {r.returncode}\n{r.stdout}\n{r.stderr}"
+
+
+def plans(sizes, gated, form):
+    from paper_2510_24051_amd import mx_product_plan
+    return [(m, mx_product_plan(m, n, k, gated, form)) for m, k, n in sizes]
+
+
+def listed(gated, form):
+    """Every product whose sums the GPU tests compare bit for bit (or, gated, to the activation's roundings)."""
+    import test_gpu_mx_sums as G
+    own = G.GATED_SIZES if gated else G.SIZES if form == "mxfp8" else G.SIZES4
+    return [(m, k, n) for g, f, m, k, n in FORM_SIZES if (g, f) == (gated, form)] + (own if form == "mxfp8" or not gated else [])
+
+
+@pytest.mark.parametrize("form", ["mxfp8", "mxfp4"])
+@pytest.mark.parametrize("gated", [False, True])
+def test_splits_and_cuts_are_listed(gated, form):
+    """Of either kind, for either format: products split over workgroups, whose sums are joined, and products cut behind whole tiles."""
+    p = plans(listed(gated, form), gated, form)
+    assert any(x["splits"] > 1 for _, x in p) and any(x["rows"] < m for m, x in p)
+    assert {(x["tile_rows"], x["tile_columns"], x["k_slices"]) for _, x in p} == FORMS[gated]
+
+
+def test_forms_of_up_to_16_rows_are_listed():
+    """8-bit rows whose two parts stand side by side: every form of one block of rows, split and whole."""
+    for gated in (False, True):
+        seen = {(x["tile_columns"], x["k_slices"], x["splits"] > 1) for m, x in plans([s for s in listed(gated, "mxfp8") if s[0] <= 16], gated, "mxfp8") if x["tile_rows"] == 32}
+        assert seen == {(c, s, split) for r, c, s in FORMS[gated] if r == 32 for split in (False, True)}
+
+
+def test_sums_of_split_products_fit_the_workspace():
+    """2^24 floats: as many copies of the sums as there are splits, their rows filled up to blocks of 32 columns."""
+    from paper_2510_24051_amd import mx_product_plan
+    rng = np.random.default_rng(1)
+    most = 0
+    for _ in range(4000):
+        m, n, k = (int(2 ** rng.uniform(0, b)) for b in (14, 15, 10))
+        gated = bool(rng.integers(2))
+        n = (n + 31) // 32 * 32 if gated else n
+        p = mx_product_plan(m, n, 32 * k, gated, ["mxfp8", "mxfp4"][rng.integers(2)])
+        if p["splits"] > 1:
+            floats = p["splits"] * p["rows"] * ((n + 31) // 32 * 32) * (2 if gated else 1)
+            assert floats <= 1 << 24
+            most = max(most, floats)
+    assert most > 1 << 21  # (some come near)
