@@ -355,6 +355,8 @@ class Pie:
         if torch._C._cuda_getCurrentRawStream(self._index) == self._raw_stream:
             st = call(*args)
             return self._check(st) if st != 0 else None
+        if self._raw_stream == 0 and torch.cuda.is_current_stream_capturing():  # (waiting there for an event of the capture has ended the process)
+            raise PieError(-6, "the context's stream is the device's default stream, which cannot be captured: give the context a stream of its own")
         current = torch.cuda.current_stream(self.device)
         self._before.record(current)
         self.stream.wait_event(self._before)
