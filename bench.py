@@ -101,6 +101,21 @@ def mixed_workload_fractions(w_dec, args):
     return out
 
 
+def microscaled(ctx, weights):
+    """The layer's weights in 4 bits, quantised by the library."""
+    import copy
+    import numpy as np
+    import torch
+    from paper_2510_24051_amd import MxRows
+    out = copy.copy(weights)
+    for name in ctx.PROJECTIONS:
+        t = torch.from_numpy(np.ascontiguousarray(getattr(weights, name)).view(np.int16)).to(ctx.device).view(torch.bfloat16)
+        rows = MxRows.empty(t.shape[0], t.shape[1], "mxfp4", ctx.device)
+        ctx.mx_quantise(t, rows)
+        setattr(out, name, rows)
+    return out
+
+
 def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--gpus", type=int, default=1)
@@ -119,7 +134,11 @@ def main():
     ap.add_argument("--layers", type=int, default=1,
                     help="run the batch through this many layers (pie_forward_all; every layer gets the same "
                          "synthetic weights and prior KV values); the default 1 is the per-layer metric")
+    ap.add_argument("--mx", action="store_true",
+                    help="layers in microscaled formats (pie_load_layer_mx): weights of 4 bits, products of 8-bit rows; no CPU baseline")
     args = ap.parse_args()
+    if args.mx and args.lora_rank > 0:
+        ap.error("--mx: microscaled layers take no adapters")
     if args.gpus != 1:
         print("bench.py: this build runs on one GPU only (no collectives, no sharding); use --gpus 1", file=sys.stderr)
         sys.exit(2)
@@ -163,8 +182,9 @@ def main():
         b.adapter_ids = (np.arange(b.n_requests) % 2).astype(np.int32)
     ctx.load_head(w.head)
     ctx.embed_write(b.in_embed_ids, w.embed_bits)
+    mx_weights = microscaled(ctx, w.weights) if args.mx else None
     for l in range(NL):
-        ctx.load_layer(l, w.weights)
+        (ctx.load_layer_mx(l, mx_weights) if args.mx else ctx.load_layer(l, w.weights))
         ctx.kv_write(l, w.prior.page_ids, w.prior.slots, w.prior.k_bits, w.prior.v_bits)
     pb = ctx.batch_create(b, validate=True)
     work = pb.work()
@@ -264,7 +284,7 @@ def main():
     roofline = {"kernel": "attn_decode_kernel", "bound": "hbm", "achieved": round(achieved, 1), "peak": HBM_PEAK_GBS,
                 "unit": "GB/s", "frac": round(achieved / HBM_PEAK_GBS, 4), "traffic": None, "traffic_source": None,
                 "algorithmic_bytes": attn_bytes, "avg_ms": round(attn_ms, 5)}
-    if (args.workload, args.requests, NL, args.lora_rank) == (PMC_TRAFFIC["workload"], PMC_TRAFFIC["requests"],
+    if not args.mx and (args.workload, args.requests, NL, args.lora_rank) == (PMC_TRAFFIC["workload"], PMC_TRAFFIC["requests"],
                                                                PMC_TRAFFIC["layers"], PMC_TRAFFIC["lora_rank"]):
         roofline["traffic"], roofline["traffic_source"] = PMC_TRAFFIC["bytes"], PMC_TRAFFIC["source"]
     if attn_b2b_ms > 0:
@@ -278,7 +298,7 @@ def main():
 
     weight_elems = (m.hidden * (m.n_q_heads + 2 * m.n_kv_heads) * m.head_dim + m.n_q_heads * m.head_dim * m.hidden
                     + 3 * m.hidden * m.mlp_dim)
-    weight_bytes = 2 * weight_elems
+    weight_bytes = weight_elems * 17 // 32 if args.mx else 2 * weight_elems  # (4 bits, and a byte to 32)
     lm_bytes = 2 * m.vocab * m.hidden
     gemm_ms = sum(stages.get(k, 0.0) for k in ("qkv", "oproj", "gateup", "down"))
     extra = {
@@ -288,6 +308,9 @@ def main():
     if T < MFMA_RIDGE_ROWS:  # few rows: the GEMMs stream their weights once (HBM-bound)
         extra["layer_gemms"] = {"bound": "hbm", "algorithmic_bytes": weight_bytes, "ms": round(gemm_ms, 5),
                                 "achieved_GBs": round(weight_bytes / (gemm_ms * 1e-3) / 1e9, 1) if gemm_ms else None}
+    elif args.mx:  # many rows of 8 bits
+        extra["layer_gemms"] = {"bound": "mfma", "algorithmic_flops": 2 * T * weight_elems, "ms": round(gemm_ms, 5),
+                                "achieved_TFLOPs": round(2 * T * weight_elems / (gemm_ms * 1e-3) / 1e12, 1)}
     else:  # many rows: dense bf16 contractions (MFMA-bound)
         gemm_flops = 2 * T * weight_elems
         extra["layer_gemms"] = {"bound": "mfma", "algorithmic_flops": gemm_flops, "ms": round(gemm_ms, 5),
@@ -315,11 +338,11 @@ def main():
                                  "frac": round(pf_flops / (pf_ms * 1e-3) / 1e12 / MFMA_BF16_PEAK_TFLOPS, 4)}
 
     other = None
-    if args.workload == "c2" and args.requests == 64 and NL == 1 and args.lora_rank == 0 and not args.no_other_workloads:
+    if args.workload == "c2" and args.requests == 64 and NL == 1 and args.lora_rank == 0 and not args.mx and not args.no_other_workloads:
         other = {"c3": mixed_workload_fractions(w, args)}
 
     cpu = None
-    if not args.no_cpu_baseline:
+    if not args.no_cpu_baseline and not args.mx:
         from oracle import pie_oracle as O
         from helpers import oracle_pools
         kv, emb = oracle_pools(w)
@@ -349,7 +372,7 @@ def main():
         "metric": "forward tokens/s per layer (8B shape) + decode-attn HBM GB/s % of peak",
         "value": round(T / (ms_per_step * 1e-3), 1), "unit": "tokens/s", "n_gpus": 1, "steps": args.steps,
         "warmup": args.warmup, "ms_per_step": round(ms_per_step, 5), "higher_is_better": True, "scaling": "weak",
-        "vs_baseline": None, "dtype": "bf16", "data": "synthetic",
+        "vs_baseline": None, "dtype": "mxfp8 x mxfp4 in the layers, bf16 elsewhere" if args.mx else "bf16", "data": "synthetic",
         "config": {"workload": desc, "tokens_per_step": T, "requests": int(b.n_requests), "dist_rows": n_dist,
                    "top_k": int(w.top_k), "layers": NL, "lora_rank": int(args.lora_rank),
                    "step": ("pie_forward (1 layer)" if NL == 1 else f"pie_forward_all ({NL} layers)") + " + pie_get_next_dist"},
