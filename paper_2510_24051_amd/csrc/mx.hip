@@ -149,10 +149,10 @@ __device__ __forceinline__ void add_splits(const float* p, int64_t stride, int s
 }
 
 // ---------------------------------------------------------------------------------------------
-// Quantisation and its inverse: eight values a lane and piece, MX_PIECES pieces of a thread requested together.  Bound by HBM: 28672 x 4096 of bf16 to
-// 4 bits 60 us (5.0 TB/s), with one piece a thread and 64-bit divisions 75; 64 x 4096 to 8 bits 3.3 us, a launch.  Back from 4 bits 53 us, 60 where
+// Quantisation and its inverse: eight values a lane and piece, MX_PIECES pieces of a thread requested together.  Bound by HBM; back to back in a graph: 28672 x 4096
+// of bf16 to 4 bits 58 us (5.1 TB/s), with one piece a thread and 64-bit divisions 75; 64 x 4096 to 8 bits 2.4 us, a launch.  Back from 4 bits 53 us, 60 where
 // its stores went through the caches; both in turn, where these are then written back underneath the other, 103 and 120.  (Loads past the caches gain
-// nothing here, and lose what they hold of a smaller input: 8320 x 4096 to 8 bits 21.4 us, 23.4.  fp32's halves of 32 bytes stored past them: 28.5, 52.)
+// nothing here, and lose what they hold of a smaller input: 8320 x 4096 to 8 bits 21.5 us, 23.4.  fp32's halves of 32 bytes stored past them: 28.5, 52.)
 // ---------------------------------------------------------------------------------------------
 constexpr int MX_PIECES = 4;
 // Row and column of piece i of rows of k values; SMALL: pieces fit 32 bits, where a division is a few instructions.
@@ -525,9 +525,11 @@ __device__ __forceinline__ void mx_plain_epilogue(const MxEpi& e, const f32x16& 
 // stage right behind the instructions that used it (as in gemm_large_async_kernel, whose order of requests, waits and barriers this is).
 // The 16-byte pieces of a row are swizzled by its number: piece c of row r is stored at c ^ (r / 2 % 8), so that the 32 rows of an operand
 // read from all banks.  What is behind K is read from the row's first piece instead: its weights are 0, and so is its scale.
+// 8192 rows of 14336 onto 4096 take 620 us with 8-bit rows, on zeros, which the power limit does not hold back, 507; 4-bit rows 217 and 164.  SwiGLU of 4096 onto
+// 2 x 14336: 1290 and 1080, 510 and 400.
 // A row's scales of a stage are 4 or 8 bytes of a cache line of their own, and the lines that a copy touches are what it costs: with the scales copied every
-// stage 8192 rows of 14336 onto 4096 took 370 us, with four stages' at a time 342, on zeros (no power limit) 295 and 267; SwiGLU of 4096 onto
-// 2 x 14336 755 and 698.  (Weights requested up to two stages earlier, copies two or three stages ahead: the same.)
+// stage 8192 rows of 14336 onto 4096 took 370 us, with four stages' at a time 342, when 8-bit rows were multiplied in one part (on zeros 295 and 267).
+// (Weights requested up to two stages earlier, copies two or three stages ahead: the same.)
 // ---------------------------------------------------------------------------------------------
 constexpr int MX_TM = 256, MX_TN = 256;
 
@@ -584,7 +586,7 @@ __device__ __forceinline__ int mx_piece_back(int p, int lane, int row_len) {
   return held && byte >= held ? byte : 0;
 }
 // From stage k to `to`; off: byte offset of the lane's row plus mx_piece_byte.  (Without a branch: one around the last stage's copies made the compiler
-// wait for weights at every step, 8192 rows of 14336 onto 4096 358 -> 391 us.)
+// wait for weights at every step: 9% of 8192 rows of 14336 onto 4096, multiplied in one part.)
 __device__ __forceinline__ void mx_copy_piece(__amdgpu_buffer_rsrc_t rsrc, int off, uint8_t* to, int k, int back, bool last) {
   __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)to, 16, off - (back & (last ? -1 : 0)), k * 128, 0, 0);
 }
@@ -767,8 +769,7 @@ __global__ __launch_bounds__(512, 2) void mx_tiles_kernel(MxRowsView a, int M, M
 // Eight waves; KS slices of the contraction (or parts of them, where the product is split over workgroups as well) with 8 / KS waves each, a
 // wave with MB x NJ accumulator tiles: 32 weight rows (SwiGLU: a gate and an up block) by 32 MB tokens.  Each wave keeps SW stages of
 // weights in registers (stages as in mx_tiles_kernel, requested non-temporally), each slice SA stages of its activations in LDS, and the
-// scales of SG stages at a time (one stage's by themselves cost as much as its activations: 333 rows of 4 bits, 4096 onto 6144, 14.8 us for 13.4; 64 of 8
-// bits 10.8 for 9.8; SwiGLU of 64, 4096 onto 2 x 14336, 20.8 for 19.9).  A slice's
+// scales of SG stages at a time (one stage's by themselves cost as much as its activations: 333 rows of 4 bits, 4096 onto 6144, 14.8 us for 13.4).  A slice's
 // stages are NS p / parts .. NS (p + 1) / parts; all walk as many as the longest has, the others doing nothing in the last.  The slices'
 // sums meet in LDS, in their order.
 // ---------------------------------------------------------------------------------------------
@@ -904,7 +905,7 @@ __global__ __launch_bounds__(512, 2) void mx_stream_kernel(MxRowsView a, int M, 
       constexpr int SLOT = decltype(slot_c)::value % SW, AT = decltype(slot_c)::value, CUR = AT % SA, NEXT = (AT + 1) % SA, FILL = (AT + SA - 1) % SA;
       constexpr bool TAIL = decltype(tail_c)::value;
       issue_a(FILL, kt + SA - 1);
-      if constexpr ((AT + SA - 1) % SG == 0) issue_s((kt + SA - 1) / SG, SG == 1 ? FILL : (kt + SA - 1) / SG % SB);  // (behind them: in front 28 us for 26, SwiGLU of 128 rows)
+      if constexpr ((AT + SA - 1) % SG == 0) issue_s((kt + SA - 1) / SG, SG == 1 ? FILL : (kt + SA - 1) / SG % SB);  // (behind them: in front 8% slower, SwiGLU of 128 rows)
       __builtin_amdgcn_sched_barrier(0);
       const int shift = FMT == PIE_MXFP8 ? ((first + kt) & 1) * 16 : 0;
       int xs[NJ], nsc[SD][MB];
