@@ -146,3 +146,23 @@ def test_scales_at_the_ends_of_their_range(ctx, form, m):
         out = torch.empty((m, n), device="cuda")
         ctx.mx_product(a, ctx.mx_weight([w]), out)
         assert np.array_equal(out.double().cpu().numpy(), mx.product(av, wv)), byte
+
+
+@pytest.mark.parametrize("m", [1, 4, 16, 17, 300])
+def test_nan_elements(ctx, m):
+    """A NaN among E4M3 elements, of either sign, makes its row NaN and no other, whichever part of the row it is in; -0 and 0 are 0."""
+    rng = np.random.default_rng(m)
+    k, n = 544, 70
+    c = few_codes(rng, m, k)
+    c[(c == 0) & (rng.random((m, k)) < 0.3)] = 0x80
+    r = m // 2
+    c[r, [3, k - 1]] = [0x7F, 0xFF] if m % 2 else [0xFF, 0x7F]
+    wc = codes(rng, (n, k), "mxfp4")
+    wc[:, 3], wc[: n // 2, k - 1] = 0, 8  # NaN times 0
+    a, av = device(c, "mxfp8", ones(m, k))
+    w, wv = device(wc, "mxfp4", ones(n, k))
+    out = torch.empty((m, n), device="cuda")
+    ctx.mx_product(a, ctx.mx_weight([w]), out)
+    got = out.double().cpu().numpy()
+    others = np.arange(m) != r
+    assert np.isnan(got[r]).all() and np.array_equal(got[others], mx.product(av[others], wv))
